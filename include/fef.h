@@ -465,6 +465,48 @@ fef_status fef_lmhead_logits(const void* hidden, const void* weight, int rows, i
                              float* logits, int64_t ldo, int32_t* device_status, void* cuda_stream);
 
 /*
+ * Penalties for repeated tokens, biases and grammar masks on the logits of speculative windows (the paper
+ * has no counterpart: requests carry such rules, and both laws of Section 3.2 have to obey them before the
+ * draws and the verification).  For window b, position i < n_b (n_b = row_len[b], or K) and vocabulary id x,
+ * in binary32 and rounded to `dt` once at the end:
+ *
+ *   h = occurrences of x in tokens[b, 0..L) and among draft_tokens[b, j], j < i
+ *   a = the same without the first prompt_len[b] of tokens[b]
+ *   y = l, or where h > 0:  l / rep for l > 0,  l * rep otherwise
+ *   y = y + (bias[b, x] - (freq * a + pres * [a > 0]))
+ *   out[b, i, x] = y where bit x of the position's mask is 1, -inf where it is 0
+ *
+ *   logits         device, [B, K, ld] row-major, dtype `dt`; layout and alignment rules of fef_spec_verify
+ *   out            device out, [B, K, ld], the same layout; may be `logits` itself (no other overlap).  Positions
+ *                  i >= n_b and the entries between V and ld are left as they were
+ *   tokens         device, [B, L] int32: the text so far (the loop's token state); entries outside [0, V), such as
+ *                  FEF_MASK_TOKEN, are not counted.  0 <= L <= 2^24; may be NULL when L = 0
+ *   prompt_len     device, [B] int32, or NULL = 0: the text's first entries that belong to the prompt
+ *   draft_tokens   device, [B, K] int32, or NULL: the window's drafts, for the target law (the draft law of a
+ *                  position does not depend on them); entries outside [0, V) are not counted
+ *   row_len        device, [B] int32 in [0, K], or NULL = K everywhere
+ *   penalties      device, [B, 3] float32 (rep > 0, freq, pres), or NULL = none (the text is then not read)
+ *   bias           device float32, V entries for window b at bias + b * bias_stride, or NULL; stride 0 shares them
+ *   allowed        device, ceil(V / 32) words for (b, i) at allowed + b * allowed_stride_b + i * allowed_stride_k
+ *                  (strides in words, 0 shares), bit x & 31 of word x >> 5 belongs to id x; or NULL = all allowed
+ *   temperature    of log2_norm alone; >= 0 and finite, 0 stands for 1 as in fef_draft_sample
+ *   log2_norm      device out, [B, K] float64, or NULL: log2 of sum_x 2^(out_x * log2(e) / T) of every adjusted row
+ *                  as it is stored: what fef_spec_verify_with_norms takes.  NaN where the adjusted row holds NaN or
+ *                  +inf or no finite entry (a mask that leaves nothing); 0 for i >= n_b
+ *   workspace      device scratch of fef_logits_adjust_workspace_bytes(B, K, V) bytes, 256-byte aligned, contents need
+ *                  not be initialised; needed with log2_norm only
+ * A masked id is -inf whatever its logit, NaN and infinities among them.  Asynchronous on `cuda_stream`; one kernel, and a
+ * second, small one with log2_norm.
+ */
+size_t fef_logits_adjust_workspace_bytes(int B, int K, int V);
+fef_status fef_logits_adjust(const void* logits, void* out, int B, int K, int V, int64_t ld, fef_dtype dt,
+                             const int32_t* tokens, int L, const int32_t* prompt_len, const int32_t* draft_tokens,
+                             const int32_t* row_len, const float* penalties, const float* bias, int64_t bias_stride,
+                             const uint32_t* allowed, int64_t allowed_stride_b, int64_t allowed_stride_k,
+                             float temperature, double* log2_norm, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream);
+
+/*
  * Seeded synthetic logits made on the device (benchmarks and tests of the decoding loop; they stand
  * in for the two model calls of Algorithm 2 and hold none of the method's arithmetic):
  *   draft  = draft_std * N(0,1), plus `boost` with probability boost_fraction (in steps of 1/512),

@@ -32,7 +32,8 @@ EXPORTS = ("fef_status_string", "fef_spec_verify_workspace_bytes", "fef_spec_ver
            "fef_vp_task_bytes", "fef_vp_local_stats", "fef_vp_accept", "fef_vp_local_residual", "fef_vp_finish",
            "fef_lmhead_verify_workspace_bytes", "fef_lmhead_verify", "fef_lmhead_logits",
            "fef_draft_sample_with_target", "fef_spec_verify_with_norms", "fef_synth_logits",
-           "fef_loop_run_synthetic_workspace_bytes", "fef_loop_run_synthetic")
+           "fef_loop_run_synthetic_workspace_bytes", "fef_loop_run_synthetic",
+           "fef_logits_adjust_workspace_bytes", "fef_logits_adjust")
 
 _lib = None
 
@@ -121,6 +122,11 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     L.fef_lmhead_verify.restype = i32
     L.fef_lmhead_logits.argtypes = [vp, vp, i32, i32, i32, vp, i64, vp, vp]
     L.fef_lmhead_logits.restype = i32
+    L.fef_logits_adjust_workspace_bytes.argtypes = [i32, i32, i32]
+    L.fef_logits_adjust_workspace_bytes.restype = sz
+    L.fef_logits_adjust.argtypes = [vp, vp, i32, i32, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, i64, vp, i64, i64, f32, vp,
+                                    vp, sz, vp]
+    L.fef_logits_adjust.restype = i32
     L.fef_remask_select.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp]
     L.fef_remask_select.restype = i32
     L.fef_remask_select_host_arena_bytes.argtypes = [i32, i32, i32]
@@ -674,3 +680,91 @@ def fef_loop_run_synthetic(B: int, L: int, K: int, V: int, dtype, temperature: f
     if st != FEF_OK:
         raise FefError(st, "fef_loop_run_synthetic")
     return dict(tokens=tokens, conf=conf, in_step=in_step, rounds=int(rnd.item()), device_status=int(status.item()))
+
+
+# ------------------------------------------------------- penalties, biases and masks on the logits ----
+class AdjustResult(NamedTuple):
+    logits: torch.Tensor                # [B, K, ld], the dtype of the input
+    log2_norm: Optional[torch.Tensor]   # [B, K] float64, when asked for
+
+
+def fef_logits_adjust_workspace_bytes(B: int, K: int, V: int) -> int:
+    return int(load().fef_logits_adjust_workspace_bytes(B, K, V))
+
+
+def fef_logits_adjust(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None,
+                      prompt_len: Optional[torch.Tensor] = None, draft_tokens: Optional[torch.Tensor] = None,
+                      penalties: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                      allowed: Optional[torch.Tensor] = None, row_len: Optional[torch.Tensor] = None,
+                      temperature: float = 1.0, V: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                      with_norm: bool = False, log2_norm: Optional[torch.Tensor] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> AdjustResult:
+    """Enqueue penalties, biases and grammar masks on a window's logits (see ``fef_logits_adjust`` in
+    include/fef.h).
+
+    ``logits``: ``[B, K, ld]`` CUDA tensor, float32 or bfloat16, contiguous; ``V`` (default ``ld``)
+    entries of each row are used.  ``tokens`` ``[B, L]`` int32 is the text so far, of which the first
+    ``prompt_len`` ``[B]`` int32 tokens are the prompt; ``draft_tokens`` ``[B, K]`` int32 (for target
+    logits): position i also counts the drafts before it.  ``penalties`` ``[B, 3]`` float32: repetition
+    (> 0), frequency, presence.  ``bias``: float32 ``[V]`` or ``[B, V]``.  ``allowed``: int32 words of 32
+    vocabulary bits each, ``[W]``, ``[B, W]`` or ``[B, K, W]`` with ``W >= ceil(V / 32)``.  Expanded
+    tensors are taken as they are, by their strides.
+
+    The result goes to ``out`` (which may be ``logits``) or a new tensor; positions behind ``row_len`` and
+    the padding behind ``V`` keep what ``out`` held.  ``with_norm`` (or a ``log2_norm`` tensor ``[B, K]``
+    float64 to write to) adds the adjusted rows' normalisers at ``temperature``, as ``fef_spec_verify``
+    takes them.  Asynchronous on the current (or given) stream.
+    """
+    where = "fef_logits_adjust"
+    _require_cuda(logits, tokens, prompt_len, draft_tokens, penalties, bias, allowed, row_len, out, log2_norm, workspace)
+    if logits.dim() != 3 or not logits.is_contiguous():
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    B, K, ld = logits.shape
+    V = ld if V is None else int(V)
+    code = _dtype_code(logits)
+    dev = logits.device
+    for t, dtype, shape in ((prompt_len, torch.int32, (B,)), (draft_tokens, torch.int32, (B, K)),
+                            (row_len, torch.int32, (B,)), (penalties, torch.float32, (B, 3)),
+                            (log2_norm, torch.float64, (B, K)), (out, logits.dtype, logits.shape)):
+        if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != dev):
+            raise FefError(FEF_ERR_INVALID_ARG, where)
+    L = 0
+    if tokens is not None:
+        if tokens.dtype != torch.int32 or tokens.dim() != 2 or tokens.shape[0] != B or not tokens.is_contiguous() or \
+                tokens.device != dev:
+            raise FefError(FEF_ERR_INVALID_ARG, where)
+        L = tokens.shape[1]
+    bias_stride = stride_b = stride_k = 0
+    if bias is not None:
+        if bias.dtype != torch.float32 or bias.dim() not in (1, 2) or bias.shape[-1] < V or bias.device != dev or \
+                (bias.stride(-1) != 1 and V > 1) or (bias.dim() == 2 and bias.shape[0] != B):
+            raise FefError(FEF_ERR_INVALID_ARG, where)
+        bias_stride = bias.stride(0) if bias.dim() == 2 and B > 1 else 0
+    if allowed is not None:
+        words = (V + 31) // 32
+        if allowed.dtype != torch.int32 or allowed.dim() not in (1, 2, 3) or allowed.shape[-1] < words or \
+                allowed.device != dev or (allowed.stride(-1) != 1 and words > 1) or \
+                tuple(allowed.shape[:-1]) != (B, K)[:allowed.dim() - 1]:
+            raise FefError(FEF_ERR_INVALID_ARG, where)
+        stride_b = allowed.stride(0) if allowed.dim() >= 2 and B > 1 else 0
+        stride_k = allowed.stride(1) if allowed.dim() == 3 and K > 1 else 0
+    plain = out is not None and not with_norm and stream is None and torch.cuda.current_device() == dev.index
+    with (contextlib.nullcontext() if plain else _on(dev, stream)):
+        if out is None:
+            out = torch.empty_like(logits)
+        if with_norm and log2_norm is None:
+            log2_norm = torch.empty((B, K), dtype=torch.float64, device=dev)
+        if log2_norm is not None and workspace is None:
+            workspace = torch.empty(max(fef_logits_adjust_workspace_bytes(B, K, V), 256), dtype=torch.uint8, device=dev)
+        p = _ptr
+        st = load().fef_logits_adjust(
+            logits.data_ptr(), out.data_ptr(), B, K, V, ld, code, p(tokens), L, p(prompt_len), p(draft_tokens), p(row_len),
+            p(penalties), p(bias), bias_stride, p(allowed), stride_b, stride_k, float(temperature), p(log2_norm),
+            p(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+    if st != FEF_OK:
+        raise FefError(st, where)
+    return AdjustResult(out, log2_norm)
+
+
+def _ptr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()

@@ -1,0 +1,420 @@
+// fef_logits_adjust: penalties for repeated tokens, biases and grammar masks on the logits of speculative
+// windows, with the normaliser of every adjusted row (the input of fef_spec_verify_with_norms).
+//
+// For window b, position i and vocabulary id x, in binary32:
+//   h = occurrences of x in tokens[b, :] and among the window's drafts j < i,
+//   a = the same without the first prompt_len[b] tokens,
+//   y = l                                    if h = 0
+//       l / rep (l > 0), l * rep (l <= 0)    if h > 0
+//   y = y + (bias[x] - (freq * a + pres * [a > 0])),   y = -inf where the mask's bit is 0,
+//   out = y rounded to the logits' type,     log2_norm = log2 sum_x 2^(out_x * log2(e) / T).
+#include <cuda_runtime.h>
+#include <cuda_bf16.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "fef.h"
+#include "fef_common.cuh"
+#include "fef_device_math.cuh"
+
+namespace fef {
+namespace adj {
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kIdsPerThread = 8;                       // one 16-byte vector of bfloat16, two of binary32
+constexpr int kChunk = kThreads * kIdsPerThread;       // vocabulary ids per CTA
+constexpr int kRowsInFlight = 4;                       // rows whose loads a thread has in flight together
+constexpr uint32_t kInPrompt = 0x80000000u;            // history word: seen in the prompt; low bits count the answer
+
+struct Params {
+    const char* logits;
+    char* out;
+    int64_t ld_bytes;
+    const int32_t* tokens;       // [B][L]
+    const int32_t* prompt_len;   // [B] or null
+    const int32_t* drafts;       // [B][K] or null
+    const int32_t* row_len;      // [B] or null
+    const float* penalties;      // [B][3] or null
+    const float* bias;           // or null
+    int64_t bias_stride;
+    const uint32_t* allowed;     // or null
+    int64_t allowed_stride_b, allowed_stride_k;
+    int L, B, K, V, chunks, rows_per_cta;
+    float c;                     // log2(e) / T
+    double c_exact;
+    float2* partials;            // [B * K][chunks]: (largest logit m, sum of 2^((l - m) c))
+    double* log2_norm;           // [B * K]
+};
+
+__device__ __forceinline__ uint4 ld_stream_v4(const void* p) {
+    // (not .nc: the output may be the input)
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+                 : "l"(p)
+                 : "memory");
+    return r;
+}
+
+template <int DT>
+struct Row8 {  // a thread's eight logits of one row, as stored
+    uint4 v[DT == FEF_F32 ? 2 : 1];
+};
+
+template <int DT>
+__device__ __forceinline__ void unpack8(const Row8<DT>& r, float (&l)[8]) {
+    if constexpr (DT == FEF_F32) {
+        unpack<FEF_F32>(r.v[0], *reinterpret_cast<float(*)[4]>(&l[0]));
+        unpack<FEF_F32>(r.v[1], *reinterpret_cast<float(*)[4]>(&l[4]));
+    } else {
+        unpack<FEF_BF16>(r.v[0], l);
+    }
+}
+
+// Rounds to the stored type; l becomes the stored values.
+template <int DT>
+__device__ __forceinline__ Row8<DT> pack8(float (&l)[8]) {
+    Row8<DT> r;
+    if constexpr (DT == FEF_F32) {
+        r.v[0] = make_uint4(__float_as_uint(l[0]), __float_as_uint(l[1]), __float_as_uint(l[2]), __float_as_uint(l[3]));
+        r.v[1] = make_uint4(__float_as_uint(l[4]), __float_as_uint(l[5]), __float_as_uint(l[6]), __float_as_uint(l[7]));
+    } else {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(l[2 * j], l[2 * j + 1]);
+            w[j] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        r.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        unpack<FEF_BF16>(r.v[0], l);
+    }
+    return r;
+}
+
+template <int DT, bool NORM>
+__global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant__ Params P) {
+    __shared__ uint32_t s_hist[kChunk];
+    __shared__ int s_draft[FEF_MAX_K];
+    __shared__ float2 s_part[NORM ? FEF_MAX_K : 1][kWarps];
+    constexpr int E = Elem<DT>::kBytes;
+
+    const int b = blockIdx.z, k0 = blockIdx.y * P.rows_per_cta;
+    const int n = P.row_len ? min(max(__ldg(P.row_len + b), 0), P.K) : P.K;
+    const int k1 = min(k0 + P.rows_per_cta, n);
+    if (k0 >= k1) return;  // uniform over the CTA
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int chunk0 = blockIdx.x * kChunk, x0 = chunk0 + tid * kIdsPerThread;
+    const int valid = min(max(P.V - x0, 0), kIdsPerThread);
+
+    // ---- what stands in the text of this chunk's ids
+    float rep = 1.f, freq = 0.f, pres = 0.f;
+    uint32_t hist[kIdsPerThread];
+#pragma unroll
+    for (int j = 0; j < kIdsPerThread; ++j) hist[j] = 0u;
+    const bool counting = P.penalties != nullptr;
+    if (counting) {
+        rep = __ldg(P.penalties + 3 * b);
+        freq = __ldg(P.penalties + 3 * b + 1);
+        pres = __ldg(P.penalties + 3 * b + 2);
+        for (int j = tid; j < kChunk; j += kThreads) s_hist[j] = 0u;
+        if (tid < P.K) s_draft[tid] = P.drafts && tid < k1 ? __ldg(P.drafts + static_cast<int64_t>(b) * P.K + tid) : -1;
+        __syncthreads();
+        const int prompt = P.prompt_len ? __ldg(P.prompt_len + b) : 0;
+        const int32_t* text = P.tokens + static_cast<int64_t>(b) * P.L;
+        const unsigned width = min(P.V - chunk0, kChunk);
+        for (int t = tid; t < P.L; t += kThreads) {
+            const unsigned at = static_cast<unsigned>(__ldg(text + t)) - chunk0;  // (a negative id ends far above `width`)
+            if (at < width) {
+                if (t < prompt)
+                    atomicOr(s_hist + at, kInPrompt);
+                else
+                    atomicAdd(s_hist + at, 1u);
+            }
+        }
+        if (tid < k0) {
+            const unsigned at = static_cast<unsigned>(s_draft[tid]) - chunk0;
+            if (at < width) atomicAdd(s_hist + at, 1u);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < kIdsPerThread; ++j) hist[j] = s_hist[tid * kIdsPerThread + j];
+    }
+
+    // ---- the additive term and the repetition flags of this thread's ids
+    float bias[kIdsPerThread], add[kIdsPerThread];
+    unsigned repeated = 0u;
+#pragma unroll
+    for (int j = 0; j < kIdsPerThread; ++j) bias[j] = P.bias && j < valid ? __ldg(P.bias + b * P.bias_stride + x0 + j) : 0.f;
+    auto term = [&](int j) {
+        const uint32_t a = hist[j] & ~kInPrompt;
+        add[j] = a ? bias[j] - fmaf(freq, static_cast<float>(a), pres) : bias[j];
+        if (hist[j]) repeated |= 1u << j;
+    };
+#pragma unroll
+    for (int j = 0; j < kIdsPerThread; ++j) term(j);
+
+    const int64_t row0 = static_cast<int64_t>(b) * P.K;
+    const char* src = P.logits + row0 * P.ld_bytes + static_cast<int64_t>(x0) * E;
+    char* dst = P.out + row0 * P.ld_bytes + static_cast<int64_t>(x0) * E;
+    const unsigned char* bits = P.allowed
+        ? reinterpret_cast<const unsigned char*>(P.allowed + b * P.allowed_stride_b) + (x0 >> 3) : nullptr;
+
+    for (int i0 = k0; i0 < k1; i0 += kRowsInFlight) {
+        Row8<DT> raw[kRowsInFlight];
+        unsigned mask[kRowsInFlight];
+#pragma unroll
+        for (int r = 0; r < kRowsInFlight; ++r) {
+            const int i = i0 + r;
+            mask[r] = 0xFFu;
+            if (i < k1 && valid) {
+                const char* p = src + i * P.ld_bytes;
+                if (valid == kIdsPerThread) {
+                    raw[r].v[0] = ld_stream_v4(p);
+                    if constexpr (DT == FEF_F32) raw[r].v[1] = ld_stream_v4(p + 16);
+                } else {
+                    float l[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        l[j] = -INFINITY;
+                        if (j < valid) {
+                            if constexpr (DT == FEF_F32)
+                                l[j] = *reinterpret_cast<const volatile float*>(p + 4 * j);
+                            else
+                                l[j] = __uint_as_float(
+                                    static_cast<uint32_t>(*reinterpret_cast<const volatile unsigned short*>(p + 2 * j)) << 16);
+                        }
+                    }
+                    raw[r] = pack8<DT>(l);
+                }
+                if (bits) mask[r] = __ldg(bits + i * P.allowed_stride_k * 4);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRowsInFlight; ++r) {
+            const int i = i0 + r;
+            if (i >= k1) break;
+            float l[8];
+            if (valid) {
+                unpack8<DT>(raw[r], l);
+                if (repeated) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (repeated >> j & 1u) l[j] = l[j] > 0.f ? l[j] / rep : l[j] * rep;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) l[j] = (mask[r] >> j & 1u) ? l[j] + add[j] : -INFINITY;
+                if (valid < kIdsPerThread) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j >= valid) l[j] = -INFINITY;
+                }
+                const Row8<DT> w = pack8<DT>(l);
+                char* q = dst + i * P.ld_bytes;
+                if (valid == kIdsPerThread) {
+                    *reinterpret_cast<uint4*>(q) = w.v[0];
+                    if constexpr (DT == FEF_F32) *reinterpret_cast<uint4*>(q + 16) = w.v[1];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < valid) {
+                            if constexpr (DT == FEF_F32)
+                                reinterpret_cast<float*>(q)[j] = l[j];
+                            else
+                                reinterpret_cast<unsigned short*>(q)[j] = static_cast<unsigned short>(__float_as_uint(l[j]) >> 16);
+                        }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) l[j] = -INFINITY;
+            }
+            if constexpr (NORM) {
+                // Relative to the warp's largest logit, subtracted before the scaling: a row whose entries are all the
+                // type's lowest value then has a normaliser like any other.
+                float m = l[0];
+#pragma unroll
+                for (int j = 1; j < 8; ++j) m = fmaxf(m, l[j]);
+                m = float_unorder(__reduce_max_sync(0xFFFFFFFFu, float_order(m != m ? -INFINITY : m)));
+                const float top = m > -INFINITY ? m : 0.f;
+                float s = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s += ex2_approx((l[j] - top) * P.c);
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+                if (lane == 0) s_part[i - k0][warp] = make_float2(top, s);
+            }
+            // the draft of this position counts for the positions behind it
+            if (counting && P.drafts) {
+                const unsigned at = static_cast<unsigned>(s_draft[i]) - x0;
+                if (at < static_cast<unsigned>(valid)) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (at == static_cast<unsigned>(j)) {
+                            ++hist[j];
+                            term(j);
+                        }
+                }
+            }
+        }
+    }
+    if constexpr (NORM) {
+        __syncthreads();
+        for (int i = k0 + tid; i < k1; i += kThreads) {
+            float top = -INFINITY, sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w)
+                if (s_part[i - k0][w].y != 0.f) top = fmaxf(top, s_part[i - k0][w].x);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w)
+                if (s_part[i - k0][w].y != 0.f) sum += s_part[i - k0][w].y * ex2_approx((s_part[i - k0][w].x - top) * P.c);
+            P.partials[(row0 + i) * P.chunks + blockIdx.x] = make_float2(top, sum);
+        }
+    }
+}
+
+// log2 of the row sums from the chunks' partial sums, in double precision: one warp per row.
+__global__ void __launch_bounds__(kThreads) adjust_norm_kernel(const __grid_constant__ Params P) {
+    cudaGridDependencySynchronize();
+    const int lane = threadIdx.x & 31;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    if (row >= static_cast<int64_t>(P.B) * P.K) return;
+    const int b = static_cast<int>(row / P.K), i = static_cast<int>(row - static_cast<int64_t>(b) * P.K);
+    const int n = P.row_len ? min(max(__ldg(P.row_len + b), 0), P.K) : P.K;
+    if (i >= n) {
+        if (lane == 0) P.log2_norm[row] = 0.0;
+        return;
+    }
+    double m = -INFINITY, s = 0.0;
+    for (int c = lane; c < P.chunks; c += 32) {
+        const float2 p = P.partials[row * P.chunks + c];
+        if (p.y != 0.f) {  // (a NaN sum poisons the row)
+            const double nm = fmax(m, static_cast<double>(p.x));
+            s = (m > -INFINITY ? s * exp2((m - nm) * P.c_exact) : 0.0) +
+                static_cast<double>(p.y) * exp2((static_cast<double>(p.x) - nm) * P.c_exact);
+            m = nm;
+        }
+    }
+    const double top = warp_max(m);
+    const double sum = warp_sum(m > -INFINITY ? s * exp2((m - top) * P.c_exact) : 0.0);
+    if (lane == 0)
+        P.log2_norm[row] = sum > 0.0 && sum < INFINITY ? top * P.c_exact + log2(sum) : static_cast<double>(NAN);
+}
+
+static int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
+
+static bool sizes_ok(int B, int K, int V) {
+    return B >= 1 && B <= FEF_MAX_B && K >= 1 && K <= FEF_MAX_K && V >= 1 && V <= (1 << 28);
+}
+
+template <int DT>
+static void launch(const Params& P, int splits, bool norm, cudaStream_t stream) {
+    const dim3 grid(P.chunks, splits, P.B);
+    if (norm)
+        adjust_kernel<DT, true><<<grid, kThreads, 0, stream>>>(P);
+    else
+        adjust_kernel<DT, false><<<grid, kThreads, 0, stream>>>(P);
+}
+
+}  // namespace adj
+}  // namespace fef
+
+extern "C" {
+
+size_t fef_logits_adjust_workspace_bytes(int B, int K, int V) {
+    using namespace fef::adj;
+    if (!sizes_ok(B, K, V)) return 0;
+    return static_cast<size_t>(B) * K * chunks_of(V) * sizeof(float2);
+}
+
+fef_status fef_logits_adjust(const void* logits, void* out, int B, int K, int V, int64_t ld, fef_dtype dt,
+                             const int32_t* tokens, int L, const int32_t* prompt_len, const int32_t* draft_tokens,
+                             const int32_t* row_len, const float* penalties, const float* bias, int64_t bias_stride,
+                             const uint32_t* allowed, int64_t allowed_stride_b, int64_t allowed_stride_k,
+                             float temperature, double* log2_norm, void* workspace, size_t workspace_bytes,
+                             void* cuda_stream) {
+    using namespace fef;
+    using namespace fef::adj;
+    if (dt != FEF_F32 && dt != FEF_BF16) return FEF_ERR_DTYPE;
+    if (!logits || !out || !sizes_ok(B, K, V) || ld < V) return FEF_ERR_INVALID_ARG;
+    if (L < 0 || L > (1 << 24) || (L > 0 && !tokens)) return FEF_ERR_INVALID_ARG;
+    if (!(temperature >= 0.0f) || isinf(temperature)) return FEF_ERR_INVALID_ARG;
+    if (bias && bias_stride != 0 && bias_stride < V) return FEF_ERR_INVALID_ARG;
+    const int64_t words = (static_cast<int64_t>(V) + 31) / 32;
+    if (allowed && ((allowed_stride_b != 0 && allowed_stride_b < words) || (allowed_stride_k != 0 && allowed_stride_k < words)))
+        return FEF_ERR_INVALID_ARG;
+    const int esize = dt == FEF_F32 ? 4 : 2;
+    if ((reinterpret_cast<uintptr_t>(logits) & 15) || (reinterpret_cast<uintptr_t>(out) & 15) || ((ld * esize) & 15))
+        return FEF_ERR_ALIGNMENT;
+    for (const void* p : {static_cast<const void*>(tokens), static_cast<const void*>(prompt_len),
+                          static_cast<const void*>(draft_tokens), static_cast<const void*>(row_len),
+                          static_cast<const void*>(penalties), static_cast<const void*>(bias),
+                          static_cast<const void*>(allowed)})
+        if (reinterpret_cast<uintptr_t>(p) & 3) return FEF_ERR_ALIGNMENT;
+    if (reinterpret_cast<uintptr_t>(log2_norm) & 7) return FEF_ERR_ALIGNMENT;
+    const uintptr_t bytes = static_cast<uintptr_t>(B) * K * ld * esize;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(logits), to = reinterpret_cast<uintptr_t>(out);
+    if (from != to && from < to + bytes && to < from + bytes) return FEF_ERR_INVALID_ARG;  // in place, or apart
+    if (log2_norm && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) ||
+                      workspace_bytes < fef_logits_adjust_workspace_bytes(B, K, V)))
+        return FEF_ERR_WORKSPACE;
+
+    Params P = {};
+    const double c = 1.4426950408889634074 / (temperature == 0.0f ? 1.0 : static_cast<double>(temperature));
+    P.c_exact = c;
+    P.c = static_cast<float>(c);
+    if (!(P.c > 0.f) || isinf(P.c)) return FEF_ERR_INVALID_ARG;
+
+    int dev = -1, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1)
+        return FEF_ERR_CUDA;
+
+    P.logits = static_cast<const char*>(logits);
+    P.out = static_cast<char*>(out);
+    P.ld_bytes = ld * esize;
+    P.tokens = tokens;
+    P.prompt_len = prompt_len;
+    P.drafts = draft_tokens;
+    P.row_len = row_len;
+    P.penalties = penalties;
+    P.bias = bias;
+    P.bias_stride = bias_stride;
+    P.allowed = allowed;
+    P.allowed_stride_b = allowed_stride_b;
+    P.allowed_stride_k = allowed_stride_k;
+    P.L = L;
+    P.B = B;
+    P.K = K;
+    P.V = V;
+    P.chunks = chunks_of(V);
+    P.partials = static_cast<float2*>(workspace);
+    P.log2_norm = log2_norm;
+    // A window's positions are shared out over CTAs only as far as the SMs need them: every CTA reads the text once.
+    int64_t splits = (static_cast<int64_t>(sms) * 8 + static_cast<int64_t>(P.chunks) * B - 1) / (static_cast<int64_t>(P.chunks) * B);
+    const int most = (K + kRowsInFlight - 1) / kRowsInFlight;
+    if (splits > most) splits = most;
+    P.rows_per_cta = ((K + static_cast<int>(splits) - 1) / static_cast<int>(splits) + kRowsInFlight - 1) / kRowsInFlight * kRowsInFlight;
+    splits = (K + P.rows_per_cta - 1) / P.rows_per_cta;
+
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (dt == FEF_F32)
+        launch<FEF_F32>(P, static_cast<int>(splits), log2_norm != nullptr, stream);
+    else
+        launch<FEF_BF16>(P, static_cast<int>(splits), log2_norm != nullptr, stream);
+    if (cudaGetLastError() != cudaSuccess) return FEF_ERR_CUDA;
+    if (log2_norm) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>(B) * K + kWarps - 1) / kWarps));
+        cfg.blockDim = dim3(kThreads);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if (cudaLaunchKernelEx(&cfg, adjust_norm_kernel, P) != cudaSuccess) return FEF_ERR_CUDA;
+    }
+    return FEF_OK;
+}
+
+}  // extern "C"
