@@ -465,6 +465,43 @@ fef_status fef_lmhead_logits(const void* hidden, const void* weight, int rows, i
                              float* logits, int64_t ldo, int32_t* device_status, void* cuda_stream);
 
 /*
+ * The output layer in 4 bits (of the paper's model outputs, Section 3.2, only their storage changes).  A row's d weights are
+ * cut into groups of 32, 64 or 128; the layer stands for the values (q - z) * s with q in 0 .. 15, one scale s
+ * (bfloat16) and one zero point z (0 .. 15; 8 for a layer without zero points) per group.
+ *
+ *   packed   device, [V][blocks * 64] bytes, blocks = ceil(d / 128): every 64 bytes hold 128 columns; of their 32-bit words,
+ *            word 4 t + w holds columns 32 w + 8 t .. 32 w + 8 t + 7, lowest nibble first
+ *   scale    device, [blocks][Vp][128 / group] bfloat16, Vp = V rounded up to a multiple of 32; zero behind d and V
+ *   zero     device, uint8, laid out like scale; or NULL
+ *   d        a multiple of `group`; all three buffers 16-byte aligned
+ *
+ * fef_lmhead_quantize writes such a layer (all three buffers in full, padding included) from weight, device, [V][d] bfloat16
+ * row-major, 16-byte aligned.  For every group, with rint to the nearest whole number, ties to even:
+ *   zero NULL:  s = bf16(max|w| / 7),  z = 8
+ *   otherwise:  lo = min(w, 0), hi = max(w, 0), s = bf16((hi - lo) / 15), z = min(max(rint(-lo / s), 0), 15)
+ *   q = min(max(rint(w / s) + z, 0), 15);  where s = 0:  q = z (8, or 0 with zero points)
+ * A group that holds NaN or an infinity (or whose range is none that binary32 has) gets the scale NaN, and device_status
+ * (device, [1] int32, or NULL) FEF_ERR_NONFINITE.  fef_lmhead_dequantize writes the values, [V][d] float32 (exact), 16-byte aligned.
+ *
+ * fef_lmhead_logits_quantized is fef_lmhead_logits with such a layer:
+ *   logits[r, v] = sum over groups g of s[v, g] * ( sum over k in g of (q[v, k] - z[v, g]) * hidden[r, k] ),
+ * products exact, both sums in binary32, the result rounded to `dt` (FEF_F32 or FEF_BF16) once.
+ *   hidden   device, [rows][d] bfloat16 row-major, 16-byte aligned, rows >= 1
+ *   logits   device out, [rows][ldo] of dtype `dt`, 16-byte aligned, ldo >= V and ldo * sizeof(element) a multiple of 16; the
+ *            entries between V and ldo are left as they were
+ *   device_status  device out, [1] int32, or NULL: FEF_OK, or FEF_ERR_TIMEOUT as in fef_spec_verify (the logits are then
+ *            incomplete)
+ * Asynchronous on `cuda_stream`.
+ */
+fef_status fef_lmhead_quantize(const void* weight, int V, int d, int group, void* packed, void* scale, void* zero,
+                               int32_t* device_status, void* cuda_stream);
+fef_status fef_lmhead_dequantize(const void* packed, const void* scale, const void* zero, int V, int d, int group,
+                                 float* values, void* cuda_stream);
+fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, const void* scale, const void* zero, int rows,
+                                       int V, int d, int group, void* logits, int64_t ldo, fef_dtype dt,
+                                       int32_t* device_status, void* cuda_stream);
+
+/*
  * Penalties for repeated tokens, biases and grammar masks on the logits of speculative windows (the paper
  * has no counterpart: requests carry such rules, and both laws of Section 3.2 have to obey them before the
  * draws and the verification).  For window b, position i < n_b (n_b = row_len[b], or K) and vocabulary id x,

@@ -33,7 +33,8 @@ EXPORTS = ("fef_status_string", "fef_spec_verify_workspace_bytes", "fef_spec_ver
            "fef_lmhead_verify_workspace_bytes", "fef_lmhead_verify", "fef_lmhead_logits",
            "fef_draft_sample_with_target", "fef_spec_verify_with_norms", "fef_synth_logits",
            "fef_loop_run_synthetic_workspace_bytes", "fef_loop_run_synthetic",
-           "fef_logits_adjust_workspace_bytes", "fef_logits_adjust")
+           "fef_logits_adjust_workspace_bytes", "fef_logits_adjust", "fef_lmhead_quantize", "fef_lmhead_dequantize",
+           "fef_lmhead_logits_quantized")
 
 _lib = None
 
@@ -122,6 +123,12 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     L.fef_lmhead_verify.restype = i32
     L.fef_lmhead_logits.argtypes = [vp, vp, i32, i32, i32, vp, i64, vp, vp]
     L.fef_lmhead_logits.restype = i32
+    L.fef_lmhead_quantize.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp]
+    L.fef_lmhead_quantize.restype = i32
+    L.fef_lmhead_dequantize.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
+    L.fef_lmhead_dequantize.restype = i32
+    L.fef_lmhead_logits_quantized.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, i32, vp, vp]
+    L.fef_lmhead_logits_quantized.restype = i32
     L.fef_logits_adjust_workspace_bytes.argtypes = [i32, i32, i32]
     L.fef_logits_adjust_workspace_bytes.restype = sz
     L.fef_logits_adjust.argtypes = [vp, vp, i32, i32, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, i64, vp, i64, i64, f32, vp,
@@ -680,6 +687,108 @@ def fef_loop_run_synthetic(B: int, L: int, K: int, V: int, dtype, temperature: f
     if st != FEF_OK:
         raise FefError(st, "fef_loop_run_synthetic")
     return dict(tokens=tokens, conf=conf, in_step=in_step, rounds=int(rnd.item()), device_status=int(status.item()))
+
+
+# ------------------------------------------------------------------ the output layer in 4 bits ----
+class QuantizedLayer(NamedTuple):
+    """An output layer [V, d] in 4 bits (layout and meaning: ``fef_lmhead_quantize`` in include/fef.h)."""
+    packed: torch.Tensor                           # [V, ceil(d / 128) * 64] uint8
+    scale: torch.Tensor                            # [ceil(d / 128), V rounded up to 32, 128 / group] bfloat16
+    zero: Optional[torch.Tensor]                   # the same shape, uint8; None: 8 everywhere
+    d: int
+    group: int
+    device_status: Optional[torch.Tensor] = None   # [1] int32 of the call that made it (read it after synchronising)
+
+
+def _quantized_layer(layer: QuantizedLayer, where: str):
+    """(V, blocks) of a layer whose tensors have the documented shapes and types."""
+    packed, scale, zero, d, group = layer[:5]
+    _require_cuda(packed, scale, zero)
+    if group not in (32, 64, 128) or d < group or d % group or packed.dim() != 2:
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    V, blocks = packed.shape[0], (d + 127) // 128
+    shape = (blocks, (V + 31) // 32 * 32, 128 // group)
+    if packed.dtype != torch.uint8 or packed.shape[1] != blocks * 64 or not packed.is_contiguous() or \
+            scale.dtype != torch.bfloat16 or scale.shape != shape or not scale.is_contiguous() or scale.device != packed.device:
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    if zero is not None and (zero.dtype != torch.uint8 or zero.shape != shape or not zero.is_contiguous() or
+                             zero.device != packed.device):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    return V, blocks
+
+
+def fef_lmhead_quantize(weight: torch.Tensor, group: int = 128, zero_points: bool = False, stream=None) -> QuantizedLayer:
+    """Bring an output layer ``weight`` ([V, d] bfloat16, ``d`` a multiple of ``group``) to 4 bits with one scale, and
+    with ``zero_points`` one zero point, per ``group`` (32, 64 or 128) weights of a row (see include/fef.h)."""
+    where = "fef_lmhead_quantize"
+    _require_cuda(weight)
+    _bf16_matrix(weight, where)
+    V, d = weight.shape
+    if group not in (32, 64, 128) or V < 1 or d < group or d % group:
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    dev, blocks = weight.device, (d + 127) // 128
+    with _on(dev, stream):
+        packed = torch.empty((V, blocks * 64), dtype=torch.uint8, device=dev)
+        scale = torch.empty((blocks, (V + 31) // 32 * 32, 128 // group), dtype=torch.bfloat16, device=dev)
+        zero = torch.empty(scale.shape, dtype=torch.uint8, device=dev) if zero_points else None
+        status = torch.empty(1, dtype=torch.int32, device=dev)
+        st = load().fef_lmhead_quantize(weight.data_ptr(), V, d, group, packed.data_ptr(), scale.data_ptr(), _ptr(zero),
+                                        status.data_ptr(), _stream_ptr(stream))
+    if st != FEF_OK:
+        raise FefError(st, where)
+    return QuantizedLayer(packed, scale, zero, d, group, status)
+
+
+def fef_lmhead_dequantize(layer: QuantizedLayer, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The values a 4-bit layer stands for, ``[V, d]`` float32 (exact)."""
+    where = "fef_lmhead_dequantize"
+    V, _ = _quantized_layer(layer, where)
+    dev = layer.packed.device
+    if out is not None and (out.dtype != torch.float32 or out.shape != (V, layer.d) or not out.is_contiguous() or out.device != dev):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    with _on(dev, stream):
+        if out is None:
+            out = torch.empty((V, layer.d), dtype=torch.float32, device=dev)
+        st = load().fef_lmhead_dequantize(layer.packed.data_ptr(), layer.scale.data_ptr(), _ptr(layer.zero), V, layer.d,
+                                          layer.group, out.data_ptr(), _stream_ptr(stream))
+    if st != FEF_OK:
+        raise FefError(st, where)
+    return out
+
+
+def fef_lmhead_logits_quantized(hidden: torch.Tensor, layer: QuantizedLayer, dtype=torch.float32,
+                                out: Optional[torch.Tensor] = None, stream=None):
+    """``fef_lmhead_logits`` with an output layer in 4 bits (see ``fef_lmhead_logits_quantized`` in include/fef.h).
+
+    ``hidden``: ``[rows, d]`` bfloat16.  Returns ``(logits [rows, ldo], device_status)``; the first ``V`` entries of
+    a row are the logits, float32 or bfloat16 (``dtype``, or that of ``out``); ``ldo`` covers whole 16-byte vectors, so
+    the result can be passed on to the verification as ``[B, K, ldo]`` with ``V=V``.
+    """
+    where = "fef_lmhead_logits_quantized"
+    V, _ = _quantized_layer(layer, where)
+    _bf16_matrix(hidden, where)
+    dev = layer.packed.device
+    rows, d = hidden.shape
+    if d != layer.d or hidden.device != dev or rows < 1:
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    if out is not None:
+        dtype = out.dtype
+        if out.dim() != 2 or out.shape[0] != rows or out.shape[1] < V or not out.is_contiguous() or out.device != dev:
+            raise FefError(FEF_ERR_INVALID_ARG, where)
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise FefError(FEF_ERR_DTYPE, where)
+    per_vec = 4 if dtype == torch.float32 else 8
+    with _on(dev, stream):
+        if out is None:
+            out = torch.empty((rows, (V + per_vec - 1) // per_vec * per_vec), dtype=dtype, device=dev)
+        status = torch.empty(1, dtype=torch.int32, device=dev)
+        st = load().fef_lmhead_logits_quantized(
+            hidden.data_ptr(), layer.packed.data_ptr(), layer.scale.data_ptr(), _ptr(layer.zero), rows, V, d, layer.group,
+            out.data_ptr(), out.shape[1], FEF_F32 if dtype == torch.float32 else FEF_BF16, status.data_ptr(),
+            _stream_ptr(stream))
+    if st != FEF_OK:
+        raise FefError(st, where)
+    return out, status
 
 
 # ------------------------------------------------------- penalties, biases and masks on the logits ----

@@ -1,0 +1,281 @@
+// The output layer in 4 bits: fef_lmhead_quantize, fef_lmhead_dequantize, fef_lmhead_logits_quantized.
+//
+// A row of d weights is cut into groups of G = 32, 64 or 128; a weight is (q - z) * s with q in 0..15, one scale s
+// (bfloat16) and one zero point z (0..15; 8 where the layer keeps none) per group.  q - z has five bits and s eight, so
+// the product is exact in binary32.
+//
+// Layout (kBlock = 128 columns are a block; a row is padded to whole blocks):
+//   packed [V][blocks * 64] bytes: of a block's sixteen 32-bit words, word 4 t + w holds the columns
+//          32 w + 8 t .. 32 w + 8 t + 7, lowest nibble first.  16 consecutive bytes (one t) therefore hold eight
+//          columns of every 32-column piece, which is what one lane of a matrix instruction's operand needs.
+//   scale, zero [blocks][V rounded up to 32][128 / G]: what a block of consecutive rows needs lies together; the
+//          entries behind d and V are zero.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "fef.h"
+#include "fef_common.cuh"
+#include "fef_device_math.cuh"
+
+namespace fef {
+namespace quant {
+
+constexpr int kBlock = 128;
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+
+struct Layer {
+    const uint8_t* packed;
+    const uint16_t* scale;
+    const uint8_t* zero;  // or null
+    int V, Vp, d, blocks, G;
+};
+
+__device__ __forceinline__ float bf16_value(uint16_t h) { return __uint_as_float(static_cast<uint32_t>(h) << 16); }
+
+// ------------------------------------------------------------------------------------------ quantize ----
+struct QuantizeParams {
+    const uint16_t* weight;  // [V][d]
+    uint8_t* packed;
+    uint16_t* scale;
+    uint8_t* zero;  // or null
+    int V, Vp, d, blocks, G;
+    int32_t* status;
+};
+
+// One warp per block of one row: lane 8 w... holds the four columns 4 lane .. 4 lane + 3.
+__global__ void __launch_bounds__(kThreads) quantize_kernel(const __grid_constant__ QuantizeParams P) {
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    if (unit >= static_cast<int64_t>(P.Vp) * P.blocks) return;
+    const int c = static_cast<int>(unit % P.blocks), v = static_cast<int>(unit / P.blocks);
+    const int k = c * kBlock + lane * 4;
+    float w[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool real = v < P.V && k < P.d;  // (d is a multiple of 32: a lane's four columns exist or do not)
+    if (real) {
+        const uint2 r = *reinterpret_cast<const uint2*>(P.weight + static_cast<int64_t>(v) * P.d + k);
+        w[0] = __uint_as_float(r.x << 16);
+        w[1] = __uint_as_float(r.x & 0xFFFF0000u);
+        w[2] = __uint_as_float(r.y << 16);
+        w[3] = __uint_as_float(r.y & 0xFFFF0000u);
+    }
+    float lo = fminf(fminf(w[0], w[1]), fminf(w[2], w[3])), hi = fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3]));
+    // (differences of infinities and NaN are NaN: bad stays 0 for numbers alone)
+    float bad = (w[0] - w[0]) + (w[1] - w[1]) + (w[2] - w[2]) + (w[3] - w[3]);
+    const int lanes = P.G / 4;
+    for (int o = 1; o < lanes; o <<= 1) {
+        lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, o));
+        hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
+        bad += __shfl_xor_sync(0xFFFFFFFFu, bad, o);
+    }
+    lo = fminf(lo, 0.f);
+    hi = fmaxf(hi, 0.f);
+    const float range = P.zero ? __fdiv_rn(hi - lo, 15.f) : __fdiv_rn(fmaxf(hi, -lo), 7.f);
+    uint16_t sbits = __bfloat16_as_ushort(__float2bfloat16_rn(range));
+    if (!(range < INFINITY)) bad = range;
+    if (bad != 0.f) sbits = 0x7FC0;  // the group's values are NaN
+    const float s = bf16_value(sbits);
+    float z = P.zero ? 0.f : 8.f;
+    if (P.zero && s > 0.f) z = fminf(fmaxf(rintf(__fdiv_rn(-lo, s)), 0.f), 15.f);
+    uint32_t nibbles = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float q = s > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(w[j], s)) + z, 0.f), 15.f) : z;
+        nibbles |= static_cast<uint32_t>(q) << (4 * j);
+    }
+    // columns 4 lane .. 4 lane + 3: piece w = lane / 8, t = (lane / 2) % 4, upper or lower half of the word
+    if (v < P.V)
+        *reinterpret_cast<uint16_t*>(P.packed + static_cast<int64_t>(v) * P.blocks * 64 + c * 64 + ((lane >> 1) & 3) * 16 +
+                                     (lane >> 3) * 4 + (lane & 1) * 2) = static_cast<uint16_t>(nibbles);
+    if (lane % lanes == 0) {
+        const int64_t at = (static_cast<int64_t>(c) * P.Vp + v) * (kBlock / P.G) + lane / lanes;
+        P.scale[at] = real ? sbits : uint16_t(0);
+        if (P.zero) P.zero[at] = real ? static_cast<uint8_t>(z) : uint8_t(0);
+        if (real && bad != 0.f) report(P.status, FEF_ERR_NONFINITE);
+    }
+}
+
+// ---------------------------------------------------------------------------------------- dequantize ----
+__global__ void __launch_bounds__(kThreads) dequantize_kernel(const __grid_constant__ Layer P, float* __restrict__ out) {
+    const int lane = threadIdx.x & 31;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    if (unit >= static_cast<int64_t>(P.V) * P.blocks) return;
+    const int c = static_cast<int>(unit % P.blocks), v = static_cast<int>(unit / P.blocks);
+    const int k = c * kBlock + lane * 4;
+    if (k >= P.d) return;
+    const uint32_t nibbles = *reinterpret_cast<const uint16_t*>(P.packed + static_cast<int64_t>(v) * P.blocks * 64 + c * 64 +
+                                                                ((lane >> 1) & 3) * 16 + (lane >> 3) * 4 + (lane & 1) * 2);
+    const int64_t at = (static_cast<int64_t>(c) * P.Vp + v) * (kBlock / P.G) + lane * 4 / P.G;
+    const float s = bf16_value(P.scale[at]);
+    const int z = P.zero ? P.zero[at] : 8;
+    float4 r;
+    r.x = static_cast<float>(static_cast<int>(nibbles & 15u) - z) * s;
+    r.y = static_cast<float>(static_cast<int>(nibbles >> 4 & 15u) - z) * s;
+    r.z = static_cast<float>(static_cast<int>(nibbles >> 8 & 15u) - z) * s;
+    r.w = static_cast<float>(static_cast<int>(nibbles >> 12) - z) * s;
+    *reinterpret_cast<float4*>(out + static_cast<int64_t>(v) * P.d + k) = r;
+}
+
+// ------------------------------------------------------------------------------------------- product ----
+struct ProductParams {
+    Layer layer;
+    const uint16_t* hidden;  // [rows][d]
+    char* out;               // [rows][ldo]
+    int64_t ldo;
+    int rows;
+    int32_t* status;
+};
+
+constexpr int kRowBlock = 8;
+
+// One warp per vocabulary row and eight hidden rows; a lane takes eight columns of every other 128-column block's half.
+template <int DT>
+__global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant__ ProductParams P) {
+    const Layer& W = P.layer;
+    const int lane = threadIdx.x & 31;
+    const int64_t v = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    const int r0 = blockIdx.y * kRowBlock, n = min(kRowBlock, P.rows - r0);
+    if (P.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *P.status = FEF_OK;
+    if (v >= W.V) return;
+    float acc[kRowBlock];
+#pragma unroll
+    for (int r = 0; r < kRowBlock; ++r) acc[r] = 0.f;
+    const int word = lane & 15;                       // t = word / 4, piece = word % 4
+    const int inside = 32 * (word & 3) + 8 * (word >> 2);
+    for (int c = lane >> 4; c < W.blocks; c += 2) {
+        const int k = c * kBlock + inside;
+        if (k >= W.d) continue;
+        const uint32_t q = *reinterpret_cast<const uint32_t*>(W.packed + v * W.blocks * 64 + c * 64 + word * 4);
+        const int64_t at = (static_cast<int64_t>(c) * W.Vp + v) * (kBlock / W.G) + inside / W.G;
+        const float s = bf16_value(W.scale[at]);
+        const int z = W.zero ? W.zero[at] : 8;
+        float w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = static_cast<float>(static_cast<int>(q >> (4 * j) & 15u) - z);
+#pragma unroll
+        for (int r = 0; r < kRowBlock; ++r) {
+            if (r >= n) break;
+            const uint16_t* h = P.hidden + static_cast<int64_t>(r0 + r) * W.d + k;
+            float part = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) part = fmaf(w[j], bf16_value(h[j]), part);
+            acc[r] = fmaf(part, s, acc[r]);
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kRowBlock; ++r) {
+        if (r >= n) break;
+        float a = acc[r];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+        if (lane == 0) {
+            const int64_t at = static_cast<int64_t>(r0 + r) * P.ldo + v;
+            if constexpr (DT == FEF_F32)
+                reinterpret_cast<float*>(P.out)[at] = a;
+            else
+                reinterpret_cast<__nv_bfloat16*>(P.out)[at] = __float2bfloat16_rn(a);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- host ----
+static bool layer_ok(int V, int d, int G) {
+    return V >= 1 && V <= (1 << 28) && (G == 32 || G == 64 || G == 128) && d >= G && d <= (1 << 20) && d % G == 0;
+}
+static Layer make_layer(const void* packed, const void* scale, const void* zero, int V, int d, int G) {
+    Layer W;
+    W.packed = static_cast<const uint8_t*>(packed);
+    W.scale = static_cast<const uint16_t*>(scale);
+    W.zero = static_cast<const uint8_t*>(zero);
+    W.V = V;
+    W.Vp = (V + 31) / 32 * 32;
+    W.d = d;
+    W.blocks = (d + kBlock - 1) / kBlock;
+    W.G = G;
+    return W;
+}
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+static bool have_device() {
+    int dev = -1;
+    return cudaGetDevice(&dev) == cudaSuccess;
+}
+
+}  // namespace quant
+}  // namespace fef
+
+extern "C" {
+
+fef_status fef_lmhead_quantize(const void* weight, int V, int d, int group, void* packed, void* scale, void* zero,
+                               int32_t* device_status, void* cuda_stream) {
+    using namespace fef;
+    using namespace fef::quant;
+    if (!weight || !packed || !scale || !layer_ok(V, d, group)) return FEF_ERR_INVALID_ARG;
+    if (!aligned16(weight) || !aligned16(packed) || !aligned16(scale) || !aligned16(zero)) return FEF_ERR_ALIGNMENT;
+    if (!have_device()) return FEF_ERR_CUDA;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (device_status && cudaMemsetAsync(device_status, 0, sizeof(int32_t), stream) != cudaSuccess) return FEF_ERR_CUDA;
+    QuantizeParams P;
+    const Layer W = make_layer(packed, scale, zero, V, d, group);
+    P.weight = static_cast<const uint16_t*>(weight);
+    P.packed = static_cast<uint8_t*>(packed);
+    P.scale = static_cast<uint16_t*>(scale);
+    P.zero = static_cast<uint8_t*>(zero);
+    P.V = V;
+    P.Vp = W.Vp;
+    P.d = d;
+    P.blocks = W.blocks;
+    P.G = group;
+    P.status = device_status;
+    const int64_t units = static_cast<int64_t>(W.Vp) * W.blocks;
+    const int64_t grid = (units + kWarps - 1) / kWarps;
+    if (grid > 0x7FFFFFFF) return FEF_ERR_INVALID_ARG;
+    quantize_kernel<<<static_cast<unsigned>(grid), kThreads, 0, stream>>>(P);
+    return cudaGetLastError() == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
+}
+
+fef_status fef_lmhead_dequantize(const void* packed, const void* scale, const void* zero, int V, int d, int group,
+                                 float* values, void* cuda_stream) {
+    using namespace fef;
+    using namespace fef::quant;
+    if (!packed || !scale || !values || !layer_ok(V, d, group)) return FEF_ERR_INVALID_ARG;
+    if (!aligned16(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(values)) return FEF_ERR_ALIGNMENT;
+    if (!have_device()) return FEF_ERR_CUDA;
+    const Layer W = make_layer(packed, scale, zero, V, d, group);
+    const int64_t grid = (static_cast<int64_t>(V) * W.blocks + kWarps - 1) / kWarps;
+    if (grid > 0x7FFFFFFF) return FEF_ERR_INVALID_ARG;
+    dequantize_kernel<<<static_cast<unsigned>(grid), kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(W, values);
+    return cudaGetLastError() == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
+}
+
+fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, const void* scale, const void* zero, int rows,
+                                       int V, int d, int group, void* logits, int64_t ldo, fef_dtype dt,
+                                       int32_t* device_status, void* cuda_stream) {
+    using namespace fef;
+    using namespace fef::quant;
+    if (dt != FEF_F32 && dt != FEF_BF16) return FEF_ERR_DTYPE;
+    if (!hidden || !packed || !scale || !logits || !layer_ok(V, d, group)) return FEF_ERR_INVALID_ARG;
+    if (rows < 1 || rows > (1 << 24) || ldo < V) return FEF_ERR_INVALID_ARG;
+    if (!aligned16(hidden) || !aligned16(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(logits) ||
+        (ldo * (dt == FEF_F32 ? 4 : 2)) % 16)
+        return FEF_ERR_ALIGNMENT;
+    if (!have_device()) return FEF_ERR_CUDA;
+    ProductParams P;
+    P.layer = make_layer(packed, scale, zero, V, d, group);
+    P.hidden = static_cast<const uint16_t*>(hidden);
+    P.out = static_cast<char*>(logits);
+    P.ldo = ldo;
+    P.rows = rows;
+    P.status = device_status;
+    const dim3 grid((V + kWarps - 1) / kWarps, (rows + kRowBlock - 1) / kRowBlock);
+    if (grid.y > 65535) return FEF_ERR_INVALID_ARG;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (dt == FEF_F32)
+        product_kernel<FEF_F32><<<grid, kThreads, 0, stream>>>(P);
+    else
+        product_kernel<FEF_BF16><<<grid, kThreads, 0, stream>>>(P);
+    return cudaGetLastError() == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
+}
+
+}  // extern "C"

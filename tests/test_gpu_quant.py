@@ -1,0 +1,222 @@
+"""The output layer in 4 bits against its definition in 64 bits (needs a B200)."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def fef():
+    import paper_2605_14305_b200 as lib
+
+    lib.load(build_if_missing=True)
+    return lib
+
+
+def _values(weight, group, zero_points):
+    """(values [V, d], scales [V, d / group]) of the quantised layer in 64 bits, on the host."""
+    V, d = weight.shape
+    w = weight.double().cpu().view(V, d // group, group)
+    if zero_points:
+        lo, hi = w.amin(-1).clamp(max=0.0), w.amax(-1).clamp(min=0.0)
+        s = ((hi - lo) / 15).to(torch.bfloat16).double()
+        z = torch.where(s > 0, (-lo / s).round().clamp(0, 15), torch.zeros_like(s))
+    else:
+        s = (w.abs().amax(-1) / 7).to(torch.bfloat16).double()
+        z = torch.full_like(s, 8.0)
+    q = torch.where(s[..., None] > 0, (w / s[..., None]).round() + z[..., None], z[..., None]).clamp(0, 15)
+    return ((q - z[..., None]) * s[..., None]).view(V, d), s
+
+
+SHAPES = [(1, 32, 32), (3, 64, 32), (33, 96, 32), (31, 128, 128), (65, 192, 64), (257, 1056, 32), (1000, 1152, 128), (100, 4096, 64)]
+
+
+@pytest.mark.parametrize("V,d,group", SHAPES)
+@pytest.mark.parametrize("zero_points", [False, True])
+def test_quantized_values(fef, V, d, group, zero_points):
+    g = torch.Generator(device="cuda").manual_seed(V + d)
+    w = torch.randn((V, d), generator=g, device="cuda") + 0.3
+    w = torch.where(torch.rand((V, d), generator=g, device="cuda") < 0.3, w.mul(4).round().div(4), w).to(torch.bfloat16)  # (ties)
+    layer = fef.fef_lmhead_quantize(w, group, zero_points)
+    got = fef.fef_lmhead_dequantize(layer)
+    torch.cuda.synchronize()
+    ref, s = _values(w, group, zero_points)
+    assert torch.equal(got.cpu().double(), ref)              # bit for bit: (q - z) s is exact in binary32
+    # half a step of the scale, and what rounding the scale to bfloat16 moves the largest weight by (15 steps at most)
+    off = (ref.view(V, -1, group) - w.cpu().double().view(V, -1, group)).abs()
+    assert (off <= s[..., None] * (0.5 + 15 * 2.0 ** -8 + (0.5 if zero_points else 0.0))).all()
+    blocks, Vp = (d + 127) // 128, (V + 31) // 32 * 32
+    flat = layer.scale.float().cpu().transpose(0, 1).reshape(Vp, -1)
+    assert torch.equal(flat[:V, :d // group].double(), s) and (flat[V:] == 0).all() and (flat[:, d // group:] == 0).all()
+    assert int(layer.device_status.item()) == 0 and (layer.zero is None) == (not zero_points)
+
+
+@pytest.mark.parametrize("zero_points", [False, True])
+def test_weights_at_the_borders(fef, zero_points):
+    w = torch.zeros((12, 64), dtype=torch.bfloat16, device="cuda")
+    w[1] = 5.0                                               # one sign only
+    w[2] = -5.0
+    w[3, 7] = 1e-40                                          # a scale below the normal numbers, or zero
+    w[4] = torch.linspace(-7.5, 7.5, 64, device="cuda").to(torch.bfloat16)
+    w[5] = torch.arange(64, device="cuda").to(torch.bfloat16) * 0.25 - 7          # quotients on ties
+    w[6, 0], w[6, 1] = 3e38, -3e38
+    w[7, 40] = math.nan
+    w[8, 3] = math.inf
+    w[9, 33] = -math.inf
+    w[10] = torch.finfo(torch.bfloat16).tiny
+    layer = fef.fef_lmhead_quantize(w, 32, zero_points)
+    got = fef.fef_lmhead_dequantize(layer).cpu()
+    ref, _ = _values(w, 32, zero_points)
+    fine = torch.ones((12, 2), dtype=torch.bool)
+    for r, c in ((7, 1), (8, 0), (9, 1)) + (((6, 0),) if zero_points else ()):    # 6e38 is no binary32 number
+        fine[r, c] = False
+    fine = fine.repeat_interleave(32, 1)
+    assert torch.equal(got[fine].double(), ref[fine]) and torch.isnan(got[~fine]).all()
+    assert int(layer.device_status.item()) == fef.FEF_ERR_NONFINITE
+
+
+def _layer(fef, V, d, group, zero_points, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    w = (torch.randn((V, d), generator=g, device="cuda") + (0.2 if zero_points else 0.0)) * (2.0 / math.sqrt(d))
+    return fef.fef_lmhead_quantize(w.to(torch.bfloat16), group, zero_points), g
+
+
+def _check_product(fef, layer, hidden, dtype, out=None):
+    got, status = fef.fef_lmhead_logits_quantized(hidden, layer, dtype=dtype, out=out)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    V, d = layer.packed.shape[0], layer.d
+    w = fef.fef_lmhead_dequantize(layer).double()
+    h = hidden.double()
+    ref, scale = h @ w.T, h.abs() @ w.abs().T
+    # A group's sum of at most 128 exact products, its scaling and the sum over the groups: every addition rounds, or in a
+    # matrix instruction cuts off, at most one step 2^-23 of what has been added up so far; d / 8 + d / 32 additions bound
+    # the length of the chain (no product is added alone: eight at least are added together), and a chain's partial sums
+    # are below sum |h w|.  The errors are independent enough for the square root of the length with a factor of 4.
+    bound = 4 * 2.0 ** -23 * math.sqrt(d / 8 + d / 32) * scale + 1e-37
+    if dtype == torch.bfloat16:
+        bound = bound + torch.finfo(dtype).eps / 2 * (ref.abs() + bound)
+    err = (got[:, :V].double() - ref).abs()
+    assert (err <= bound).all(), float((err / bound).max())
+    return got
+
+
+PRODUCTS = [
+    # rows, V, d, group, zero points, dtype
+    (1, 1, 32, 32, True, torch.float32),
+    (1, 5, 96, 32, False, torch.bfloat16),
+    (2, 33, 64, 64, True, torch.float32),
+    (3, 31, 160, 32, True, torch.bfloat16),
+    (5, 257, 192, 64, False, torch.float32),
+    (7, 300, 384, 128, True, torch.float32),
+    (8, 1000, 1056, 32, True, torch.bfloat16),
+    (9, 1001, 1152, 128, False, torch.float32),
+    (15, 511, 4096, 128, True, torch.float32),
+    (16, 513, 4096, 64, False, torch.bfloat16),
+    (17, 700, 256, 32, False, torch.float32),
+    (31, 129, 576, 64, True, torch.float32),
+    (33, 2049, 1280, 128, True, torch.bfloat16),
+    (64, 5003, 1024, 128, False, torch.float32),
+    (65, 130, 3584, 64, True, torch.float32),
+    (100, 385, 8192, 128, True, torch.bfloat16),
+    (128, 4099, 512, 32, True, torch.float32),
+    (257, 1027, 1152, 128, False, torch.float32),
+    (600, 900, 320, 64, True, torch.bfloat16),
+    (1, 20000, 4096, 128, False, torch.float32),
+    (4, 40001, 2048, 64, True, torch.bfloat16),
+    (12, 126464, 1024, 128, False, torch.float32),
+    (16, 600, 16384, 128, True, torch.float32),
+]
+
+
+@pytest.mark.parametrize("rows,V,d,group,zero_points,dtype", PRODUCTS)
+def test_product(fef, rows, V, d, group, zero_points, dtype):
+    layer, g = _layer(fef, V, d, group, zero_points, seed=rows + V + d)
+    hidden = torch.randn((rows, d), generator=g, device="cuda").to(torch.bfloat16)
+    _check_product(fef, layer, hidden, dtype)
+
+
+def test_product_leaves_the_padding_and_repeats_itself(fef):
+    for rows in (3, 40, 300):
+        layer, g = _layer(fef, 1003, 640, 64, True, seed=rows)
+        hidden = torch.randn((rows, 640), generator=g, device="cuda").to(torch.bfloat16)
+        out = torch.full((rows, 1064), 55.0, device="cuda")
+        first = _check_product(fef, layer, hidden, torch.float32, out=out).clone()
+        assert (out[:, 1003:] == 55).all()
+        again, _ = fef.fef_lmhead_logits_quantized(hidden, layer, out=out)
+        assert torch.equal(first, again)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        other, _ = fef.fef_lmhead_logits_quantized(hidden, layer, stream=s)
+        s.synchronize()
+        assert torch.equal(first[:, :1003], other[:, :1003])
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            fef.fef_lmhead_logits_quantized(hidden, layer, out=out)
+        hidden.mul_(2.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[:, :1003], first[:, :1003] * 2)
+
+
+@pytest.mark.parametrize("rows", [2, 24, 200])
+def test_values_that_are_not_numbers_stay_in_their_rows(fef, rows):
+    layer, g = _layer(fef, 700, 256, 128, False, seed=1)
+    hidden = torch.randn((rows, 256), generator=g, device="cuda").to(torch.bfloat16)
+    clean = _check_product(fef, layer, hidden, torch.float32).clone()
+    hidden[1, 77] = math.nan
+    dirty, _ = fef.fef_lmhead_logits_quantized(hidden, layer)
+    keep = torch.arange(rows, device="cuda") != 1
+    assert torch.equal(dirty[keep][:, :700], clean[keep][:, :700]) and torch.isnan(dirty[1, :700]).all()
+    scale = layer.scale.clone()
+    scale[1, 5, 0] = math.nan
+    hidden[1, 77] = 0.5
+    dirty, _ = fef.fef_lmhead_logits_quantized(hidden, layer._replace(scale=scale))
+    other = torch.arange(700, device="cuda") != 5
+    base, _ = fef.fef_lmhead_logits_quantized(hidden, layer)
+    assert torch.equal(dirty[:, :700][:, other], base[:, :700][:, other]) and torch.isnan(dirty[:, 5]).all()
+
+
+@pytest.mark.parametrize("rows", [1, 20])
+def test_offsets_beyond_32_bits(fef, rows):
+    V, d = 300000, 16384                                     # 2.5 GB of nibbles, 9.8 GB of weights
+    row = torch.randn((1, d), device="cuda").to(torch.bfloat16)
+    last = fef.fef_lmhead_quantize(row, 128)
+    Vp = (V + 31) // 32 * 32
+    packed = torch.zeros((V, d // 2), dtype=torch.uint8, device="cuda")
+    scale = torch.zeros((d // 128, Vp, 1), dtype=torch.bfloat16, device="cuda")
+    packed[-1], scale[:, V - 1] = last.packed[0], last.scale[:, 0]
+    hidden = torch.randn((rows, d), device="cuda").to(torch.bfloat16)
+    got, _ = fef.fef_lmhead_logits_quantized(hidden, fef.QuantizedLayer(packed, scale, None, d, 128))
+    ref, _ = fef.fef_lmhead_logits_quantized(hidden, last)
+    torch.cuda.synchronize()
+    assert torch.allclose(got[:, V - 1], ref[:, 0], rtol=1e-4, atol=1e-3) and (got[:, :V - 1] == 0).all()
+
+
+def test_refusals(fef):
+    w = torch.randn((40, 128), device="cuda").to(torch.bfloat16)
+    for args in ((w.float(),), (w[:, ::2],), (w[0],), (w, 16), (w, 256), (w[:, :96].contiguous(), 64), (w[:0],)):
+        with pytest.raises(fef.FefError):
+            fef.fef_lmhead_quantize(*args)
+    layer = fef.fef_lmhead_quantize(w, 64, True)
+    hidden = torch.zeros((3, 128), dtype=torch.bfloat16, device="cuda")
+    changes = [dict(packed=layer.packed[:, :32].contiguous()), dict(packed=layer.packed.int()), dict(scale=layer.scale.float()),
+               dict(scale=layer.scale[:, :40].contiguous()), dict(zero=layer.zero.int()), dict(zero=layer.zero[:, :32].contiguous()),
+               dict(d=256), dict(group=32), dict(group=128), dict(packed=layer.packed[:3])]
+    for change in changes:
+        broken = layer._replace(**change)
+        with pytest.raises(fef.FefError):
+            fef.fef_lmhead_dequantize(broken)
+        with pytest.raises(fef.FefError):
+            fef.fef_lmhead_logits_quantized(hidden, broken)
+    for h, kw in ((hidden.float(), {}), (hidden[:, :64].contiguous(), {}), (hidden[:0], {}), (hidden, dict(dtype=torch.float16)),
+                  (hidden, dict(out=torch.zeros((2, 40), device="cuda"))), (hidden, dict(out=torch.zeros((3, 36), device="cuda"))),
+                  (hidden, dict(out=torch.zeros((3, 42), device="cuda"))), (hidden, dict(out=torch.zeros((3, 40), device="cuda").half()))):
+        with pytest.raises(fef.FefError):
+            fef.fef_lmhead_logits_quantized(h, layer, **kw)
+    with pytest.raises(fef.FefError):
+        fef.fef_lmhead_dequantize(layer, out=torch.zeros((40, 64), device="cuda"))
+    with pytest.raises(ValueError):
+        fef.fef_lmhead_logits_quantized(hidden, layer._replace(packed=layer.packed.cpu()))
