@@ -11,9 +11,9 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libfef.so")
 SOURCES = ["fef_verify.cu", "fef_remask.cu", "fef_draft.cu", "fef_loop.cu", "fef_lmhead.cu", "fef_synth.cu",
-           "fef_adjust.cu", "fef_quant.cu"]
+           "fef_adjust.cu", "fef_quant.cu", "fef_quant_rows.cu"]
 HEADERS = [os.path.join(CSRC, h) for h in ("fef_common.cuh", "fef_device_math.cuh", "fef_verify_params.cuh",
-                                            "fef_residual.cuh")] + [os.path.join(INCLUDE, "fef.h")]
+                                            "fef_residual.cuh", "fef_tensor_core.cuh", "fef_quant.cuh")] + [os.path.join(INCLUDE, "fef.h")]
 
 
 def nvcc_path() -> str:

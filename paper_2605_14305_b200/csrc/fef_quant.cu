@@ -1,15 +1,5 @@
-// The output layer in 4 bits: fef_lmhead_quantize, fef_lmhead_dequantize, fef_lmhead_logits_quantized.
-//
-// A row of d weights is cut into groups of G = 32, 64 or 128; a weight is (q - z) * s with q in 0..15, one scale s
-// (bfloat16) and one zero point z (0..15; 8 where the layer keeps none) per group.  q - z has five bits and s eight, so
-// the product is exact in binary32.
-//
-// Layout (kBlock = 128 columns are a block; a row is padded to whole blocks):
-//   packed [V][blocks * 64] bytes: of a block's sixteen 32-bit words, word 4 t + w holds the columns
-//          32 w + 8 t .. 32 w + 8 t + 7, lowest nibble first.  16 consecutive bytes (one t) therefore hold eight
-//          columns of every 32-column piece, which is what one lane of a matrix instruction's operand needs.
-//   scale, zero [blocks][V rounded up to 32][128 / G]: what a block of consecutive rows needs lies together; the
-//          entries behind d and V are zero.
+// The output layer in 4 bits: fef_lmhead_quantize, fef_lmhead_dequantize, and the entry point of
+// fef_lmhead_logits_quantized (layout: fef_quant.cuh).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
@@ -18,22 +8,13 @@
 #include "fef.h"
 #include "fef_common.cuh"
 #include "fef_device_math.cuh"
+#include "fef_quant.cuh"
 
 namespace fef {
 namespace quant {
 
-constexpr int kBlock = 128;
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-
-struct Layer {
-    const uint8_t* packed;
-    const uint16_t* scale;
-    const uint8_t* zero;  // or null
-    int V, Vp, d, blocks, G;
-};
-
-__device__ __forceinline__ float bf16_value(uint16_t h) { return __uint_as_float(static_cast<uint32_t>(h) << 16); }
 
 // ------------------------------------------------------------------------------------------ quantize ----
 struct QuantizeParams {
@@ -119,15 +100,6 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------------------------------- product ----
-struct ProductParams {
-    Layer layer;
-    const uint16_t* hidden;  // [rows][d]
-    char* out;               // [rows][ldo]
-    int64_t ldo;
-    int rows;
-    int32_t* status;
-};
-
 constexpr int kRowBlock = 8;
 
 // One warp per vocabulary row and eight hidden rows; a lane takes eight columns of every other 128-column block's half.
@@ -197,9 +169,12 @@ static Layer make_layer(const void* packed, const void* scale, const void* zero,
     return W;
 }
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
-static bool have_device() {
-    int dev = -1;
-    return cudaGetDevice(&dev) == cudaSuccess;
+static int device_and_sms(int* dev) {
+    static int sms[64];
+    *dev = -1;
+    if (cudaGetDevice(dev) != cudaSuccess || *dev < 0 || *dev >= 64) return 0;
+    if (!sms[*dev] && cudaDeviceGetAttribute(&sms[*dev], cudaDevAttrMultiProcessorCount, *dev) != cudaSuccess) return 0;
+    return sms[*dev];
 }
 
 }  // namespace quant
@@ -213,7 +188,9 @@ fef_status fef_lmhead_quantize(const void* weight, int V, int d, int group, void
     using namespace fef::quant;
     if (!weight || !packed || !scale || !layer_ok(V, d, group)) return FEF_ERR_INVALID_ARG;
     if (!aligned16(weight) || !aligned16(packed) || !aligned16(scale) || !aligned16(zero)) return FEF_ERR_ALIGNMENT;
-    if (!have_device()) return FEF_ERR_CUDA;
+    int dev;
+    const int sms = device_and_sms(&dev);
+    if (sms < 1) return FEF_ERR_CUDA;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (device_status && cudaMemsetAsync(device_status, 0, sizeof(int32_t), stream) != cudaSuccess) return FEF_ERR_CUDA;
     QuantizeParams P;
@@ -241,7 +218,9 @@ fef_status fef_lmhead_dequantize(const void* packed, const void* scale, const vo
     using namespace fef::quant;
     if (!packed || !scale || !values || !layer_ok(V, d, group)) return FEF_ERR_INVALID_ARG;
     if (!aligned16(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(values)) return FEF_ERR_ALIGNMENT;
-    if (!have_device()) return FEF_ERR_CUDA;
+    int dev;
+    const int sms = device_and_sms(&dev);
+    if (sms < 1) return FEF_ERR_CUDA;
     const Layer W = make_layer(packed, scale, zero, V, d, group);
     const int64_t grid = (static_cast<int64_t>(V) * W.blocks + kWarps - 1) / kWarps;
     if (grid > 0x7FFFFFFF) return FEF_ERR_INVALID_ARG;
@@ -260,7 +239,9 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
     if (!aligned16(hidden) || !aligned16(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(logits) ||
         (ldo * (dt == FEF_F32 ? 4 : 2)) % 16)
         return FEF_ERR_ALIGNMENT;
-    if (!have_device()) return FEF_ERR_CUDA;
+    int dev;
+    const int sms = device_and_sms(&dev);
+    if (sms < 1) return FEF_ERR_CUDA;
     ProductParams P;
     P.layer = make_layer(packed, scale, zero, V, d, group);
     P.hidden = static_cast<const uint16_t*>(hidden);
@@ -268,9 +249,10 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
     P.ldo = ldo;
     P.rows = rows;
     P.status = device_status;
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (rows_kernel_takes(P, sms)) return launch_rows_kernel(P, dt, dev, sms, stream);
     const dim3 grid((V + kWarps - 1) / kWarps, (rows + kRowBlock - 1) / kRowBlock);
     if (grid.y > 65535) return FEF_ERR_INVALID_ARG;
-    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (dt == FEF_F32)
         product_kernel<FEF_F32><<<grid, kThreads, 0, stream>>>(P);
     else
