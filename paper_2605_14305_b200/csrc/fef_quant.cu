@@ -250,7 +250,7 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
     P.rows = rows;
     P.status = device_status;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (rows_kernel_takes(P, sms)) return launch_rows_kernel(P, dt, dev, sms, stream);
+    if (rows_kernel_takes(P)) return launch_rows_kernel(P, dt, dev, sms, stream);
     const dim3 grid((V + kWarps - 1) / kWarps, (rows + kRowBlock - 1) / kRowBlock);
     if (grid.y > 65535) return FEF_ERR_INVALID_ARG;
     if (dt == FEF_F32)

@@ -52,7 +52,7 @@ __device__ __forceinline__ uint32_t nibble_pair(uint32_t word, uint32_t centre) 
 __device__ __forceinline__ uint32_t centre_of(uint32_t z) { return 0x43004300u | z | (z << 16); }
 
 // Logits from few hidden rows: false when this size is not for that kernel.
-bool rows_kernel_takes(const ProductParams& P, int sms);
+bool rows_kernel_takes(const ProductParams& P);
 fef_status launch_rows_kernel(const ProductParams& P, fef_dtype dt, int dev, int sms, cudaStream_t stream);
 
 }  // namespace quant

@@ -16,8 +16,10 @@
 // root mean square of their weights instead of 2.6).  The products of a group are added up in binary32 by the matrix
 // instructions, then scaled in binary32.
 //
-// One CTA of 16 warps per SM takes an even share of the vocabulary, unit by unit of 32 rows; a unit's blocks are shared out
-// over `parts` warps, whose sums meet in shared memory at its end.  Every warp loads its weights straight into registers,
+// One CTA of 16 warps per SM takes an even share of the vocabulary in units of 32 rows; all blocks of its units in a row are
+// cut into 16 equal runs, one per warp, so that all end together.  A unit that lies in more than one run is joined at the
+// very end: the warps behind leave their sums in shared memory, the warp that holds its beginning adds them up, in order.
+// Every warp loads its weights straight into registers,
 // kAhead blocks ahead of the arithmetic: 126464 x 2048 bytes in this order and nothing else took 42 us (6.1 TB/s), as did TMA
 // boxes through a shared-memory ring; with the arithmetic the ring took 75 us, its waits and hand-overs being most of the
 // instructions.  The hidden rows stay in shared memory, rearranged into operand order once.
@@ -38,30 +40,14 @@ constexpr int kUsualShift = 100;
 
 struct Plan {
     int units;    // of the whole vocabulary
-    int parts;    // warps per unit, a power of two
-    int piece;    // blocks of a part
-    uint32_t join_at;
-    size_t smem;  // 0: not for this kernel
+    size_t smem;  // hidden rows, their groups' sums, one place per warp for the sums of a shared unit; 0: not for this kernel
 };
 
-Plan make_plan(const ProductParams& P, int sms) {
+Plan make_plan(const ProductParams& P) {
     Plan L = {};
-    const Layer& W = P.layer;
     const int nt = P.rows > 8 ? 2 : 1;
-    L.units = (W.V + kUnit - 1) / kUnit;
-    const int64_t share = (L.units + sms - 1) / sms;
-    // rounds of 16 warps x (blocks + what beginning and ending a unit costs, about two)
-    int64_t best = INT64_MAX;
-    for (int parts = 1; parts <= kWarps; parts *= 2) {
-        const int64_t cost = (share * parts + kWarps - 1) / kWarps * ((W.blocks + parts - 1) / parts + 2);
-        if (cost < best) {
-            best = cost;
-            L.parts = parts;
-        }
-    }
-    L.piece = (W.blocks + L.parts - 1) / L.parts;
-    L.join_at = static_cast<uint32_t>(W.blocks) * (2048 + 128) * nt;   // hidden rows and their groups' sums
-    const size_t smem = static_cast<size_t>(W.blocks) * (2048 + 128) * nt + (L.parts > 1 ? 2 * kWarps * 1024 * nt : 0);
+    L.units = (P.layer.V + kUnit - 1) / kUnit;
+    const size_t smem = static_cast<size_t>(P.layer.blocks) * (2048 + 128) * nt + kWarps * 1024 * nt;
     L.smem = smem <= kSmemLimit - 1024 ? smem : 0;
     return L;
 }
@@ -83,11 +69,17 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Two bfloat16 numbers times a power of two, given by its bits.
+__device__ __forceinline__ uint32_t times(uint32_t x, uint32_t power) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(power | power << 16));
+    return r;
+}
 __device__ __forceinline__ float exp2_int(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }  // |e| < 127
-// The power of two a hidden row is scaled by, from the bfloat16 bits of its largest finite value.
+// The power of two a hidden row is scaled by, from the bfloat16 bits of its largest value.
 __device__ __forceinline__ int row_shift(uint32_t largest) {
-    const int e = static_cast<int>(largest >> 7);   // biased
-    return largest == 0u || (e >= 47 && e < 154) ? kUsualShift : 253 - e;
+    const int e = static_cast<int>(largest >> 7);   // biased; 255: the row's logits are no numbers anyway
+    return largest == 0u || (e >= 47 && e < 154) || e == 255 ? kUsualShift : 253 - e;
 }
 
 // What a warp needs of one block of its unit: operand rows 4 g + i, their scales and zero points.
@@ -102,11 +94,6 @@ struct Fetched {
     }
 };
 
-// All warps of a unit.
-__device__ __forceinline__ void unit_barrier(int slot, int warps) {
-    asm volatile("bar.sync %0, %1;" ::"r"(1 + slot), "r"(warps * 32) : "memory");
-}
-
 template <int NT, int N, bool ZERO>   // 8 NT hidden rows, N groups per block
 __global__ void __launch_bounds__(kThreads, 1)
 product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ Plan L, int out_bf16) {
@@ -116,28 +103,29 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
     const Layer& W = P.layer;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
-    const int slot = warp / L.parts, part = warp - slot * L.parts, together = kWarps / L.parts;
     const int unit_begin = static_cast<int>(static_cast<int64_t>(L.units) * blockIdx.x / gridDim.x);
     const int unit_end = static_cast<int>(static_cast<int64_t>(L.units) * (blockIdx.x + 1) / gridDim.x);
-    const int first = part * L.piece, blocks = min(max(W.blocks - first, 0), L.piece);
+    const int64_t total_blocks = static_cast<int64_t>(unit_end - unit_begin) * W.blocks;
+    auto run_begin = [&](int w) { return static_cast<int>(total_blocks * w / kWarps); };
+    const int begin = run_begin(warp), end = run_begin(warp + 1);
     const int64_t pitch = static_cast<int64_t>(W.blocks) * 64;
 
     // ---- the flat sequence of this warp's blocks, fetched ahead
-    int fetch_unit = unit_begin + slot, fetch_block = 0;
+    int fetch_at = begin, fetch_unit = unit_begin + begin / W.blocks, fetch_block = begin % W.blocks;
     const uint8_t* fetch_w = nullptr;
     uint32_t row_at[4];
     auto seek = [&]() {   // (rows behind V are read as the last one; their logits are not stored)
         const int64_t v = static_cast<int64_t>(fetch_unit) * kUnit + 4 * g;
         const int64_t v0 = min(v, static_cast<int64_t>(W.V - 1));
-        fetch_w = W.packed + v0 * pitch + first * 64 + t * 16;
+        fetch_w = W.packed + v0 * pitch + t * 16;
 #pragma unroll
         for (int i = 0; i < 4; ++i) row_at[i] = static_cast<uint32_t>((min(v + i, static_cast<int64_t>(W.V - 1)) - v0) * pitch);
     };
     auto fetch = [&](Fetched<N, ZERO>& f) {
-        if (fetch_unit < unit_end && blocks > 0) {
+        if (fetch_at < end) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) f.q[i] = ld_global_nc_v4(fetch_w + row_at[i] + fetch_block * 64);
-            const int64_t at = (static_cast<int64_t>(first + fetch_block) * W.Vp + static_cast<int64_t>(fetch_unit) * kUnit + 4 * g) * N;
+            const int64_t at = (static_cast<int64_t>(fetch_block) * W.Vp + static_cast<int64_t>(fetch_unit) * kUnit + 4 * g) * N;
             if constexpr (N == 1) {
                 const uint2 x = __ldg(reinterpret_cast<const uint2*>(W.scale + at));
                 f.s[0] = x.x;
@@ -156,15 +144,16 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < N; ++i) f.z[i] = __ldg(reinterpret_cast<const uint32_t*>(W.zero + at) + i);
             }
-            if (++fetch_block == blocks) {
+            ++fetch_at;
+            if (++fetch_block == W.blocks) {
                 fetch_block = 0;
-                fetch_unit += together;
-                if (fetch_unit < unit_end) seek();
+                ++fetch_unit;
+                if (fetch_at < end) seek();
             }
         }
     };
     Fetched<N, ZERO> ahead[kAhead];
-    if (fetch_unit < unit_end) seek();
+    if (begin < end) seek();
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fetch(ahead[i]);
 
@@ -175,58 +164,63 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
     float* sums = reinterpret_cast<float*>(smem + pieces * 16);
     if (threadIdx.x < 16) s_largest[threadIdx.x] = 0u;
     __syncthreads();
-    auto stage_hidden = [&](bool usual) {
-        for (int at0 = threadIdx.x; at0 < pieces; at0 += 4 * kThreads) {
-            uint4 x[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {   // (four loads in flight; whole warps: the pieces are a multiple of 32)
-                const int at = at0 + u * kThreads, row = at / 4 % (8 * NT), cw = at / kPieces;
-                const int k = (cw >> 2) * kBlock + (cw & 3) * 32 + (at & 3) * 8;
-                x[u] = make_uint4(0u, 0u, 0u, 0u);
-                if (at < pieces && row < P.rows && k < W.d)
-                    x[u] = __ldg(reinterpret_cast<const uint4*>(P.hidden + static_cast<int64_t>(row) * W.d + k));
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int at = at0 + u * kThreads, row = at / 4 % (8 * NT);
-                if (at >= pieces) break;
-                int shift = kUsualShift;
-                if (!usual) shift = row_shift(s_largest[row]);
-                const float f = exp2_int(shift / 2), f0 = exp2_int(shift - shift / 2);
-                float v[8];
-                unpack<FEF_BF16>(x[u], v);
-                float total = 0.f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    v[j] = v[j] * f * f0;
-                    total += v[j] * exp2_int(-67) * exp2_int(-66);
-                }
-                uint4 y;
-                y.x = bf16_pair(v[0], v[4]);
-                y.y = bf16_pair(v[1] * 0.0625f, v[5] * 0.0625f);
-                y.z = bf16_pair(v[2], v[6]);
-                y.w = bf16_pair(v[3] * 0.0625f, v[7] * 0.0625f);
-                *reinterpret_cast<uint4*>(smem + at * 16) = y;
-                total += __shfl_xor_sync(0xFFFFFFFFu, total, 1);
-                total += __shfl_xor_sync(0xFFFFFFFFu, total, 2);
-                if ((at & 3) == 0) sums[at / 4] = total;
-                if (usual) {
-                    uint32_t top = 0u;
-                    for (uint32_t w : {x[u].x, x[u].y, x[u].z, x[u].w})
-                        for (uint32_t h : {w & 0x7FFFu, w >> 16 & 0x7FFFu})
-                            if (h < 0x7F80u) top = max(top, h);
-                    if (top != 0u) atomicMax(&s_largest[row], top);
-                }
-            }
-        }
+    auto piece = [&](int at, int& row) {   // one row's eight columns as they are
+        const int cw = at / kPieces, k = (cw >> 2) * kBlock + (cw & 3) * 32 + (at & 3) * 8;
+        row = at / 4 % (8 * NT);
+        uint4 x = make_uint4(0u, 0u, 0u, 0u);
+        if (at < pieces && row < P.rows && k < W.d)
+            x = __ldg(reinterpret_cast<const uint4*>(P.hidden + static_cast<int64_t>(row) * W.d + k));
+        return x;
     };
-    stage_hidden(true);
+    auto group_sum = [&](int at, float total) {   // (whole warps: the pieces are a multiple of 32)
+        total += __shfl_xor_sync(0xFFFFFFFFu, total, 1);
+        total += __shfl_xor_sync(0xFFFFFFFFu, total, 2);
+        if ((at & 3) == 0) sums[at / 4] = total;
+    };
+    for (int at0 = threadIdx.x; at0 < pieces; at0 += 4 * kThreads) {
+        uint4 x[4];
+        int row[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = piece(at0 + u * kThreads, row[u]);   // (four loads in flight)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int at = at0 + u * kThreads;
+            if (at >= pieces) break;
+            uint4 y;
+            y.x = times(__byte_perm(x[u].x, x[u].z, 0x5410), 0x7180u);   // 2^100
+            y.y = times(__byte_perm(x[u].x, x[u].z, 0x7632), 0x6F80u);   // 2^96
+            y.z = times(__byte_perm(x[u].y, x[u].w, 0x5410), 0x7180u);
+            y.w = times(__byte_perm(x[u].y, x[u].w, 0x7632), 0x6F80u);
+            *reinterpret_cast<uint4*>(smem + at * 16) = y;
+            float v[8];
+            unpack<FEF_BF16>(x[u], v);
+            group_sum(at, (((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]))) * exp2_int(kUsualShift - 133));
+            const uint32_t top = __vmaxu2(__vmaxu2(x[u].x & 0x7FFF7FFFu, x[u].y & 0x7FFF7FFFu),
+                                          __vmaxu2(x[u].z & 0x7FFF7FFFu, x[u].w & 0x7FFF7FFFu));
+            if (top != 0u) atomicMax(&s_largest[row[u]], max(top & 0xFFFFu, top >> 16));
+        }
+    }
     __syncthreads();
     bool usual = true;
 #pragma unroll
     for (int r = 0; r < 8 * NT; ++r) usual = usual && row_shift(s_largest[r]) == kUsualShift;
-    if (!usual) {
-        stage_hidden(false);
+    if (!usual) {   // some row's values are out of the ordinary: all again, each row with its own power of two
+        for (int at = threadIdx.x; at < pieces; at += kThreads) {
+            int row;
+            const uint4 x = piece(at, row);
+            const int shift = row_shift(s_largest[row]);
+            float v[8], total = 0.f;
+            unpack<FEF_BF16>(x, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = v[j] * exp2_int(shift / 2) * exp2_int(shift - shift / 2);
+                total += v[j] * exp2_int(-67) * exp2_int(-66);
+            }
+            *reinterpret_cast<uint4*>(smem + at * 16) =
+                make_uint4(bf16_pair(v[0], v[4]), bf16_pair(v[1] * 0.0625f, v[5] * 0.0625f), bf16_pair(v[2], v[6]),
+                           bf16_pair(v[3] * 0.0625f, v[7] * 0.0625f));
+            group_sum(at, total);
+        }
         __syncthreads();
     }
     if constexpr (N < 4) {   // the words of a group, into its first word's place
@@ -242,7 +236,6 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
 
     // ---- the units
     float acc[2][NT][4];
-    int round = 0;
     auto clear = [&]() {
 #pragma unroll
         for (int m = 0; m < 2; ++m)
@@ -297,35 +290,9 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
             }
         }
     };
-    // A unit is done: its warps' sums meet, and part 0 stores the logits.  Lane (g, t) holds vocabulary rows 4 g .. 4 g + 3 of
-    // hidden rows 8 n + 2 t and 8 n + 2 t + 1: acc[0][n][c], acc[0][n][2 + c], acc[1][n][c], acc[1][n][2 + c].
-    auto finish = [&](int unit) {
-        if (L.parts > 1) {
-            // two places in turn: a warp writes to one again only after a barrier that the reader has passed
-            float4* join = reinterpret_cast<float4*>(smem + L.join_at) + ((round & 1) * kWarps + slot * L.parts) * (64 * NT);
-            ++round;
-            if (part > 0) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-                        join[part * (64 * NT) + (2 * n + c) * 32 + lane] =
-                            make_float4(acc[0][n][c], acc[0][n][2 + c], acc[1][n][c], acc[1][n][2 + c]);
-            }
-            unit_barrier(slot, L.parts);
-            if (part > 0) return;
-            for (int p = 1; p < L.parts; ++p)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const float4 x = join[p * (64 * NT) + (2 * n + c) * 32 + lane];
-                        acc[0][n][c] += x.x;
-                        acc[0][n][2 + c] += x.y;
-                        acc[1][n][c] += x.z;
-                        acc[1][n][2 + c] += x.w;
-                    }
-        }
+    // Lane (g, t) holds vocabulary rows 4 g .. 4 g + 3 of hidden rows 8 n + 2 t + c: acc[0][n][c], acc[0][n][2 + c],
+    // acc[1][n][c], acc[1][n][2 + c].
+    auto store = [&](int unit) {
         const int64_t v = static_cast<int64_t>(unit) * kUnit + 4 * g;
         const int many = static_cast<int>(min(max(W.V - v, static_cast<int64_t>(0)), static_cast<int64_t>(4)));
 #pragma unroll
@@ -356,27 +323,58 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
                 }
             }
     };
+    float4* places = reinterpret_cast<float4*>(smem + W.blocks * (2048 + 128) * NT);   // [warp][2 NT][lane]
     if (P.status && blockIdx.x == 0 && threadIdx.x == 0) *P.status = FEF_OK;
     clear();
-    if (blocks == 0) {   // (a part without blocks still takes its place at the barriers)
-        for (int unit = unit_begin + slot; unit < unit_end; unit += together) finish(unit);
-        return;
-    }
-    int unit = unit_begin + slot, block = 0;
-    while (unit < unit_end) {
+    int at = begin, unit = unit_begin + begin / W.blocks, block = begin % W.blocks;
+    bool whole = block == 0;   // the sums go back to the unit's first block
+    while (at < end) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (unit < unit_end) {
-                multiply(ahead[i], first + block);
+            if (at < end) {
+                multiply(ahead[i], block);
                 fetch(ahead[i]);
-                if (++block == blocks) {
-                    finish(unit);
+                ++at;
+                ++block;
+                if (!whole && (block == W.blocks || at == end)) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+                            places[warp * (64 * NT) + (2 * n + c) * 32 + lane] =
+                                make_float4(acc[0][n][c], acc[0][n][2 + c], acc[1][n][c], acc[1][n][2 + c]);
+                } else if (block == W.blocks) {
+                    store(unit);
+                }
+                if (block == W.blocks) {
                     clear();
                     block = 0;
-                    unit += together;
+                    whole = true;
+                    ++unit;
                 }
             }
         }
+    }
+    __syncthreads();
+    if (begin < end && whole && block > 0) {   // the unit goes on in the runs behind
+        int left = W.blocks - block;
+        for (int w = warp + 1; left > 0; ++w) {
+            const int run = run_begin(w + 1) - run_begin(w);
+            if (run > 0) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const float4 x = places[w * (64 * NT) + (2 * n + c) * 32 + lane];
+                        acc[0][n][c] += x.x;
+                        acc[0][n][2 + c] += x.y;
+                        acc[1][n][c] += x.z;
+                        acc[1][n][2 + c] += x.w;
+                    }
+            }
+            left -= run;
+        }
+        store(unit);
     }
 }
 
@@ -411,10 +409,10 @@ fef_status launch_g(const ProductParams& P, const Plan& L, fef_dtype dt, int dev
 
 }  // namespace
 
-bool rows_kernel_takes(const ProductParams& P, int sms) { return P.rows <= 16 && make_plan(P, sms).smem > 0; }
+bool rows_kernel_takes(const ProductParams& P) { return P.rows <= 16 && make_plan(P).smem > 0; }
 
 fef_status launch_rows_kernel(const ProductParams& P, fef_dtype dt, int dev, int sms, cudaStream_t stream) {
-    const Plan L = make_plan(P, sms);
+    const Plan L = make_plan(P);
     const int grid = L.units < sms ? L.units : sms;
     return P.rows > 8 ? launch_g<2>(P, L, dt, dev, grid, stream) : launch_g<1>(P, L, dt, dev, grid, stream);
 }
