@@ -110,9 +110,10 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
     const int begin = run_begin(warp), end = run_begin(warp + 1);
     const int64_t pitch = static_cast<int64_t>(W.blocks) * 64;
 
-    // ---- the flat sequence of this warp's blocks, fetched ahead
+    // ---- the flat sequence of this warp's blocks, fetched ahead.  Past its end the last block is fetched again: with a branch
+    //      around the loads, waiting for one block's waits for the blocks behind it too (52 against 45 us for the loads alone).
     int fetch_at = begin, fetch_unit = unit_begin + begin / W.blocks, fetch_block = begin % W.blocks;
-    const uint8_t* fetch_w = nullptr;
+    const uint8_t* fetch_w;
     uint32_t row_at[4];
     auto seek = [&]() {   // (rows behind V are read as the last one; their logits are not stored)
         const int64_t v = static_cast<int64_t>(fetch_unit) * kUnit + 4 * g;
@@ -122,38 +123,38 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
         for (int i = 0; i < 4; ++i) row_at[i] = static_cast<uint32_t>((min(v + i, static_cast<int64_t>(W.V - 1)) - v0) * pitch);
     };
     auto fetch = [&](Fetched<N, ZERO>& f) {
-        if (fetch_at < end) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) f.q[i] = ld_global_nc_v4(fetch_w + row_at[i] + fetch_block * 64);
-            const int64_t at = (static_cast<int64_t>(fetch_block) * W.Vp + static_cast<int64_t>(fetch_unit) * kUnit + 4 * g) * N;
-            if constexpr (N == 1) {
-                const uint2 x = __ldg(reinterpret_cast<const uint2*>(W.scale + at));
-                f.s[0] = x.x;
-                f.s[1] = x.y;
-            } else {
+        for (int i = 0; i < 4; ++i) f.q[i] = ld_global_nc_v4(fetch_w + row_at[i] + fetch_block * 64);
+        const int64_t at = (static_cast<int64_t>(fetch_block) * W.Vp + static_cast<int64_t>(fetch_unit) * kUnit + 4 * g) * N;
+        if constexpr (N == 1) {
+            const uint2 x = __ldg(reinterpret_cast<const uint2*>(W.scale + at));
+            f.s[0] = x.x;
+            f.s[1] = x.y;
+        } else {
 #pragma unroll
-                for (int i = 0; i < N / 2; ++i) {
-                    const uint4 x = __ldg(reinterpret_cast<const uint4*>(W.scale + at) + i);
-                    f.s[4 * i] = x.x;
-                    f.s[4 * i + 1] = x.y;
-                    f.s[4 * i + 2] = x.z;
-                    f.s[4 * i + 3] = x.w;
-                }
+            for (int i = 0; i < N / 2; ++i) {
+                const uint4 x = __ldg(reinterpret_cast<const uint4*>(W.scale + at) + i);
+                f.s[4 * i] = x.x;
+                f.s[4 * i + 1] = x.y;
+                f.s[4 * i + 2] = x.z;
+                f.s[4 * i + 3] = x.w;
             }
-            if constexpr (ZERO) {
+        }
+        if constexpr (ZERO) {
 #pragma unroll
-                for (int i = 0; i < N; ++i) f.z[i] = __ldg(reinterpret_cast<const uint32_t*>(W.zero + at) + i);
-            }
-            ++fetch_at;
-            if (++fetch_block == W.blocks) {
-                fetch_block = 0;
-                ++fetch_unit;
-                if (fetch_at < end) seek();
-            }
+            for (int i = 0; i < N; ++i) f.z[i] = __ldg(reinterpret_cast<const uint32_t*>(W.zero + at) + i);
+        }
+        const int more = fetch_at + 1 < end ? 1 : 0;
+        fetch_at += more;
+        fetch_block += more;
+        if (fetch_block == W.blocks) {
+            fetch_block = 0;
+            ++fetch_unit;
+            seek();
         }
     };
     Fetched<N, ZERO> ahead[kAhead];
-    if (begin < end) seek();
+    seek();
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fetch(ahead[i]);
 
@@ -328,33 +329,40 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
     clear();
     int at = begin, unit = unit_begin + begin / W.blocks, block = begin % W.blocks;
     bool whole = block == 0;   // the sums go back to the unit's first block
-    while (at < end) {
+    auto next_block = [&]() {
+        ++at;
+        ++block;
+        if (!whole && (block == W.blocks || at == end)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    places[warp * (64 * NT) + (2 * n + c) * 32 + lane] =
+                        make_float4(acc[0][n][c], acc[0][n][2 + c], acc[1][n][c], acc[1][n][2 + c]);
+        } else if (block == W.blocks) {
+            store(unit);
+        }
+        if (block == W.blocks) {
+            clear();
+            block = 0;
+            whole = true;
+            ++unit;
+        }
+    };
+    while (at + kAhead <= end) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            if (at < end) {
-                multiply(ahead[i], block);
-                fetch(ahead[i]);
-                ++at;
-                ++block;
-                if (!whole && (block == W.blocks || at == end)) {
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int c = 0; c < 2; ++c)
-                            places[warp * (64 * NT) + (2 * n + c) * 32 + lane] =
-                                make_float4(acc[0][n][c], acc[0][n][2 + c], acc[1][n][c], acc[1][n][2 + c]);
-                } else if (block == W.blocks) {
-                    store(unit);
-                }
-                if (block == W.blocks) {
-                    clear();
-                    block = 0;
-                    whole = true;
-                    ++unit;
-                }
-            }
+            multiply(ahead[i], block);
+            fetch(ahead[i]);
+            next_block();
         }
     }
+#pragma unroll
+    for (int i = 0; i < kAhead - 1; ++i)
+        if (at < end) {
+            multiply(ahead[i], block);
+            next_block();
+        }
     __syncthreads();
     if (begin < end && whole && block > 0) {   // the unit goes on in the runs behind
         int left = W.blocks - block;
