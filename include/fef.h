@@ -491,15 +491,20 @@ fef_status fef_lmhead_logits(const void* hidden, const void* weight, int rows, i
  *            entries between V and ldo are left as they were
  *   device_status  device out, [1] int32, or NULL: FEF_OK, or FEF_ERR_TIMEOUT as in fef_spec_verify (the logits are then
  *            incomplete)
- * Asynchronous on `cuda_stream`.
+ *   workspace  device scratch of fef_lmhead_logits_quantized_workspace_bytes(rows, V, d, group) bytes, 256-byte aligned, contents
+ *            need not be initialised (it takes the hidden rows in the matrix instructions' order); not used for few rows
+ * A row of hidden states that holds NaN or an infinity has logits that are no numbers (NaN, or an infinity where only one
+ * product is one); other rows are not affected.
+ * Asynchronous on `cuda_stream`; one kernel for few rows (up to 16), otherwise two.
  */
 fef_status fef_lmhead_quantize(const void* weight, int V, int d, int group, void* packed, void* scale, void* zero,
                                int32_t* device_status, void* cuda_stream);
 fef_status fef_lmhead_dequantize(const void* packed, const void* scale, const void* zero, int V, int d, int group,
                                  float* values, void* cuda_stream);
+size_t fef_lmhead_logits_quantized_workspace_bytes(int rows, int V, int d, int group);
 fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, const void* scale, const void* zero, int rows,
                                        int V, int d, int group, void* logits, int64_t ldo, fef_dtype dt,
-                                       int32_t* device_status, void* cuda_stream);
+                                       void* workspace, size_t workspace_bytes, int32_t* device_status, void* cuda_stream);
 
 /*
  * Penalties for repeated tokens, biases and grammar masks on the logits of speculative windows (the paper

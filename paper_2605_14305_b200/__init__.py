@@ -34,7 +34,7 @@ EXPORTS = ("fef_status_string", "fef_spec_verify_workspace_bytes", "fef_spec_ver
            "fef_draft_sample_with_target", "fef_spec_verify_with_norms", "fef_synth_logits",
            "fef_loop_run_synthetic_workspace_bytes", "fef_loop_run_synthetic",
            "fef_logits_adjust_workspace_bytes", "fef_logits_adjust", "fef_lmhead_quantize", "fef_lmhead_dequantize",
-           "fef_lmhead_logits_quantized")
+           "fef_lmhead_logits_quantized_workspace_bytes", "fef_lmhead_logits_quantized")
 
 _lib = None
 
@@ -127,7 +127,9 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     L.fef_lmhead_quantize.restype = i32
     L.fef_lmhead_dequantize.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp]
     L.fef_lmhead_dequantize.restype = i32
-    L.fef_lmhead_logits_quantized.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, i32, vp, vp]
+    L.fef_lmhead_logits_quantized_workspace_bytes.argtypes = [i32, i32, i32, i32]
+    L.fef_lmhead_logits_quantized_workspace_bytes.restype = sz
+    L.fef_lmhead_logits_quantized.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, i32, vp, sz, vp, vp]
     L.fef_lmhead_logits_quantized.restype = i32
     L.fef_logits_adjust_workspace_bytes.argtypes = [i32, i32, i32]
     L.fef_logits_adjust_workspace_bytes.restype = sz
@@ -756,8 +758,12 @@ def fef_lmhead_dequantize(layer: QuantizedLayer, out: Optional[torch.Tensor] = N
     return out
 
 
+def fef_lmhead_logits_quantized_workspace_bytes(rows: int, V: int, d: int, group: int) -> int:
+    return int(load().fef_lmhead_logits_quantized_workspace_bytes(rows, V, d, group))
+
+
 def fef_lmhead_logits_quantized(hidden: torch.Tensor, layer: QuantizedLayer, dtype=torch.float32,
-                                out: Optional[torch.Tensor] = None, stream=None):
+                                out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """``fef_lmhead_logits`` with an output layer in 4 bits (see ``fef_lmhead_logits_quantized`` in include/fef.h).
 
     ``hidden``: ``[rows, d]`` bfloat16.  Returns ``(logits [rows, ldo], device_status)``; the first ``V`` entries of
@@ -767,6 +773,7 @@ def fef_lmhead_logits_quantized(hidden: torch.Tensor, layer: QuantizedLayer, dty
     where = "fef_lmhead_logits_quantized"
     V, _ = _quantized_layer(layer, where)
     _bf16_matrix(hidden, where)
+    _require_cuda(out, workspace)
     dev = layer.packed.device
     rows, d = hidden.shape
     if d != layer.d or hidden.device != dev or rows < 1:
@@ -782,10 +789,13 @@ def fef_lmhead_logits_quantized(hidden: torch.Tensor, layer: QuantizedLayer, dty
         if out is None:
             out = torch.empty((rows, (V + per_vec - 1) // per_vec * per_vec), dtype=dtype, device=dev)
         status = torch.empty(1, dtype=torch.int32, device=dev)
+        if workspace is None:
+            workspace = torch.empty(max(fef_lmhead_logits_quantized_workspace_bytes(rows, V, d, layer.group), 256),
+                                    dtype=torch.uint8, device=dev)
         st = load().fef_lmhead_logits_quantized(
             hidden.data_ptr(), layer.packed.data_ptr(), layer.scale.data_ptr(), _ptr(layer.zero), rows, V, d, layer.group,
-            out.data_ptr(), out.shape[1], FEF_F32 if dtype == torch.float32 else FEF_BF16, status.data_ptr(),
-            _stream_ptr(stream))
+            out.data_ptr(), out.shape[1], FEF_F32 if dtype == torch.float32 else FEF_BF16, workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), status.data_ptr(), _stream_ptr(stream))
     if st != FEF_OK:
         raise FefError(st, where)
     return out, status

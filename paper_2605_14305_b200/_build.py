@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libfef.so")
 SOURCES = ["fef_verify.cu", "fef_remask.cu", "fef_draft.cu", "fef_loop.cu", "fef_lmhead.cu", "fef_synth.cu",
-           "fef_adjust.cu", "fef_quant.cu", "fef_quant_rows.cu"]
+           "fef_adjust.cu", "fef_quant.cu", "fef_quant_rows.cu", "fef_quant_tiles.cu"]
 HEADERS = [os.path.join(CSRC, h) for h in ("fef_common.cuh", "fef_device_math.cuh", "fef_verify_params.cuh",
                                             "fef_residual.cuh", "fef_tensor_core.cuh", "fef_quant.cuh")] + [os.path.join(INCLUDE, "fef.h")]
 

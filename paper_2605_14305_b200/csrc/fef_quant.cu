@@ -99,59 +99,6 @@ __global__ void __launch_bounds__(kThreads) dequantize_kernel(const __grid_const
     *reinterpret_cast<float4*>(out + static_cast<int64_t>(v) * P.d + k) = r;
 }
 
-// ------------------------------------------------------------------------------------------- product ----
-constexpr int kRowBlock = 8;
-
-// One warp per vocabulary row and eight hidden rows; a lane takes eight columns of every other 128-column block's half.
-template <int DT>
-__global__ void __launch_bounds__(kThreads) product_kernel(const __grid_constant__ ProductParams P) {
-    const Layer& W = P.layer;
-    const int lane = threadIdx.x & 31;
-    const int64_t v = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-    const int r0 = blockIdx.y * kRowBlock, n = min(kRowBlock, P.rows - r0);
-    if (P.status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *P.status = FEF_OK;
-    if (v >= W.V) return;
-    float acc[kRowBlock];
-#pragma unroll
-    for (int r = 0; r < kRowBlock; ++r) acc[r] = 0.f;
-    const int word = lane & 15;                       // t = word / 4, piece = word % 4
-    const int inside = 32 * (word & 3) + 8 * (word >> 2);
-    for (int c = lane >> 4; c < W.blocks; c += 2) {
-        const int k = c * kBlock + inside;
-        if (k >= W.d) continue;
-        const uint32_t q = *reinterpret_cast<const uint32_t*>(W.packed + v * W.blocks * 64 + c * 64 + word * 4);
-        const int64_t at = (static_cast<int64_t>(c) * W.Vp + v) * (kBlock / W.G) + inside / W.G;
-        const float s = bf16_value(W.scale[at]);
-        const int z = W.zero ? W.zero[at] : 8;
-        float w[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) w[j] = static_cast<float>(static_cast<int>(q >> (4 * j) & 15u) - z);
-#pragma unroll
-        for (int r = 0; r < kRowBlock; ++r) {
-            if (r >= n) break;
-            const uint16_t* h = P.hidden + static_cast<int64_t>(r0 + r) * W.d + k;
-            float part = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) part = fmaf(w[j], bf16_value(h[j]), part);
-            acc[r] = fmaf(part, s, acc[r]);
-        }
-    }
-#pragma unroll
-    for (int r = 0; r < kRowBlock; ++r) {
-        if (r >= n) break;
-        float a = acc[r];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-        if (lane == 0) {
-            const int64_t at = static_cast<int64_t>(r0 + r) * P.ldo + v;
-            if constexpr (DT == FEF_F32)
-                reinterpret_cast<float*>(P.out)[at] = a;
-            else
-                reinterpret_cast<__nv_bfloat16*>(P.out)[at] = __float2bfloat16_rn(a);
-        }
-    }
-}
-
 // ---------------------------------------------------------------------------------------------- host ----
 static bool layer_ok(int V, int d, int G) {
     return V >= 1 && V <= (1 << 28) && (G == 32 || G == 64 || G == 128) && d >= G && d <= (1 << 20) && d % G == 0;
@@ -228,9 +175,18 @@ fef_status fef_lmhead_dequantize(const void* packed, const void* scale, const vo
     return cudaGetLastError() == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
 }
 
+size_t fef_lmhead_logits_quantized_workspace_bytes(int rows, int V, int d, int group) {
+    using namespace fef::quant;
+    if (rows < 1 || rows > (1 << 24) || !layer_ok(V, d, group)) return 0;
+    ProductParams P = {};
+    P.layer = make_layer(nullptr, nullptr, nullptr, V, d, group);
+    P.rows = rows;
+    return rows_kernel_takes(P) ? 256 : tiles_kernel_workspace(P);
+}
+
 fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, const void* scale, const void* zero, int rows,
                                        int V, int d, int group, void* logits, int64_t ldo, fef_dtype dt,
-                                       int32_t* device_status, void* cuda_stream) {
+                                       void* workspace, size_t workspace_bytes, int32_t* device_status, void* cuda_stream) {
     using namespace fef;
     using namespace fef::quant;
     if (dt != FEF_F32 && dt != FEF_BF16) return FEF_ERR_DTYPE;
@@ -239,9 +195,6 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
     if (!aligned16(hidden) || !aligned16(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(logits) ||
         (ldo * (dt == FEF_F32 ? 4 : 2)) % 16)
         return FEF_ERR_ALIGNMENT;
-    int dev;
-    const int sms = device_and_sms(&dev);
-    if (sms < 1) return FEF_ERR_CUDA;
     ProductParams P;
     P.layer = make_layer(packed, scale, zero, V, d, group);
     P.hidden = static_cast<const uint16_t*>(hidden);
@@ -249,15 +202,15 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
     P.ldo = ldo;
     P.rows = rows;
     P.status = device_status;
+    const bool few = rows_kernel_takes(P);
+    if (!few && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < tiles_kernel_workspace(P)))
+        return FEF_ERR_WORKSPACE;
+    int dev;
+    const int sms = device_and_sms(&dev);
+    if (sms < 1) return FEF_ERR_CUDA;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (rows_kernel_takes(P)) return launch_rows_kernel(P, dt, dev, sms, stream);
-    const dim3 grid((V + kWarps - 1) / kWarps, (rows + kRowBlock - 1) / kRowBlock);
-    if (grid.y > 65535) return FEF_ERR_INVALID_ARG;
-    if (dt == FEF_F32)
-        product_kernel<FEF_F32><<<grid, kThreads, 0, stream>>>(P);
-    else
-        product_kernel<FEF_BF16><<<grid, kThreads, 0, stream>>>(P);
-    return cudaGetLastError() == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
+    if (few) return launch_rows_kernel(P, dt, dev, sms, stream);
+    return launch_tiles_kernel(P, dt, workspace, dev, sms, stream);
 }
 
 }  // extern "C"

@@ -6,15 +6,10 @@
 // their four words two k-steps.  In the same way operand row g of the i-th eight rows of a unit of 32 is vocabulary row
 // 4 g + i: a lane's four scales lie together, and so do its four logits of a hidden row.
 //
-// A nibble becomes a bfloat16 number by masking alone: the bit pattern v < 256 in the lower half of a bfloat16 (the mantissa
-// and the lowest exponent bit) is the number v 2^-133, below and above the smallest normal number alike.  So the nibbles at
-// bits 0..3 of each half of a word stand for q 2^-133 and those at bits 4..7 for 16 q 2^-133: two masks, one shift, two masks
-// for eight weights.  The hidden rows are scaled by 2^100 (the products then lie in binary32's normal range; a row with
-// values beyond 2^27, or with none above 2^-80, by the power of two that brings its largest value near 2^126), a further 1/16
-// for the columns of the upper nibbles, all exact; the inverse is applied to the logits.  The zero points are taken off the
-// group's sum: sum (q - z) x = sum q x - z sum x, which costs two bits of the binary32 sum's accuracy (addends of 8.8 in the
-// root mean square of their weights instead of 2.6).  The products of a group are added up in binary32 by the matrix
-// instructions, then scaled in binary32.
+// Nibbles become bfloat16 numbers by masking alone, the hidden rows are scaled to suit (fef_quant.cuh).  The zero points are
+// taken off the group's sum: sum (q - z) x = sum q x - z sum x, which costs two bits of the binary32 sum's accuracy (addends of
+// 8.8 in the root mean square of their weights instead of 2.6).  The products of a group are added up in binary32 by the
+// matrix instructions, then scaled in binary32.
 //
 // One CTA of 16 warps per SM takes an even share of the vocabulary in units of 32 rows; all blocks of its units in a row are
 // cut into 16 equal runs, one per warp, so that all end together.  A unit that lies in more than one run is joined at the
@@ -36,7 +31,6 @@ constexpr int kUnit = 32;    // vocabulary rows of a warp: two 16-row operands
 constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
 constexpr size_t kSmemLimit = 232448;
-constexpr int kUsualShift = 100;
 
 struct Plan {
     int units;    // of the whole vocabulary
@@ -65,21 +59,11 @@ __device__ __forceinline__ void mma_16816_first(float (&d)[4], uint32_t a0, uint
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
 // Two bfloat16 numbers times a power of two, given by its bits.
 __device__ __forceinline__ uint32_t times(uint32_t x, uint32_t power) {
     uint32_t r;
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(power | power << 16));
     return r;
-}
-__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }  // |e| < 127
-// The power of two a hidden row is scaled by, from the bfloat16 bits of its largest value.
-__device__ __forceinline__ int row_shift(uint32_t largest) {
-    const int e = static_cast<int>(largest >> 7);   // biased; 255: the row's logits are no numbers anyway
-    return largest == 0u || (e >= 47 && e < 154) || e == 255 ? kUsualShift : 253 - e;
 }
 
 // What a warp needs of one block of its unit: operand rows 4 g + i, their scales and zero points.
@@ -260,9 +244,9 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
                     const uint4 &lo = f.q[2 * m], &hi = f.q[2 * m + 1];
                     const uint32_t a = w == 0 ? lo.x : w == 1 ? lo.y : w == 2 ? lo.z : lo.w;
                     const uint32_t b = w == 0 ? hi.x : w == 1 ? hi.y : w == 2 ? hi.z : hi.w;
-                    const uint32_t a0 = a & 0x000F000Fu, b0 = b & 0x000F000Fu, a1 = a & 0x00F000F0u, b1 = b & 0x00F000F0u;
-                    const uint32_t a2 = a >> 8 & 0x000F000Fu, b2 = b >> 8 & 0x000F000Fu;
-                    const uint32_t a3 = a >> 8 & 0x00F000F0u, b3 = b >> 8 & 0x00F000F0u;
+                    const uint32_t a0 = a & kLowNibbles, b0 = b & kLowNibbles, a1 = a & kHighNibbles, b1 = b & kHighNibbles;
+                    const uint32_t a2 = a >> 8 & kLowNibbles, b2 = b >> 8 & kLowNibbles;
+                    const uint32_t a3 = a >> 8 & kHighNibbles, b3 = b >> 8 & kHighNibbles;
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         if (w == j * (4 / N))

@@ -24,8 +24,8 @@ def test_argument_checks_return_before_touching_the_device(fef):
     def dequantize(p=A, s=A, z=A, V=10, d=128, g=32, out=A):
         return lib.fef_lmhead_dequantize(p, s, z, V, d, g, out, None)
 
-    def product(h=A, p=A, s=A, z=A, rows=3, V=10, d=128, g=32, out=A, ldo=12, dt=0, st=None):
-        return lib.fef_lmhead_logits_quantized(h, p, s, z, rows, V, d, g, out, ldo, dt, st, None)
+    def product(h=A, p=A, s=A, z=A, rows=3, V=10, d=128, g=32, out=A, ldo=12, dt=0, ws=A, wsb=1 << 20, st=None):
+        return lib.fef_lmhead_logits_quantized(h, p, s, z, rows, V, d, g, out, ldo, dt, ws, wsb, st, None)
 
     for call in (quantize, dequantize, product):
         assert call(p=None) == bad and call(s=None) == bad
@@ -40,5 +40,11 @@ def test_argument_checks_return_before_touching_the_device(fef):
     assert product(h=None) == bad and product(out=None) == bad and product(rows=0) == bad and product(rows=(1 << 24) + 1) == bad
     assert product(ldo=8) == bad and product(ldo=11) == align and product(ldo=12, dt=1) == align and product(dt=2) == fef.FEF_ERR_DTYPE
     assert product(h=A + 2) == align and product(out=A + 8) == align
+    for kw in (dict(ws=None), dict(ws=A + 16), dict(wsb=16000)):
+        assert product(rows=40, **kw) == fef.FEF_ERR_WORKSPACE and product(rows=4, **kw) == fef.FEF_ERR_CUDA
+    assert product(rows=40) == fef.FEF_ERR_CUDA
+    need = fef.fef_lmhead_logits_quantized_workspace_bytes
+    assert need(0, 10, 128, 32) == 0 and need(3, 10, 100, 32) == 0 and need(3, 10, 128, 48) == 0 and need(3, 10, 128, 32) == 256
+    assert need(40, 10, 128, 32) >= 64 * 128 * 2 + 64 * 4 * 4 + 64 * 4
     with pytest.raises(RuntimeError):
         fef.fef_lmhead_quantize(torch.zeros((2, 32), dtype=torch.bfloat16))
