@@ -473,7 +473,7 @@ fef_status fef_lmhead_logits(const void* hidden, const void* weight, int rows, i
  *            word 4 t + w holds columns 32 w + 8 t .. 32 w + 8 t + 7, lowest nibble first
  *   scale    device, [blocks][Vp][128 / group] bfloat16, Vp = V rounded up to a multiple of 32; zero behind d and V
  *   zero     device, uint8, laid out like scale; or NULL
- *   d        a multiple of `group`; all three buffers 16-byte aligned
+ *   d        a multiple of `group`; packed 32-byte aligned, scale and zero 16-byte aligned
  *
  * fef_lmhead_quantize writes such a layer (all three buffers in full, padding included) from weight, device, [V][d] bfloat16
  * row-major, 16-byte aligned.  For every group, with rint to the nearest whole number, ties to even:

@@ -115,6 +115,7 @@ static Layer make_layer(const void* packed, const void* scale, const void* zero,
     W.G = G;
     return W;
 }
+static bool aligned32(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 31) == 0; }
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 static int device_and_sms(int* dev) {
     static int sms[64];
@@ -134,7 +135,7 @@ fef_status fef_lmhead_quantize(const void* weight, int V, int d, int group, void
     using namespace fef;
     using namespace fef::quant;
     if (!weight || !packed || !scale || !layer_ok(V, d, group)) return FEF_ERR_INVALID_ARG;
-    if (!aligned16(weight) || !aligned16(packed) || !aligned16(scale) || !aligned16(zero)) return FEF_ERR_ALIGNMENT;
+    if (!aligned16(weight) || !aligned32(packed) || !aligned16(scale) || !aligned16(zero)) return FEF_ERR_ALIGNMENT;
     int dev;
     const int sms = device_and_sms(&dev);
     if (sms < 1) return FEF_ERR_CUDA;
@@ -164,7 +165,7 @@ fef_status fef_lmhead_dequantize(const void* packed, const void* scale, const vo
     using namespace fef;
     using namespace fef::quant;
     if (!packed || !scale || !values || !layer_ok(V, d, group)) return FEF_ERR_INVALID_ARG;
-    if (!aligned16(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(values)) return FEF_ERR_ALIGNMENT;
+    if (!aligned32(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(values)) return FEF_ERR_ALIGNMENT;
     int dev;
     const int sms = device_and_sms(&dev);
     if (sms < 1) return FEF_ERR_CUDA;
@@ -192,7 +193,7 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
     if (dt != FEF_F32 && dt != FEF_BF16) return FEF_ERR_DTYPE;
     if (!hidden || !packed || !scale || !logits || !layer_ok(V, d, group)) return FEF_ERR_INVALID_ARG;
     if (rows < 1 || rows > (1 << 24) || ldo < V) return FEF_ERR_INVALID_ARG;
-    if (!aligned16(hidden) || !aligned16(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(logits) ||
+    if (!aligned16(hidden) || !aligned32(packed) || !aligned16(scale) || !aligned16(zero) || !aligned16(logits) ||
         (ldo * (dt == FEF_F32 ? 4 : 2)) % 16)
         return FEF_ERR_ALIGNMENT;
     ProductParams P;

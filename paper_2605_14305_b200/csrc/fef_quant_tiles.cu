@@ -3,17 +3,23 @@
 //
 // prepare_kernel brings the hidden rows into the operand's form once (workspace): scaled by a power of two, the eight columns
 // of every packed word in the order 0 4, 1 5, 2 6, 3 7 in which masking delivers them (fef_quant.cuh), with the sums of every
-// group.  product_tiles_kernel then takes tiles of 128 vocabulary rows x NT hidden rows, one CTA per SM:
-//   warps 8..15   weights: packed nibbles from global memory (kAhead blocks in flight per warp) to bfloat16 numbers in the
-//                 128-byte-swizzled layout in shared memory;
-//   warp 16       one thread brings the hidden rows of the same 128 columns in by TMA;
-//   warp 17       one thread issues the MMAs (128 x NT x 16), a fresh accumulator for every group of a row's weights;
-//   warps 0..7    take each group's accumulator out of tensor memory, subtract z times the group's sum, scale it and add it
-//                 to the logits in registers: the vocabulary rows are the lanes, so a group's scale is one number per thread.
-// The weights are the left operand for that reason.  Every wait is bounded.
+// group.  product_tiles_kernel then takes tiles of 256 vocabulary rows x NT hidden rows, one CTA of 20 warps per SM, as two
+// pipelines of 128 vocabulary rows that share the hidden rows and nothing else:
+//   2 x 4 warps  weights: packed nibbles from global memory (kAhead blocks in flight per warp) to bfloat16 numbers in tensor
+//                memory, a vocabulary row per lane (through shared memory, writing and reading them took 512 of its cycles a
+//                block: 160 us at 64 rows x 126464 x 4096);
+//   1 warp       brings the hidden rows of the same 128 columns in by TMA, and on a ring of their own the groups' sums,
+//                scales and zero points (read from global memory by the warps that need them, their latency set the pace);
+//   2 x 1 warp   issue the MMAs (128 x NT x 16), a fresh accumulator for every group of a row's weights;
+//   2 x 4 warps  take each group's accumulator out of tensor memory, subtract z times the group's sum, scale it and add it to
+//                the logits in registers: the vocabulary rows are the lanes, so a group's scale is one number per thread.  The
+//                weights are the left operand for that reason.
+// A block's hand-overs from warp to warp, not its arithmetic, set the pace: hence two pipelines side by side, few warps with
+// much to do each, and waits that poll several barriers at once.  Every wait is bounded.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <stddef.h>
 
 #include "fef_device_math.cuh"
 #include "fef_quant.cuh"
@@ -23,28 +29,47 @@ namespace fef {
 namespace quant {
 namespace {
 
-constexpr int kTileV = 128;                   // vocabulary rows of a tile
-constexpr int kStages = 3;
-constexpr int kAccumulators = 4;
-constexpr int kABytes = kTileV * kBlock * 2;  // 32 KiB: two halves of 64 columns
-constexpr int kAhead = 4;
-constexpr int kEpilogueWarps = 8, kWeightWarps = 8;
-constexpr int kThreads = (kEpilogueWarps + kWeightWarps + 2) * 32;
+constexpr int kPipes = 2;
+constexpr int kPipeV = 128, kTileV = kPipes * kPipeV;   // vocabulary rows
+constexpr int kAStages = 2;                   // of a pipeline: blocks of unpacked weights in tensor memory
+constexpr int kACols = kBlock / 2;            // 32-bit columns of such a block
+constexpr int kSides = 4;                     // ring of what the epilogue needs of a block: sums, scales, zero points
+constexpr int kAhead = 2;                     // blocks of weights in flight per warp
+constexpr int kRoleWarps = 4;                 // warps of a pipeline's epilogue, and of its weights
+constexpr int kThreads = (2 * kPipes * kRoleWarps + 4) * 32;   // the last four warps: TMA, an issuer per pipeline, one idle
+constexpr int kWeightWarp0 = kPipes * kRoleWarps, kTmaWarp = 2 * kPipes * kRoleWarps, kIssueWarp0 = kTmaWarp + 1;
+// Registers per thread: what the kernel is launched with, and what the three kinds of warpgroups keep of it; the shares add up
+// to the launch's total exactly.
+constexpr int kLaunchRegs = 96, kEpilogueRegs = 112, kWeightRegs = 88, kControlRegs = 80;
+static_assert(kPipes * kRoleWarps * (kEpilogueRegs + kWeightRegs) + 4 * kControlRegs == kThreads / 32 * kLaunchRegs, "");
 constexpr unsigned long long kWaitNs = 1000000000ull;
 
 struct TileParams {
     ProductParams P;
     int tiles, row_blocks, items, padded;   // padded: hidden rows rounded up to whole tiles
     const float* sums;                      // [blocks * 128 / G][padded]
-    const int* shifts;                      // [padded]
+    const float2* backs;                    // [padded]: two powers of two that scale the logits back
     int out_bf16;
 };
 
+template <int NT>
+struct Sizes {
+    static constexpr int kBBytes = NT * kBlock * 2, kBStages = 6;
+    // tensor memory of a pipeline: accumulators, then weights
+    static constexpr int kAccumulators = NT == 64 ? 2 : 4;
+    static constexpr int kPipeCols = kAccumulators * NT + kAStages * kACols, kTmemCols = kPipes * kPipeCols;
+    static_assert(kTmemCols == 512, "");
+};
+
 struct Shared {
-    uint64_t full[kStages];
-    uint64_t empty[kStages];
-    uint64_t acc_full[kAccumulators];
-    uint64_t acc_empty[kAccumulators];
+    uint64_t a_full[kPipes][kAStages];
+    uint64_t a_empty[kPipes][kAStages];
+    uint64_t acc_full[kPipes][4];
+    uint64_t acc_empty[kPipes][4];
+    uint64_t b_full[6];
+    uint64_t b_empty[6];
+    uint64_t side_full[kSides];
+    uint64_t side_empty[kSides];
     uint64_t drained;
     uint32_t tmem_base;
     int abort_flag;
@@ -55,7 +80,7 @@ struct PrepareParams {
     const uint16_t* hidden;   // [rows][d]
     uint16_t* operand;        // [padded][blocks * 128]
     float* sums;
-    int* shifts;
+    float2* backs;
     int rows, padded, d, blocks, words;   // words: 32-column pieces per group
     int32_t* status;
 };
@@ -69,6 +94,7 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const __grid_c
     if (tid == 0) s_top = 0u;
     __syncthreads();
     const uint16_t* src = P.hidden + static_cast<int64_t>(row) * P.d;
+    uint4* to = reinterpret_cast<uint4*>(P.operand + static_cast<int64_t>(row) * P.blocks * kBlock);
     const int pieces = P.blocks * 16;   // of eight columns; d is a multiple of 32
     auto load = [&](int p) {
         return row < P.rows && p * 8 < P.d ? __ldg(reinterpret_cast<const uint4*>(src) + p) : make_uint4(0u, 0u, 0u, 0u);
@@ -83,7 +109,7 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const __grid_c
     __syncthreads();
     const int shift = row_shift(s_top);
     const float f0 = exp2_int(shift / 2), f1 = exp2_int(shift - shift / 2);
-    if (tid == 0) P.shifts[row] = shift;
+    if (tid == 0) P.backs[row] = make_float2(exp2_int((133 - shift) / 2), exp2_int(133 - shift - (133 - shift) / 2));
     for (int p = tid; p < pieces; p += kPrepareThreads) {   // (pieces is a multiple of 16: a group's lanes come together)
         const uint4 x = load(p);
         float v[8], total = 0.f;
@@ -93,8 +119,7 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const __grid_c
             v[j] = v[j] * f0 * f1;
             total += v[j] * exp2_int(-67) * exp2_int(-66);
         }
-        reinterpret_cast<uint4*>(P.operand + static_cast<int64_t>(row) * P.blocks * kBlock)[p] =
-            make_uint4(bf16_pair(v[0], v[4]), bf16_pair(v[1] * 0.0625f, v[5] * 0.0625f), bf16_pair(v[2], v[6]),
+        to[p] = make_uint4(bf16_pair(v[0], v[4]), bf16_pair(v[1] * 0.0625f, v[5] * 0.0625f), bf16_pair(v[2], v[6]),
                        bf16_pair(v[3] * 0.0625f, v[7] * 0.0625f));
         const unsigned lanes = __activemask();
         for (int o = 1; o < P.words * 4; o <<= 1) total += __shfl_xor_sync(lanes, total, o);
@@ -103,6 +128,34 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const __grid_c
 }
 
 // ------------------------------------------------------------------------------------------- tiles ----
+// A bounded wait that reads no clock as long as it is short (the hand-overs between warps set this kernel's pace).
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
+    for (int poll = 0; poll < 4; ++poll)
+        if (mbar_try_wait(bar, parity)) return true;
+    return mbar_wait_bounded(bar, parity, abort_flag, kWaitNs);
+}
+
+// A warp waits for three barriers (given by their offset in Shared) at once, each polled by a lane of its own: one round trip.
+__device__ __forceinline__ bool wait_for_all(Shared& sh, uint32_t o0, uint32_t p0, uint32_t o1, uint32_t p1, uint32_t o2, uint32_t p2) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t offset = lane == 0 ? o0 : lane == 1 ? o1 : o2, parity = lane == 0 ? p0 : lane == 1 ? p1 : p2;
+    uint64_t* bar = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(&sh) + offset);
+    return __all_sync(0xFFFFFFFFu, lane > 2 || wait_for(bar, parity, &sh.abort_flag));
+}
+
+// A place in a ring of S and the phase of its barriers.
+template <int S>
+struct Turn {
+    int at = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void advance() {
+        if (++at == S) {
+            at = 0;
+            phase ^= 1u;
+        }
+    }
+};
+
 // 16 consecutive columns of this thread's accumulator row; the caller waits for them.
 __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
     asm volatile(
@@ -111,7 +164,12 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, uint32_t (&r)[16]) {
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
 }
-__device__ __forceinline__ void tmem_wait_load() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// (the registers are tied to the wait, so that nothing that reads them moves before it)
+__device__ __forceinline__ void tmem_wait_load(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                   "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])::"memory");
+}
 __device__ __forceinline__ uint64_t pair(float lo, float hi) {
     return static_cast<uint64_t>(__float_as_uint(hi)) << 32 | __float_as_uint(lo);
 }
@@ -121,140 +179,237 @@ __device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c)
     return d;
 }
 
+// 1-D bulk copy global -> shared.
+__device__ __forceinline__ void bulk_copy(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem_u32(dst)),
+                 "l"(src), "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// Of a block: sums [N][NT], scales [256][N], zero points [256][N].
+template <int NT, int N>
+struct Side {
+    float sums[N][NT];
+    uint16_t scale[kTileV * N];
+    uint8_t zero[kTileV * N];
+};
+
+// The lower word of smem_desc_sw128's descriptor (the upper one is the same for all), and the MMA that takes it and a left
+// operand in tensor memory: D (+)= A * B^T.
+__device__ __forceinline__ uint32_t desc_low(uint32_t smem_addr) { return (smem_addr >> 4 & 0x3FFFu) | 1u << 16; }
+__device__ __forceinline__ void tc_mma_low(uint32_t tmem_d, uint32_t tmem_a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
+    constexpr uint32_t kHigh = 1024u >> 4 | 1u << 14 | 2u << 29;
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        ".reg .b64 db;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, {%6, %6, %6, %6}, p;\n\t"
+        "}\n" ::"r"(tmem_d),
+        "r"(tmem_a), "r"(b), "r"(idesc), "r"(accumulate), "r"(kHigh), "r"(0u)
+        : "memory");
+}
+// 16 columns of this thread's row; the caller waits for the stores.
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(
+            addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 32 bytes, 32-byte aligned.
+__device__ __forceinline__ void load_sector(const void* p, uint32_t (&r)[8]) {
+    asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "l"(p));
+}
+
+__device__ __forceinline__ void put_logit(float* at, float y) { *at = y; }
+__device__ __forceinline__ void put_logit(__nv_bfloat16* at, float y) { *at = __float2bfloat16_rn(y); }
+
+// One vocabulary row's logits of `kCols` hidden rows (the first `many` of them exist), scaled back.
+template <int kCols, typename Out>
+__device__ __forceinline__ void store_column(Out* out, int64_t ldo, const uint64_t (&total)[kCols / 2],
+                                             const float2* __restrict__ backs, int many) {
+#pragma unroll
+    for (int h = 0; h < kCols; h += 8) {
+        float4 back[4];   // (padded: always within the array)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) back[i] = __ldg(reinterpret_cast<const float4*>(backs + h) + i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t two = total[h / 2 + i];
+            if (h + 2 * i < many) put_logit(out, __uint_as_float(static_cast<uint32_t>(two)) * back[i].x * back[i].y);
+            out += ldo;
+            if (h + 2 * i + 1 < many) put_logit(out, __uint_as_float(static_cast<uint32_t>(two >> 32)) * back[i].z * back[i].w);
+            out += ldo;
+        }
+    }
+}
+
 template <int NT, int N>   // hidden rows of a tile, groups per block
 __global__ void __launch_bounds__(kThreads, 1)
 product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ TileParams T) {
-    constexpr int kBBytes = NT * kBlock * 2, kStageBytes = kABytes + kBBytes;
-    constexpr int kTmemCols = NT * kAccumulators;
-    constexpr uint32_t kInstr = (1u << 4) | (1u << 7) | (1u << 10) | ((NT >> 3) << 17) | ((kTileV >> 4) << 24);
+    using S = Sizes<NT>;
+    constexpr int kAccumulators = S::kAccumulators;
+    constexpr uint32_t kInstr = (1u << 4) | (1u << 7) | (1u << 10) | ((NT >> 3) << 17) | ((kPipeV >> 4) << 24);
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    Shared& sh = *reinterpret_cast<Shared*>(smem + kStages * kStageBytes);
+    Side<NT, N>* side = reinterpret_cast<Side<NT, N>*>(smem + S::kBStages * S::kBBytes);
+    Shared& sh = *reinterpret_cast<Shared*>(side + kSides);
     volatile int* abort_flag = &sh.abort_flag;
     const ProductParams& P = T.P;
     const Layer& W = P.layer;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(sh.full + s, 1 + kWeightWarps);
-            mbar_init(sh.empty + s, 1);
+        for (int p = 0; p < kPipes; ++p) {
+            for (int s = 0; s < kAStages; ++s) {
+                mbar_init(&sh.a_full[p][s], kRoleWarps);
+                mbar_init(&sh.a_empty[p][s], 1);
+            }
+            for (int a = 0; a < kAccumulators; ++a) {
+                mbar_init(&sh.acc_full[p][a], 1);
+                mbar_init(&sh.acc_empty[p][a], kRoleWarps);
+            }
         }
-        for (int a = 0; a < kAccumulators; ++a) {
-            mbar_init(sh.acc_full + a, 1);
-            mbar_init(sh.acc_empty + a, kEpilogueWarps);
+        for (int s = 0; s < S::kBStages; ++s) {
+            mbar_init(sh.b_full + s, 1);
+            mbar_init(sh.b_empty + s, kPipes);
         }
-        mbar_init(&sh.drained, 1);
+        for (int q = 0; q < kSides; ++q) {
+            mbar_init(sh.side_full + q, 1);
+            mbar_init(sh.side_empty + q, kPipes * kRoleWarps);
+        }
+        mbar_init(&sh.drained, kPipes);
         sh.abort_flag = 0;
         mbar_fence_init();
     }
-    if (warp == 0) tmem_alloc(&sh.tmem_base, kTmemCols);  // (one CTA per SM: the columns are always free)
+    if (warp == 0) tmem_alloc(&sh.tmem_base, S::kTmemCols);  // (one CTA per SM: the columns are always free)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&sh.tmem_base);
-    int issued = 0;
+    int issued = 0, sides = 0;
     auto gave_up = [&]() {
         *abort_flag = 1;
-        if (lane == 0) report(P.status, FEF_ERR_TIMEOUT);
+        report(P.status, FEF_ERR_TIMEOUT);
     };
+    const int items = blockIdx.x < T.items ? (T.items - 1 - blockIdx.x) / gridDim.x + 1 : 0;   // of this CTA
+    const int count = items * W.blocks;
 
-    if (warp == kEpilogueWarps + kWeightWarps) {
+    if (warp >= kTmaWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kControlRegs));
+    if (warp == kTmaWarp) {
         // ------------------------------------------------------------ hidden rows, one thread
-        if (lane == 0) {
+        if (elect_one()) {
             cudaGridDependencySynchronize();
-            int stage = 0;
-            uint32_t phase = 0;
+            Turn<S::kBStages> stage;
+            Turn<kSides> slot;
             bool ok = true;
             for (int item = blockIdx.x; ok && item < T.items; item += gridDim.x) {
                 const int row0 = item % T.row_blocks * NT;
+                const int64_t v0 = static_cast<int64_t>(item / T.row_blocks) * kTileV;
+                const uint32_t rows = static_cast<uint32_t>(min(static_cast<int64_t>(kTileV), W.Vp - v0));   // a multiple of 32
                 for (int c = 0; c < W.blocks; ++c) {
-                    if (!mbar_wait_bounded(sh.empty + stage, phase ^ 1u, abort_flag, kWaitNs)) {
+                    if (!wait_for(sh.b_empty + stage.at, stage.phase ^ 1u, abort_flag)) {
                         gave_up();
                         ok = false;
                         break;
                     }
-                    unsigned char* dst = smem + stage * kStageBytes + kABytes;
-                    mbar_arrive_expect_tx(sh.full + stage, kBBytes);
-                    tma_load_2d(dst, &map, c * kBlock, row0, sh.full + stage);
-                    tma_load_2d(dst + kBBytes / 2, &map, c * kBlock + 64, row0, sh.full + stage);
+                    unsigned char* dst = smem + stage.at * S::kBBytes;
+                    mbar_arrive_expect_tx(sh.b_full + stage.at, S::kBBytes);
+                    tma_load_2d(dst, &map, c * kBlock, row0, sh.b_full + stage.at);
+                    tma_load_2d(dst + S::kBBytes / 2, &map, c * kBlock + 64, row0, sh.b_full + stage.at);
                     ++issued;
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1u;
+                    stage.advance();
+                    if (!wait_for(sh.side_empty + slot.at, slot.phase ^ 1u, abort_flag)) {
+                        gave_up();
+                        ok = false;
+                        break;
                     }
+                    uint64_t* bar = sh.side_full + slot.at;
+                    Side<NT, N>& to = side[slot.at];
+                    const int64_t at = (static_cast<int64_t>(c) * W.Vp + v0) * N;
+                    mbar_arrive_expect_tx(bar, N * NT * 4 + rows * N * (W.zero ? 3 : 2));
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        bulk_copy(to.sums[j], T.sums + static_cast<int64_t>(c * N + j) * T.padded + row0, NT * 4, bar);
+                    if (W.zero) bulk_copy(to.zero, W.zero + at, rows * N, bar);
+                    bulk_copy(to.scale, W.scale + at, rows * N * 2, bar);
+                    ++sides;
+                    slot.advance();
                 }
             }
         }
-    } else if (warp == kEpilogueWarps + kWeightWarps + 1) {
-        // -------------------------------------------------------------------------- MMAs, one thread
-        if (lane == 0) {
-            int stage = 0, acc = 0;
-            uint32_t phase = 0, acc_phase = 0;
-            bool ok = true;
-            for (int item = blockIdx.x; ok && item < T.items; item += gridDim.x)
-                for (int c = 0; ok && c < W.blocks; ++c) {
-                    if (!mbar_wait_bounded(sh.full + stage, phase, abort_flag, kWaitNs)) {
-                        gave_up();
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t a_at = smem_u32(smem + stage * kStageBytes), b_at = a_at + kABytes;
+    } else if (warp >= kIssueWarp0 + kPipes) {
+        // (the control warpgroup's fourth warp)
+    } else if (warp >= kIssueWarp0) {
+        // -------------------------------------------------------------------------- MMAs
+        // A whole warp runs the loop and the elected lane issues: in a branch of lane 0 alone, bringing the descriptors into
+        // uniform registers took most of the time.
+        const int pipe = warp - kIssueWarp0;
+        const uint32_t b_base = desc_low(smem_u32(smem));
+        const uint32_t tmem = tmem_base + pipe * S::kPipeCols;
+        Turn<kAStages> a;
+        Turn<S::kBStages> b;
+        Turn<kAccumulators> acc;
+        bool ok = true;
+        for (int at = 0; ok && at < count; ++at) {
+            const uint32_t a_at = tmem + kAccumulators * NT + a.at * kACols, b_at = b_base + b.at * (S::kBBytes / 16);
 #pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        if (!mbar_wait_bounded(sh.acc_empty + acc, acc_phase ^ 1u, abort_flag, kWaitNs)) {
-                            gave_up();
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
+            for (int j = 0; j < N; ++j) {
+                if (!wait_for_all(sh, offsetof(Shared, a_full) + (pipe * kAStages + a.at) * 8, a.phase, offsetof(Shared, b_full) + b.at * 8,
+                                  b.phase, offsetof(Shared, acc_empty) + (pipe * 4 + acc.at) * 8, acc.phase ^ 1u)) {
+                    gave_up();
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                if (elect_one()) {
 #pragma unroll
-                        for (int k = 0; k < 8 / N; ++k) {
-                            const int step = j * (8 / N) + k, half = step / 4, inside = step % 4;
-                            tc_mma(tmem_base + acc * NT,
-                                   smem_desc_sw128(a_at + half * (kABytes / 2)) + static_cast<uint64_t>(2 * inside),
-                                   smem_desc_sw128(b_at + half * (kBBytes / 2)) + static_cast<uint64_t>(2 * inside), kInstr,
-                                   k != 0 ? 1u : 0u);
-                        }
-                        tc_commit(sh.acc_full + acc);
-                        if (++acc == kAccumulators) {
-                            acc = 0;
-                            acc_phase ^= 1u;
-                        }
+                    for (int k = 0; k < 8 / N; ++k) {
+                        const int step = j * (8 / N) + k, half = step / 4, inside = step % 4;
+                        tc_mma_low(tmem + acc.at * NT, a_at + 8 * step,
+                                   b_at + half * (S::kBBytes / 32) + 2 * inside, kInstr, k != 0 ? 1u : 0u);
                     }
-                    if (ok) tc_commit(sh.empty + stage);   // arrives when these MMAs have read the stage
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1u;
+                    tc_commit(&sh.acc_full[pipe][acc.at]);
+                    if (j == N - 1) {   // (they arrive when these MMAs have read the stages)
+                        tc_commit(&sh.a_empty[pipe][a.at]);
+                        tc_commit(sh.b_empty + b.at);
                     }
                 }
-            // everything issued has finished before the tensor memory goes back
-            tc_commit(&sh.drained);
-            mbar_wait_bounded(&sh.drained, 0u, abort_flag, kWaitNs);
+                __syncwarp();
+                acc.advance();
+            }
+            a.advance();
+            b.advance();
         }
-    } else if (warp >= kEpilogueWarps) {
+        // everything issued has finished before the tensor memory goes back
+        if (elect_one()) tc_commit(&sh.drained);
+        __syncwarp();
+        wait_for(&sh.drained, 0u, abort_flag);
+    } else if (warp >= kWeightWarp0) {
         // ------------------------------------------------------------------------------------ weights
-        // Warp w takes rows 16 w .. 16 w + 15 of the tile.  A lane's 16 bytes (one t) of a row are four chunks of eight columns of
-        // the operand; rows r and r + 4 side by side in a quarter-warp lie in different halves of the swizzled 128 bytes.
-        const int w = warp - kEpilogueWarps, g = lane >> 2, t = lane & 3;
-        const int r = (g >> 1) + 4 * (g & 1);
-        const int64_t pitch = static_cast<int64_t>(W.blocks) * 64;
-        const int mine = blockIdx.x < T.items ? (T.items - 1 - blockIdx.x) / gridDim.x + 1 : 0;   // items of this CTA
-        const int64_t count = static_cast<int64_t>(mine) * W.blocks;
-        int64_t fetch_at = 0;
-        int fetch_item = blockIdx.x, fetch_block = 0;
-        const uint8_t* from[2];
+        // A lane takes one row: the 64 bytes of a block are its word 4 t + w, of columns 32 w + 8 t .. + 7, for every t and w.
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWeightRegs));
+        const int pipe = (warp - kWeightWarp0) / kRoleWarps, quarter = (warp - kWeightWarp0) % kRoleWarps;
+        const uint32_t tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + pipe * S::kPipeCols + kAccumulators * NT;
+        const int blocks = count;
+        int left = blocks, fetch_item = blockIdx.x, fetch_block = 0;
+        const uint8_t* fetch_w = nullptr;
         auto seek = [&]() {   // (rows behind V are read as the last one; their logits are not stored)
-            const int64_t v = static_cast<int64_t>(fetch_item / T.row_blocks) * kTileV + w * 16 + r;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) from[i] = W.packed + min(v + 8 * i, static_cast<int64_t>(W.V - 1)) * pitch + t * 16;
+            const int64_t v = static_cast<int64_t>(fetch_item / T.row_blocks) * kTileV + pipe * kPipeV + quarter * 32 + lane;
+            fetch_w = W.packed + min(v, static_cast<int64_t>(W.V - 1)) * (static_cast<int64_t>(W.blocks) * 64);
         };
-        uint4 ahead[kAhead][2];
-        auto fetch = [&](uint4 (&q)[2]) {   // past the end the last block is fetched again: no branch around the loads
+        uint32_t ahead[kAhead][2][8];   // words 4 t + w: t = 0, 1 and t = 2, 3
+        auto fetch = [&](uint32_t (&q)[2][8]) {   // past the end the last block is fetched again: no branch around the loads
 #pragma unroll
-            for (int i = 0; i < 2; ++i) q[i] = ld_global_nc_v4(from[i] + fetch_block * 64);
-            const int more = fetch_at + 1 < count ? 1 : 0;
-            fetch_at += more;
+            for (int i = 0; i < 2; ++i) load_sector(fetch_w + fetch_block * 64 + i * 32, q[i]);
+            const int more = left > 1 ? 1 : 0;
+            left -= more;
             fetch_block += more;
             if (fetch_block == W.blocks) {
                 fetch_block = 0;
@@ -262,111 +417,121 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 seek();
             }
         };
-        if (count > 0) {
+        if (blocks > 0) {
             seek();
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) fetch(ahead[i]);
-            int stage = 0;
-            uint32_t phase = 0;
+            Turn<kAStages> stage;
             bool ok = true;
-            for (int64_t at = 0; ok && at < count; at += kAhead) {
+            // (after a wait that ran out the rest goes by without waits and arrivals)
+            auto put = [&](const uint32_t (&q)[2][8]) {
+                if (ok && !__all_sync(0xFFFFFFFFu, lane > 0 || wait_for(&sh.a_empty[pipe][stage.at], stage.phase ^ 1u, abort_flag))) {
+                    gave_up();
+                    ok = false;
+                }
+                tc_fence_after();
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {   // 32 columns of the operand
+                    uint32_t y[16];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const uint32_t x = q[t >> 1][(t & 1) * 4 + w];
+                        y[4 * t] = x & kLowNibbles;
+                        y[4 * t + 1] = x & kHighNibbles;
+                        y[4 * t + 2] = x >> 8 & kLowNibbles;
+                        y[4 * t + 3] = x >> 8 & kHighNibbles;
+                    }
+                    tmem_store16(tmem + stage.at * kACols + w * 16, y);
+                }
+            };
+            auto hand_over = [&]() {
+                tmem_wait_store();
+                tc_fence_before();
+                __syncwarp();
+                if (ok && lane == 0) mbar_arrive(&sh.a_full[pipe][stage.at]);
+                stage.advance();
+            };
+            int at = 0;
+            for (; at + kAhead <= blocks; at += kAhead) {
 #pragma unroll
                 for (int n = 0; n < kAhead; ++n) {
-                    if (!ok || at + n >= count) break;
-                    if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(sh.empty + stage, phase ^ 1u, abort_flag, kWaitNs))) {
-                        gave_up();
-                        ok = false;
-                        break;
-                    }
-                    unsigned char* dst = smem + stage * kStageBytes + (w * 16 + r) * 128;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint4& q = ahead[n][i];
-                            const uint32_t x = j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w;
-                            // chunk 4 j + t of the block's sixteen: half j / 2, column 4 (j % 2) + t of its eight
-                            *reinterpret_cast<uint4*>(dst + (j / 2) * (kABytes / 2) + i * 1024 + (((j & 1) * 4 + t) ^ r) * 16) =
-                                make_uint4(x & kLowNibbles, x & kHighNibbles, x >> 8 & kLowNibbles, x >> 8 & kHighNibbles);
-                        }
+                    put(ahead[n]);
                     fetch(ahead[n]);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(sh.full + stage);
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1u;
-                    }
+                    hand_over();
                 }
             }
+#pragma unroll
+            for (int n = 0; n < kAhead - 1; ++n)
+                if (at + n < blocks) {
+                    put(ahead[n]);
+                    hand_over();
+                }
         }
     } else {
         // ----------------------------------------------------------------------------------- epilogue
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
         cudaGridDependencySynchronize();
-        constexpr int kCols = NT / 2;                 // hidden rows of this warp
-        const int quarter = warp & 3, col0 = (warp >> 2) * kCols;
-        const uint32_t tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + col0;
-        int acc = 0;
-        uint32_t acc_phase = 0;
+        const int pipe = warp / kRoleWarps, quarter = warp % kRoleWarps, row_in_tile = pipe * kPipeV + quarter * 32 + lane;
+        const uint32_t tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + pipe * S::kPipeCols;
+        const bool zeros = W.zero != nullptr;
+        Turn<kAccumulators> acc;
+        Turn<kSides> slot;
         bool ok = true;
         for (int item = blockIdx.x; ok && item < T.items; item += gridDim.x) {
-            const int row0 = item % T.row_blocks * NT + col0;
-            const int64_t v = static_cast<int64_t>(item / T.row_blocks) * kTileV + quarter * 32 + lane;
-            const int64_t vs = min(v, static_cast<int64_t>(W.Vp - 1));
-            uint64_t total[kCols / 2];
+            uint64_t total[NT / 2];
 #pragma unroll
-            for (int i = 0; i < kCols / 2; ++i) total[i] = 0ull;
+            for (int i = 0; i < NT / 2; ++i) total[i] = 0ull;
             for (int c = 0; ok && c < W.blocks; ++c) {
 #pragma unroll 1
                 for (int j = 0; j < N; ++j) {
-                    const int64_t at = (static_cast<int64_t>(c) * W.Vp + vs) * N + j;
-                    const float s = bf16_value(__ldg(W.scale + at));
-                    const float z = W.zero ? static_cast<float>(__ldg(W.zero + at)) : 8.f;
-                    const uint64_t s2 = pair(s, s), z2 = pair(-z, -z);
-                    const ulonglong2* x = reinterpret_cast<const ulonglong2*>(T.sums + static_cast<int64_t>(c * N + j) * T.padded + row0);
-                    if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(sh.acc_full + acc, acc_phase, abort_flag, kWaitNs))) {
+                    const uint32_t full = offsetof(Shared, acc_full) + (pipe * 4 + acc.at) * 8;
+                    if (!wait_for_all(sh, full, acc.phase, offsetof(Shared, side_full) + slot.at * 8, slot.phase, full, acc.phase)) {
                         gave_up();
                         ok = false;
                         break;
                     }
                     tc_fence_after();
+                    constexpr int kPart = 16;
+                    uint32_t d[kPart];
+                    tmem_load16(tmem + acc.at * NT, d);
+                    const Side<NT, N>& from = side[slot.at];
+                    const float s = bf16_value(from.scale[row_in_tile * N + j]);
+                    const float z = zeros ? static_cast<float>(from.zero[row_in_tile * N + j]) : 8.f;
+                    const uint64_t s2 = pair(s, s), z2 = pair(-z, -z);
+                    const ulonglong2* x = reinterpret_cast<const ulonglong2*>(from.sums[j]);
 #pragma unroll
-                    for (int h = 0; h < kCols / 16; ++h) {
-                        uint32_t d[16];
-                        tmem_load16(tmem + acc * NT + h * 16, d);
-                        ulonglong2 xs[4];
+                    for (int h = 0; h < NT / kPart; ++h) {
+                        if (h > 0) tmem_load16(tmem + acc.at * NT + h * kPart, d);
+                        ulonglong2 xs[kPart / 4];   // (read while the accumulator is on its way)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) xs[i] = x[h * 4 + i];
-                        tmem_wait_load();
+                        for (int i = 0; i < kPart / 4; ++i) xs[i] = x[h * (kPart / 4) + i];
+                        tmem_wait_load(d);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const uint64_t sum = static_cast<uint64_t>(d[2 * i + 1]) << 32 | d[2 * i];
-                            total[h * 8 + i] = fma_pair(fma_pair(z2, i & 1 ? xs[i / 2].y : xs[i / 2].x, sum), s2, total[h * 8 + i]);
+                        for (int i = 0; i < kPart / 4; ++i) {
+                            uint64_t& t0 = total[(h * kPart + 4 * i) / 2];
+                            uint64_t& t1 = total[(h * kPart + 4 * i) / 2 + 1];
+                            t0 = fma_pair(fma_pair(z2, xs[i].x, static_cast<uint64_t>(d[4 * i + 1]) << 32 | d[4 * i]), s2, t0);
+                            t1 = fma_pair(fma_pair(z2, xs[i].y, static_cast<uint64_t>(d[4 * i + 3]) << 32 | d[4 * i + 2]), s2, t1);
                         }
                     }
+                    // the accumulator may be written again, and after the block's last group its scales too
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(sh.acc_empty + acc);
-                    if (++acc == kAccumulators) {
-                        acc = 0;
-                        acc_phase ^= 1u;
-                    }
+                    if (lane == 0) mbar_arrive(&sh.acc_empty[pipe][acc.at]);
+                    if (lane == 1 && j == N - 1) mbar_arrive(sh.side_empty + slot.at);
+                    acc.advance();
                 }
+                slot.advance();
             }
+            const int row0 = item % T.row_blocks * NT;
+            const int64_t v = static_cast<int64_t>(item / T.row_blocks) * kTileV + row_in_tile;
             if (ok && v < W.V) {
-#pragma unroll
-                for (int i = 0; i < kCols; ++i) {
-                    const int row = row0 + i;
-                    if (row < P.rows) {
-                        const int back = 133 - T.shifts[row];
-                        const float y = __uint_as_float(static_cast<uint32_t>(i & 1 ? total[i / 2] >> 32 : total[i / 2])) *
-                                        exp2_int(back / 2) * exp2_int(back - back / 2);
-                        if (T.out_bf16)
-                            reinterpret_cast<__nv_bfloat16*>(P.out)[row * P.ldo + v] = __float2bfloat16_rn(y);
-                        else
-                            reinterpret_cast<float*>(P.out)[row * P.ldo + v] = y;
-                    }
-                }
+                if (T.out_bf16)
+                    store_column<NT>(reinterpret_cast<__nv_bfloat16*>(P.out) + row0 * P.ldo + v, P.ldo, total, T.backs + row0,
+                                     P.rows - row0);
+                else
+                    store_column<NT>(reinterpret_cast<float*>(P.out) + row0 * P.ldo + v, P.ldo, total, T.backs + row0,
+                                     P.rows - row0);
             }
         }
     }
@@ -376,21 +541,24 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (*abort_flag && warp == kEpilogueWarps + kWeightWarps && lane == 0) {
-        const int first = issued > kStages ? issued - kStages : 0;
-        for (int k = first; k < issued; ++k) {
+    if (*abort_flag && warp == kTmaWarp) {   // (the lanes that issued nothing have nothing to wait for)
+        for (int k = issued > S::kBStages ? issued - S::kBStages : 0; k < issued; ++k) {
             volatile int never = 0;
-            mbar_wait_bounded(sh.full + (k % kStages), static_cast<uint32_t>((k / kStages) & 1), &never, kWaitNs);
+            mbar_wait_bounded(sh.b_full + (k % S::kBStages), static_cast<uint32_t>((k / S::kBStages) & 1), &never, kWaitNs);
+        }
+        for (int k = sides > kSides ? sides - kSides : 0; k < sides; ++k) {
+            volatile int never = 0;
+            mbar_wait_bounded(sh.side_full + (k % kSides), static_cast<uint32_t>((k / kSides) & 1), &never, kWaitNs);
         }
     }
     __syncthreads();
     if (warp == 0) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, kTmemCols);
+        tmem_dealloc(tmem_base, S::kTmemCols);
     }
 }
 
-int tile_rows(int rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : 128; }
+int tile_rows(int rows) { return rows <= 32 ? 32 : 64; }
 int64_t padded_rows(int rows) {
     const int nt = tile_rows(rows);
     return (static_cast<int64_t>(rows) + nt - 1) / nt * nt;
@@ -398,25 +566,30 @@ int64_t padded_rows(int rows) {
 size_t round256(size_t n) { return (n + 255) / 256 * 256; }
 
 struct Workspace {
-    size_t operand, sums, shifts, total;
+    size_t operand, sums, backs, total;
 };
 Workspace workspace_layout(const ProductParams& P) {
     Workspace L;
     const size_t rows = static_cast<size_t>(padded_rows(P.rows)), blocks = P.layer.blocks;
     L.operand = 0;
     L.sums = round256(rows * blocks * kBlock * 2);
-    L.shifts = L.sums + round256(rows * blocks * (kBlock / P.layer.G) * 4);
-    L.total = L.shifts + round256(rows * 4);
+    L.backs = L.sums + round256(rows * blocks * (kBlock / P.layer.G) * 4);
+    L.total = L.backs + round256(rows * 8);
     return L;
 }
 
-bool g_attr[64][3][3];
+bool g_attr[64][2][3];
 
 template <int NT, int N>
 fef_status launch(const CUtensorMap& map, const TileParams& T, int dev, int grid, cudaStream_t stream) {
-    constexpr size_t smem = static_cast<size_t>(kStages) * (kABytes + NT * kBlock * 2) + sizeof(Shared) + 1024;
-    bool& done = g_attr[dev][NT == 32 ? 0 : NT / 64][N / 2];
+    constexpr size_t smem = Sizes<NT>::kBStages * Sizes<NT>::kBBytes + kSides * sizeof(Side<NT, N>) + sizeof(Shared) + 1024;
+    static_assert(smem <= 232448, "");
+    bool& done = g_attr[dev][NT / 64][N / 2];
     if (!done) {
+        // (a warpgroup that asks for more registers than the launch left waits for good: never launch with another number)
+        cudaFuncAttributes attr;
+        if (cudaFuncGetAttributes(&attr, product_tiles_kernel<NT, N>) != cudaSuccess || (attr.numRegs + 7) / 8 * 8 != kLaunchRegs)
+            return FEF_ERR_CUDA;
         if (cudaFuncSetAttribute(product_tiles_kernel<NT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  static_cast<int>(smem)) != cudaSuccess)
             return FEF_ERR_CUDA;
@@ -457,7 +630,7 @@ fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* works
     H.hidden = P.hidden;
     H.operand = reinterpret_cast<uint16_t*>(ws + L.operand);
     H.sums = reinterpret_cast<float*>(ws + L.sums);
-    H.shifts = reinterpret_cast<int*>(ws + L.shifts);
+    H.backs = reinterpret_cast<float2*>(ws + L.backs);
     H.rows = P.rows;
     H.padded = static_cast<int>(padded_rows(P.rows));
     H.d = W.d;
@@ -468,11 +641,11 @@ fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* works
     T.P = P;
     T.tiles = (W.V + kTileV - 1) / kTileV;
     T.row_blocks = H.padded / nt;
-    if (static_cast<int64_t>(T.tiles) * T.row_blocks > 0x7FFFFFFF) return FEF_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(T.tiles) * T.row_blocks * W.blocks > 0x7FFFFFFF) return FEF_ERR_INVALID_ARG;   // (counted in 32 bits)
     T.items = T.tiles * T.row_blocks;
     T.padded = H.padded;
     T.sums = H.sums;
-    T.shifts = H.shifts;
+    T.backs = H.backs;
     T.out_bf16 = dt == FEF_BF16;
     CUtensorMap map;
     const uint64_t cols = static_cast<uint64_t>(W.blocks) * kBlock;
@@ -482,11 +655,7 @@ fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* works
     if (cudaGetLastError() != cudaSuccess) return FEF_ERR_CUDA;
 
     const int grid = T.items < sms ? T.items : sms;
-    switch (nt) {
-        case 32: return launch_g<32>(map, T, dev, grid, stream);
-        case 64: return launch_g<64>(map, T, dev, grid, stream);
-        default: return launch_g<128>(map, T, dev, grid, stream);
-    }
+    return nt == 32 ? launch_g<32>(map, T, dev, grid, stream) : launch_g<64>(map, T, dev, grid, stream);
 }
 
 }  // namespace quant

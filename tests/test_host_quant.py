@@ -33,7 +33,7 @@ def test_argument_checks_return_before_touching_the_device(fef):
         assert call(d=0) == bad and call(d=96, g=64) == bad and call(d=(1 << 20) + 128) == bad and call(d=-128) == bad
         for g in (0, 1, 16, 48, 256, -32):
             assert call(g=g) == bad
-        assert call(p=A + 8) == align and call(s=A + 2) == align and call(z=A + 1) == align
+        assert call(p=A + 16) == align and call(s=A + 2) == align and call(z=A + 1) == align
         assert call() == fef.FEF_ERR_CUDA and call(z=None) == fef.FEF_ERR_CUDA
     assert quantize(w=None) == bad and quantize(w=A + 8) == align
     assert dequantize(out=None) == bad and dequantize(out=A + 4) == align
