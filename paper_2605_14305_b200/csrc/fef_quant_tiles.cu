@@ -1,21 +1,22 @@
 // fef_lmhead_logits_quantized for any number of hidden rows: the fifth-generation tensor cores (tcgen05.mma), accumulators in
 // tensor memory.
 //
-// prepare_kernel brings the hidden rows into the operand's form once (workspace): scaled by a power of two, the eight columns
-// of every packed word in the order 0 4, 1 5, 2 6, 3 7 in which masking delivers them (fef_quant.cuh), with the sums of every
-// group.  product_tiles_kernel then takes tiles of 256 vocabulary rows x NT hidden rows, one CTA of 20 warps per SM, as two
-// pipelines of 128 vocabulary rows that share the hidden rows and nothing else:
-//   2 x 4 warps  weights: packed nibbles from global memory (kAhead blocks in flight per warp) to bfloat16 numbers in tensor
-//                memory, a vocabulary row per lane (through shared memory, writing and reading them took 512 of its cycles a
-//                block: 160 us at 64 rows x 126464 x 4096);
-//   1 warp       brings the hidden rows of the same 128 columns in by TMA, and on a ring of their own the groups' sums,
-//                scales and zero points (read from global memory by the warps that need them, their latency set the pace);
+// prepare_kernel brings the hidden rows into the operand's form once (workspace): the eight columns of every packed word in
+// the order 0 4, 1 5, 2 6, 3 7 in which the nibbles come apart (fef_quant.cuh).  product_tiles_kernel then takes tiles of 256
+// vocabulary rows x NT hidden rows, one CTA of 20 warps per SM, as two pipelines of 128 vocabulary rows that share the hidden
+// rows and nothing else:
+//   2 x 4 warps  weights: packed nibbles from global memory (kAhead blocks in flight per warp) to the bfloat16 numbers q - z in
+//                tensor memory, a vocabulary row per lane (through shared memory, writing and reading them took 512 of its
+//                cycles a block: 160 us at 64 rows x 126464 x 4096);
+//   1 warp       brings the hidden rows of the same 128 columns in by TMA, and on a ring of their own the groups' scales (read
+//                from global memory by the warps that need them, their latency set the pace);
 //   2 x 1 warp   issue the MMAs (128 x NT x 16), a fresh accumulator for every group of a row's weights;
-//   2 x 4 warps  take each group's accumulator out of tensor memory, subtract z times the group's sum, scale it and add it to
-//                the logits in registers: the vocabulary rows are the lanes, so a group's scale is one number per thread.  The
-//                weights are the left operand for that reason.
+//   2 x 4 warps  take each group's accumulator out of tensor memory, scale it and add it to the logits in registers: the
+//                vocabulary rows are the lanes, so a group's scale is one number per thread.  The weights are the left operand
+//                for that reason.
 // A block's hand-overs from warp to warp, not its arithmetic, set the pace: hence two pipelines side by side, few warps with
-// much to do each, and waits that poll several barriers at once.  Every wait is bounded.
+// much to do each, and waits that poll several barriers at once.  The epilogue has most to do, so the weights' warps subtract
+// the zero points (taking them off the groups' sums, as the kernel for few rows does, was 126 us).  Every wait is bounded.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -33,22 +34,16 @@ constexpr int kPipes = 2;
 constexpr int kPipeV = 128, kTileV = kPipes * kPipeV;   // vocabulary rows
 constexpr int kAStages = 2;                   // of a pipeline: blocks of unpacked weights in tensor memory
 constexpr int kACols = kBlock / 2;            // 32-bit columns of such a block
-constexpr int kSides = 4;                     // ring of what the epilogue needs of a block: sums, scales, zero points
-constexpr int kAhead = 2;                     // blocks of weights in flight per warp
+constexpr int kSides = 4;                     // ring of the blocks' scales
 constexpr int kRoleWarps = 4;                 // warps of a pipeline's epilogue, and of its weights
 constexpr int kThreads = (2 * kPipes * kRoleWarps + 4) * 32;   // the last four warps: TMA, an issuer per pipeline, one idle
 constexpr int kWeightWarp0 = kPipes * kRoleWarps, kTmaWarp = 2 * kPipes * kRoleWarps, kIssueWarp0 = kTmaWarp + 1;
-// Registers per thread: what the kernel is launched with, and what the three kinds of warpgroups keep of it; the shares add up
-// to the launch's total exactly.
-constexpr int kLaunchRegs = 96, kEpilogueRegs = 112, kWeightRegs = 88, kControlRegs = 80;
-static_assert(kPipes * kRoleWarps * (kEpilogueRegs + kWeightRegs) + 4 * kControlRegs == kThreads / 32 * kLaunchRegs, "");
+constexpr int kLaunchRegs = 96;               // per thread
 constexpr unsigned long long kWaitNs = 1000000000ull;
 
 struct TileParams {
     ProductParams P;
     int tiles, row_blocks, items, padded;   // padded: hidden rows rounded up to whole tiles
-    const float* sums;                      // [blocks * 128 / G][padded]
-    const float2* backs;                    // [padded]: two powers of two that scale the logits back
     int out_bf16;
 };
 
@@ -59,6 +54,11 @@ struct Sizes {
     static constexpr int kAccumulators = NT == 64 ? 2 : 4;
     static constexpr int kPipeCols = kAccumulators * NT + kAStages * kACols, kTmemCols = kPipes * kPipeCols;
     static_assert(kTmemCols == 512, "");
+    // Registers per thread that the three kinds of warpgroups keep of the launch's: the shares add up to its total exactly.
+    // (Chosen so that nothing spills: with this much shared memory in use a spilled register comes back from L2.)
+    static constexpr int kEpilogueRegs = NT == 64 ? 128 : 112, kWeightRegs = NT == 64 ? 80 : 88, kControlRegs = NT == 64 ? 64 : 80;
+    static_assert(kPipes * kRoleWarps * (kEpilogueRegs + kWeightRegs) + 4 * kControlRegs == kThreads / 32 * kLaunchRegs, "");
+    static constexpr int kAhead = NT == 64 ? 2 : 3;   // blocks of weights in flight per warp
 };
 
 struct Shared {
@@ -79,51 +79,21 @@ struct Shared {
 struct PrepareParams {
     const uint16_t* hidden;   // [rows][d]
     uint16_t* operand;        // [padded][blocks * 128]
-    float* sums;
-    float2* backs;
-    int rows, padded, d, blocks, words;   // words: 32-column pieces per group
+    int rows, d, blocks;
     int32_t* status;
 };
 constexpr int kPrepareThreads = 256;
 
 __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const __grid_constant__ PrepareParams P) {
-    __shared__ uint32_t s_top;
     cudaTriggerProgrammaticLaunchCompletion();   // (the tiles' kernel may begin to fetch weights; it waits for the rest)
-    const int row = blockIdx.x, tid = threadIdx.x;
-    if (P.status && row == 0 && tid == 0) *P.status = FEF_OK;
-    if (tid == 0) s_top = 0u;
-    __syncthreads();
-    const uint16_t* src = P.hidden + static_cast<int64_t>(row) * P.d;
+    const int row = blockIdx.x;
+    if (P.status && row == 0 && threadIdx.x == 0) *P.status = FEF_OK;
+    const uint4* src = reinterpret_cast<const uint4*>(P.hidden + static_cast<int64_t>(row) * P.d);
     uint4* to = reinterpret_cast<uint4*>(P.operand + static_cast<int64_t>(row) * P.blocks * kBlock);
-    const int pieces = P.blocks * 16;   // of eight columns; d is a multiple of 32
-    auto load = [&](int p) {
-        return row < P.rows && p * 8 < P.d ? __ldg(reinterpret_cast<const uint4*>(src) + p) : make_uint4(0u, 0u, 0u, 0u);
-    };
-    uint32_t top = 0u;
-    for (int p = tid; p < pieces; p += kPrepareThreads) {
-        const uint4 x = load(p);
-        const uint32_t m = __vmaxu2(__vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
-        top = max(top, max(m & 0xFFFFu, m >> 16));
-    }
-    if (top != 0u) atomicMax(&s_top, top);
-    __syncthreads();
-    const int shift = row_shift(s_top);
-    const float f0 = exp2_int(shift / 2), f1 = exp2_int(shift - shift / 2);
-    if (tid == 0) P.backs[row] = make_float2(exp2_int((133 - shift) / 2), exp2_int(133 - shift - (133 - shift) / 2));
-    for (int p = tid; p < pieces; p += kPrepareThreads) {   // (pieces is a multiple of 16: a group's lanes come together)
-        const uint4 x = load(p);
-        float v[8], total = 0.f;
-        unpack<FEF_BF16>(x, v);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = v[j] * f0 * f1;
-            total += v[j] * exp2_int(-67) * exp2_int(-66);
-        }
-        to[p] = make_uint4(bf16_pair(v[0], v[4]), bf16_pair(v[1] * 0.0625f, v[5] * 0.0625f), bf16_pair(v[2], v[6]),
-                       bf16_pair(v[3] * 0.0625f, v[7] * 0.0625f));
-        const unsigned lanes = __activemask();
-        for (int o = 1; o < P.words * 4; o <<= 1) total += __shfl_xor_sync(lanes, total, o);
-        if (p % (P.words * 4) == 0) P.sums[static_cast<int64_t>(p / (P.words * 4)) * P.padded + row] = total;
+    for (int p = threadIdx.x; p < P.blocks * 16; p += kPrepareThreads) {   // pieces of eight columns; d is a multiple of 32
+        const uint4 x = row < P.rows && p * 8 < P.d ? __ldg(src + p) : make_uint4(0u, 0u, 0u, 0u);
+        to[p] = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
+                           __byte_perm(x.y, x.w, 0x7632));
     }
 }
 
@@ -186,12 +156,10 @@ __device__ __forceinline__ void bulk_copy(void* dst, const void* src, uint32_t b
                  : "memory");
 }
 
-// Of a block: sums [N][NT], scales [256][N], zero points [256][N].
-template <int NT, int N>
+// Of a block: the scales of all 256 rows.
+template <int N>
 struct Side {
-    float sums[N][NT];
     uint16_t scale[kTileV * N];
-    uint8_t zero[kTileV * N];
 };
 
 // The lower word of smem_desc_sw128's descriptor (the upper one is the same for all), and the MMA that takes it and a left
@@ -230,23 +198,13 @@ __device__ __forceinline__ void load_sector(const void* p, uint32_t (&r)[8]) {
 __device__ __forceinline__ void put_logit(float* at, float y) { *at = y; }
 __device__ __forceinline__ void put_logit(__nv_bfloat16* at, float y) { *at = __float2bfloat16_rn(y); }
 
-// One vocabulary row's logits of `kCols` hidden rows (the first `many` of them exist), scaled back.
+// One vocabulary row's logits of `kCols` hidden rows, the first `many` of which exist.
 template <int kCols, typename Out>
-__device__ __forceinline__ void store_column(Out* out, int64_t ldo, const uint64_t (&total)[kCols / 2],
-                                             const float2* __restrict__ backs, int many) {
+__device__ __forceinline__ void store_column(Out* out, int64_t ldo, const uint64_t (&total)[kCols / 2], int many) {
 #pragma unroll
-    for (int h = 0; h < kCols; h += 8) {
-        float4 back[4];   // (padded: always within the array)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) back[i] = __ldg(reinterpret_cast<const float4*>(backs + h) + i);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint64_t two = total[h / 2 + i];
-            if (h + 2 * i < many) put_logit(out, __uint_as_float(static_cast<uint32_t>(two)) * back[i].x * back[i].y);
-            out += ldo;
-            if (h + 2 * i + 1 < many) put_logit(out, __uint_as_float(static_cast<uint32_t>(two >> 32)) * back[i].z * back[i].w);
-            out += ldo;
-        }
+    for (int i = 0; i < kCols; ++i) {
+        if (i < many) put_logit(out, __uint_as_float(static_cast<uint32_t>(i & 1 ? total[i / 2] >> 32 : total[i / 2])));
+        out += ldo;
     }
 }
 
@@ -254,11 +212,11 @@ template <int NT, int N>   // hidden rows of a tile, groups per block
 __global__ void __launch_bounds__(kThreads, 1)
 product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ TileParams T) {
     using S = Sizes<NT>;
-    constexpr int kAccumulators = S::kAccumulators;
+    constexpr int kAccumulators = S::kAccumulators, kAhead = S::kAhead;
     constexpr uint32_t kInstr = (1u << 4) | (1u << 7) | (1u << 10) | ((NT >> 3) << 17) | ((kPipeV >> 4) << 24);
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    Side<NT, N>* side = reinterpret_cast<Side<NT, N>*>(smem + S::kBStages * S::kBBytes);
+    Side<N>* side = reinterpret_cast<Side<N>*>(smem + S::kBStages * S::kBBytes);
     Shared& sh = *reinterpret_cast<Shared*>(side + kSides);
     volatile int* abort_flag = &sh.abort_flag;
     const ProductParams& P = T.P;
@@ -301,7 +259,7 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     const int items = blockIdx.x < T.items ? (T.items - 1 - blockIdx.x) / gridDim.x + 1 : 0;   // of this CTA
     const int count = items * W.blocks;
 
-    if (warp >= kTmaWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kControlRegs));
+    if (warp >= kTmaWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kControlRegs));
     if (warp == kTmaWarp) {
         // ------------------------------------------------------------ hidden rows, one thread
         if (elect_one()) {
@@ -331,14 +289,8 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                         break;
                     }
                     uint64_t* bar = sh.side_full + slot.at;
-                    Side<NT, N>& to = side[slot.at];
-                    const int64_t at = (static_cast<int64_t>(c) * W.Vp + v0) * N;
-                    mbar_arrive_expect_tx(bar, N * NT * 4 + rows * N * (W.zero ? 3 : 2));
-#pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        bulk_copy(to.sums[j], T.sums + static_cast<int64_t>(c * N + j) * T.padded + row0, NT * 4, bar);
-                    if (W.zero) bulk_copy(to.zero, W.zero + at, rows * N, bar);
-                    bulk_copy(to.scale, W.scale + at, rows * N * 2, bar);
+                    mbar_arrive_expect_tx(bar, rows * N * 2);
+                    bulk_copy(side[slot.at].scale, W.scale + (static_cast<int64_t>(c) * W.Vp + v0) * N, rows * N * 2, bar);
                     ++sides;
                     slot.advance();
                 }
@@ -394,20 +346,31 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     } else if (warp >= kWeightWarp0) {
         // ------------------------------------------------------------------------------------ weights
         // A lane takes one row: the 64 bytes of a block are its word 4 t + w, of columns 32 w + 8 t .. + 7, for every t and w.
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWeightRegs));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kWeightRegs));
         const int pipe = (warp - kWeightWarp0) / kRoleWarps, quarter = (warp - kWeightWarp0) % kRoleWarps;
         const uint32_t tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + pipe * S::kPipeCols + kAccumulators * NT;
         const int blocks = count;
         int left = blocks, fetch_item = blockIdx.x, fetch_block = 0;
-        const uint8_t* fetch_w = nullptr;
+        const uint8_t *fetch_w = nullptr, *fetch_z = nullptr;
+        const bool zeros = W.zero != nullptr;
         auto seek = [&]() {   // (rows behind V are read as the last one; their logits are not stored)
-            const int64_t v = static_cast<int64_t>(fetch_item / T.row_blocks) * kTileV + pipe * kPipeV + quarter * 32 + lane;
-            fetch_w = W.packed + min(v, static_cast<int64_t>(W.V - 1)) * (static_cast<int64_t>(W.blocks) * 64);
+            const int64_t v = min(static_cast<int64_t>(fetch_item / T.row_blocks) * kTileV + pipe * kPipeV + quarter * 32 + lane,
+                                  static_cast<int64_t>(W.V - 1));
+            fetch_w = W.packed + v * (static_cast<int64_t>(W.blocks) * 64);
+            fetch_z = W.zero + v * N;
         };
-        uint32_t ahead[kAhead][2][8];   // words 4 t + w: t = 0, 1 and t = 2, 3
-        auto fetch = [&](uint32_t (&q)[2][8]) {   // past the end the last block is fetched again: no branch around the loads
+        struct Fetched {
+            uint32_t q[2][8];   // words 4 t + w: t = 0, 1 and t = 2, 3
+            uint32_t z;         // N zero points
+        } ahead[kAhead];
+        auto fetch = [&](Fetched& f) {   // past the end the last block is fetched again: no branch around the loads
 #pragma unroll
-            for (int i = 0; i < 2; ++i) load_sector(fetch_w + fetch_block * 64 + i * 32, q[i]);
+            for (int i = 0; i < 2; ++i) load_sector(fetch_w + fetch_block * 64 + i * 32, f.q[i]);
+            f.z = 0x08080808u;
+            if (zeros) {
+                const uint8_t* z = fetch_z + static_cast<int64_t>(fetch_block) * W.Vp * N;
+                f.z = N == 1 ? __ldg(z) : N == 2 ? __ldg(reinterpret_cast<const uint16_t*>(z)) : __ldg(reinterpret_cast<const uint32_t*>(z));
+            }
             const int more = left > 1 ? 1 : 0;
             left -= more;
             fetch_block += more;
@@ -424,7 +387,7 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             Turn<kAStages> stage;
             bool ok = true;
             // (after a wait that ran out the rest goes by without waits and arrivals)
-            auto put = [&](const uint32_t (&q)[2][8]) {
+            auto put = [&](const Fetched& f) {
                 if (ok && !__all_sync(0xFFFFFFFFu, lane > 0 || wait_for(&sh.a_empty[pipe][stage.at], stage.phase ^ 1u, abort_flag))) {
                     gave_up();
                     ok = false;
@@ -432,14 +395,15 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 tc_fence_after();
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {   // 32 columns of the operand
+                    const uint32_t centre = centre_of(f.z >> (8 * (w * N / 4)) & 0xFFu);
                     uint32_t y[16];
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
-                        const uint32_t x = q[t >> 1][(t & 1) * 4 + w];
-                        y[4 * t] = x & kLowNibbles;
-                        y[4 * t + 1] = x & kHighNibbles;
-                        y[4 * t + 2] = x >> 8 & kLowNibbles;
-                        y[4 * t + 3] = x >> 8 & kHighNibbles;
+                        const uint32_t x = f.q[t >> 1][(t & 1) * 4 + w];
+                        y[4 * t] = centred_pair(x, centre);
+                        y[4 * t + 1] = centred_pair(x >> 4, centre);
+                        y[4 * t + 2] = centred_pair(x >> 8, centre);
+                        y[4 * t + 3] = centred_pair(x >> 12, centre);
                     }
                     tmem_store16(tmem + stage.at * kACols + w * 16, y);
                 }
@@ -469,11 +433,10 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         }
     } else {
         // ----------------------------------------------------------------------------------- epilogue
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kEpilogueRegs));
         cudaGridDependencySynchronize();
         const int pipe = warp / kRoleWarps, quarter = warp % kRoleWarps, row_in_tile = pipe * kPipeV + quarter * 32 + lane;
         const uint32_t tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + pipe * S::kPipeCols;
-        const bool zeros = W.zero != nullptr;
         Turn<kAccumulators> acc;
         Turn<kSides> slot;
         bool ok = true;
@@ -491,27 +454,21 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                         break;
                     }
                     tc_fence_after();
-                    constexpr int kPart = 16;
-                    uint32_t d[kPart];
-                    tmem_load16(tmem + acc.at * NT, d);
-                    const Side<NT, N>& from = side[slot.at];
-                    const float s = bf16_value(from.scale[row_in_tile * N + j]);
-                    const float z = zeros ? static_cast<float>(from.zero[row_in_tile * N + j]) : 8.f;
-                    const uint64_t s2 = pair(s, s), z2 = pair(-z, -z);
-                    const ulonglong2* x = reinterpret_cast<const ulonglong2*>(from.sums[j]);
+                    // (the next part is under way while one is added up)
+                    constexpr int kPart = 16, kParts = NT / kPart;
+                    uint32_t d[2][kPart];
+                    tmem_load16(tmem + acc.at * NT, d[0]);
+                    const float s = bf16_value(side[slot.at].scale[row_in_tile * N + j]);
+                    const uint64_t s2 = pair(s, s);
 #pragma unroll
-                    for (int h = 0; h < NT / kPart; ++h) {
-                        if (h > 0) tmem_load16(tmem + acc.at * NT + h * kPart, d);
-                        ulonglong2 xs[kPart / 4];   // (read while the accumulator is on its way)
+                    for (int h = 0; h < kParts; ++h) {
+                        uint32_t (&now)[kPart] = d[h & 1];
+                        tmem_wait_load(now);
+                        if (h + 1 < kParts) tmem_load16(tmem + acc.at * NT + (h + 1) * kPart, d[(h + 1) & 1]);
 #pragma unroll
-                        for (int i = 0; i < kPart / 4; ++i) xs[i] = x[h * (kPart / 4) + i];
-                        tmem_wait_load(d);
-#pragma unroll
-                        for (int i = 0; i < kPart / 4; ++i) {
-                            uint64_t& t0 = total[(h * kPart + 4 * i) / 2];
-                            uint64_t& t1 = total[(h * kPart + 4 * i) / 2 + 1];
-                            t0 = fma_pair(fma_pair(z2, xs[i].x, static_cast<uint64_t>(d[4 * i + 1]) << 32 | d[4 * i]), s2, t0);
-                            t1 = fma_pair(fma_pair(z2, xs[i].y, static_cast<uint64_t>(d[4 * i + 3]) << 32 | d[4 * i + 2]), s2, t1);
+                        for (int i = 0; i < kPart / 2; ++i) {
+                            uint64_t& t = total[h * (kPart / 2) + i];
+                            t = fma_pair(static_cast<uint64_t>(now[2 * i + 1]) << 32 | now[2 * i], s2, t);
                         }
                     }
                     // the accumulator may be written again, and after the block's last group its scales too
@@ -527,11 +484,9 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             const int64_t v = static_cast<int64_t>(item / T.row_blocks) * kTileV + row_in_tile;
             if (ok && v < W.V) {
                 if (T.out_bf16)
-                    store_column<NT>(reinterpret_cast<__nv_bfloat16*>(P.out) + row0 * P.ldo + v, P.ldo, total, T.backs + row0,
-                                     P.rows - row0);
+                    store_column<NT>(reinterpret_cast<__nv_bfloat16*>(P.out) + row0 * P.ldo + v, P.ldo, total, P.rows - row0);
                 else
-                    store_column<NT>(reinterpret_cast<float*>(P.out) + row0 * P.ldo + v, P.ldo, total, T.backs + row0,
-                                     P.rows - row0);
+                    store_column<NT>(reinterpret_cast<float*>(P.out) + row0 * P.ldo + v, P.ldo, total, P.rows - row0);
             }
         }
     }
@@ -563,26 +518,11 @@ int64_t padded_rows(int rows) {
     const int nt = tile_rows(rows);
     return (static_cast<int64_t>(rows) + nt - 1) / nt * nt;
 }
-size_t round256(size_t n) { return (n + 255) / 256 * 256; }
-
-struct Workspace {
-    size_t operand, sums, backs, total;
-};
-Workspace workspace_layout(const ProductParams& P) {
-    Workspace L;
-    const size_t rows = static_cast<size_t>(padded_rows(P.rows)), blocks = P.layer.blocks;
-    L.operand = 0;
-    L.sums = round256(rows * blocks * kBlock * 2);
-    L.backs = L.sums + round256(rows * blocks * (kBlock / P.layer.G) * 4);
-    L.total = L.backs + round256(rows * 8);
-    return L;
-}
-
 bool g_attr[64][2][3];
 
 template <int NT, int N>
 fef_status launch(const CUtensorMap& map, const TileParams& T, int dev, int grid, cudaStream_t stream) {
-    constexpr size_t smem = Sizes<NT>::kBStages * Sizes<NT>::kBBytes + kSides * sizeof(Side<NT, N>) + sizeof(Shared) + 1024;
+    constexpr size_t smem = Sizes<NT>::kBStages * Sizes<NT>::kBBytes + kSides * sizeof(Side<N>) + sizeof(Shared) + 1024;
     static_assert(smem <= 232448, "");
     bool& done = g_attr[dev][NT / 64][N / 2];
     if (!done) {
@@ -619,39 +559,34 @@ fef_status launch_g(const CUtensorMap& map, const TileParams& T, int dev, int gr
 
 }  // namespace
 
-size_t tiles_kernel_workspace(const ProductParams& P) { return workspace_layout(P).total; }
+size_t tiles_kernel_workspace(const ProductParams& P) {
+    return (static_cast<size_t>(padded_rows(P.rows)) * P.layer.blocks * kBlock * 2 + 255) / 256 * 256;
+}
 
 fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* workspace, int dev, int sms, cudaStream_t stream) {
     const Layer& W = P.layer;
-    const Workspace L = workspace_layout(P);
-    char* ws = static_cast<char*>(workspace);
     const int nt = tile_rows(P.rows);
     PrepareParams H;
     H.hidden = P.hidden;
-    H.operand = reinterpret_cast<uint16_t*>(ws + L.operand);
-    H.sums = reinterpret_cast<float*>(ws + L.sums);
-    H.backs = reinterpret_cast<float2*>(ws + L.backs);
+    H.operand = static_cast<uint16_t*>(workspace);
     H.rows = P.rows;
-    H.padded = static_cast<int>(padded_rows(P.rows));
     H.d = W.d;
     H.blocks = W.blocks;
-    H.words = W.G / 32;
     H.status = P.status;
+
     TileParams T;
     T.P = P;
     T.tiles = (W.V + kTileV - 1) / kTileV;
-    T.row_blocks = H.padded / nt;
+    T.padded = static_cast<int>(padded_rows(P.rows));
+    T.row_blocks = T.padded / nt;
     if (static_cast<int64_t>(T.tiles) * T.row_blocks * W.blocks > 0x7FFFFFFF) return FEF_ERR_INVALID_ARG;   // (counted in 32 bits)
     T.items = T.tiles * T.row_blocks;
-    T.padded = H.padded;
-    T.sums = H.sums;
-    T.backs = H.backs;
     T.out_bf16 = dt == FEF_BF16;
     CUtensorMap map;
     const uint64_t cols = static_cast<uint64_t>(W.blocks) * kBlock;
-    if (!map_2d(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, H.operand, cols, H.padded, cols * 2, 64, nt, CU_TENSOR_MAP_SWIZZLE_128B))
+    if (!map_2d(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, H.operand, cols, T.padded, cols * 2, 64, nt, CU_TENSOR_MAP_SWIZZLE_128B))
         return FEF_ERR_CUDA;
-    prepare_kernel<<<H.padded, kPrepareThreads, 0, stream>>>(H);
+    prepare_kernel<<<T.padded, kPrepareThreads, 0, stream>>>(H);
     if (cudaGetLastError() != cudaSuccess) return FEF_ERR_CUDA;
 
     const int grid = T.items < sms ? T.items : sms;

@@ -45,6 +45,6 @@ def test_argument_checks_return_before_touching_the_device(fef):
     assert product(rows=40) == fef.FEF_ERR_CUDA
     need = fef.fef_lmhead_logits_quantized_workspace_bytes
     assert need(0, 10, 128, 32) == 0 and need(3, 10, 100, 32) == 0 and need(3, 10, 128, 48) == 0 and need(3, 10, 128, 32) == 256
-    assert need(40, 10, 128, 32) >= 64 * 128 * 2 + 64 * 4 * 4 + 64 * 4
+    assert need(40, 10, 128, 32) >= 64 * 128 * 2
     with pytest.raises(RuntimeError):
         fef.fef_lmhead_quantize(torch.zeros((2, 32), dtype=torch.bfloat16))
