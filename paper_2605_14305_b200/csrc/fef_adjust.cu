@@ -72,24 +72,66 @@ __device__ __forceinline__ void unpack8(const Row8<DT>& r, float (&l)[8]) {
     }
 }
 
-// Rounds to the stored type; l becomes the stored values.
-template <int DT>
-__device__ __forceinline__ Row8<DT> pack8(float (&l)[8]) {
-    Row8<DT> r;
-    if constexpr (DT == FEF_F32) {
-        r.v[0] = make_uint4(__float_as_uint(l[0]), __float_as_uint(l[1]), __float_as_uint(l[2]), __float_as_uint(l[3]));
-        r.v[1] = make_uint4(__float_as_uint(l[4]), __float_as_uint(l[5]), __float_as_uint(l[6]), __float_as_uint(l[7]));
-    } else {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const __nv_bfloat162 h = __floats2bfloat162_rn(l[2 * j], l[2 * j + 1]);
-            w[j] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-        r.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
-        unpack<FEF_BF16>(r.v[0], l);
-    }
+// Two binary32 numbers as one operand.
+__device__ __forceinline__ uint64_t two(float a, float b) { return static_cast<uint64_t>(__float_as_uint(b)) << 32 | __float_as_uint(a); }
+__device__ __forceinline__ float first_of(uint64_t x) { return __uint_as_float(static_cast<uint32_t>(x)); }
+__device__ __forceinline__ float second_of(uint64_t x) { return __uint_as_float(static_cast<uint32_t>(x >> 32)); }
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
+}
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// Largest of the warp's numbers (NaN does not count).
+__device__ __forceinline__ float warp_max_f32(float x) {
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(x));
+    return r;
+}
+// Bits 0..3 at the tops of four bytes, and bytes filled with the top bit of one of them (selectors 8 + byte).
+__device__ __forceinline__ uint32_t byte_tops(uint32_t bits) { return (bits & 15u) * 0x10204080u; }
+__device__ __forceinline__ uint32_t spread_tops(uint32_t tops, uint32_t selectors) {
+    uint32_t r;
+    asm("prmt.b32 %0, %1, 0, %2;" : "=r"(r) : "r"(tops), "r"(selectors));
+    return r;
+}
+__device__ __forceinline__ uint32_t pick(uint32_t x, uint32_t otherwise, uint32_t mask) { return (x & mask) | (otherwise & ~mask); }
+
+// Rounds to the stored type, -inf where the mask's bit is 0; l becomes the stored values.
+template <int DT>
+__device__ __forceinline__ Row8<DT> pack8(float (&l)[8], uint32_t allowed) {
+    Row8<DT> r;
+    uint32_t w[DT == FEF_F32 ? 8 : 4];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t tops = byte_tops(allowed >> (4 * h));
+        if constexpr (DT == FEF_F32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[4 * h + j] = pick(__float_as_uint(l[4 * h + j]), 0xFF800000u, spread_tops(tops, 0x8888u + 0x1111u * j));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const __nv_bfloat162 v = __floats2bfloat162_rn(l[4 * h + 2 * j], l[4 * h + 2 * j + 1]);
+                w[2 * h + j] = pick(*reinterpret_cast<const uint32_t*>(&v), 0xFF80FF80u, spread_tops(tops, j == 0 ? 0x9988u : 0xBBAAu));
+            }
+        }
+    }
+    r.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    if constexpr (DT == FEF_F32) r.v[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    unpack8<DT>(r, l);
+    return r;
+}
+
+// l / rep for l > 0, l * rep otherwise; `inv` = 1 / rep.  The quotient takes one correction step (an infinite l skips it).
+__device__ __forceinline__ float repeat_penalty(float l, float rep, float inv) {
+    if (!(l > 0.f)) return l * rep;
+    const float q = l * inv, fixed = fmaf(fmaf(-q, rep, l), inv, q);
+    return l < INFINITY ? fixed : q;
 }
 
 template <int DT, bool NORM>
@@ -123,13 +165,19 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
         const int prompt = P.prompt_len ? __ldg(P.prompt_len + b) : 0;
         const int32_t* text = P.tokens + static_cast<int64_t>(b) * P.L;
         const unsigned width = min(P.V - chunk0, kChunk);
-        for (int t = tid; t < P.L; t += kThreads) {
-            const unsigned at = static_cast<unsigned>(__ldg(text + t)) - chunk0;  // (a negative id ends far above `width`)
-            if (at < width) {
-                if (t < prompt)
-                    atomicOr(s_hist + at, kInPrompt);
-                else
-                    atomicAdd(s_hist + at, 1u);
+        for (int t0 = tid; t0 < P.L; t0 += 4 * kThreads) {
+            int id[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) id[u] = t0 + u * kThreads < P.L ? __ldg(text + t0 + u * kThreads) : -1;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const unsigned at = static_cast<unsigned>(id[u]) - chunk0;  // (a negative id ends far above `width`)
+                if (at < width) {
+                    if (t0 + u * kThreads < prompt)
+                        atomicOr(s_hist + at, kInPrompt);
+                    else
+                        atomicAdd(s_hist + at, 1u);
+                }
             }
         }
         if (tid < k0) {
@@ -142,17 +190,20 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
     }
 
     // ---- the additive term and the repetition flags of this thread's ids
-    float bias[kIdsPerThread], add[kIdsPerThread];
+    const float inv = 1.f / rep;
+    float bias[kIdsPerThread];
+    uint64_t add[kIdsPerThread / 2];
     unsigned repeated = 0u;
 #pragma unroll
     for (int j = 0; j < kIdsPerThread; ++j) bias[j] = P.bias && j < valid ? __ldg(P.bias + b * P.bias_stride + x0 + j) : 0.f;
     auto term = [&](int j) {
         const uint32_t a = hist[j] & ~kInPrompt;
-        add[j] = a ? bias[j] - fmaf(freq, static_cast<float>(a), pres) : bias[j];
+        const float t = a ? bias[j] - fmaf(freq, static_cast<float>(a), pres) : bias[j];
         if (hist[j]) repeated |= 1u << j;
+        return t;
     };
 #pragma unroll
-    for (int j = 0; j < kIdsPerThread; ++j) term(j);
+    for (int j = 0; j < kIdsPerThread; j += 2) add[j / 2] = two(term(j), term(j + 1));
 
     const int64_t row0 = static_cast<int64_t>(b) * P.K;
     const char* src = P.logits + row0 * P.ld_bytes + static_cast<int64_t>(x0) * E;
@@ -160,6 +211,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
     const unsigned char* bits = P.allowed
         ? reinterpret_cast<const unsigned char*>(P.allowed + b * P.allowed_stride_b) + (x0 >> 3) : nullptr;
 
+    const unsigned exist = (1u << valid) - 1u;   // ids behind V: -inf, never stored
     for (int i0 = k0; i0 < k1; i0 += kRowsInFlight) {
         Row8<DT> raw[kRowsInFlight];
         unsigned mask[kRowsInFlight];
@@ -176,7 +228,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
                     float l[8];
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        l[j] = -INFINITY;
+                        l[j] = 0.f;
                         if (j < valid) {
                             if constexpr (DT == FEF_F32)
                                 l[j] = *reinterpret_cast<const volatile float*>(p + 4 * j);
@@ -185,31 +237,31 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
                                     static_cast<uint32_t>(*reinterpret_cast<const volatile unsigned short*>(p + 2 * j)) << 16);
                         }
                     }
-                    raw[r] = pack8<DT>(l);
+                    raw[r] = pack8<DT>(l, 0xFFu);
                 }
                 if (bits) mask[r] = __ldg(bits + i * P.allowed_stride_k * 4);
             }
         }
+        float top[kRowsInFlight], sum[kRowsInFlight];
 #pragma unroll
         for (int r = 0; r < kRowsInFlight; ++r) {
             const int i = i0 + r;
-            if (i >= k1) break;
-            float l[8];
-            if (valid) {
+            top[r] = sum[r] = 0.f;
+            if (i < k1) {   // (uniform over the CTA)
+                float l[8];
                 unpack8<DT>(raw[r], l);
                 if (repeated) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (repeated >> j & 1u) l[j] = l[j] > 0.f ? l[j] / rep : l[j] * rep;
+                        if (repeated >> j & 1u) l[j] = repeat_penalty(l[j], rep, inv);
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) l[j] = (mask[r] >> j & 1u) ? l[j] + add[j] : -INFINITY;
-                if (valid < kIdsPerThread) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j >= valid) l[j] = -INFINITY;
+                for (int j = 0; j < 8; j += 2) {
+                    const uint64_t y = add_two(two(l[j], l[j + 1]), add[j / 2]);
+                    l[j] = first_of(y);
+                    l[j + 1] = second_of(y);
                 }
-                const Row8<DT> w = pack8<DT>(l);
+                const Row8<DT> w = pack8<DT>(l, mask[r] & exist);
                 char* q = dst + i * P.ld_bytes;
                 if (valid == kIdsPerThread) {
                     *reinterpret_cast<uint4*>(q) = w.v[0];
@@ -224,37 +276,50 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
                                 reinterpret_cast<unsigned short*>(q)[j] = static_cast<unsigned short>(__float_as_uint(l[j]) >> 16);
                         }
                 }
-            } else {
+                if constexpr (NORM) {
+                    // Relative to the warp's largest logit, subtracted before the scaling: a row whose entries are all the
+                    // type's lowest value then has a normaliser like any other.
+                    const float m = warp_max_f32(fmaxf(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])),
+                                                       fmaxf(fmaxf(l[4], l[5]), fmaxf(l[6], l[7]))));
+                    top[r] = m > -INFINITY ? m : 0.f;
+                    const uint64_t down = two(-top[r], -top[r]), c2 = two(P.c, P.c);
+                    float s[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) l[j] = -INFINITY;
-            }
-            if constexpr (NORM) {
-                // Relative to the warp's largest logit, subtracted before the scaling: a row whose entries are all the
-                // type's lowest value then has a normaliser like any other.
-                float m = l[0];
+                    for (int j = 0; j < 8; j += 2) {
+                        const uint64_t e = mul_two(add_two(two(l[j], l[j + 1]), down), c2);
+                        s[j / 2] = ex2_approx(first_of(e)) + ex2_approx(second_of(e));
+                    }
+                    sum[r] = (s[0] + s[1]) + (s[2] + s[3]);
+                }
+                // the draft of this position counts for the positions behind it
+                if (counting && P.drafts) {
+                    const unsigned at = static_cast<unsigned>(s_draft[i]) - x0;
+                    if (at < static_cast<unsigned>(valid)) {
 #pragma unroll
-                for (int j = 1; j < 8; ++j) m = fmaxf(m, l[j]);
-                m = float_unorder(__reduce_max_sync(0xFFFFFFFFu, float_order(m != m ? -INFINITY : m)));
-                const float top = m > -INFINITY ? m : 0.f;
-                float s = 0.f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s += ex2_approx((l[j] - top) * P.c);
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-                if (lane == 0) s_part[i - k0][warp] = make_float2(top, s);
-            }
-            // the draft of this position counts for the positions behind it
-            if (counting && P.drafts) {
-                const unsigned at = static_cast<unsigned>(s_draft[i]) - x0;
-                if (at < static_cast<unsigned>(valid)) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (at == static_cast<unsigned>(j)) {
-                            ++hist[j];
-                            term(j);
-                        }
+                        for (int j = 0; j < 8; ++j)
+                            if (at == static_cast<unsigned>(j)) {
+                                ++hist[j];
+                                const float t = term(j);
+                                add[j / 2] = j & 1 ? two(first_of(add[j / 2]), t) : two(t, second_of(add[j / 2]));
+                            }
+                    }
                 }
             }
+        }
+        if constexpr (NORM) {
+            // four rows' sums over the warp with six shuffles: lanes 8 r .. 8 r + 7 end with row r's
+            static_assert(kRowsInFlight == 4, "");
+            const bool upper = lane & 16, odd = lane & 8;
+            float a = upper ? sum[2] : sum[0], c = upper ? sum[3] : sum[1];
+            a += __shfl_xor_sync(0xFFFFFFFFu, upper ? sum[0] : sum[2], 16);
+            c += __shfl_xor_sync(0xFFFFFFFFu, upper ? sum[1] : sum[3], 16);
+            float s = (odd ? c : a) + __shfl_xor_sync(0xFFFFFFFFu, odd ? a : c, 8);
+            s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
+            s += __shfl_xor_sync(0xFFFFFFFFu, s, 2);
+            s += __shfl_xor_sync(0xFFFFFFFFu, s, 1);
+            const int r = lane >> 3, i = i0 + r;
+            const float t = upper ? (odd ? top[3] : top[2]) : (odd ? top[1] : top[0]);
+            if ((lane & 7) == 0 && i < k1) s_part[i - k0][warp] = make_float2(t, s);
         }
     }
     if constexpr (NORM) {
