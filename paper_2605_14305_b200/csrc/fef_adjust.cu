@@ -13,6 +13,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fef.h"
 #include "fef_common.cuh"
 #include "fef_device_math.cuh"
@@ -129,9 +131,8 @@ __device__ __forceinline__ Row8<DT> pack8(float (&l)[8], uint32_t allowed) {
 
 // l / rep for l > 0, l * rep otherwise; `inv` = 1 / rep.  The quotient takes one correction step (an infinite l skips it).
 __device__ __forceinline__ float repeat_penalty(float l, float rep, float inv) {
-    if (!(l > 0.f)) return l * rep;
     const float q = l * inv, fixed = fmaf(fmaf(-q, rep, l), inv, q);
-    return l < INFINITY ? fixed : q;
+    return l > 0.f ? (l < INFINITY ? fixed : q) : l * rep;
 }
 
 template <int DT, bool NORM>
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
     uint32_t hist[kIdsPerThread];
 #pragma unroll
     for (int j = 0; j < kIdsPerThread; ++j) hist[j] = 0u;
-    const bool counting = P.penalties != nullptr;
+    const bool counting = P.penalties != nullptr, drafts = counting && P.drafts != nullptr;
     if (counting) {
         rep = __ldg(P.penalties + 3 * b);
         freq = __ldg(P.penalties + 3 * b + 1);
@@ -204,6 +205,7 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
     };
 #pragma unroll
     for (int j = 0; j < kIdsPerThread; j += 2) add[j / 2] = two(term(j), term(j + 1));
+    unsigned anywhere = rep != 1.f ? __reduce_or_sync(0xFFFFFFFFu, repeated) : 0u;   // ids that some lane has to penalise
 
     const int64_t row0 = static_cast<int64_t>(b) * P.K;
     const char* src = P.logits + row0 * P.ld_bytes + static_cast<int64_t>(x0) * E;
@@ -212,16 +214,22 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
         ? reinterpret_cast<const unsigned char*>(P.allowed + b * P.allowed_stride_b) + (x0 >> 3) : nullptr;
 
     const unsigned exist = (1u << valid) - 1u;   // ids behind V: -inf, never stored
-    for (int i0 = k0; i0 < k1; i0 += kRowsInFlight) {
+    const int64_t to_out = dst - src;            // (the same place of the output)
+    const bool whole = __all_sync(0xFFFFFFFFu, valid == kIdsPerThread);
+    const char* from = src + k0 * P.ld_bytes;
+    if (bits) bits += k0 * P.allowed_stride_k * 4;
+
+    // Up to four rows: all of them and all ids there (FULL), or any.
+    auto batch = [&](auto full, int i0) {
+        constexpr bool FULL = decltype(full)::value;
         Row8<DT> raw[kRowsInFlight];
         unsigned mask[kRowsInFlight];
 #pragma unroll
         for (int r = 0; r < kRowsInFlight; ++r) {
-            const int i = i0 + r;
+            const char* p = from + r * P.ld_bytes;
             mask[r] = 0xFFu;
-            if (i < k1 && valid) {
-                const char* p = src + i * P.ld_bytes;
-                if (valid == kIdsPerThread) {
+            if (FULL || (i0 + r < k1 && valid)) {
+                if (FULL || valid == kIdsPerThread) {
                     raw[r].v[0] = ld_stream_v4(p);
                     if constexpr (DT == FEF_F32) raw[r].v[1] = ld_stream_v4(p + 16);
                 } else {
@@ -239,21 +247,23 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
                     }
                     raw[r] = pack8<DT>(l, 0xFFu);
                 }
-                if (bits) mask[r] = __ldg(bits + i * P.allowed_stride_k * 4);
+                if (bits) mask[r] = __ldg(bits + r * P.allowed_stride_k * 4);
             }
         }
         float top[kRowsInFlight], sum[kRowsInFlight];
 #pragma unroll
         for (int r = 0; r < kRowsInFlight; ++r) {
-            const int i = i0 + r;
             top[r] = sum[r] = 0.f;
-            if (i < k1) {   // (uniform over the CTA)
+            if (FULL || i0 + r < k1) {   // (uniform over the CTA)
                 float l[8];
                 unpack8<DT>(raw[r], l);
-                if (repeated) {
+                if (anywhere) {   // (uniform over the warp, and so is every test in it)
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (repeated >> j & 1u) l[j] = repeat_penalty(l[j], rep, inv);
+                        if (anywhere >> j & 1u) {
+                            const float y = repeat_penalty(l[j], rep, inv);
+                            l[j] = repeated >> j & 1u ? y : l[j];
+                        }
                 }
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
@@ -261,9 +271,9 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
                     l[j] = first_of(y);
                     l[j + 1] = second_of(y);
                 }
-                const Row8<DT> w = pack8<DT>(l, mask[r] & exist);
-                char* q = dst + i * P.ld_bytes;
-                if (valid == kIdsPerThread) {
+                const Row8<DT> w = pack8<DT>(l, FULL ? mask[r] : mask[r] & exist);
+                char* q = const_cast<char*>(from) + r * P.ld_bytes + to_out;
+                if (FULL || valid == kIdsPerThread) {
                     *reinterpret_cast<uint4*>(q) = w.v[0];
                     if constexpr (DT == FEF_F32) *reinterpret_cast<uint4*>(q + 16) = w.v[1];
                 } else {
@@ -292,16 +302,18 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
                     sum[r] = (s[0] + s[1]) + (s[2] + s[3]);
                 }
                 // the draft of this position counts for the positions behind it
-                if (counting && P.drafts) {
-                    const unsigned at = static_cast<unsigned>(s_draft[i]) - x0;
-                    if (at < static_cast<unsigned>(valid)) {
+                if (drafts) {
+                    const unsigned at = static_cast<unsigned>(s_draft[i0 + r]) - x0;
+                    const bool mine = at < static_cast<unsigned>(valid);
+                    if (__any_sync(0xFFFFFFFFu, mine)) {
 #pragma unroll
                         for (int j = 0; j < 8; ++j)
-                            if (at == static_cast<unsigned>(j)) {
+                            if (mine && at == static_cast<unsigned>(j)) {
                                 ++hist[j];
                                 const float t = term(j);
                                 add[j / 2] = j & 1 ? two(first_of(add[j / 2]), t) : two(t, second_of(add[j / 2]));
                             }
+                        anywhere = rep != 1.f ? __reduce_or_sync(0xFFFFFFFFu, repeated) : 0u;
                     }
                 }
             }
@@ -317,11 +329,17 @@ __global__ void __launch_bounds__(kThreads) adjust_kernel(const __grid_constant_
             s += __shfl_xor_sync(0xFFFFFFFFu, s, 4);
             s += __shfl_xor_sync(0xFFFFFFFFu, s, 2);
             s += __shfl_xor_sync(0xFFFFFFFFu, s, 1);
-            const int r = lane >> 3, i = i0 + r;
+            const int r = lane >> 3;
             const float t = upper ? (odd ? top[3] : top[2]) : (odd ? top[1] : top[0]);
-            if ((lane & 7) == 0 && i < k1) s_part[i - k0][warp] = make_float2(t, s);
+            if ((lane & 7) == 0 && (FULL || i0 + r < k1)) s_part[i0 + r - k0][warp] = make_float2(t, s);
         }
-    }
+        from += kRowsInFlight * P.ld_bytes;
+        if (bits) bits += kRowsInFlight * P.allowed_stride_k * 4;
+    };
+    int i0 = k0;
+    if (whole)
+        for (; i0 + kRowsInFlight <= k1; i0 += kRowsInFlight) batch(std::true_type{}, i0);
+    for (; i0 < k1; i0 += kRowsInFlight) batch(std::false_type{}, i0);
     if constexpr (NORM) {
         __syncthreads();
         for (int i = k0 + tid; i < k1; i += kThreads) {
