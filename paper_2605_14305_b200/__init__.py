@@ -347,6 +347,28 @@ def fef_draft_sample(draft_logits: torch.Tensor, temperature: float, seed: int, 
     return out
 
 
+def _all_cuda(*tensors):
+    """As ``_require_cuda``, without asking the driver when every tensor is where it should be."""
+    for t in tensors:
+        if t is not None and not t.is_cuda:
+            _require_cuda(t)
+
+
+def _is(t: Optional[torch.Tensor], dtype, shape, dev) -> bool:
+    return t is None or (t.dtype == dtype and t.shape == shape and t.is_contiguous() and t.device == dev)
+
+
+def _at(device, stream):
+    """``_on``, or nothing when that device is current and no stream is given (it matters for small calls)."""
+    if stream is None and torch.cuda.current_device() == device.index:
+        return contextlib.nullcontext()
+    return _on(device, stream)
+
+
+def _raw_stream(device, stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else int(stream.cuda_stream)
+
+
 MASK_TOKEN = -1
 
 
@@ -705,7 +727,7 @@ class QuantizedLayer(NamedTuple):
 def _quantized_layer(layer: QuantizedLayer, where: str):
     """(V, blocks) of a layer whose tensors have the documented shapes and types."""
     packed, scale, zero, d, group = layer[:5]
-    _require_cuda(packed, scale, zero)
+    _all_cuda(packed, scale, zero)
     if group not in (32, 64, 128) or d < group or d % group or packed.dim() != 2:
         raise FefError(FEF_ERR_INVALID_ARG, where)
     V, blocks = packed.shape[0], (d + 127) // 128
@@ -723,19 +745,19 @@ def fef_lmhead_quantize(weight: torch.Tensor, group: int = 128, zero_points: boo
     """Bring an output layer ``weight`` ([V, d] bfloat16, ``d`` a multiple of ``group``) to 4 bits with one scale, and
     with ``zero_points`` one zero point, per ``group`` (32, 64 or 128) weights of a row (see include/fef.h)."""
     where = "fef_lmhead_quantize"
-    _require_cuda(weight)
+    _all_cuda(weight)
     _bf16_matrix(weight, where)
     V, d = weight.shape
     if group not in (32, 64, 128) or V < 1 or d < group or d % group:
         raise FefError(FEF_ERR_INVALID_ARG, where)
     dev, blocks = weight.device, (d + 127) // 128
-    with _on(dev, stream):
+    with _at(dev, stream):
         packed = torch.empty((V, blocks * 64), dtype=torch.uint8, device=dev)
         scale = torch.empty((blocks, (V + 31) // 32 * 32, 128 // group), dtype=torch.bfloat16, device=dev)
         zero = torch.empty(scale.shape, dtype=torch.uint8, device=dev) if zero_points else None
         status = torch.empty(1, dtype=torch.int32, device=dev)
         st = load().fef_lmhead_quantize(weight.data_ptr(), V, d, group, packed.data_ptr(), scale.data_ptr(), _ptr(zero),
-                                        status.data_ptr(), _stream_ptr(stream))
+                                        status.data_ptr(), _raw_stream(dev, stream))
     if st != FEF_OK:
         raise FefError(st, where)
     return QuantizedLayer(packed, scale, zero, d, group, status)
@@ -748,11 +770,11 @@ def fef_lmhead_dequantize(layer: QuantizedLayer, out: Optional[torch.Tensor] = N
     dev = layer.packed.device
     if out is not None and (out.dtype != torch.float32 or out.shape != (V, layer.d) or not out.is_contiguous() or out.device != dev):
         raise FefError(FEF_ERR_INVALID_ARG, where)
-    with _on(dev, stream):
+    with _at(dev, stream):
         if out is None:
             out = torch.empty((V, layer.d), dtype=torch.float32, device=dev)
         st = load().fef_lmhead_dequantize(layer.packed.data_ptr(), layer.scale.data_ptr(), _ptr(layer.zero), V, layer.d,
-                                          layer.group, out.data_ptr(), _stream_ptr(stream))
+                                          layer.group, out.data_ptr(), _raw_stream(dev, stream))
     if st != FEF_OK:
         raise FefError(st, where)
     return out
@@ -773,7 +795,7 @@ def fef_lmhead_logits_quantized(hidden: torch.Tensor, layer: QuantizedLayer, dty
     where = "fef_lmhead_logits_quantized"
     V, _ = _quantized_layer(layer, where)
     _bf16_matrix(hidden, where)
-    _require_cuda(out, workspace)
+    _all_cuda(hidden, out, workspace)
     dev = layer.packed.device
     rows, d = hidden.shape
     if d != layer.d or hidden.device != dev or rows < 1:
@@ -785,7 +807,7 @@ def fef_lmhead_logits_quantized(hidden: torch.Tensor, layer: QuantizedLayer, dty
     if dtype not in (torch.float32, torch.bfloat16):
         raise FefError(FEF_ERR_DTYPE, where)
     per_vec = 4 if dtype == torch.float32 else 8
-    with _on(dev, stream):
+    with _at(dev, stream):
         if out is None:
             out = torch.empty((rows, (V + per_vec - 1) // per_vec * per_vec), dtype=dtype, device=dev)
         status = torch.empty(1, dtype=torch.int32, device=dev)
@@ -795,7 +817,7 @@ def fef_lmhead_logits_quantized(hidden: torch.Tensor, layer: QuantizedLayer, dty
         st = load().fef_lmhead_logits_quantized(
             hidden.data_ptr(), layer.packed.data_ptr(), layer.scale.data_ptr(), _ptr(layer.zero), rows, V, d, layer.group,
             out.data_ptr(), out.shape[1], FEF_F32 if dtype == torch.float32 else FEF_BF16, workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), status.data_ptr(), _stream_ptr(stream))
+            workspace.numel() * workspace.element_size(), status.data_ptr(), _raw_stream(dev, stream))
     if st != FEF_OK:
         raise FefError(st, where)
     return out, status
@@ -835,51 +857,52 @@ def fef_logits_adjust(logits: torch.Tensor, tokens: Optional[torch.Tensor] = Non
     takes them.  Asynchronous on the current (or given) stream.
     """
     where = "fef_logits_adjust"
-    _require_cuda(logits, tokens, prompt_len, draft_tokens, penalties, bias, allowed, row_len, out, log2_norm, workspace)
+    _all_cuda(logits, tokens, prompt_len, draft_tokens, penalties, bias, allowed, row_len, out, log2_norm, workspace)
     if logits.dim() != 3 or not logits.is_contiguous():
         raise FefError(FEF_ERR_INVALID_ARG, where)
-    B, K, ld = logits.shape
+    B, K, ld = shape = logits.shape
     V = ld if V is None else int(V)
     code = _dtype_code(logits)
     dev = logits.device
-    for t, dtype, shape in ((prompt_len, torch.int32, (B,)), (draft_tokens, torch.int32, (B, K)),
-                            (row_len, torch.int32, (B,)), (penalties, torch.float32, (B, 3)),
-                            (log2_norm, torch.float64, (B, K)), (out, logits.dtype, logits.shape)):
-        if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != dev):
-            raise FefError(FEF_ERR_INVALID_ARG, where)
-    L = 0
+    L = bias_stride = stride_b = stride_k = 0
     if tokens is not None:
         if tokens.dtype != torch.int32 or tokens.dim() != 2 or tokens.shape[0] != B or not tokens.is_contiguous() or \
                 tokens.device != dev:
             raise FefError(FEF_ERR_INVALID_ARG, where)
         L = tokens.shape[1]
-    bias_stride = stride_b = stride_k = 0
+    if not (_is(prompt_len, torch.int32, (B,), dev) and _is(draft_tokens, torch.int32, (B, K), dev) and
+            _is(row_len, torch.int32, (B,), dev) and _is(penalties, torch.float32, (B, 3), dev) and
+            _is(log2_norm, torch.float64, (B, K), dev) and _is(out, logits.dtype, shape, dev)):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
     if bias is not None:
         if bias.dtype != torch.float32 or bias.dim() not in (1, 2) or bias.shape[-1] < V or bias.device != dev or \
                 (bias.stride(-1) != 1 and V > 1) or (bias.dim() == 2 and bias.shape[0] != B):
             raise FefError(FEF_ERR_INVALID_ARG, where)
         bias_stride = bias.stride(0) if bias.dim() == 2 and B > 1 else 0
     if allowed is not None:
-        words = (V + 31) // 32
-        if allowed.dtype != torch.int32 or allowed.dim() not in (1, 2, 3) or allowed.shape[-1] < words or \
+        words, dims = (V + 31) // 32, allowed.dim()
+        if allowed.dtype != torch.int32 or dims not in (1, 2, 3) or allowed.shape[-1] < words or \
                 allowed.device != dev or (allowed.stride(-1) != 1 and words > 1) or \
-                tuple(allowed.shape[:-1]) != (B, K)[:allowed.dim() - 1]:
+                tuple(allowed.shape[:-1]) != (B, K)[:dims - 1]:
             raise FefError(FEF_ERR_INVALID_ARG, where)
-        stride_b = allowed.stride(0) if allowed.dim() >= 2 and B > 1 else 0
-        stride_k = allowed.stride(1) if allowed.dim() == 3 and K > 1 else 0
-    plain = out is not None and not with_norm and stream is None and torch.cuda.current_device() == dev.index
-    with (contextlib.nullcontext() if plain else _on(dev, stream)):
+        stride_b = allowed.stride(0) if dims >= 2 and B > 1 else 0
+        stride_k = allowed.stride(1) if dims == 3 and K > 1 else 0
+    with _at(dev, stream):
         if out is None:
             out = torch.empty_like(logits)
         if with_norm and log2_norm is None:
             log2_norm = torch.empty((B, K), dtype=torch.float64, device=dev)
-        if log2_norm is not None and workspace is None:
-            workspace = torch.empty(max(fef_logits_adjust_workspace_bytes(B, K, V), 256), dtype=torch.uint8, device=dev)
-        p = _ptr
+        size = 0
+        if log2_norm is not None:
+            if workspace is None:
+                workspace = torch.empty(max(fef_logits_adjust_workspace_bytes(B, K, V), 256), dtype=torch.uint8, device=dev)
+            size = workspace.numel() * workspace.element_size()
         st = load().fef_logits_adjust(
-            logits.data_ptr(), out.data_ptr(), B, K, V, ld, code, p(tokens), L, p(prompt_len), p(draft_tokens), p(row_len),
-            p(penalties), p(bias), bias_stride, p(allowed), stride_b, stride_k, float(temperature), p(log2_norm),
-            p(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream))
+            logits.data_ptr(), out.data_ptr(), B, K, V, ld, code, _ptr(tokens), L, _ptr(prompt_len), _ptr(draft_tokens),
+            _ptr(row_len), _ptr(penalties), _ptr(bias), bias_stride, _ptr(allowed), stride_b, stride_k, temperature,
+            _ptr(log2_norm), _ptr(workspace), size, _raw_stream(dev, stream))
     if st != FEF_OK:
         raise FefError(st, where)
     return AdjustResult(out, log2_norm)
