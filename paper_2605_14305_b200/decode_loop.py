@@ -83,10 +83,21 @@ def run_decode_loop(B: int, L: int, K: int, n_steps: int, remask_k: int,
     return dict(tokens=tokens, conf=conf, rounds=rnd - first_round, committed_per_round=committed_hist)
 
 
+def _adjusted_draws(fef, adjust, rnd, q, p, tokens, window, row_len, temperature, seed, step, V, device_round=None):
+    """Draft logits adjusted, draws, target logits adjusted: (q, p, draws, the target rows' normalisers)."""
+    rules = adjust if callable(adjust) else (lambda *_: adjust)
+    common = dict(tokens=tokens, row_len=row_len, V=V, temperature=temperature)
+    q = fef.fef_logits_adjust(q, **common, **rules(rnd, window, row_len, None)).logits
+    draft = fef.fef_draft_sample(q, temperature, seed, step, row_len=row_len, V=V, device_round=device_round)
+    p, p_norm = fef.fef_logits_adjust(p, draft_tokens=draft.tokens, with_norm=True, **common,
+                                      **rules(rnd, window, row_len, draft.tokens))
+    return q, p, draft, p_norm
+
+
 def run_decode_loop_device(fef, B: int, L: int, K: int, n_steps: int, remask_k: int, logits_fn: Callable,
                            temperature: float, seed: int, on_round: Optional[Callable] = None,
                            first_round: int = 0, reuse_draft_norm: bool = True, build_inputs: bool = False,
-                           reuse_target_norm: bool = False, V: Optional[int] = None):
+                           reuse_target_norm: bool = False, V: Optional[int] = None, adjust=None):
     """Algorithm 2 with the whole state resident on the device: every step of a round is one
     library call (``fef_loop_next_window`` -> [``fef_loop_verification_inputs``] ->
     ``fef_draft_sample`` -> ``fef_spec_verify`` -> ``fef_loop_commit``), and a denoising step ends
@@ -100,6 +111,11 @@ def run_decode_loop_device(fef, B: int, L: int, K: int, n_steps: int, remask_k: 
     reuse_target_norm: the draft draws also reduce the target rows (``fef_draft_sample(target_logits=)``)
     and the verification takes both normalisers, so both tensors are read once per round.
     V: vocabulary size when the logits' row pitch is larger.
+    adjust: rules every request's logits obey (penalties, biases, grammar masks): a dict of arguments of
+    ``fef_logits_adjust`` (prompt_len, penalties, bias, allowed), or a function of (round, window_pos, row_len,
+    draft_tokens or None) that returns one.  The draft logits are adjusted before the draws, by the tokens
+    resolved so far; the target logits after them, by those and the window's earlier drafts, and their
+    normalisers go to the verification with the draws' own.  The hook then sees the adjusted logits.
 
     Returns dict(tokens [B,L] int32, conf [B,L] float32 (CUDA), rounds, committed_per_round, loop_seconds).
     """
@@ -118,14 +134,17 @@ def run_decode_loop_device(fef, B: int, L: int, K: int, n_steps: int, remask_k: 
                 break
             inputs = None
             q, p = logits_fn(rnd, window, row_len, None)
-            draft = fef.fef_draft_sample(q, temperature, seed, rnd, row_len=row_len, V=V,
-                                         target_logits=p if reuse_target_norm else None)
+            if adjust is not None:
+                q, p, draft, p_norm = _adjusted_draws(fef, adjust, rnd, q, p, tokens, window, row_len, temperature, seed, rnd, V)
+            else:
+                draft = fef.fef_draft_sample(q, temperature, seed, rnd, row_len=row_len, V=V,
+                                             target_logits=p if reuse_target_norm else None)
+                p_norm = draft.target_log2_norm if reuse_target_norm else None
             if build_inputs:
                 inputs = fef.fef_loop_verification_inputs(tokens, window, row_len, draft.tokens)
-            norm = draft.log2_norm if (reuse_draft_norm or reuse_target_norm) else None
+            norm = draft.log2_norm if (reuse_draft_norm or p_norm is not None) else None
             res = fef.fef_spec_verify(q, p, draft.tokens, temperature, seed, rnd, row_len=row_len, V=V,
-                                      draft_log2_norm=norm,
-                                      target_log2_norm=draft.target_log2_norm if reuse_target_norm else None)
+                                      draft_log2_norm=norm, target_log2_norm=p_norm)
             before = (tokens.clone(), conf.clone(), in_step.clone()) if on_round is not None else None
             committed = fef.fef_loop_commit(window, row_len, res, tokens, conf, in_step)
             if on_round is not None:
@@ -151,7 +170,7 @@ def run_decode_loop_device(fef, B: int, L: int, K: int, n_steps: int, remask_k: 
 
 def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: int, logits_fn: Callable,
                           temperature: float, seed: int, first_round: int = 0, reuse_draft_norm: bool = True,
-                          rounds_per_check: int = 4):
+                          rounds_per_check: int = 4, adjust=None):
     """``run_decode_loop_device`` with one whole round captured as a CUDA graph and replayed.
 
     The round's number lives in a device word that ``fef_draft_sample`` / ``fef_spec_verify`` add
@@ -161,7 +180,8 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
     the last real round of a denoising step change nothing.
 
     logits_fn(device_round [1] int32 CUDA, window_pos, row_len) -> (draft_logits, target_logits):
-    must be capturable (device work only, the round read from the tensor).
+    must be capturable (device work only, the round read from the tensor).  ``adjust`` as there; a function
+    of it gets the round's tensor and must be capturable too.
 
     Returns dict(tokens, conf (CUDA), rounds, loop_seconds: wall time of the replay loop alone).
     """
@@ -174,9 +194,15 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
     def one_round():
         window, row_len, unresolved = fef.fef_loop_next_window(tokens, K)
         q, p = logits_fn(rnd, window, row_len)
-        draft = fef.fef_draft_sample(q, temperature, seed, first_round, row_len=row_len, device_round=rnd)
+        p_norm = None
+        if adjust is not None:
+            q, p, draft, p_norm = _adjusted_draws(fef, adjust, rnd, q, p, tokens, window, row_len, temperature, seed, first_round,
+                                                  None, device_round=rnd)
+        else:
+            draft = fef.fef_draft_sample(q, temperature, seed, first_round, row_len=row_len, device_round=rnd)
         res = fef.fef_spec_verify(q, p, draft.tokens, temperature, seed, first_round, row_len=row_len,
-                                  draft_log2_norm=draft.log2_norm if reuse_draft_norm else None, device_round=rnd)
+                                  draft_log2_norm=draft.log2_norm if (reuse_draft_norm or p_norm is not None) else None,
+                                  device_round=rnd, target_log2_norm=p_norm)
         fef.fef_loop_commit(window, row_len, res, tokens, conf, in_step)
         fef.fef_loop_advance_round(rnd, unresolved)
         return unresolved
