@@ -2,21 +2,22 @@
 // tensor memory.
 //
 // prepare_kernel brings the hidden rows into the operand's form once (workspace): the eight columns of every packed word in
-// the order 0 4, 1 5, 2 6, 3 7 in which the nibbles come apart (fef_quant.cuh).  product_tiles_kernel then takes tiles of 256
-// vocabulary rows x NT hidden rows, one CTA of 20 warps per SM, as two pipelines of 128 vocabulary rows that share the hidden
-// rows and nothing else:
-//   2 x 4 warps  weights: packed nibbles from global memory (kAhead blocks in flight per warp) to the bfloat16 numbers q - z in
-//                tensor memory, a vocabulary row per lane (through shared memory, writing and reading them took 512 of its
-//                cycles a block: 160 us at 64 rows x 126464 x 4096);
-//   1 warp       brings the hidden rows of the same 128 columns in by TMA, and on a ring of their own the groups' scales (read
-//                from global memory by the warps that need them, their latency set the pace);
-//   2 x 1 warp   issue the MMAs (128 x NT x 16), a fresh accumulator for every group of a row's weights;
-//   2 x 4 warps  take each group's accumulator out of tensor memory, scale it and add it to the logits in registers: the
-//                vocabulary rows are the lanes, so a group's scale is one number per thread.  The weights are the left operand
-//                for that reason.
-// A block's hand-overs from warp to warp, not its arithmetic, set the pace: hence two pipelines side by side, few warps with
-// much to do each, and waits that poll several barriers at once.  The epilogue has most to do, so the weights' warps subtract
-// the zero points (taking them off the groups' sums, as the kernel for few rows does, was 126 us).  Every wait is bounded.
+// the order 0 4, 1 5, 2 6, 3 7 in which the nibbles come apart (fef_quant.cuh).  product_tiles_kernel then takes tiles of
+// vocabulary rows x NT hidden rows, one CTA of 20 warps per SM: up to 64 hidden rows as two pipelines of 128 vocabulary rows that
+// share the hidden rows and nothing else, beyond that as one pipeline with twice the warps.
+//   8 warps  weights: packed nibbles from global memory (kAhead blocks in flight per warp) to the bfloat16 numbers q - z in tensor
+//            memory, a vocabulary row per lane (through shared memory, writing and reading them took 512 of its cycles a block:
+//            160 us at 64 rows x 126464 x 4096);
+//   1 warp   brings the hidden rows of the same 128 columns in by TMA, and on a ring of their own the groups' scales (read from
+//            global memory by the warps that need them, their latency set the pace);
+//   1 warp a pipeline issues the MMAs (128 x NT x 16), a fresh accumulator for every group of a row's weights;
+//   8 warps  take each group's accumulator out of tensor memory, scale it and add it to the logits in registers: the vocabulary
+//            rows are the lanes, so a group's scale is one number per thread.  The weights are the left operand for that reason.
+// A block's hand-overs from warp to warp and the instructions of the weights' and the epilogue's warps set the pace (64 rows:
+// 109 us, 1350 cycles for two blocks of 128 x 128 weights, of which the MMAs need 512 and the weights' bytes 660; 512 rows:
+// 588 us = 0.90 PFLOP/s): hence few warps with much to do each, and waits that poll several barriers at once.  The epilogue has most
+// to do, so the weights' warps subtract the zero points (taking them off the groups' sums, as the kernel for few rows does,
+// was 126 us).  Every wait is bounded.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -30,14 +31,12 @@ namespace fef {
 namespace quant {
 namespace {
 
-constexpr int kPipes = 2;
-constexpr int kPipeV = 128, kTileV = kPipes * kPipeV;   // vocabulary rows
-constexpr int kAStages = 2;                   // of a pipeline: blocks of unpacked weights in tensor memory
-constexpr int kACols = kBlock / 2;            // 32-bit columns of such a block
+constexpr int kPipeV = 128;                   // vocabulary rows of a pipeline
+constexpr int kACols = kBlock / 2;            // 32-bit columns of a block of unpacked weights in tensor memory
 constexpr int kSides = 4;                     // ring of the blocks' scales
-constexpr int kRoleWarps = 4;                 // warps of a pipeline's epilogue, and of its weights
-constexpr int kThreads = (2 * kPipes * kRoleWarps + 4) * 32;   // the last four warps: TMA, an issuer per pipeline, one idle
-constexpr int kWeightWarp0 = kPipes * kRoleWarps, kTmaWarp = 2 * kPipes * kRoleWarps, kIssueWarp0 = kTmaWarp + 1;
+constexpr int kRoleWarps = 4;                 // warps that share a pipeline's rows
+constexpr int kThreads = (4 * kRoleWarps + 4) * 32;   // the last four warps: TMA, up to two issuers, idle
+constexpr int kWeightWarp0 = 2 * kRoleWarps, kTmaWarp = 4 * kRoleWarps, kIssueWarp0 = kTmaWarp + 1;
 constexpr int kLaunchRegs = 96;               // per thread
 constexpr unsigned long long kWaitNs = 1000000000ull;
 
@@ -47,25 +46,29 @@ struct TileParams {
     int out_bf16;
 };
 
-template <int NT>
+// PIPES = 2: two pipelines, each with four warps for its weights and four for its epilogue.  PIPES = 1: one, whose weights two
+// teams of four warps unpack block by block in turn, and whose hidden rows two teams of four take half each in the epilogue.
+template <int NT, int PIPES>
 struct Sizes {
-    static constexpr int kBBytes = NT * kBlock * 2, kBStages = 6;
+    static constexpr int kTileV = PIPES * kPipeV, kTeams = 2 / PIPES, kCols = NT / kTeams;
+    static_assert(kCols == 64, "");   // the registers' shares below are for 64 columns per thread of the epilogue
+    static constexpr int kBBytes = NT * kBlock * 2, kBStages = NT == 128 ? 5 : 6;
     // tensor memory of a pipeline: accumulators, then weights
-    static constexpr int kAccumulators = NT == 64 ? 2 : 4;
-    static constexpr int kPipeCols = kAccumulators * NT + kAStages * kACols, kTmemCols = kPipes * kPipeCols;
-    static_assert(kTmemCols == 512, "");
+    static constexpr int kAStages = PIPES == 2 ? 2 : 4;
+    static constexpr int kPipeCols = 512 / PIPES, kAccumulators = 2;
+    static_assert(kAccumulators * NT + kAStages * kACols <= kPipeCols, "");
     // Registers per thread that the three kinds of warpgroups keep of the launch's: the shares add up to its total exactly.
     // (Chosen so that nothing spills: with this much shared memory in use a spilled register comes back from L2.)
-    static constexpr int kEpilogueRegs = NT == 64 ? 128 : 112, kWeightRegs = NT == 64 ? 80 : 88, kControlRegs = NT == 64 ? 64 : 80;
-    static_assert(kPipes * kRoleWarps * (kEpilogueRegs + kWeightRegs) + 4 * kControlRegs == kThreads / 32 * kLaunchRegs, "");
-    static constexpr int kAhead = NT == 64 ? 2 : 3;   // blocks of weights in flight per warp
+    static constexpr int kEpilogueRegs = 128, kWeightRegs = 80, kControlRegs = 64;
+    static_assert(2 * kRoleWarps * (kEpilogueRegs + kWeightRegs) + 4 * kControlRegs == kThreads / 32 * kLaunchRegs, "");
+    static constexpr int kAhead = 2;   // blocks of weights in flight per warp
 };
 
 struct Shared {
-    uint64_t a_full[kPipes][kAStages];
-    uint64_t a_empty[kPipes][kAStages];
-    uint64_t acc_full[kPipes][4];
-    uint64_t acc_empty[kPipes][4];
+    uint64_t a_full[2][4];
+    uint64_t a_empty[2][4];
+    uint64_t acc_full[2][4];
+    uint64_t acc_empty[2][4];
     uint64_t b_full[6];
     uint64_t b_empty[6];
     uint64_t side_full[kSides];
@@ -156,10 +159,10 @@ __device__ __forceinline__ void bulk_copy(void* dst, const void* src, uint32_t b
                  : "memory");
 }
 
-// Of a block: the scales of all 256 rows.
+// Of a block: the scales of all rows.
 template <int N>
 struct Side {
-    uint16_t scale[kTileV * N];
+    uint16_t scale[2 * kPipeV * N];
 };
 
 // The lower word of smem_desc_sw128's descriptor (the upper one is the same for all), and the MMA that takes it and a left
@@ -208,10 +211,11 @@ __device__ __forceinline__ void store_column(Out* out, int64_t ldo, const uint64
     }
 }
 
-template <int NT, int N>   // hidden rows of a tile, groups per block
+template <int NT, int PIPES, int N>   // hidden rows of a tile, pipelines, groups per block
 __global__ void __launch_bounds__(kThreads, 1)
 product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_constant__ TileParams T) {
-    using S = Sizes<NT>;
+    using S = Sizes<NT, PIPES>;
+    constexpr int kTileV = S::kTileV, kTeams = S::kTeams, kCols = S::kCols, kAStages = S::kAStages;
     constexpr int kAccumulators = S::kAccumulators, kAhead = S::kAhead;
     constexpr uint32_t kInstr = (1u << 4) | (1u << 7) | (1u << 10) | ((NT >> 3) << 17) | ((kPipeV >> 4) << 24);
     extern __shared__ unsigned char smem_raw[];
@@ -224,29 +228,29 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        for (int p = 0; p < kPipes; ++p) {
+        for (int p = 0; p < PIPES; ++p) {
             for (int s = 0; s < kAStages; ++s) {
                 mbar_init(&sh.a_full[p][s], kRoleWarps);
                 mbar_init(&sh.a_empty[p][s], 1);
             }
             for (int a = 0; a < kAccumulators; ++a) {
                 mbar_init(&sh.acc_full[p][a], 1);
-                mbar_init(&sh.acc_empty[p][a], kRoleWarps);
+                mbar_init(&sh.acc_empty[p][a], kTeams * kRoleWarps);
             }
         }
         for (int s = 0; s < S::kBStages; ++s) {
             mbar_init(sh.b_full + s, 1);
-            mbar_init(sh.b_empty + s, kPipes);
+            mbar_init(sh.b_empty + s, PIPES);
         }
         for (int q = 0; q < kSides; ++q) {
             mbar_init(sh.side_full + q, 1);
-            mbar_init(sh.side_empty + q, kPipes * kRoleWarps);
+            mbar_init(sh.side_empty + q, 2 * kRoleWarps);
         }
-        mbar_init(&sh.drained, kPipes);
+        mbar_init(&sh.drained, PIPES);
         sh.abort_flag = 0;
         mbar_fence_init();
     }
-    if (warp == 0) tmem_alloc(&sh.tmem_base, S::kTmemCols);  // (one CTA per SM: the columns are always free)
+    if (warp == 0) tmem_alloc(&sh.tmem_base, 512);  // (one CTA per SM: the columns are always free)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -296,7 +300,7 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 }
             }
         }
-    } else if (warp >= kIssueWarp0 + kPipes) {
+    } else if (warp >= kIssueWarp0 + PIPES) {
         // (the control warpgroup's fourth warp)
     } else if (warp >= kIssueWarp0) {
         // -------------------------------------------------------------------------- MMAs
@@ -313,7 +317,7 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             const uint32_t a_at = tmem + kAccumulators * NT + a.at * kACols, b_at = b_base + b.at * (S::kBBytes / 16);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                if (!wait_for_all(sh, offsetof(Shared, a_full) + (pipe * kAStages + a.at) * 8, a.phase, offsetof(Shared, b_full) + b.at * 8,
+                if (!wait_for_all(sh, offsetof(Shared, a_full) + (pipe * 4 + a.at) * 8, a.phase, offsetof(Shared, b_full) + b.at * 8,
                                   b.phase, offsetof(Shared, acc_empty) + (pipe * 4 + acc.at) * 8, acc.phase ^ 1u)) {
                     gave_up();
                     ok = false;
@@ -347,13 +351,18 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         // ------------------------------------------------------------------------------------ weights
         // A lane takes one row: the 64 bytes of a block are its word 4 t + w, of columns 32 w + 8 t .. + 7, for every t and w.
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(S::kWeightRegs));
-        const int pipe = (warp - kWeightWarp0) / kRoleWarps, quarter = (warp - kWeightWarp0) % kRoleWarps;
+        const int which = (warp - kWeightWarp0) / kRoleWarps, quarter = (warp - kWeightWarp0) % kRoleWarps;
+        const int pipe = PIPES == 2 ? which : 0, team = PIPES == 2 ? 0 : which;
         const uint32_t tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + pipe * S::kPipeCols + kAccumulators * NT;
-        const int blocks = count;
-        int left = blocks, fetch_item = blockIdx.x, fetch_block = 0;
+        const int blocks = (count - team + kTeams - 1) / kTeams;   // of this team
+        int left = blocks, fetch_item = blockIdx.x, fetch_block = team;
         const uint8_t *fetch_w = nullptr, *fetch_z = nullptr;
         const bool zeros = W.zero != nullptr;
         auto seek = [&]() {   // (rows behind V are read as the last one; their logits are not stored)
+            while (fetch_block >= W.blocks) {
+                fetch_block -= W.blocks;
+                fetch_item += gridDim.x;
+            }
             const int64_t v = min(static_cast<int64_t>(fetch_item / T.row_blocks) * kTileV + pipe * kPipeV + quarter * 32 + lane,
                                   static_cast<int64_t>(W.V - 1));
             fetch_w = W.packed + v * (static_cast<int64_t>(W.blocks) * 64);
@@ -373,18 +382,15 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             }
             const int more = left > 1 ? 1 : 0;
             left -= more;
-            fetch_block += more;
-            if (fetch_block == W.blocks) {
-                fetch_block = 0;
-                fetch_item += gridDim.x;
-                seek();
-            }
+            fetch_block += more * kTeams;
+            if (fetch_block >= W.blocks) seek();
         };
         if (blocks > 0) {
             seek();
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) fetch(ahead[i]);
             Turn<kAStages> stage;
+            stage.at = team;
             bool ok = true;
             // (after a wait that ran out the rest goes by without waits and arrivals)
             auto put = [&](const Fetched& f) {
@@ -413,7 +419,8 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 tc_fence_before();
                 __syncwarp();
                 if (ok && lane == 0) mbar_arrive(&sh.a_full[pipe][stage.at]);
-                stage.advance();
+#pragma unroll
+                for (int t = 0; t < kTeams; ++t) stage.advance();
             };
             int at = 0;
             for (; at + kAhead <= blocks; at += kAhead) {
@@ -435,15 +442,17 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
         // ----------------------------------------------------------------------------------- epilogue
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(S::kEpilogueRegs));
         cudaGridDependencySynchronize();
-        const int pipe = warp / kRoleWarps, quarter = warp % kRoleWarps, row_in_tile = pipe * kPipeV + quarter * 32 + lane;
-        const uint32_t tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + pipe * S::kPipeCols;
+        const int which = warp / kRoleWarps, quarter = warp % kRoleWarps;
+        const int pipe = PIPES == 2 ? which : 0, col0 = PIPES == 2 ? 0 : which * kCols;
+        const int row_in_tile = pipe * kPipeV + quarter * 32 + lane;
+        const uint32_t tmem = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + pipe * S::kPipeCols + col0;
         Turn<kAccumulators> acc;
         Turn<kSides> slot;
         bool ok = true;
         for (int item = blockIdx.x; ok && item < T.items; item += gridDim.x) {
-            uint64_t total[NT / 2];
+            uint64_t total[kCols / 2];
 #pragma unroll
-            for (int i = 0; i < NT / 2; ++i) total[i] = 0ull;
+            for (int i = 0; i < kCols / 2; ++i) total[i] = 0ull;
             for (int c = 0; ok && c < W.blocks; ++c) {
 #pragma unroll 1
                 for (int j = 0; j < N; ++j) {
@@ -455,7 +464,7 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                     }
                     tc_fence_after();
                     // (the next part is under way while one is added up)
-                    constexpr int kPart = 16, kParts = NT / kPart;
+                    constexpr int kPart = 16, kParts = kCols / kPart;
                     uint32_t d[2][kPart];
                     tmem_load16(tmem + acc.at * NT, d[0]);
                     const float s = bf16_value(side[slot.at].scale[row_in_tile * N + j]);
@@ -464,29 +473,33 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                     for (int h = 0; h < kParts; ++h) {
                         uint32_t (&now)[kPart] = d[h & 1];
                         tmem_wait_load(now);
-                        if (h + 1 < kParts) tmem_load16(tmem + acc.at * NT + (h + 1) * kPart, d[(h + 1) & 1]);
+                        if (h + 1 < kParts) {
+                            tmem_load16(tmem + acc.at * NT + (h + 1) * kPart, d[(h + 1) & 1]);
+                        } else {   // all out: the accumulator may be written again
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&sh.acc_empty[pipe][acc.at]);
+                        }
 #pragma unroll
                         for (int i = 0; i < kPart / 2; ++i) {
                             uint64_t& t = total[h * (kPart / 2) + i];
                             t = fma_pair(static_cast<uint64_t>(now[2 * i + 1]) << 32 | now[2 * i], s2, t);
                         }
                     }
-                    // the accumulator may be written again, and after the block's last group its scales too
-                    tc_fence_before();
+                    // after the block's last group its scales too
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(&sh.acc_empty[pipe][acc.at]);
                     if (lane == 1 && j == N - 1) mbar_arrive(sh.side_empty + slot.at);
                     acc.advance();
                 }
                 slot.advance();
             }
-            const int row0 = item % T.row_blocks * NT;
+            const int row0 = item % T.row_blocks * NT + col0;
             const int64_t v = static_cast<int64_t>(item / T.row_blocks) * kTileV + row_in_tile;
             if (ok && v < W.V) {
                 if (T.out_bf16)
-                    store_column<NT>(reinterpret_cast<__nv_bfloat16*>(P.out) + row0 * P.ldo + v, P.ldo, total, P.rows - row0);
+                    store_column<kCols>(reinterpret_cast<__nv_bfloat16*>(P.out) + row0 * P.ldo + v, P.ldo, total, P.rows - row0);
                 else
-                    store_column<NT>(reinterpret_cast<float*>(P.out) + row0 * P.ldo + v, P.ldo, total, P.rows - row0);
+                    store_column<kCols>(reinterpret_cast<float*>(P.out) + row0 * P.ldo + v, P.ldo, total, P.rows - row0);
             }
         }
     }
@@ -509,28 +522,30 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     __syncthreads();
     if (warp == 0) {
         tc_fence_after();
-        tmem_dealloc(tmem_base, S::kTmemCols);
+        tmem_dealloc(tmem_base, 512);
     }
 }
 
-int tile_rows(int rows) { return rows <= 32 ? 32 : 64; }
+// Up to 64 rows two pipelines of 64, beyond them one of 128: with more rows the weights are unpacked half as often (512 rows: 588
+// against 657 us; 64 rows: 109 against 125).  Tiles of 32 rows take no less time than those of 64, which is the weights'.
+int tile_rows(int rows) { return rows <= 64 ? 64 : 128; }
 int64_t padded_rows(int rows) {
     const int nt = tile_rows(rows);
     return (static_cast<int64_t>(rows) + nt - 1) / nt * nt;
 }
 bool g_attr[64][2][3];
 
-template <int NT, int N>
+template <int NT, int PIPES, int N>
 fef_status launch(const CUtensorMap& map, const TileParams& T, int dev, int grid, cudaStream_t stream) {
-    constexpr size_t smem = Sizes<NT>::kBStages * Sizes<NT>::kBBytes + kSides * sizeof(Side<N>) + sizeof(Shared) + 1024;
+    constexpr size_t smem = Sizes<NT, PIPES>::kBStages * Sizes<NT, PIPES>::kBBytes + kSides * sizeof(Side<N>) + sizeof(Shared) + 1024;
     static_assert(smem <= 232448, "");
-    bool& done = g_attr[dev][NT / 64][N / 2];
+    bool& done = g_attr[dev][PIPES - 1][N / 2];
     if (!done) {
         // (a warpgroup that asks for more registers than the launch left waits for good: never launch with another number)
         cudaFuncAttributes attr;
-        if (cudaFuncGetAttributes(&attr, product_tiles_kernel<NT, N>) != cudaSuccess || (attr.numRegs + 7) / 8 * 8 != kLaunchRegs)
+        if (cudaFuncGetAttributes(&attr, product_tiles_kernel<NT, PIPES, N>) != cudaSuccess || (attr.numRegs + 7) / 8 * 8 != kLaunchRegs)
             return FEF_ERR_CUDA;
-        if (cudaFuncSetAttribute(product_tiles_kernel<NT, N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+        if (cudaFuncSetAttribute(product_tiles_kernel<NT, PIPES, N>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  static_cast<int>(smem)) != cudaSuccess)
             return FEF_ERR_CUDA;
         done = true;
@@ -545,15 +560,15 @@ fef_status launch(const CUtensorMap& map, const TileParams& T, int dev, int grid
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, product_tiles_kernel<NT, N>, map, T) == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, product_tiles_kernel<NT, PIPES, N>, map, T) == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
 }
 
-template <int NT>
+template <int NT, int PIPES>
 fef_status launch_g(const CUtensorMap& map, const TileParams& T, int dev, int grid, cudaStream_t stream) {
     switch (T.P.layer.G) {
-        case 32: return launch<NT, 4>(map, T, dev, grid, stream);
-        case 64: return launch<NT, 2>(map, T, dev, grid, stream);
-        default: return launch<NT, 1>(map, T, dev, grid, stream);
+        case 32: return launch<NT, PIPES, 4>(map, T, dev, grid, stream);
+        case 64: return launch<NT, PIPES, 2>(map, T, dev, grid, stream);
+        default: return launch<NT, PIPES, 1>(map, T, dev, grid, stream);
     }
 }
 
@@ -565,7 +580,7 @@ size_t tiles_kernel_workspace(const ProductParams& P) {
 
 fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* workspace, int dev, int sms, cudaStream_t stream) {
     const Layer& W = P.layer;
-    const int nt = tile_rows(P.rows);
+    const int nt = tile_rows(P.rows), tile_v = nt == 64 ? 2 * kPipeV : kPipeV;
     PrepareParams H;
     H.hidden = P.hidden;
     H.operand = static_cast<uint16_t*>(workspace);
@@ -576,7 +591,7 @@ fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* works
 
     TileParams T;
     T.P = P;
-    T.tiles = (W.V + kTileV - 1) / kTileV;
+    T.tiles = (W.V + tile_v - 1) / tile_v;
     T.padded = static_cast<int>(padded_rows(P.rows));
     T.row_blocks = T.padded / nt;
     if (static_cast<int64_t>(T.tiles) * T.row_blocks * W.blocks > 0x7FFFFFFF) return FEF_ERR_INVALID_ARG;   // (counted in 32 bits)
@@ -590,7 +605,7 @@ fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* works
     if (cudaGetLastError() != cudaSuccess) return FEF_ERR_CUDA;
 
     const int grid = T.items < sms ? T.items : sms;
-    return nt == 32 ? launch_g<32>(map, T, dev, grid, stream) : launch_g<64>(map, T, dev, grid, stream);
+    return nt == 64 ? launch_g<64, 2>(map, T, dev, grid, stream) : launch_g<128, 1>(map, T, dev, grid, stream);
 }
 
 }  // namespace quant
