@@ -492,9 +492,10 @@ fef_status fef_lmhead_logits(const void* hidden, const void* weight, int rows, i
  *   device_status  device out, [1] int32, or NULL: FEF_OK, or FEF_ERR_TIMEOUT as in fef_spec_verify (the logits are then
  *            incomplete)
  *   workspace  device scratch of fef_lmhead_logits_quantized_workspace_bytes(rows, V, d, group) bytes, 256-byte aligned, contents
- *            need not be initialised (it takes the hidden rows in the matrix instructions' order); not used for few rows
- * A row of hidden states that holds NaN or an infinity has logits that are no numbers (NaN, or an infinity where only one
- * product is one); other rows are not affected.
+ *            need not be initialised (it takes the hidden rows in the matrix instructions' order); not used for few rows.  Two
+ *            calls that may overlap on the GPU need separate ones
+ * A row of hidden states that holds NaN or an infinity has logits that are no numbers (NaN or infinite); other rows are not
+ * affected.  For few rows the sums are kept 2^-33 times smaller: scales below 2^-80 begin to lose accuracy there.
  * Asynchronous on `cuda_stream`; one kernel for few rows (up to 16), otherwise two.
  */
 fef_status fef_lmhead_quantize(const void* weight, int V, int d, int group, void* packed, void* scale, void* zero,
@@ -527,7 +528,8 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
  *   draft_tokens   device, [B, K] int32, or NULL: the window's drafts, for the target law (the draft law of a
  *                  position does not depend on them); entries outside [0, V) are not counted
  *   row_len        device, [B] int32 in [0, K], or NULL = K everywhere
- *   penalties      device, [B, 3] float32 (rep > 0, freq, pres), or NULL = none (the text is then not read)
+ *   penalties      device, [B, 3] float32 (rep > 0 with a reciprocal that is a number, freq, pres), or NULL = none (the
+ *                  text is then not read)
  *   bias           device float32, V entries for window b at bias + b * bias_stride, or NULL; stride 0 shares them
  *   allowed        device, ceil(V / 32) words for (b, i) at allowed + b * allowed_stride_b + i * allowed_stride_k
  *                  (strides in words, 0 shares), bit x & 31 of word x >> 5 belongs to id x; or NULL = all allowed
@@ -536,7 +538,7 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
  *                  as it is stored: what fef_spec_verify_with_norms takes.  NaN where the adjusted row holds NaN or
  *                  +inf or no finite entry (a mask that leaves nothing); 0 for i >= n_b
  *   workspace      device scratch of fef_logits_adjust_workspace_bytes(B, K, V) bytes, 256-byte aligned, contents need
- *                  not be initialised; needed with log2_norm only
+ *                  not be initialised; needed with log2_norm only.  Two calls that may overlap need separate ones
  * A masked id is -inf whatever its logit, NaN and infinities among them.  Asynchronous on `cuda_stream`; one kernel, and a
  * second, small one with log2_norm.
  */

@@ -129,10 +129,10 @@ __device__ __forceinline__ Row8<DT> pack8(float (&l)[8], uint32_t allowed) {
     return r;
 }
 
-// l / rep for l > 0, l * rep otherwise; `inv` = 1 / rep.  The quotient takes one correction step (an infinite l skips it).
+// l / rep for l > 0, l * rep otherwise; `inv` = 1 / rep.  The quotient takes one correction step (an infinite one skips it).
 __device__ __forceinline__ float repeat_penalty(float l, float rep, float inv) {
     const float q = l * inv, fixed = fmaf(fmaf(-q, rep, l), inv, q);
-    return l > 0.f ? (l < INFINITY ? fixed : q) : l * rep;
+    return l > 0.f ? (q < INFINITY ? fixed : q) : l * rep;
 }
 
 template <int DT, bool NORM>

@@ -33,6 +33,7 @@ namespace {
 
 constexpr int kPipeV = 128;                   // vocabulary rows of a pipeline
 constexpr int kACols = kBlock / 2;            // 32-bit columns of a block of unpacked weights in tensor memory
+constexpr int kMaxBStages = 6;                // ring of the hidden rows
 constexpr int kSides = 4;                     // ring of the blocks' scales
 constexpr int kRoleWarps = 4;                 // warps that share a pipeline's rows
 constexpr int kThreads = (4 * kRoleWarps + 4) * 32;   // the last four warps: TMA, up to two issuers, idle
@@ -53,6 +54,7 @@ struct Sizes {
     static constexpr int kTileV = PIPES * kPipeV, kTeams = 2 / PIPES, kCols = NT / kTeams;
     static_assert(kCols == 64, "");   // the registers' shares below are for 64 columns per thread of the epilogue
     static constexpr int kBBytes = NT * kBlock * 2, kBStages = NT == 128 ? 5 : 6;
+    static_assert(kBStages <= kMaxBStages, "");
     // tensor memory of a pipeline: accumulators, then weights
     static constexpr int kAStages = PIPES == 2 ? 2 : 4;
     static constexpr int kPipeCols = 512 / PIPES, kAccumulators = 2;
@@ -69,8 +71,8 @@ struct Shared {
     uint64_t a_empty[2][4];
     uint64_t acc_full[2][4];
     uint64_t acc_empty[2][4];
-    uint64_t b_full[6];
-    uint64_t b_empty[6];
+    uint64_t b_full[kMaxBStages];
+    uint64_t b_empty[kMaxBStages];
     uint64_t side_full[kSides];
     uint64_t side_empty[kSides];
     uint64_t drained;
@@ -103,7 +105,7 @@ __global__ void __launch_bounds__(kPrepareThreads) prepare_kernel(const __grid_c
 // ------------------------------------------------------------------------------------------- tiles ----
 // A bounded wait that reads no clock as long as it is short (the hand-overs between warps set this kernel's pace).
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatile int* abort_flag) {
-    for (int poll = 0; poll < 4; ++poll)
+    for (int poll = 0; poll < 32; ++poll)
         if (mbar_try_wait(bar, parity)) return true;
     return mbar_wait_bounded(bar, parity, abort_flag, kWaitNs);
 }

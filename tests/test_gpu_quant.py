@@ -179,6 +179,32 @@ def test_values_that_are_not_numbers_stay_in_their_rows(fef, rows):
     assert torch.equal(dirty[:, :700][:, other], base[:, :700][:, other]) and torch.isnan(dirty[:, 5]).all()
 
 
+@pytest.mark.parametrize("rows", [8, 16, 40, 150])
+def test_rows_of_any_magnitude(fef, rows):
+    """A row's power of two passes through exactly: products and sums are binary32 numbers far from its limits."""
+    layer, g = _layer(fef, 333, 384, 64, True, seed=3)
+    hidden = torch.randn((rows, 384), generator=g, device="cuda").to(torch.bfloat16)
+    base, _ = fef.fef_lmhead_logits_quantized(hidden, layer)
+    powers = torch.tensor([0, 90, -60, 26, 30, -81, 60, -100], dtype=torch.float64, device="cuda").repeat((rows + 7) // 8)[:rows]
+    scaled = (hidden.double() * torch.exp2(powers)[:, None]).to(torch.bfloat16)
+    scaled[rows - 1] = 0.0
+    got, _ = fef.fef_lmhead_logits_quantized(scaled, layer)
+    want = base.double() * torch.exp2(powers)[:, None]
+    want[rows - 1] = 0.0
+    torch.cuda.synchronize()
+    V = 333
+    assert torch.equal(got[:, :V].double(), want[:, :V].float().double())
+    # one value of another order of magnitude, an infinity in a row of its own
+    scaled[2, 5], scaled[3, 7] = 1e20, math.inf
+    got, _ = fef.fef_lmhead_logits_quantized(scaled, layer)
+    ref = scaled[2].double() @ fef.fef_lmhead_dequantize(layer).double().T
+    assert torch.allclose(got[2, :V].double(), ref, rtol=2e-6, atol=float(ref.abs().max()) * 2e-6)
+    assert not torch.isfinite(got[3, :V]).any()
+    keep = torch.ones(rows, dtype=torch.bool, device="cuda")
+    keep[2:4] = False
+    assert torch.equal(got[keep][:, :V].double(), want[keep][:, :V].float().double())
+
+
 @pytest.mark.parametrize("rows", [1, 20])
 def test_offsets_beyond_32_bits(fef, rows):
     V, d = 300000, 16384                                     # 2.5 GB of nibbles, 9.8 GB of weights
@@ -193,6 +219,30 @@ def test_offsets_beyond_32_bits(fef, rows):
     ref, _ = fef.fef_lmhead_logits_quantized(hidden, last)
     torch.cuda.synchronize()
     assert torch.allclose(got[:, V - 1], ref[:, 0], rtol=1e-4, atol=1e-3) and (got[:, :V - 1] == 0).all()
+
+
+def test_two_streams_and_graphs_at_once(fef):
+    """Calls that overlap, each with scratch of its own: eager ones on two streams, two captured ones replayed together."""
+    layer, g = _layer(fef, 20011, 1024, 128, False, seed=12)
+    inputs = [torch.randn((rows, 1024), generator=g, device="cuda").to(torch.bfloat16) for rows in (12, 90, 70, 16)]
+    alone = [fef.fef_lmhead_logits_quantized(h, layer)[0].clone() for h in inputs]
+    outs = [torch.zeros_like(a) for a in alone]
+    graphs = []
+    for h, out in zip(inputs, outs):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            fef.fef_lmhead_logits_quantized(h, layer, out=out)
+        graphs.append(graph)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in inputs]
+    for _ in range(5):
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        eager = [fef.fef_lmhead_logits_quantized(h, layer, stream=s)[0] for h, s in zip(inputs, streams)]
+        torch.cuda.synchronize()
+        for a, out, e in zip(alone, outs, eager):
+            assert torch.equal(a[:, :20011], out[:, :20011]) and torch.equal(a[:, :20011], e[:, :20011])
 
 
 def test_refusals(fef):
@@ -218,5 +268,10 @@ def test_refusals(fef):
             fef.fef_lmhead_logits_quantized(h, layer, **kw)
     with pytest.raises(fef.FefError):
         fef.fef_lmhead_dequantize(layer, out=torch.zeros((40, 64), device="cuda"))
+    many = torch.zeros((40, 128), dtype=torch.bfloat16, device="cuda")
+    need = fef.fef_lmhead_logits_quantized_workspace_bytes(40, 40, 128, 64)
+    with pytest.raises(fef.FefError):
+        fef.fef_lmhead_logits_quantized(many, layer, workspace=torch.zeros(need - 1, dtype=torch.uint8, device="cuda"))
+    fef.fef_lmhead_logits_quantized(many, layer, workspace=torch.zeros(need, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         fef.fef_lmhead_logits_quantized(hidden, layer._replace(packed=layer.packed.cpu()))
