@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import os
 from typing import NamedTuple, Optional
 
@@ -780,6 +781,7 @@ def fef_lmhead_dequantize(layer: QuantizedLayer, out: Optional[torch.Tensor] = N
     return out
 
 
+@functools.lru_cache(maxsize=256)   # (a function of the sizes alone)
 def fef_lmhead_logits_quantized_workspace_bytes(rows: int, V: int, d: int, group: int) -> int:
     return int(load().fef_lmhead_logits_quantized_workspace_bytes(rows, V, d, group))
 
@@ -829,6 +831,7 @@ class AdjustResult(NamedTuple):
     log2_norm: Optional[torch.Tensor]   # [B, K] float64, when asked for
 
 
+@functools.lru_cache(maxsize=256)   # (a function of the sizes alone)
 def fef_logits_adjust_workspace_bytes(B: int, K: int, V: int) -> int:
     return int(load().fef_logits_adjust_workspace_bytes(B, K, V))
 
@@ -910,3 +913,8 @@ def fef_logits_adjust(logits: torch.Tensor, tokens: Optional[torch.Tensor] = Non
 
 def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
+
+
+__all__ += ["QuantizedLayer", "fef_lmhead_quantize", "fef_lmhead_dequantize", "fef_lmhead_logits_quantized",
+            "fef_lmhead_logits_quantized_workspace_bytes", "AdjustResult", "fef_logits_adjust",
+            "fef_logits_adjust_workspace_bytes"]
