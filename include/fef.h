@@ -528,8 +528,8 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
  *   draft_tokens   device, [B, K] int32, or NULL: the window's drafts, for the target law (the draft law of a
  *                  position does not depend on them); entries outside [0, V) are not counted
  *   row_len        device, [B] int32 in [0, K], or NULL = K everywhere
- *   penalties      device, [B, 3] float32 (rep > 0 with a reciprocal that is a number, freq, pres), or NULL = none (the
- *                  text is then not read)
+ *   penalties      device, [B, 3] float32 (rep > 0, it and its reciprocal finite; freq; pres), or NULL = none (the text is
+ *                  then not read)
  *   bias           device float32, V entries for window b at bias + b * bias_stride, or NULL; stride 0 shares them
  *   allowed        device, ceil(V / 32) words for (b, i) at allowed + b * allowed_stride_b + i * allowed_stride_k
  *                  (strides in words, 0 shares), bit x & 31 of word x >> 5 belongs to id x; or NULL = all allowed

@@ -281,3 +281,46 @@ def test_refusals(fef):
     with pytest.raises(ValueError):
         fef.fef_logits_adjust(c["logits"], tokens=c["tokens"].cpu())
     fef.fef_logits_adjust(c["logits"], **args)              # and the call itself is fine
+
+
+@pytest.mark.parametrize("dtype,ld", [(torch.float32, 4), (torch.bfloat16, 8)])
+def test_the_largest_batch(fef, dtype, ld):
+    B, V = 65535, 3
+    logits = torch.randn((B, 1, ld), device="cuda").to(dtype)
+    bias = torch.randint(-8, 9, (B, V), device="cuda").float()
+    allowed = (torch.arange(B, device="cuda", dtype=torch.int32) % 7 + 1)[:, None]
+    r = fef.fef_logits_adjust(logits, bias=bias, allowed=allowed, V=V, with_norm=True)
+    want = (logits[:, 0, :V].float() + bias).to(dtype)
+    want[(allowed >> torch.arange(V, device="cuda")) & 1 == 0] = -math.inf
+    assert torch.equal(r.logits[:, 0, :V], want)
+    ref, tol = _norm_reference(want.cpu(), 1.0)
+    assert ((r.log2_norm[:, 0].cpu() - ref).abs() <= tol).all()
+
+
+def test_the_longest_text(fef):
+    L = 1 << 24
+    tokens = torch.full((1, L), 5, dtype=torch.int32, device="cuda")
+    tokens[0, 0] = 2
+    pen = torch.tensor([[2.0, 2.0 ** -24, 0.5]], device="cuda")
+    logits = torch.ones((1, 3, 8), device="cuda")
+    r = fef.fef_logits_adjust(logits, tokens=tokens, prompt_len=torch.tensor([L // 2], dtype=torch.int32, device="cuda"),
+                              draft_tokens=torch.tensor([[2, 5, 7]], dtype=torch.int32, device="cuda"), penalties=pen)
+    want = torch.ones((3, 8))
+    want[:, 2], want[:, 5] = 0.5, 0.5 - (0.5 + 0.5)
+    want[1:, 2] = 0.5 - (2.0 ** -24 + 0.5)
+    # (position 2, id 5: freq a + pres = 1 + 2^-24 lies between two numbers of binary32 and goes to the even one, 1)
+    torch.cuda.synchronize()
+    assert torch.equal(r.logits[0].cpu(), want)
+
+
+def test_calls_on_two_streams_at_once(fef):
+    cases = [_case(8, 32, 50001, 300, torch.bfloat16, seed=21), _case(8, 16, 50001, 700, torch.float32, seed=22)]
+    args = [{k: v for k, v in c.items() if k != "logits"} for c in cases]
+    alone = [fef.fef_logits_adjust(c["logits"], with_norm=True, **a) for c, a in zip(cases, args)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        both = [fef.fef_logits_adjust(c["logits"], with_norm=True, stream=s, **a) for c, a, s in zip(cases, args, streams)]
+        torch.cuda.synchronize()
+        for x, y in zip(alone, both):
+            assert torch.equal(x.logits[..., :50001], y.logits[..., :50001]) and torch.equal(x.log2_norm, y.log2_norm)

@@ -275,3 +275,68 @@ def test_refusals(fef):
     fef.fef_lmhead_logits_quantized(many, layer, workspace=torch.zeros(need, dtype=torch.uint8, device="cuda"))
     with pytest.raises(ValueError):
         fef.fef_lmhead_logits_quantized(hidden, layer._replace(packed=layer.packed.cpu()))
+
+
+@pytest.mark.parametrize("rows,V,d,group", [
+    (8, 100, 12544, 128), (8, 100, 12672, 128),              # the hidden rows just fit one SM's shared memory, and do not
+    (16, 100, 5760, 64), (16, 100, 5888, 64),
+    (1, 33, 1 << 20, 32), (20, 33, 1 << 20, 128),            # the longest rows
+    (70001, 40, 32, 32),                                     # many
+])
+def test_product_at_the_ends_of_its_ranges(fef, rows, V, d, group):
+    layer, g = _layer(fef, V, d, group, True, seed=rows)
+    hidden = torch.randn((rows, d), generator=g, device="cuda").to(torch.bfloat16)
+    _check_product(fef, layer, hidden, torch.float32)
+
+
+def test_quantize_beyond_32_bits(fef):
+    V, d = 300001, 16384                                     # 9.8 GB of weights, 19.7 GB of values
+    w = torch.zeros((V, d), dtype=torch.bfloat16, device="cuda")
+    w[-1] = torch.randn(d, device="cuda").to(torch.bfloat16)
+    alone = fef.fef_lmhead_quantize(w[-1:].contiguous(), 64, True)
+    layer = fef.fef_lmhead_quantize(w, 64, True)
+    del w
+    assert int(layer.device_status.item()) == 0
+    assert torch.equal(layer.packed[-1], alone.packed[0]) and torch.equal(layer.scale[:, V - 1], alone.scale[:, 0])
+    values = fef.fef_lmhead_dequantize(layer)
+    assert torch.equal(values[-1], fef.fef_lmhead_dequantize(alone)[0]) and not values[:-1].any()
+
+
+FIRST_CALLS = """
+import torch
+import paper_2605_14305_b200 as fef
+
+fef.load()
+g = torch.Generator(device="cuda").manual_seed(1)
+w = torch.randn((1003, 256), generator=g, device="cuda").to(torch.bfloat16)
+hidden = [torch.randn((rows, 256), generator=g, device="cuda").to(torch.bfloat16) for rows in (4, 40, 140)]
+bias = torch.randn(1003, generator=g, device="cuda")
+
+def chain():
+    layer = fef.fef_lmhead_quantize(w, 64, True)
+    out = [fef.fef_lmhead_dequantize(layer)]
+    for h in hidden:
+        logits = fef.fef_lmhead_logits_quantized(h, layer)[0]
+        out += list(fef.fef_logits_adjust(logits.view(4, -1, logits.shape[-1]), bias=bias, V=1003, with_norm=True))
+    return out
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    captured = chain()
+graph.replay()
+eager = chain()
+torch.cuda.synchronize()
+for a, b in zip(captured, eager):
+    a, b = (x[..., :1003] if x.dim() == 3 else x for x in (a, b))
+    assert torch.equal(a, b) and torch.isfinite(a).all()
+"""
+
+
+def test_first_calls_of_a_process_captured(fef):
+    """Nothing has to have run before a capture."""
+    import subprocess
+    import sys
+
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
