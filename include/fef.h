@@ -495,7 +495,7 @@ fef_status fef_lmhead_logits(const void* hidden, const void* weight, int rows, i
  *            need not be initialised (it takes the hidden rows in the matrix instructions' order); not used for few rows.  Two
  *            calls that may overlap on the GPU need separate ones
  * A row of hidden states that holds NaN or an infinity has logits that are no numbers (NaN or infinite); other rows are not
- * affected.  For few rows the sums are kept 2^-33 times smaller: scales below 2^-80 begin to lose accuracy there.
+ * affected, and a weight with q = z adds exactly zero to a row of finite ones, however large its hidden state is.
  * Asynchronous on `cuda_stream`; one kernel for few rows (up to 16), otherwise two.
  */
 fef_status fef_lmhead_quantize(const void* weight, int V, int d, int group, void* packed, void* scale, void* zero,

@@ -42,17 +42,8 @@ struct ProductParams {
 
 __device__ __forceinline__ float bf16_value(uint32_t h) { return __uint_as_float(h << 16); }
 
-// A nibble becomes a bfloat16 number by masking alone: the bit pattern v < 256 in the lower half of a bfloat16 (the mantissa
-// and the lowest exponent bit) is the number v 2^-133, below and above the smallest normal number alike.  So the nibbles at
-// bits 0..3 of each half of a word (columns 0 and 4 of its eight; after a shift by 8: 2 and 6) stand for q 2^-133, and those at
-// bits 4..7 (1 and 5; 3 and 7) for 16 q 2^-133: two masks, one shift, two masks for eight weights.  The other operand is
-// scaled by a power of two that keeps the products in binary32's normal range, a further 1/16 for the columns of the upper
-// nibbles; all of this is exact, and the inverse is applied to the logits.
-constexpr uint32_t kLowNibbles = 0x000F000Fu, kHighNibbles = 0x00F000F0u;
-constexpr int kUsualShift = 100;
-
-// The numbers q - z of such a pair (after shifts by 0, 4, 8, 12), exact: 0x4300 | q is 128 + q in bfloat16, `centre` holds 128 + z
-// twice.  Three more instructions for four weights, and nothing left to correct.
+// The numbers q - z of the nibbles at bits 0..3 of a word's two halves (columns 0 and 4 of its eight; after shifts by 4, 8 and
+// 12: 1 and 5, 2 and 6, 3 and 7), exact: 0x4300 | q is 128 + q in bfloat16, `centre` holds 128 + z twice.
 __device__ __forceinline__ uint32_t centred_pair(uint32_t word, uint32_t centre) {
     uint32_t x, r;
     asm("lop3.b32 %0, %1, 0x000F000F, 0x43004300, 0xEA;" : "=r"(x) : "r"(word));  // (word & mask) | 128, 128
@@ -61,14 +52,6 @@ __device__ __forceinline__ uint32_t centred_pair(uint32_t word, uint32_t centre)
 }
 __device__ __forceinline__ uint32_t centre_of(uint32_t z) { return 0x43004300u | z | z << 16; }
 
-// The power of two a hidden row is scaled by, from the bfloat16 bits of its largest value: 2^100, or, for a row with values
-// beyond 2^27 or with none above 2^-80, the one that brings its largest value near 2^126.  (An exponent of 255: the row holds
-// NaN or an infinity, its logits are no numbers anyway.)
-__device__ __forceinline__ int row_shift(uint32_t largest) {
-    const int e = static_cast<int>(largest >> 7);   // biased
-    return largest == 0u || (e >= 47 && e < 154) || e == 255 ? kUsualShift : 253 - e;
-}
-__device__ __forceinline__ float exp2_int(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }  // |e| < 127
 __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);

@@ -6,10 +6,10 @@
 // their four words two k-steps.  In the same way operand row g of the i-th eight rows of a unit of 32 is vocabulary row
 // 4 g + i: a lane's four scales lie together, and so do its four logits of a hidden row.
 //
-// Nibbles become bfloat16 numbers by masking alone, the hidden rows are scaled to suit (fef_quant.cuh).  The zero points are
-// taken off the group's sum: sum (q - z) x = sum q x - z sum x, which costs two bits of the binary32 sum's accuracy (addends of
-// 8.8 in the root mean square of their weights instead of 2.6).  The products of a group are added up in binary32 by the
-// matrix instructions, then scaled in binary32.
+// Nibbles become the bfloat16 numbers (q - z) / 64 before they are multiplied, nine instructions for eight weights (low_pair below).
+// Masking alone would be five, with the zero points taken off the group's sum, sum q x - z sum x; but then a large x loses the
+// group's other products even where q = z, without a bound (logits off by 2e-3 at one channel of 1e5 in 4096).  The products of
+// a group are added up in binary32 by the matrix instructions, then scaled in binary32; the 64 comes back with the logits.
 //
 // One CTA of 16 warps per SM takes an even share of the vocabulary in units of 32 rows; all blocks of its units in a row are
 // cut into 16 equal runs, one per warp, so that all end together.  A unit that lies in more than one run is joined at the
@@ -34,14 +34,14 @@ constexpr size_t kSmemLimit = 232448;
 
 struct Plan {
     int units;    // of the whole vocabulary
-    size_t smem;  // hidden rows, their groups' sums, one place per warp for the sums of a shared unit; 0: not for this kernel
+    size_t smem;  // hidden rows, one place per warp for the sums of a shared unit; 0: not for this kernel
 };
 
 Plan make_plan(const ProductParams& P) {
     Plan L = {};
     const int nt = P.rows > 8 ? 2 : 1;
     L.units = (P.layer.V + kUnit - 1) / kUnit;
-    const size_t smem = static_cast<size_t>(P.layer.blocks) * (2048 + 128) * nt + kWarps * 1024 * nt;
+    const size_t smem = static_cast<size_t>(P.layer.blocks) * 2048 * nt + kWarps * 1024 * nt;
     L.smem = smem <= kSmemLimit - 1024 ? smem : 0;
     return L;
 }
@@ -59,12 +59,28 @@ __device__ __forceinline__ void mma_16816_first(float (&d)[4], uint32_t a0, uint
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// Two bfloat16 numbers times a power of two, given by its bits.
-__device__ __forceinline__ uint32_t times(uint32_t x, uint32_t power) {
+// Two nibbles of a word, less their zero points: a nibble becomes a bfloat16 number by masking alone, since the bit pattern v < 256 in
+// the lower half of a bfloat16 (the mantissa and the lowest exponent bit) is the number v 2^-133, below and above the smallest
+// normal number alike.  Bits 0..3 of each half of a word (columns 0 and 4 of its eight; after a shift by 8: 2 and 6) stand for
+// q 2^-133, bits 4..7 (1 and 5; 3 and 7) for 16 q 2^-133; one fused multiply-add takes either to (q - z) 2^-6, exactly.  The
+// form with 128 + q (centred_pair) needs two more shifts, and the pipe of shifts and masks is the busiest: 54 against 51 us at 1 row x
+// 126464 x 4096, 67 against 59 us at 8 rows x 152064 x 3584 in groups of 64 with zero points.
+__device__ __forceinline__ uint32_t fma_bf16_pair(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t r;
-    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(power | power << 16));
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
+__device__ __forceinline__ uint32_t low_pair(uint32_t word, uint32_t centre) {
+    return fma_bf16_pair(word & 0x000F000Fu, 0x7F007F00u, centre);   // 2^127
+}
+__device__ __forceinline__ uint32_t high_pair(uint32_t word, uint32_t centre) {
+    return fma_bf16_pair(word & 0x00F000F0u, 0x7D007D00u, centre);   // 2^123
+}
+// -z / 64 twice, from byte `i` of a word of zero points.
+__device__ __forceinline__ uint32_t centre_of_byte(uint32_t z, int i) {
+    return fma_bf16_pair(__byte_perm(z, 0u, 0x4040u + 0x0101u * i), 0xFF00FF00u, 0u);   // -2^127
+}
+constexpr uint32_t kCentre8 = 0xBE00BE00u;   // -8 / 64
 
 // What a warp needs of one block of its unit: operand rows 4 g + i, their scales and zero points.
 template <int N, bool ZERO>
@@ -73,8 +89,8 @@ struct Fetched {
     uint32_t s[2 * N];          // 4 rows x N groups, two to a word
     uint32_t z[ZERO ? N : 1];   // ..., four to a word
     __device__ __forceinline__ uint32_t scale(int i, int j) const { return s[(i * N + j) / 2] >> (16 * ((i * N + j) & 1)) & 0xFFFFu; }
-    __device__ __forceinline__ float zero(int i, int j) const {
-        return ZERO ? static_cast<float>(z[(i * N + j) / 4] >> (8 * ((i * N + j) & 3)) & 0xFFu) : 8.f;
+    __device__ __forceinline__ uint32_t centre(int i, int j) const {
+        return ZERO ? centre_of_byte(z[(i * N + j) / 4], (i * N + j) & 3) : kCentre8;
     }
 };
 
@@ -82,7 +98,6 @@ template <int NT, int N, bool ZERO>   // 8 NT hidden rows, N groups per block
 __global__ void __launch_bounds__(kThreads, 1)
 product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ Plan L, int out_bf16) {
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ uint32_t s_largest[16];   // of each hidden row
     constexpr int kAhead = NT == 1 ? 3 : 2;
     const Layer& W = P.layer;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -142,82 +157,27 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fetch(ahead[i]);
 
-    // ---- hidden rows into operand order, scaled: 16 bytes per (block, word, row, t), columns 0 4, 1 5, 2 6, 3 7 of the
-    //      eight; behind them the sums of each group
+    // ---- hidden rows into operand order: 16 bytes per (block, word, row, t), columns 0 4, 1 5, 2 6, 3 7 of the eight
     constexpr int kPieces = 32 * NT;   // 16-byte pieces per block and word
     const int pieces = W.blocks * 4 * kPieces;
-    float* sums = reinterpret_cast<float*>(smem + pieces * 16);
-    if (threadIdx.x < 16) s_largest[threadIdx.x] = 0u;
-    __syncthreads();
-    auto piece = [&](int at, int& row) {   // one row's eight columns as they are
-        const int cw = at / kPieces, k = (cw >> 2) * kBlock + (cw & 3) * 32 + (at & 3) * 8;
-        row = at / 4 % (8 * NT);
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (at < pieces && row < P.rows && k < W.d)
-            x = __ldg(reinterpret_cast<const uint4*>(P.hidden + static_cast<int64_t>(row) * W.d + k));
-        return x;
-    };
-    auto group_sum = [&](int at, float total) {   // (whole warps: the pieces are a multiple of 32)
-        total += __shfl_xor_sync(0xFFFFFFFFu, total, 1);
-        total += __shfl_xor_sync(0xFFFFFFFFu, total, 2);
-        if ((at & 3) == 0) sums[at / 4] = total;
-    };
     for (int at0 = threadIdx.x; at0 < pieces; at0 += 4 * kThreads) {
         uint4 x[4];
-        int row[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x[u] = piece(at0 + u * kThreads, row[u]);   // (four loads in flight)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int at = at0 + u * kThreads;
-            if (at >= pieces) break;
-            uint4 y;
-            y.x = times(__byte_perm(x[u].x, x[u].z, 0x5410), 0x7180u);   // 2^100
-            y.y = times(__byte_perm(x[u].x, x[u].z, 0x7632), 0x6F80u);   // 2^96
-            y.z = times(__byte_perm(x[u].y, x[u].w, 0x5410), 0x7180u);
-            y.w = times(__byte_perm(x[u].y, x[u].w, 0x7632), 0x6F80u);
-            *reinterpret_cast<uint4*>(smem + at * 16) = y;
-            float v[8];
-            unpack<FEF_BF16>(x[u], v);
-            group_sum(at, (((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]))) * exp2_int(kUsualShift - 133));
-            const uint32_t top = __vmaxu2(__vmaxu2(x[u].x & 0x7FFF7FFFu, x[u].y & 0x7FFF7FFFu),
-                                          __vmaxu2(x[u].z & 0x7FFF7FFFu, x[u].w & 0x7FFF7FFFu));
-            if (top != 0u) atomicMax(&s_largest[row[u]], max(top & 0xFFFFu, top >> 16));
+        for (int u = 0; u < 4; ++u) {   // (four loads in flight)
+            const int at = at0 + u * kThreads, cw = at / kPieces, k = (cw >> 2) * kBlock + (cw & 3) * 32 + (at & 3) * 8;
+            const int row = at / 4 % (8 * NT);
+            x[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (at < pieces && row < P.rows && k < W.d)
+                x[u] = __ldg(reinterpret_cast<const uint4*>(P.hidden + static_cast<int64_t>(row) * W.d + k));
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (at0 + u * kThreads < pieces)
+                *reinterpret_cast<uint4*>(smem + (at0 + u * kThreads) * 16) =
+                    make_uint4(__byte_perm(x[u].x, x[u].z, 0x5410), __byte_perm(x[u].x, x[u].z, 0x7632),
+                               __byte_perm(x[u].y, x[u].w, 0x5410), __byte_perm(x[u].y, x[u].w, 0x7632));
     }
     __syncthreads();
-    bool usual = true;
-#pragma unroll
-    for (int r = 0; r < 8 * NT; ++r) usual = usual && row_shift(s_largest[r]) == kUsualShift;
-    if (!usual) {   // some row's values are out of the ordinary: all again, each row with its own power of two
-        for (int at = threadIdx.x; at < pieces; at += kThreads) {
-            int row;
-            const uint4 x = piece(at, row);
-            const int shift = row_shift(s_largest[row]);
-            float v[8], total = 0.f;
-            unpack<FEF_BF16>(x, v);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                v[j] = v[j] * exp2_int(shift / 2) * exp2_int(shift - shift / 2);
-                total += v[j] * exp2_int(-67) * exp2_int(-66);
-            }
-            *reinterpret_cast<uint4*>(smem + at * 16) =
-                make_uint4(bf16_pair(v[0], v[4]), bf16_pair(v[1] * 0.0625f, v[5] * 0.0625f), bf16_pair(v[2], v[6]),
-                           bf16_pair(v[3] * 0.0625f, v[7] * 0.0625f));
-            group_sum(at, total);
-        }
-        __syncthreads();
-    }
-    if constexpr (N < 4) {   // the words of a group, into its first word's place
-        for (int at = threadIdx.x; at < W.blocks * N * 8 * NT; at += kThreads) {
-            float* to = sums + at / (8 * NT) * (4 / N) * (8 * NT) + at % (8 * NT);
-            float total = to[0];
-#pragma unroll
-            for (int w = 1; w < 4 / N; ++w) total += to[w * (8 * NT)];
-            to[0] = total;
-        }
-        __syncthreads();
-    }
 
     // ---- the units
     float acc[2][NT][4];
@@ -234,6 +194,9 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             float sum[2][NT][4];
+            uint32_t centre[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) centre[i] = f.centre(i, j);
 #pragma unroll
             for (int w = j * (4 / N); w < (j + 1) * (4 / N); ++w) {
                 uint4 h[NT];
@@ -244,9 +207,10 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
                     const uint4 &lo = f.q[2 * m], &hi = f.q[2 * m + 1];
                     const uint32_t a = w == 0 ? lo.x : w == 1 ? lo.y : w == 2 ? lo.z : lo.w;
                     const uint32_t b = w == 0 ? hi.x : w == 1 ? hi.y : w == 2 ? hi.z : hi.w;
-                    const uint32_t a0 = a & kLowNibbles, b0 = b & kLowNibbles, a1 = a & kHighNibbles, b1 = b & kHighNibbles;
-                    const uint32_t a2 = a >> 8 & kLowNibbles, b2 = b >> 8 & kLowNibbles;
-                    const uint32_t a3 = a >> 8 & kHighNibbles, b3 = b >> 8 & kHighNibbles;
+                    const uint32_t ca = centre[2 * m], cb = centre[2 * m + 1];
+                    const uint32_t a0 = low_pair(a, ca), b0 = low_pair(b, cb), a1 = high_pair(a, ca), b1 = high_pair(b, cb);
+                    const uint32_t a2 = low_pair(a >> 8, ca), b2 = low_pair(b >> 8, cb);
+                    const uint32_t a3 = high_pair(a >> 8, ca), b3 = high_pair(b >> 8, cb);
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
                         if (w == j * (4 / N))
@@ -257,20 +221,15 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
                     }
                 }
             }
-            float2 x[NT];   // the group's sums of hidden rows 2 t, 2 t + 1
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-                x[n] = *reinterpret_cast<const float2*>(sums + (block * 4 + j * (4 / N)) * 8 * NT + n * 8 + 2 * t);
 #pragma unroll
             for (int m = 0; m < 2; ++m) {
                 const float sa = bf16_value(f.scale(2 * m, j)), sb = bf16_value(f.scale(2 * m + 1, j));
-                const float za = f.zero(2 * m, j), zb = f.zero(2 * m + 1, j);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    acc[m][n][0] = fmaf(fmaf(-za, x[n].x, sum[m][n][0]), sa, acc[m][n][0]);
-                    acc[m][n][1] = fmaf(fmaf(-za, x[n].y, sum[m][n][1]), sa, acc[m][n][1]);
-                    acc[m][n][2] = fmaf(fmaf(-zb, x[n].x, sum[m][n][2]), sb, acc[m][n][2]);
-                    acc[m][n][3] = fmaf(fmaf(-zb, x[n].y, sum[m][n][3]), sb, acc[m][n][3]);
+                    acc[m][n][0] = fmaf(sum[m][n][0], sa, acc[m][n][0]);
+                    acc[m][n][1] = fmaf(sum[m][n][1], sa, acc[m][n][1]);
+                    acc[m][n][2] = fmaf(sum[m][n][2], sb, acc[m][n][2]);
+                    acc[m][n][3] = fmaf(sum[m][n][3], sb, acc[m][n][3]);
                 }
             }
         }
@@ -286,10 +245,7 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
             for (int c = 0; c < 2; ++c) {
                 const int row = n * 8 + 2 * t + c;
                 if (row >= P.rows) continue;
-                const int back = 133 - row_shift(s_largest[row]);
-                const float f0 = exp2_int(back / 2), f1 = exp2_int(back - back / 2);
-                const float y[4] = {acc[0][n][c] * f0 * f1, acc[0][n][2 + c] * f0 * f1, acc[1][n][c] * f0 * f1,
-                                    acc[1][n][2 + c] * f0 * f1};
+                const float y[4] = {acc[0][n][c] * 64.f, acc[0][n][2 + c] * 64.f, acc[1][n][c] * 64.f, acc[1][n][2 + c] * 64.f};
                 const int64_t at = row * P.ldo + v;
                 if (out_bf16) {
                     __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(P.out) + at;
@@ -308,7 +264,7 @@ product_rows_kernel(const __grid_constant__ ProductParams P, const __grid_consta
                 }
             }
     };
-    float4* places = reinterpret_cast<float4*>(smem + W.blocks * (2048 + 128) * NT);   // [warp][2 NT][lane]
+    float4* places = reinterpret_cast<float4*>(smem + W.blocks * 2048 * NT);   // [warp][2 NT][lane]
     if (P.status && blockIdx.x == 0 && threadIdx.x == 0) *P.status = FEF_OK;
     clear();
     int at = begin, unit = unit_begin + begin / W.blocks, block = begin % W.blocks;

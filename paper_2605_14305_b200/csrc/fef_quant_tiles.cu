@@ -16,8 +16,8 @@
 // A block's hand-overs from warp to warp and the instructions of the weights' and the epilogue's warps set the pace (64 rows:
 // 109 us, 1350 cycles for two blocks of 128 x 128 weights, of which the MMAs need 512 and the weights' bytes 660; 512 rows:
 // 588 us = 0.90 PFLOP/s): hence few warps with much to do each, and waits that poll several barriers at once.  The epilogue has most
-// to do, so the weights' warps subtract the zero points (taking them off the groups' sums, as the kernel for few rows does,
-// was 126 us).  Every wait is bounded.
+// to do, so the weights' warps subtract the zero points (taking them off the groups' sums was 126 us, and inexact where a hidden
+// value is large).  Every wait is bounded.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

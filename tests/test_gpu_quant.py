@@ -205,6 +205,61 @@ def test_rows_of_any_magnitude(fef, rows):
     assert torch.equal(got[keep][:, :V].double(), want[keep][:, :V].float().double())
 
 
+@pytest.mark.parametrize("rows", [1, 8, 16, 17, 65])
+@pytest.mark.parametrize("d,group,zero_points", [(384, 64, True), (256, 32, False), (4096, 128, True), (4096, 128, False)])
+def test_outlier_channels_over_weights_of_zero(fef, rows, d, group, zero_points):
+    """Hidden channels far larger than the rest, over columns whose weights are zero (q = z): (q - z) h is exactly zero there, however
+    large h is, so the logits are as exact as without those channels."""
+    V = 700
+    g = torch.Generator(device="cuda").manual_seed(d + rows)
+    w = (torch.randn((V, d), generator=g, device="cuda") + (0.2 if zero_points else 0.0)) * (2.0 / math.sqrt(d))
+    columns = torch.tensor([3, 100, 101, 180, d - 1], device="cuda")
+    w[:, columns] = 0.0
+    layer = fef.fef_lmhead_quantize(w.to(torch.bfloat16), group, zero_points)
+    assert not fef.fef_lmhead_dequantize(layer)[:, columns].any()
+    hidden = torch.randn((rows, d), generator=g, device="cuda")
+    hidden[:, columns] *= torch.tensor([1e3, 1e4, 1e5, 3e6, 1e8], device="cuda")
+    hidden = hidden.to(torch.bfloat16)
+    got = _check_product(fef, layer, hidden, torch.float32)         # (the bound counts |w h|: the outliers add nothing to it)
+    clean = hidden.clone()
+    clean[:, columns] = 0.0
+    assert torch.equal(got[:, :V], _check_product(fef, layer, clean, torch.float32)[:, :V])
+    # nothing but outliers: exact zeros
+    alone = torch.zeros_like(hidden)
+    alone[:, columns] = hidden[:, columns]
+    got, _ = fef.fef_lmhead_logits_quantized(alone, layer)
+    assert not got[:, :V].any()
+
+
+@pytest.mark.parametrize("rows", [1, 8, 16, 17])
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_single_columns_give_the_values_themselves(fef, rows, group):
+    """One hidden value per row: the logits are one column of the layer times it, exactly, for every nibble and zero point."""
+    V, d = 300, 384
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    packed = torch.randint(0, 256, (V, d // 2), generator=g, device="cuda").to(torch.uint8)
+    shape = (d // 128, (V + 31) // 32 * 32, 128 // group)
+    scale = (torch.rand(shape, generator=g, device="cuda") + 0.5).to(torch.bfloat16)
+    zero = torch.randint(0, 16, shape, generator=g, device="cuda").to(torch.uint8)
+    for z in (zero, None):
+        layer = fef.QuantizedLayer(packed, scale, z, d, group)
+        w = fef.fef_lmhead_dequantize(layer).double()
+        for at in range(0, d, rows):
+            hidden = torch.zeros((rows, d), dtype=torch.bfloat16, device="cuda")
+            row = torch.arange(min(rows, d - at), device="cuda")
+            value = torch.exp2((row * 37 + at * 11).double() % 180 - 90)
+            hidden[row, at + row] = value.to(torch.bfloat16)
+            got, _ = fef.fef_lmhead_logits_quantized(hidden, layer)
+            assert torch.equal(got[row, :V].double(), w[:, at + row].T * value[:, None])
+
+
+@pytest.mark.parametrize("rows,d", [(8, 13440), (8, 13568), (1, 13440), (16, 6144), (16, 6272), (9, 6144)])
+def test_product_where_the_hidden_rows_just_fit_shared_memory(fef, rows, d):
+    """... and where they do not."""
+    layer, g = _layer(fef, 100, d, 128, True, seed=d)
+    _check_product(fef, layer, torch.randn((rows, d), generator=g, device="cuda").to(torch.bfloat16), torch.float32)
+
+
 @pytest.mark.parametrize("rows", [1, 20])
 def test_offsets_beyond_32_bits(fef, rows):
     V, d = 300000, 16384                                     # 2.5 GB of nibbles, 9.8 GB of weights
