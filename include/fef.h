@@ -241,7 +241,9 @@ fef_status fef_spec_verify_static(const void* draft_logits, const void* target_l
  *   draft_tokens   device out, [B, K] int32; -1 for i >= n_b and for positions with a data error
  *   log2_norm      device out, [B, K] float64, or NULL: log2 of sum_x 2^(l_x * log2(e) / T), the
  *                  normaliser of rho_i (rho_i(x) = 2^(l_x log2(e) / T - log2_norm)); at T = 0 the
- *                  T = 1 value; 0 where no token was drawn
+ *                  T = 1 value; 0 where no token was drawn.  (bfloat16 laws are evaluated with log2(e) / T rounded
+ *                  to binary32; all normalisers that calls return or take are ones for log2(e) / T itself, that
+ *                  law's times the quotient of the two scales, and the verification undoes exactly that)
  *   workspace      device scratch of at least fef_draft_sample_workspace_bytes(...) bytes,
  *                  256-byte aligned, contents need not be initialised
  *   device_status  device out, [1] int32, or NULL: FEF_OK, or FEF_ERR_NONFINITE when a used row
@@ -535,8 +537,8 @@ fef_status fef_lmhead_logits_quantized(const void* hidden, const void* packed, c
  *                  (strides in words, 0 shares), bit x & 31 of word x >> 5 belongs to id x; or NULL = all allowed
  *   temperature    of log2_norm alone; >= 0 and finite, 0 stands for 1 as in fef_draft_sample
  *   log2_norm      device out, [B, K] float64, or NULL: log2 of sum_x 2^(out_x * log2(e) / T) of every adjusted row
- *                  as it is stored: what fef_spec_verify_with_norms takes.  NaN where the adjusted row holds NaN or
- *                  +inf or no finite entry (a mask that leaves nothing); 0 for i >= n_b
+ *                  as it is stored: what fef_spec_verify_with_norms takes (bfloat16: see fef_draft_sample).  NaN where
+ *                  the adjusted row holds NaN or +inf or no finite entry (a mask that leaves nothing); 0 for i >= n_b
  *   workspace      device scratch of fef_logits_adjust_workspace_bytes(B, K, V) bytes, 256-byte aligned, contents need
  *                  not be initialised; needed with log2_norm only.  Two calls that may overlap need separate ones
  * A masked id is -inf whatever its logit, NaN and infinities among them.  Asynchronous on `cuda_stream`; one kernel, and a

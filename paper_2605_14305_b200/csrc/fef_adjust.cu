@@ -44,7 +44,7 @@ struct Params {
     int64_t allowed_stride_b, allowed_stride_k;
     int L, B, K, V, chunks, rows_per_cta;
     float c;                     // log2(e) / T
-    double c_exact;
+    double c_law, norm_scale;    // the law's scale in double precision, and what turns its normaliser into one for log2(e) / T
     float2* partials;            // [B * K][chunks]: (largest logit m, sum of 2^((l - m) c))
     double* log2_norm;           // [B * K]
 };
@@ -358,7 +358,8 @@ __global__ void __launch_bounds__(kThreads, DT == FEF_F32 ? 3 : 5) adjust_kernel
     }
 }
 
-// log2 of the row sums from the chunks' partial sums, in double precision: one warp per row.
+// log2 of the row sums from the chunks' partial sums, in double precision: one warp per row.  A bfloat16 law is the one that the
+// draws and the verification evaluate: with log2(e) / T rounded to binary32 (c), and its normaliser scaled as theirs are.
 __global__ void __launch_bounds__(kThreads) adjust_norm_kernel(const __grid_constant__ Params P) {
     cudaGridDependencySynchronize();
     const int lane = threadIdx.x & 31;
@@ -375,15 +376,15 @@ __global__ void __launch_bounds__(kThreads) adjust_norm_kernel(const __grid_cons
         const float2 p = P.partials[row * P.chunks + c];
         if (p.y != 0.f) {  // (a NaN sum poisons the row)
             const double nm = fmax(m, static_cast<double>(p.x));
-            s = (m > -INFINITY ? s * exp2((m - nm) * P.c_exact) : 0.0) +
-                static_cast<double>(p.y) * exp2((static_cast<double>(p.x) - nm) * P.c_exact);
+            s = (m > -INFINITY ? s * exp2((m - nm) * P.c_law) : 0.0) +
+                static_cast<double>(p.y) * exp2((static_cast<double>(p.x) - nm) * P.c_law);
             m = nm;
         }
     }
     const double top = warp_max(m);
-    const double sum = warp_sum(m > -INFINITY ? s * exp2((m - top) * P.c_exact) : 0.0);
+    const double sum = warp_sum(m > -INFINITY ? s * exp2((m - top) * P.c_law) : 0.0);
     if (lane == 0)
-        P.log2_norm[row] = sum > 0.0 && sum < INFINITY ? top * P.c_exact + log2(sum) : static_cast<double>(NAN);
+        P.log2_norm[row] = sum > 0.0 && sum < INFINITY ? (top * P.c_law + log2(sum)) * P.norm_scale : static_cast<double>(NAN);
 }
 
 static int chunks_of(int V) { return (V + kChunk - 1) / kChunk; }
@@ -446,8 +447,9 @@ fef_status fef_logits_adjust(const void* logits, void* out, int B, int K, int V,
 
     Params P = {};
     const double c = 1.4426950408889634074 / (temperature == 0.0f ? 1.0 : static_cast<double>(temperature));
-    P.c_exact = c;
     P.c = static_cast<float>(c);
+    P.c_law = dt == FEF_F32 ? c : static_cast<double>(P.c);
+    P.norm_scale = c / P.c_law;
     if (!(P.c > 0.f) || isinf(P.c)) return FEF_ERR_INVALID_ARG;
 
     int dev = -1, sms = 0;

@@ -40,6 +40,7 @@ struct DraftParams {
     int parts;           // CTAs per row
     int64_t ld_bytes;
     float c_hi, c_lo;    // log2(e)/T split in two binary32 numbers (c_lo = 0 for bfloat16)
+    double norm_scale;   // log2(e)/T over c_hi + c_lo: what the normalisers are multiplied by (see the verification's norm_scale)
     uint64_t seed;
     uint32_t step;
     const uint32_t* round; // device word added to `step` when the kernel runs, or null
@@ -434,12 +435,12 @@ __global__ void __launch_bounds__(kDraftThreads, WITH_TARGET ? 3 : 4) draft_kern
         const double tMw = warp_max(tm);
         const double tS = warp_sum(tm > -INFINITY ? ts * exp2(tm - tMw) : 0.0);
         tbad = __any_sync(0xFFFFFFFFu, tbad) || !(tS > 0.0) || !(tS < INFINITY);
-        if (lane == 0) P.target_log2_norm[row] = tbad ? __longlong_as_double(0x7FF8000000000000ll) : tMw + log2(tS);
+        if (lane == 0) P.target_log2_norm[row] = tbad ? __longlong_as_double(0x7FF8000000000000ll) : (tMw + log2(tS)) * P.norm_scale;
     }
     if (lane == 0) {
         const bool ok = !bad && score > -INFINITY;
         P.tokens[row] = ok ? Z : -1;
-        if (P.log2_norm) P.log2_norm[row] = ok ? Mw + log2(S) : 0.0;
+        if (P.log2_norm) P.log2_norm[row] = ok ? (Mw + log2(S)) * P.norm_scale : 0.0;
         if (!ok) report(P.status, FEF_ERR_NONFINITE);
     }
 }
@@ -524,6 +525,7 @@ static fef_status draft_impl(const void* draft_logits, const int32_t* row_len, i
     }
     P.c_hi = c_hi;
     if (!(P.c_hi > 0.f) || isinf(P.c_hi)) return FEF_ERR_INVALID_ARG;
+    P.norm_scale = dt == FEF_F32 ? 1.0 : c / static_cast<double>(c_hi);
     P.seed = seed;
     P.keys = philox_round_keys(seed);
     P.step = step;

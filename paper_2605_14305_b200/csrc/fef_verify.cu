@@ -903,7 +903,7 @@ __device__ __forceinline__ int window_accept(const VerifyParams& P, int b, int n
             }
             RowNorm np;
             if (P.target_norm) {  // both laws' normalisers came with the drafts: nothing was streamed
-                np.M = P.target_norm[row];
+                np.M = P.target_norm[row] * P.norm_scale;
                 np.S = 1.0;
                 np.bad = !(fabs(np.M) < INFINITY);
             } else {
@@ -911,7 +911,7 @@ __device__ __forceinline__ int window_accept(const VerifyParams& P, int b, int n
             }
             RowNorm nq;
             if (P.draft_norm) {  // rho(x) = 2^(l_x c - norm): the normaliser came with the drafts
-                nq.M = P.draft_norm[row];
+                nq.M = P.draft_norm[row] * P.norm_scale;
                 nq.S = 1.0;
                 nq.bad = !(fabs(nq.M) < INFINITY);
             } else {
@@ -927,7 +927,7 @@ __device__ __forceinline__ int window_accept(const VerifyParams& P, int b, int n
             const int64_t row = static_cast<int64_t>(b) * G.K + i;
             RowNorm np;
             if (P.target_norm) {
-                np.M = P.target_norm[row];
+                np.M = P.target_norm[row] * P.norm_scale;
                 np.S = 1.0;
                 np.bad = !(fabs(np.M) < INFINITY);
             } else {
@@ -935,7 +935,7 @@ __device__ __forceinline__ int window_accept(const VerifyParams& P, int b, int n
             }
             RowNorm nq;
             if (P.draft_norm) {
-                nq.M = P.draft_norm[row];
+                nq.M = P.draft_norm[row] * P.norm_scale;
                 nq.S = 1.0;
                 nq.bad = !(fabs(nq.M) < INFINITY);
             } else {
@@ -1646,6 +1646,7 @@ static fef_status verify_impl(const void* draft_logits, const void* target_logit
     }
     P.c_hi = c_hi;
     P.c_exact = c;
+    P.norm_scale = dt == FEF_F32 ? 1.0 : static_cast<double>(c_hi) / c;
     if (!(P.c_hi > 0.f) || isinf(P.c_hi)) return FEF_ERR_INVALID_ARG;
     P.wait_limit_ns = kWaitLimitNs;
     P.withhold_stage = -1;

@@ -43,6 +43,9 @@ struct VerifyParams {
                                // then nothing is streamed)
     float c_hi, c_lo;     // log2(e)/T split in two binary32 numbers, c_lo > 0 (or 0 for bfloat16)
     double c_exact;       // log2(e)/T in double precision (the double-precision pass of the residual draw)
+    double norm_scale;    // c_hi + c_lo over log2(e)/T: what given normalisers are multiplied by.  A bfloat16 law is evaluated with
+                          // c_hi, a normaliser handed from call to call is one for log2(e)/T, and off by 2^-25 of itself
+                          // (of the logits, that is) it would be worth more than all other errors together
     unsigned long long wait_limit_ns;  // how long a wait inside the streaming kernel may last
     int withhold_stage;   // test builds only: CTA 0 never delivers its stage of this number (-1: none)
     uint64_t seed;

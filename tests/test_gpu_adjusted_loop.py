@@ -68,6 +68,36 @@ def test_from_hidden_states_to_verified_tokens(fef, B, K, V, d, group, dtype):
             assert all(x < 0 or words[b, x // 32].item() >> (x % 32) & 1 for x in row)
 
 
+@pytest.mark.parametrize("T", [0.05, 0.1, 0.2, 1.0])
+@pytest.mark.parametrize("top", [60.0, 25.0, -60.0])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_normalisers_of_adjusted_rows_belong_to_the_laws_of_the_verification(fef, T, top, dtype):
+    """Low temperatures and large logits: a normaliser under another rounding of log2(e) / T than the one the verification
+    evaluates the law with is off in proportion to the logits."""
+    B, K, V = 6, 16, 3000
+    g = torch.Generator(device="cuda").manual_seed(int(top) + 100)
+    q = torch.randn((B, K, V), generator=g, device="cuda") * 0.25 + top
+    p = (q + 0.1 * torch.randn((B, K, V), generator=g, device="cuda")).to(dtype)
+    q = q.to(dtype)
+    rules = dict(bias=torch.randn((B, V), generator=g, device="cuda") * 0.1, temperature=T)
+    q = fef.fef_logits_adjust(q, **rules).logits
+    draft = fef.fef_draft_sample(q, T, 5, 8)
+    p, norm = fef.fef_logits_adjust(p, draft_tokens=draft.tokens, with_norm=True, **rules)
+    got = fef.fef_spec_verify(q, p, draft.tokens, T, 5, 8, draft_log2_norm=draft.log2_norm, target_log2_norm=norm)
+    both = fef.fef_draft_sample(q, T, 5, 8, target_logits=p)
+    torch.cuda.synchronize()
+    assert int(got.device_status.item()) == 0 and torch.equal(both.tokens, draft.tokens)
+    _verified(got, q, p, draft.tokens, T, 5, 8)
+    # the two calls that deliver the target rows' normalisers agree within what each may be off by
+    assert float((norm - both.target_log2_norm).abs().max()) <= 2 * 2e-6 / math.log(2.0)
+    # and each of them is, within that and the law's rounded scale (2^-24 of log2 V at most), what the header says
+    z = p.double() * (math.log2(math.e) / float(torch.tensor(T, dtype=torch.float32)))
+    peak = z.amax(-1, keepdim=True)
+    exact = peak[..., 0] + torch.log2(torch.exp2(z - peak).sum(-1))
+    for n in (norm, both.target_log2_norm):
+        assert float((n - exact).abs().max()) <= 2e-6 / math.log(2.0) + 2.0 ** -24 * math.log2(V)
+
+
 def test_a_mask_that_leaves_nothing_is_reported(fef):
     V = 500
     q = torch.randn((2, 3, 504), device="cuda")
