@@ -283,6 +283,42 @@ def test_refusals(fef):
     fef.fef_logits_adjust(c["logits"], **args)              # and the call itself is fine
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [2048, 5003, 126464])
+def test_normalisers_within_what_the_residual_draw_counts_on(fef, dtype, V):
+    """2e-6 relative (fef_residual.cuh).  A term 2^((l - m) c) carries a rounding of the difference, of the product and, in binary32, of c
+    (2^-24 each, relative to its argument e; bfloat16 laws have c itself in binary32), in two steps that add up to e: to its warp's
+    largest and from there to the largest of 2048 ids; ex2 is within 2^-22 and applied twice, and the term passes eight additions
+    in its warp and one rounding of the joined sum (the rest is in double precision).  The weighted mean of |e| over 2048 ids is
+    largest when one id stands at 0 and all others together at one x."""
+    x = torch.linspace(0.0, 20.0, 10001, dtype=torch.float64)
+    mean = float((2047 * x * torch.exp2(-x) / (1 + 2047 * torch.exp2(-x))).max())
+    roundings = 2 if dtype == torch.bfloat16 else 3
+    bound = 1.01 * (roundings * 2.0 ** -24 * mean * math.log(2.0) + 2 * 2.0 ** -22 + 9 * 2.0 ** -24)
+    assert bound < 2e-6
+    g = torch.Generator(device="cuda").manual_seed(V)
+    for T in (0.3, 1.0, 2.7):
+        T = float(torch.tensor(T, dtype=torch.float32))
+        rows = []
+        for down in (1.0, 3.3, 4.9, 6.0, 8.0, 8.6, 11.0, 14.0, 20.0, 0.0):
+            row = torch.full((V,), 7.0 - down * T * math.log(2.0), device="cuda")
+            row[int(down * 100) % V] = 7.0
+            rows.append(row)
+        rows += [torch.randn(V, generator=g, device="cuda") * s for s in (0.1, 1.0, 3.0, 10.0)]
+        ld = (V + 7) // 8 * 8
+        logits = torch.zeros((2, 7, ld), device="cuda")
+        logits[..., :V] = torch.stack(rows).view(2, 7, V)
+        logits = logits.to(dtype)
+        norm = fef.fef_logits_adjust(logits, V=V, temperature=T, with_norm=True).log2_norm
+        c = LOG2E / T
+        law = c if dtype == torch.float32 else float(torch.tensor(c, dtype=torch.float64).float())
+        z = logits[..., :V].double() * law
+        top = z.amax(-1, keepdim=True)
+        ref = top[..., 0] + torch.log2(torch.exp2(z - top).sum(-1))
+        off = (norm * (law / c) - ref).abs() * math.log(2.0)
+        assert float(off.max()) <= bound, float(off.max())
+
+
 @pytest.mark.parametrize("dtype,ld", [(torch.float32, 4), (torch.bfloat16, 8)])
 def test_the_largest_batch(fef, dtype, ld):
     B, V = 65535, 3
