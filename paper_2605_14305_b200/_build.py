@@ -52,8 +52,8 @@ TEST_HOOKS_LIB_PATH = os.path.join(HERE, "libfef_testhooks.so")
 
 
 def build_test_hooks(force: bool = False) -> str:
-    """The library compiled with -DFEF_TEST_HOOKS (adds fef_test_withhold_stage_once, which lets a test
-    make one bounded wait of the streaming kernel run out).  Used by the GPU tests only."""
+    """The library compiled with -DFEF_TEST_HOOKS (adds fef_test_withhold_*_once, which let a test make one
+    bounded wait of a kernel run out).  Used by the GPU tests only."""
     deps = [os.path.join(CSRC, s) for s in SOURCES] + HEADERS
     if not force and os.path.exists(TEST_HOOKS_LIB_PATH) and \
             all(os.path.getmtime(d) <= os.path.getmtime(TEST_HOOKS_LIB_PATH) for d in deps):

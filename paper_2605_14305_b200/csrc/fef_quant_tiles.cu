@@ -45,6 +45,9 @@ struct TileParams {
     ProductParams P;
     int tiles, row_blocks, items, padded;   // padded: hidden rows rounded up to whole tiles
     int out_bf16;
+#ifdef FEF_TEST_HOOKS
+    int withhold;   // CTA 0 never delivers its block of hidden rows of this number (-1: none)
+#endif
 };
 
 // PIPES = 2: two pipelines, each with four warps for its weights and four for its epilogue.  PIPES = 1: one, whose weights two
@@ -278,6 +281,13 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
                 const int64_t v0 = static_cast<int64_t>(item / T.row_blocks) * kTileV;
                 const uint32_t rows = static_cast<uint32_t>(min(static_cast<int64_t>(kTileV), W.Vp - v0));   // a multiple of 32
                 for (int c = 0; c < W.blocks; ++c) {
+#ifdef FEF_TEST_HOOKS
+                    // Test build: nothing is copied from here on and nothing arrives, so the waits for it run out.
+                    if (blockIdx.x == 0 && T.withhold >= 0 && issued >= T.withhold) {
+                        ok = false;
+                        break;
+                    }
+#endif
                     if (!wait_for(sh.b_empty + stage.at, stage.phase ^ 1u, abort_flag)) {
                         gave_up();
                         ok = false;
@@ -345,10 +355,12 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             a.advance();
             b.advance();
         }
-        // everything issued has finished before the tensor memory goes back
+        // everything issued has finished before the tensor memory goes back, after a wait that ran out too: this one does not
+        // look at the abort flag (both issuers always commit, so it ends)
         if (elect_one()) tc_commit(&sh.drained);
         __syncwarp();
-        wait_for(&sh.drained, 0u, abort_flag);
+        volatile int never = 0;
+        wait_for(&sh.drained, 0u, &never);
     } else if (warp >= kWeightWarp0) {
         // ------------------------------------------------------------------------------------ weights
         // A lane takes one row: the 64 bytes of a block are its word 4 t + w, of columns 32 w + 8 t .. + 7, for every t and w.
@@ -536,6 +548,9 @@ int64_t padded_rows(int rows) {
     return (static_cast<int64_t>(rows) + nt - 1) / nt * nt;
 }
 bool g_attr[64][2][3];
+#ifdef FEF_TEST_HOOKS
+int g_test_withhold = -1;
+#endif
 
 template <int NT, int PIPES, int N>
 fef_status launch(const CUtensorMap& map, const TileParams& T, int dev, int grid, cudaStream_t stream) {
@@ -599,6 +614,10 @@ fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* works
     if (static_cast<int64_t>(T.tiles) * T.row_blocks * W.blocks > 0x7FFFFFFF) return FEF_ERR_INVALID_ARG;   // (counted in 32 bits)
     T.items = T.tiles * T.row_blocks;
     T.out_bf16 = dt == FEF_BF16;
+#ifdef FEF_TEST_HOOKS
+    T.withhold = g_test_withhold;   // one call only
+    g_test_withhold = -1;
+#endif
     CUtensorMap map;
     const uint64_t cols = static_cast<uint64_t>(W.blocks) * kBlock;
     if (!map_2d(&map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, H.operand, cols, T.padded, cols * 2, 64, nt, CU_TENSOR_MAP_SWIZZLE_128B))
@@ -612,3 +631,9 @@ fef_status launch_tiles_kernel(const ProductParams& P, fef_dtype dt, void* works
 
 }  // namespace quant
 }  // namespace fef
+
+#ifdef FEF_TEST_HOOKS
+// Test builds only (never part of the shipped library): in the next product of more than 16 rows CTA 0 withholds the hidden rows of
+// its block number `block`, so that the waits for them run out after their second.
+extern "C" void fef_test_withhold_product_block_once(int block) { fef::quant::g_test_withhold = block; }
+#endif
