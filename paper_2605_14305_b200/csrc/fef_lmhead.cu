@@ -70,6 +70,9 @@ struct GemmParams {
     float* logits_out;      // kStore: [rows of both matrices][ldo]
     int64_t ldo;
     int32_t* status;
+#ifdef FEF_TEST_HOOKS
+    int withhold;           // CTA 0 never delivers its stage of this number (-1: none)
+#endif
 };
 
 struct GemmShared {
@@ -132,6 +135,13 @@ lmhead_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_cons
                 const int n_begin = chunk * P.tiles_per_chunk, n_end = min(n_begin + P.tiles_per_chunk, P.n_tiles);
                 for (int n = n_begin; ok && n < n_end; ++n)
                     for (int kb = 0; kb < P.k_blocks; ++kb) {
+#ifdef FEF_TEST_HOOKS
+                        // Test build: nothing is copied from here on and nothing arrives, so the waits for it run out.
+                        if (blockIdx.x == 0 && P.withhold >= 0 && issued >= P.withhold) {
+                            ok = false;
+                            break;
+                        }
+#endif
                         if (!mbar_wait_bounded(sh.empty + stage, phase ^ 1u, abort_flag, kGemmWaitNs)) {
                             *abort_flag = 1;
                             report(P.status, FEF_ERR_TIMEOUT);
@@ -196,9 +206,11 @@ lmhead_gemm_kernel(const __grid_constant__ CUtensorMap map_a0, const __grid_cons
                     if (ok) tc_commit(sh.tmem_full + acc);  // arrives when the tile's accumulator is complete
                 }
             }
-            // everything issued has finished before the tensor memory goes back
+            // everything issued has finished before the tensor memory goes back, after a wait that ran out too: this one does
+            // not look at the abort flag
             tc_commit(&sh.drained);
-            mbar_wait_bounded(&sh.drained, 0u, abort_flag, kGemmWaitNs);
+            volatile int never = 0;
+            mbar_wait_bounded(&sh.drained, 0u, &never, kGemmWaitNs);
         }
     } else {
         // ---------------------------------------------------------------- epilogue
@@ -495,6 +507,10 @@ static cudaError_t launch_pdl(void (*kernel)(Args...), dim3 grid, dim3 block, si
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
+#ifdef FEF_TEST_HOOKS
+static int g_test_withhold = -1;
+#endif
+
 // One product: rows of `a0` (and, if given, of `a1`) times `weight`^T, epilogue MODE.
 template <int MODE>
 static cudaError_t launch_gemm(const void* a0, const void* a1, int rows, const void* weight, int V, int d, GemmParams P,
@@ -516,6 +532,10 @@ static cudaError_t launch_gemm(const void* a0, const void* a1, int rows, const v
     P.rows = rows;
     P.V = V;
     if (MODE == kStore) P.tiles_per_chunk = 1;
+#ifdef FEF_TEST_HOOKS
+    P.withhold = g_test_withhold;   // one product only
+    g_test_withhold = -1;
+#endif
     P.chunks = (P.n_tiles + P.tiles_per_chunk - 1) / P.tiles_per_chunk;
     const int items = P.m_tiles * P.chunks;
     const int grid = items < sms ? items : sms;
@@ -708,3 +728,9 @@ fef_status fef_lmhead_verify(const void* draft_hidden, const void* target_hidden
 }
 
 }  // extern "C"
+
+#ifdef FEF_TEST_HOOKS
+// Test builds only (never part of the shipped library): in the next product CTA 0 withholds its stage number `stage`, so that the
+// waits for it run out after their second.
+extern "C" void fef_test_withhold_gemm_stage_once(int stage) { fef::lm::g_test_withhold = stage; }
+#endif

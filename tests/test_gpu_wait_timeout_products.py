@@ -23,8 +23,10 @@ def hooks():
     L = ctypes.CDLL(_build.build_test_hooks())
     L.fef_lmhead_logits_quantized.argtypes = [vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, i32, vp, sz, vp, vp]
     L.fef_lmhead_logits_quantized.restype = i32
-    L.fef_test_withhold_product_block_once.argtypes = [i32]
-    L.fef_test_withhold_product_block_once.restype = None
+    L.fef_lmhead_logits.argtypes = [vp, vp, i32, i32, i32, vp, i64, vp, vp]
+    L.fef_lmhead_logits.restype = i32
+    for f in (L.fef_test_withhold_product_block_once, L.fef_test_withhold_gemm_stage_once):
+        f.argtypes, f.restype = [i32], None
     return L
 
 
@@ -59,3 +61,32 @@ def test_product_of_the_4_bit_layer(hooks, rows, block):
     assert call() == 0                               # the same stream, scratch and output
     torch.cuda.synchronize()
     assert int(status.item()) == 0 and torch.equal(out[:, :V], want[:, :V])
+
+
+@pytest.mark.parametrize("stage", [0, 2, 30])      # (of the 40 that the first CTA takes, through a ring of a few)
+def test_product_of_the_16_bit_layer(hooks, stage):
+    import paper_2605_14305_b200 as fef
+
+    rows, V, d = 300, 60000, 512
+    fef.load(build_if_missing=True)
+    g = torch.Generator(device="cuda").manual_seed(stage)
+    weight = (torch.randn((V, d), generator=g, device="cuda") * 0.1).to(torch.bfloat16)
+    hidden = torch.randn((rows, d), generator=g, device="cuda").to(torch.bfloat16)
+    want = torch.zeros((rows, V), device="cuda")
+    fef.fef_lmhead_logits(hidden, weight, out=want)
+    out = torch.zeros_like(want)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+
+    def call():
+        return hooks.fef_lmhead_logits(hidden.data_ptr(), weight.data_ptr(), rows, V, d, out.data_ptr(), V, status.data_ptr(),
+                                       torch.cuda.current_stream().cuda_stream)
+
+    hooks.fef_test_withhold_gemm_stage_once(stage)
+    start = time.monotonic()
+    assert call() == 0
+    torch.cuda.synchronize()
+    assert time.monotonic() - start < 10.0
+    assert int(status.item()) == FEF_ERR_TIMEOUT
+    assert call() == 0
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0 and torch.equal(out, want)
