@@ -113,12 +113,20 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, volatil
     return mbar_wait_bounded(bar, parity, abort_flag, kWaitNs);
 }
 
+// The warp's vote on what its lanes waited for.  A vote orders no memory accesses: the barrier behind it does, so that what one lane's
+// wait has made visible to it (copies that landed, registers read out of tensor memory) is visible to all.
+__device__ __forceinline__ bool all_waited(bool mine) {
+    const bool all = __all_sync(0xFFFFFFFFu, mine);
+    __syncwarp();
+    return all;
+}
+
 // A warp waits for three barriers (given by their offset in Shared) at once, each polled by a lane of its own: one round trip.
 __device__ __forceinline__ bool wait_for_all(Shared& sh, uint32_t o0, uint32_t p0, uint32_t o1, uint32_t p1, uint32_t o2, uint32_t p2) {
     const int lane = threadIdx.x & 31;
     const uint32_t offset = lane == 0 ? o0 : lane == 1 ? o1 : o2, parity = lane == 0 ? p0 : lane == 1 ? p1 : p2;
     uint64_t* bar = reinterpret_cast<uint64_t*>(reinterpret_cast<char*>(&sh) + offset);
-    return __all_sync(0xFFFFFFFFu, lane > 2 || wait_for(bar, parity, &sh.abort_flag));
+    return all_waited(lane > 2 || wait_for(bar, parity, &sh.abort_flag));
 }
 
 // A place in a ring of S and the phase of its barriers.
@@ -408,7 +416,7 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
             bool ok = true;
             // (after a wait that ran out the rest goes by without waits and arrivals)
             auto put = [&](const Fetched& f) {
-                if (ok && !__all_sync(0xFFFFFFFFu, lane > 0 || wait_for(&sh.a_empty[pipe][stage.at], stage.phase ^ 1u, abort_flag))) {
+                if (ok && !all_waited(lane > 0 || wait_for(&sh.a_empty[pipe][stage.at], stage.phase ^ 1u, abort_flag))) {
                     gave_up();
                     ok = false;
                 }
