@@ -185,6 +185,12 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
+def _check_scratch(workspace: Optional[torch.Tensor], dev, where: str):
+    """Scratch that the caller gives: on the device of the call, and as large as its size says (an expanded tensor is not)."""
+    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+
+
 def fef_spec_verify_workspace_bytes(B: int, K: int, V: int, dtype) -> int:
     code = dtype if isinstance(dtype, int) else (FEF_F32 if dtype == torch.float32 else FEF_BF16)
     return int(load().fef_spec_verify_workspace_bytes(B, K, V, code))
@@ -232,6 +238,7 @@ def fef_spec_verify(draft_logits: torch.Tensor, target_logits: torch.Tensor, dra
     V = ld if V is None else int(V)
     code = _dtype_code(draft_logits)
     dev = draft_logits.device
+    _check_scratch(workspace, dev, "fef_spec_verify")
     # (nothing to allocate and the device already current: no context to enter, which matters for small calls)
     plain = out is not None and workspace is not None and stream is None and torch.cuda.current_device() == dev.index
     with (contextlib.nullcontext() if plain else _on(dev, stream)):
@@ -311,6 +318,7 @@ def fef_draft_sample(draft_logits: torch.Tensor, temperature: float, seed: int, 
     V = ld if V is None else int(V)
     code = _dtype_code(draft_logits)
     dev = draft_logits.device
+    _check_scratch(workspace, dev, "fef_draft_sample")
     with _on(dev, stream):
         if out is None:
             out = DraftResult(torch.empty((B, K), dtype=torch.int32, device=dev),
@@ -627,6 +635,7 @@ def fef_lmhead_verify(draft_hidden: torch.Tensor, target_hidden: torch.Tensor, w
     if row_len is not None and row_len.dtype != torch.int32:
         raise FefError(FEF_ERR_INVALID_ARG, "fef_lmhead_verify")
     dev = weight.device
+    _check_scratch(workspace, dev, "fef_lmhead_verify")
     with _on(dev, stream):
         if out is None:
             out = VerifyResult(torch.empty(B, dtype=torch.int32, device=dev),
@@ -802,6 +811,7 @@ def fef_lmhead_logits_quantized(hidden: torch.Tensor, layer: QuantizedLayer, dty
     rows, d = hidden.shape
     if d != layer.d or hidden.device != dev or rows < 1:
         raise FefError(FEF_ERR_INVALID_ARG, where)
+    _check_scratch(workspace, dev, where)
     if out is not None:
         dtype = out.dtype
         if out.dim() != 2 or out.shape[0] != rows or out.shape[1] < V or not out.is_contiguous() or out.device != dev:
@@ -877,8 +887,7 @@ def fef_logits_adjust(logits: torch.Tensor, tokens: Optional[torch.Tensor] = Non
             _is(row_len, torch.int32, (B,), dev) and _is(penalties, torch.float32, (B, 3), dev) and
             _is(log2_norm, torch.float64, (B, K), dev) and _is(out, logits.dtype, shape, dev)):
         raise FefError(FEF_ERR_INVALID_ARG, where)
-    if workspace is not None and (workspace.device != dev or not workspace.is_contiguous()):
-        raise FefError(FEF_ERR_INVALID_ARG, where)
+    _check_scratch(workspace, dev, where)
     if bias is not None:
         if bias.dtype != torch.float32 or bias.dim() not in (1, 2) or bias.shape[-1] < V or bias.device != dev or \
                 (bias.stride(-1) != 1 and V > 1) or (bias.dim() == 2 and bias.shape[0] != B):
