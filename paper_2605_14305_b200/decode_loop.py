@@ -181,7 +181,9 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
 
     logits_fn(device_round [1] int32 CUDA, window_pos, row_len) -> (draft_logits, target_logits):
     must be capturable (device work only, the round read from the tensor).  ``adjust`` as there; a function
-    of it gets the round's tensor and must be capturable too.
+    of it gets the round's tensor and must be capturable too.  A round in which the verification reports a
+    data error (a mask that leaves nothing, logits that are no numbers) ends the loop with RuntimeError, at
+    the next of those reads.
 
     Returns dict(tokens, conf (CUDA), rounds, loop_seconds: wall time of the replay loop alone).
     """
@@ -190,6 +192,7 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
     conf = torch.full((B, L), -1.0, dtype=torch.float32, device=dev)
     in_step = torch.zeros((B, L), dtype=torch.uint8, device=dev)
     rnd = torch.zeros(1, dtype=torch.int32, device=dev)
+    worst = torch.zeros(B, dtype=torch.int32, device=dev)   # smallest count committed so far: -1 where a round had a data error
 
     def one_round():
         window, row_len, unresolved = fef.fef_loop_next_window(tokens, K)
@@ -203,7 +206,7 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
         res = fef.fef_spec_verify(q, p, draft.tokens, temperature, seed, first_round, row_len=row_len,
                                   draft_log2_norm=draft.log2_norm if (reuse_draft_norm or p_norm is not None) else None,
                                   device_round=rnd, target_log2_norm=p_norm)
-        fef.fef_loop_commit(window, row_len, res, tokens, conf, in_step)
+        torch.minimum(worst, fef.fef_loop_commit(window, row_len, res, tokens, conf, in_step), out=worst)
         fef.fef_loop_advance_round(rnd, unresolved)
         return unresolved
 
@@ -218,6 +221,7 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
     conf.fill_(-1.0)
     in_step.zero_()
     rnd.zero_()
+    worst.zero_()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
@@ -229,7 +233,10 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
         while True:
             for _ in range(rounds_per_check):
                 graph.replay()
-            if int(unresolved.max().item()) == 0:   # counted before the last replay: nothing was left
+            left, error = torch.stack((unresolved.max(), worst.min())).tolist()
+            if error < 0:   # (the window would stay unresolved for good)
+                raise RuntimeError("verification reported a data error by round %d" % int(rnd.item()))
+            if left == 0:   # counted before the last replay: nothing was left
                 break
         if s < n_steps - 1 and remask_k > 0:
             positions, count = fef.fef_remask_select(conf, in_step, remask_k)

@@ -112,6 +112,33 @@ def test_a_mask_that_leaves_nothing_is_reported(fef):
     assert int(got.accept_len[1]) == -1 and int(got.accept_len[0]) >= 0
 
 
+@pytest.mark.parametrize("when", [0, 3])
+def test_a_mask_that_leaves_nothing_ends_the_loops(fef, when):
+    """... with an error, from the first round on or from a later one, the replayed loop like the eager one."""
+    from paper_2605_14305_b200.decode_loop import run_decode_loop_device, run_decode_loop_graph
+
+    B, L, K, V = 2, 40, 4, 300
+    words = torch.full((B, K, (V + 31) // 32), -1, dtype=torch.int32, device="cuda")
+    last = torch.full((B, 1, 1), L, dtype=torch.int32, device="cuda")
+    last[1] = when * K                                       # sequence 1: nothing is allowed from this position on
+
+    def rules(rnd, window, row_len, drafts):
+        return dict(allowed=torch.where(window[:, :, None] < last, words, 0))
+
+    def eager(rnd, window, row_len, inputs):
+        return fef.fef_synth_logits(B, K, V, torch.float32, 2.0, 0.7, 4, rnd)
+
+    def captured(rnd, window, row_len):
+        return fef.fef_synth_logits(B, K, V, torch.float32, 2.0, 0.7, 4, 0, device_round=rnd)
+
+    with pytest.raises(RuntimeError, match="data error"):
+        run_decode_loop_device(fef, B, L, K, 1, 0, eager, 1.0, 3, adjust=rules)
+    with pytest.raises(RuntimeError, match="data error"):
+        run_decode_loop_graph(fef, B, L, K, 1, 0, captured, 1.0, 3, adjust=rules)
+    last[1] = L
+    run_decode_loop_graph(fef, B, L, K, 1, 0, captured, 1.0, 3, adjust=rules)
+
+
 @pytest.mark.parametrize("T", [1.0, 0.0])
 def test_decoding_loop_with_rules(fef, T):
     from paper_2605_14305_b200.decode_loop import run_decode_loop_device, run_decode_loop_graph
