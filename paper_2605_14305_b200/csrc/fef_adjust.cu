@@ -129,7 +129,8 @@ __device__ __forceinline__ Row8<DT> pack8(float (&l)[8], uint32_t allowed) {
     return r;
 }
 
-// l / rep for l > 0, l * rep otherwise; `inv` = 1 / rep.  The quotient takes one correction step (an infinite one skips it).
+// l / rep for l > 0, l * rep otherwise; `inv` = 1 / rep.  The quotient takes one step of Markstein's correction (an infinite one
+// skips it).
 __device__ __forceinline__ float repeat_penalty(float l, float rep, float inv) {
     const float q = l * inv, fixed = fmaf(fmaf(-q, rep, l), inv, q);
     return l > 0.f ? (q < INFINITY ? fixed : q) : l * rep;
@@ -139,8 +140,8 @@ __device__ __forceinline__ float repeat_penalty(float l, float rep, float inv) {
 // repetition flags in registers, their counts in shared memory, so that the text is counted once and a position's draft is added
 // for the positions behind it without a barrier.  Four rows are in flight per thread.  The bound is memory (every logit read
 // and written once) with instruction issue close behind: 64 windows x 32 x 126464 bfloat16 with every rule and the normalisers
-// 212 us = 5.2 TB/s (0.8 of the copy rate), 16 x 32 x 152064 binary32 119 us = 5.2 TB/s.  More resident CTAs pay although a few
-// registers spill (bfloat16: three 245, four 219, five 212 us; binary32: two 129, three 119, four 139 us).
+// 215 to 225 us by GPU = 5.0 TB/s (0.78 of the copy rate), 16 x 32 x 152064 binary32 118 to 123 us = 5.2 TB/s.  More resident CTAs pay
+// although a few registers spill (on one GPU, bfloat16: three 245, four 219, five 212 us; binary32: two 129, three 119, four 139).
 template <int DT, bool NORM>
 __global__ void __launch_bounds__(kThreads, DT == FEF_F32 ? 3 : 5) adjust_kernel(const __grid_constant__ Params P) {
     __shared__ uint32_t s_hist[kChunk];

@@ -32,8 +32,9 @@ struct QuantizeParams {
     int32_t* status;
 };
 
-// Half a warp per block of one row, kUnits blocks in turn; a lane takes eight columns, one word of nibbles.  Bound by the bytes of the weights read once;
-// with an IEEE division for every weight the arithmetic took four times as long (126464 x 4096: 1.5 ms).
+// Half a warp per block of one row, kUnits blocks in turn; a lane takes eight columns, one word of nibbles.  Bound by instruction issue
+// (85 % of the issue slots used, 29 % of the memory's time: 40000 x 4096 in 151 us = 2.7 TB/s): the rounding of every weight and a
+// division by the blocks per row for every block; with an IEEE division for every weight the whole took four times as long.
 //
 // rint(w / s) without a division: w and s are bfloat16 numbers, w / s is below 16, and so a quotient that is no tie lies at
 // least 1/1020 from every tie: |w/s - (n + 1/2)| = |2 w - (2 n + 1) s| / (2 s), whose numerator, unless it is zero, is at least
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const __grid_constan
 }
 
 // ---------------------------------------------------------------------------------------- dequantize ----
-// The same lanes; bound by the bytes of the values written.
+// The same lanes; bound by the bytes of the values written (40000 x 4096 in 136 us = 5.4 TB/s).
 __global__ void __launch_bounds__(kThreads) dequantize_kernel(const __grid_constant__ Layer P, float* __restrict__ out) {
     const int lane = threadIdx.x & 31, p = lane & 15;
     const int64_t unit = (static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * 2 + (lane >> 4);

@@ -13,11 +13,13 @@
 //   1 warp a pipeline issues the MMAs (128 x NT x 16), a fresh accumulator for every group of a row's weights;
 //   8 warps  take each group's accumulator out of tensor memory, scale it and add it to the logits in registers: the vocabulary
 //            rows are the lanes, so a group's scale is one number per thread.  The weights are the left operand for that reason.
-// A block's hand-overs from warp to warp and the instructions of the weights' and the epilogue's warps set the pace (64 rows:
-// 109 us, 1350 cycles for two blocks of 128 x 128 weights, of which the MMAs need 512 and the weights' bytes 660; 512 rows:
-// 588 us = 0.90 PFLOP/s): hence few warps with much to do each, and waits that poll several barriers at once.  The epilogue has most
-// to do, so the weights' warps subtract the zero points (taking them off the groups' sums was 126 us, and inexact where a hidden
-// value is large).  Every wait is bounded.
+// A block's hand-overs from warp to warp and the instructions of the weights' and the epilogue's warps set the pace: hence few warps
+// with much to do each, and waits that poll several barriers at once.  126464 x 4096 in groups of 128: 64 rows 119 us (102 when the
+// logits stay in L2), 512 rows 700 us = 0.76 PFLOP/s.  A CTA takes whole tiles: 494 of 256 rows on 148 SMs are four rounds for
+// 3.34, a sixth of the time at 64 rows.  Groups of 64 and 32 take 1.6 and 2.6 times as long (64 rows 164 and 270 us, 512 rows 980
+// and 1700): the epilogue's waits, accumulators and arrivals are per group.  The epilogue has most to do, so the weights' warps
+// subtract the zero points (taking them off the groups' sums took longer, and is inexact where a hidden value is large).
+// Every wait is bounded.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -548,8 +550,8 @@ product_tiles_kernel(const __grid_constant__ CUtensorMap map, const __grid_const
     }
 }
 
-// Up to 64 rows two pipelines of 64, beyond them one of 128: with more rows the weights are unpacked half as often (512 rows: 588
-// against 657 us; 64 rows: 109 against 125).  Tiles of 32 rows take no less time than those of 64, which is the weights'.
+// Up to 64 rows two pipelines of 64, beyond them one of 128: with more rows the weights are unpacked half as often (126464 x 4096, 512
+// rows: 650 against 705 us; 64 rows: 154 against 102).  Tiles of 32 rows take no less time than those of 64, which is the weights'.
 int tile_rows(int rows) { return rows <= 64 ? 64 : 128; }
 int64_t padded_rows(int rows) {
     const int nt = tile_rows(rows);
