@@ -50,6 +50,9 @@ typedef enum { FEF_F32 = 0, FEF_BF16 = 1 } fef_dtype;
 #define FEF_MAX_B 65535
 #define FEF_MAX_K 64
 #define FEF_MAX_REMASK_L 8192
+/* Largest vocabulary whose laws are cut, and largest number of rows or columns of fef_hidden_transform. */
+#define FEF_MAX_TRUNCATE_V (1 << 20)
+#define FEF_MAX_TRANSFORM (1 << 20)
 /* Token id of a masked (unresolved) position in the decode-loop state. */
 #define FEF_MASK_TOKEN (-1)
 
@@ -551,6 +554,94 @@ fef_status fef_logits_adjust(const void* logits, void* out, int B, int K, int V,
                              const uint32_t* allowed, int64_t allowed_stride_b, int64_t allowed_stride_k,
                              float temperature, double* log2_norm, void* workspace, size_t workspace_bytes,
                              void* cuda_stream);
+
+/*
+ * Laws cut to their top-k, top-p and min-p sets (the paper has no counterpart: requests carry such sampling rules, and the draft
+ * law rho and the target law pi of Section 3.2 both have to obey them, or the emitted tokens follow neither).
+ *
+ * A row's entries stand in one order: larger logit first, lower id among equal ones, -inf not at all.  With M the row's largest
+ * logit and w_x = exp((l_x - M) / T):
+ *   top_k   keeps the first min(top_k, entries); 0, a negative number and V or more turn it off
+ *   top_p   keeps the shortest prefix whose weight is at least top_p times the weight of what top_k left (one entry at least);
+ *           1 or more turns it off
+ *   min_p   keeps the entries with w_x >= min_p; 0 and less turn it off, more than 1 is 1
+ * and the law keeps the shortest of these prefixes: pi(x) = w_x / (sum of the kept weights) there, 0 elsewhere.
+ * Borders are decided on sums of weights in 64 bits, the same in every call and on every device.
+ *
+ * A cut law is handed from call to call as three numbers per position, and used with the logits it belongs to:
+ *   log2_norm   device out, [B, K] float64: log2 of the sum over the kept entries of 2^(l_x * log2(e) / T), as elsewhere
+ *   cut_logit   device out, [B, K] float32, and
+ *   cut_id      device out, [B, K] int32: the last kept entry.  x is in the law iff l_x > cut_logit, or l_x = cut_logit and
+ *               x <= cut_id.  (-inf, -1) where the position's window has no rule turned on
+ *   kept        device out, [B, K] int32, or NULL: how many entries are in the law
+ * Positions i >= n_b (n_b = row_len[b], or K) get (0, 0, -1), kept 0.  A row that holds NaN or +inf or no finite logit, or whose
+ * limits or random number are NaN, gets (NaN, NaN, -1), kept 0, no token (-1, confidence -1), and device_status
+ * FEF_ERR_NONFINITE; verifying against such a law reports the same for its window.
+ *
+ *   logits         device, [B, K, ld] row-major, dtype `dt`; layout and alignment rules of fef_spec_verify, V <= FEF_MAX_TRUNCATE_V
+ *   row_len        device, [B] int32 in [0, K], or NULL = K everywhere
+ *   top_k          device, [B] int32, or NULL = off;  top_p, min_p: device, [B] float32, or NULL = off: each window's own
+ *   temperature    > 0 (0 draws the arg-max, which no rule removes: fef_draft_sample and fef_spec_verify serve it)
+ *   device_status  device out, [1] int32, or NULL
+ * Asynchronous on `cuda_stream`; one kernel.
+ *
+ * fef_draft_sample_truncated also draws one token per position, with one random number u:
+ *   draft_tokens   device out, [B, K] int32: the lowest id x for which the kept weights of the ids <= x sum to more than u
+ *                  times the sum of the kept weights; -1 for i >= n_b
+ *   conf           device out, [B, K] float32, or NULL: the token's probability under its cut law; -1 where there is none
+ *   uniforms       device, [B, K] float32 in [0, 1) (values outside count as the nearest one inside), or NULL: then u comes from
+ *                  Philox4x32-10 keyed like fef_spec_verify, stream 2: counter (2 << 30, b, i, step), output word 0,
+ *                  u = ((r >> 9) + 0.5) * 2^-23 (the number that fef_draft_sample uses for id 0)
+ *   seed, step     not used with uniforms; device_round: NULL, or the device-resident round counter of the *_at_round calls
+ *
+ * fef_spec_verify_truncated is fef_spec_verify with both laws cut (the cuts of fef_draft_sample_truncated and fef_law_truncate
+ * for the same logits and temperature): acceptance rule, residual law [pi - rho]_+ and confidences are those of the cut laws,
+ * random numbers, outputs and everything else as in fef_spec_verify_with_norms.  A draft outside its own law counts as
+ * rho(x) = 0.  temperature > 0.
+ */
+fef_status fef_law_truncate(const void* logits, const int32_t* row_len, int B, int K, int V, int64_t ld, fef_dtype dt,
+                            float temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                            double* log2_norm, float* cut_logit, int32_t* cut_id, int32_t* kept,
+                            int32_t* device_status, void* cuda_stream);
+fef_status fef_draft_sample_truncated(const void* draft_logits, const int32_t* row_len, int B, int K, int V, int64_t ld,
+                                      fef_dtype dt, float temperature, const int32_t* top_k, const float* top_p,
+                                      const float* min_p, const float* uniforms, uint64_t seed, uint32_t step,
+                                      const uint32_t* device_round, int32_t* draft_tokens, float* conf,
+                                      double* log2_norm, float* cut_logit, int32_t* cut_id, int32_t* kept,
+                                      int32_t* device_status, void* cuda_stream);
+fef_status fef_spec_verify_truncated(const void* draft_logits, const void* target_logits, const int32_t* draft_tokens,
+                                     const double* draft_log2_norm, const float* draft_cut_logit,
+                                     const int32_t* draft_cut_id, const double* target_log2_norm,
+                                     const float* target_cut_logit, const int32_t* target_cut_id,
+                                     const int32_t* row_len, int B, int K, int V, int64_t ld, fef_dtype dt,
+                                     float temperature, uint64_t seed, uint32_t step, const uint32_t* device_round,
+                                     int32_t* accept_len, int32_t* tokens, float* conf,
+                                     void* workspace, size_t workspace_bytes,
+                                     int32_t* device_status, void* cuda_stream);
+
+/*
+ * Hidden states through one layer of a prediction head, ahead of the output layer (of the paper's model outputs, Section 3.2: the
+ * layer between a model's last hidden states and fef_lmhead_logits or fef_lmhead_verify; with n = V and a bias also an output
+ * layer that has one):
+ *   out[r, j] = act( sum_k hidden[r, k] * weight[j, k] + bias[j] ) + residual[r, j],
+ * products exact, sums and everything behind them in binary32, the result rounded to `dt` once.  With Phi the standard normal
+ * distribution: relu y = max(y, 0); silu y = y / (1 + e^-y); gelu y = y Phi(y);
+ * gelu_tanh y = y / (1 + e^(-2 z)), z = sqrt(2 / pi) (y + 0.044715 y^3).
+ *   hidden      device, bfloat16, row r at hidden + r * ld_hidden, 16-byte aligned, ld_hidden (elements) a multiple of 8
+ *   weight      device, [n, d] bfloat16 row-major, 16-byte aligned
+ *   bias        device, [n] bfloat16, or NULL
+ *   residual    device, bfloat16, row r at residual + r * ld_residual, or NULL
+ *   rows, n, d  1 .. FEF_MAX_TRANSFORM each, d a multiple of 8
+ *   out         device out of dtype `dt`, row r at out + r * ldo; the entries between n and ldo are left as they were.  May be
+ *               the residual itself (same rows, bfloat16); no other overlap
+ *   device_status  device out, [1] int32, or NULL: FEF_OK, or FEF_ERR_TIMEOUT as in fef_spec_verify (`out` is then incomplete)
+ * A row that holds NaN or an infinity affects no other row.  Asynchronous on `cuda_stream`; one kernel.
+ */
+typedef enum { FEF_ACT_NONE = 0, FEF_ACT_RELU = 1, FEF_ACT_SILU = 2, FEF_ACT_GELU = 3, FEF_ACT_GELU_TANH = 4 } fef_activation;
+fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden, const void* weight, const void* bias,
+                                const void* residual, int64_t ld_residual, int rows, int n, int d,
+                                fef_activation activation, void* out, int64_t ldo, fef_dtype dt,
+                                int32_t* device_status, void* cuda_stream);
 
 /*
  * Seeded synthetic logits made on the device (benchmarks and tests of the decoding loop; they stand

@@ -23,6 +23,7 @@ FEF_ERR_CUDA, FEF_ERR_TIMEOUT, FEF_ERR_NONFINITE, FEF_ERR_TOKEN_RANGE, FEF_ERR_T
 FEF_STATIC_SCRATCH_BYTES = 8 << 20
 FEF_F32, FEF_BF16 = 0, 1
 FEF_MAX_K, FEF_MAX_REMASK_L = 64, 8192
+FEF_MAX_TRUNCATE_V = FEF_MAX_TRANSFORM = 1 << 20
 
 EXPORTS = ("fef_status_string", "fef_spec_verify_workspace_bytes", "fef_spec_verify", "fef_spec_verify_profiled",
            "fef_spec_verify_host_arena_bytes", "fef_spec_verify_host", "fef_remask_select",
@@ -35,7 +36,8 @@ EXPORTS = ("fef_status_string", "fef_spec_verify_workspace_bytes", "fef_spec_ver
            "fef_draft_sample_with_target", "fef_spec_verify_with_norms", "fef_synth_logits",
            "fef_loop_run_synthetic_workspace_bytes", "fef_loop_run_synthetic",
            "fef_logits_adjust_workspace_bytes", "fef_logits_adjust", "fef_lmhead_quantize", "fef_lmhead_dequantize",
-           "fef_lmhead_logits_quantized_workspace_bytes", "fef_lmhead_logits_quantized")
+           "fef_lmhead_logits_quantized_workspace_bytes", "fef_lmhead_logits_quantized",
+           "fef_law_truncate", "fef_draft_sample_truncated", "fef_spec_verify_truncated", "fef_hidden_transform")
 
 _lib = None
 
@@ -137,6 +139,16 @@ def load(build_if_missing: bool = False) -> ctypes.CDLL:
     L.fef_logits_adjust.argtypes = [vp, vp, i32, i32, i32, i64, i32, vp, i32, vp, vp, vp, vp, vp, i64, vp, i64, i64, f32, vp,
                                     vp, sz, vp]
     L.fef_logits_adjust.restype = i32
+    L.fef_law_truncate.argtypes = [vp, vp, i32, i32, i32, i64, i32, f32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.fef_law_truncate.restype = i32
+    L.fef_draft_sample_truncated.argtypes = [vp, vp, i32, i32, i32, i64, i32, f32, vp, vp, vp, vp, u64, u32, vp, vp, vp, vp, vp,
+                                             vp, vp, vp, vp]
+    L.fef_draft_sample_truncated.restype = i32
+    L.fef_spec_verify_truncated.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i64, i32, f32, u64, u32, vp,
+                                            vp, vp, vp, vp, sz, vp, vp]
+    L.fef_spec_verify_truncated.restype = i32
+    L.fef_hidden_transform.argtypes = [vp, i64, vp, vp, vp, i64, i32, i32, i32, i32, vp, i64, i32, vp, vp]
+    L.fef_hidden_transform.restype = i32
     L.fef_remask_select.argtypes = [vp, vp, i32, i32, i32, vp, vp, vp]
     L.fef_remask_select.restype = i32
     L.fef_remask_select_host_arena_bytes.argtypes = [i32, i32, i32]
@@ -924,6 +936,207 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+# ------------------------------------------------------------------- laws cut to top-k, top-p and min-p ----
+class TruncatedLaw(NamedTuple):
+    log2_norm: torch.Tensor               # [B, K] float64
+    cut_logit: torch.Tensor               # [B, K] float32, and
+    cut_id: torch.Tensor                  # [B, K] int32: the last entry in the law; (-inf, -1): nothing is cut
+    kept: Optional[torch.Tensor]          # [B, K] int32: entries in the law
+    device_status: Optional[torch.Tensor]  # [1] int32 (read it after synchronising)
+
+
+class TruncatedDraft(NamedTuple):
+    tokens: torch.Tensor    # [B, K] int32, -1 where nothing was drawn
+    conf: torch.Tensor      # [B, K] float32: the tokens' probabilities, -1 where there is none
+    law: TruncatedLaw
+
+
+def _law_arguments(where, logits, temperature, top_k, top_p, min_p, row_len, V, law):
+    """Checks what both calls take; (B, K, V, ld, dtype code, device)."""
+    _all_cuda(logits, top_k, top_p, min_p, row_len, *(law or ()))
+    if logits.dim() != 3 or not logits.is_contiguous():
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    B, K, ld = logits.shape
+    dev = logits.device
+    if not (_is(top_k, torch.int32, (B,), dev) and _is(top_p, torch.float32, (B,), dev) and
+            _is(min_p, torch.float32, (B,), dev) and _is(row_len, torch.int32, (B,), dev)):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    if law is not None and not _is_law(law, (B, K), dev):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    return B, K, ld if V is None else int(V), ld, _dtype_code(logits), dev
+
+
+def _is_law(law: TruncatedLaw, shape, dev) -> bool:
+    return law.log2_norm is not None and law.cut_logit is not None and law.cut_id is not None and \
+        _is(law.log2_norm, torch.float64, shape, dev) and _is(law.cut_logit, torch.float32, shape, dev) and \
+        _is(law.cut_id, torch.int32, shape, dev) and _is(law.kept, torch.int32, shape, dev) and \
+        _is(law.device_status, torch.int32, (1,), dev)
+
+
+def _new_law(B, K, dev) -> TruncatedLaw:
+    return TruncatedLaw(torch.empty((B, K), dtype=torch.float64, device=dev), torch.empty((B, K), dtype=torch.float32, device=dev),
+                        torch.empty((B, K), dtype=torch.int32, device=dev), torch.empty((B, K), dtype=torch.int32, device=dev),
+                        torch.empty(1, dtype=torch.int32, device=dev))
+
+
+def fef_law_truncate(logits: torch.Tensor, temperature: float, top_k: Optional[torch.Tensor] = None,
+                     top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                     row_len: Optional[torch.Tensor] = None, V: Optional[int] = None,
+                     out: Optional[TruncatedLaw] = None, stream=None) -> TruncatedLaw:
+    """Enqueue the cutting of a window's laws to their top-k, top-p and min-p sets (see ``fef_law_truncate`` in
+    include/fef.h): what ``fef_spec_verify_truncated`` takes for the target side.
+
+    ``logits``: ``[B, K, ld]`` CUDA tensor, float32 or bfloat16, contiguous; ``V`` (default ``ld``) entries of each row
+    are used.  ``top_k`` ``[B]`` int32, ``top_p`` and ``min_p`` ``[B]`` float32: each window's own limits; ``None`` turns a
+    rule off for all, 0, 1 and 0 for one window.  Asynchronous on the current (or given) stream.
+    """
+    where = "fef_law_truncate"
+    B, K, V, ld, code, dev = _law_arguments(where, logits, temperature, top_k, top_p, min_p, row_len, V, out)
+    with _at(dev, stream):
+        if out is None:
+            out = _new_law(B, K, dev)
+        st = load().fef_law_truncate(logits.data_ptr(), _ptr(row_len), B, K, V, ld, code, float(temperature), _ptr(top_k),
+                                     _ptr(top_p), _ptr(min_p), out.log2_norm.data_ptr(), out.cut_logit.data_ptr(),
+                                     out.cut_id.data_ptr(), _ptr(out.kept), _ptr(out.device_status), _raw_stream(dev, stream))
+    if st != FEF_OK:
+        raise FefError(st, where)
+    return out
+
+
+def fef_draft_sample_truncated(draft_logits: torch.Tensor, temperature: float, seed: int = 0, step: int = 0,
+                               top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+                               min_p: Optional[torch.Tensor] = None, uniforms: Optional[torch.Tensor] = None,
+                               row_len: Optional[torch.Tensor] = None, V: Optional[int] = None,
+                               out: Optional[TruncatedDraft] = None, stream=None,
+                               device_round: Optional[torch.Tensor] = None) -> TruncatedDraft:
+    """Enqueue one draw per position from laws cut to their top-k, top-p and min-p sets (see
+    ``fef_draft_sample_truncated`` in include/fef.h).
+
+    Arguments as in ``fef_law_truncate``; the random numbers are ``uniforms`` (``[B, K]`` float32 in [0, 1)), or without
+    them Philox's of ``seed`` and ``step`` (plus ``device_round[0]`` when the kernel runs, if given).
+    """
+    where = "fef_draft_sample_truncated"
+    B, K, V, ld, code, dev = _law_arguments(where, draft_logits, temperature, top_k, top_p, min_p, row_len, V,
+                                            None if out is None else out.law)
+    _all_cuda(uniforms, device_round)
+    if not (_is(uniforms, torch.float32, (B, K), dev) and _is(device_round, torch.int32, (1,), dev)):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    if out is not None:
+        _all_cuda(out.tokens, out.conf)
+        if out.tokens is None or not (_is(out.tokens, torch.int32, (B, K), dev) and _is(out.conf, torch.float32, (B, K), dev)):
+            raise FefError(FEF_ERR_INVALID_ARG, where)
+    with _at(dev, stream):
+        if out is None:
+            out = TruncatedDraft(torch.empty((B, K), dtype=torch.int32, device=dev),
+                                 torch.empty((B, K), dtype=torch.float32, device=dev), _new_law(B, K, dev))
+        law = out.law
+        st = load().fef_draft_sample_truncated(
+            draft_logits.data_ptr(), _ptr(row_len), B, K, V, ld, code, float(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+            _ptr(uniforms), int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, _ptr(device_round), out.tokens.data_ptr(),
+            _ptr(out.conf), law.log2_norm.data_ptr(), law.cut_logit.data_ptr(), law.cut_id.data_ptr(), _ptr(law.kept),
+            _ptr(law.device_status), _raw_stream(dev, stream))
+    if st != FEF_OK:
+        raise FefError(st, where)
+    return out
+
+
+def fef_spec_verify_truncated(draft_logits: torch.Tensor, target_logits: torch.Tensor, draft_tokens: torch.Tensor,
+                              temperature: float, seed: int, step: int, draft_law: TruncatedLaw, target_law: TruncatedLaw,
+                              row_len: Optional[torch.Tensor] = None, V: Optional[int] = None,
+                              out: Optional[VerifyResult] = None, workspace: Optional[torch.Tensor] = None, stream=None,
+                              device_round: Optional[torch.Tensor] = None) -> VerifyResult:
+    """Enqueue one verification with both laws cut (see ``fef_spec_verify_truncated`` in include/fef.h): ``draft_law`` from
+    ``fef_draft_sample_truncated`` and ``target_law`` from ``fef_law_truncate``, made from the same logits at the same
+    temperature.  Everything else as in ``fef_spec_verify``."""
+    where = "fef_spec_verify_truncated"
+    _all_cuda(draft_logits, target_logits, draft_tokens, row_len, device_round, workspace, *(out or ()))
+    if draft_logits.dim() != 3 or draft_logits.shape != target_logits.shape or draft_logits.dtype != target_logits.dtype or \
+            not draft_logits.is_contiguous() or not target_logits.is_contiguous():
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    B, K, ld = draft_logits.shape
+    V = ld if V is None else int(V)
+    code, dev = _dtype_code(draft_logits), draft_logits.device
+    if not (target_logits.device == dev and _is(draft_tokens, torch.int32, (B, K), dev) and
+            _is(row_len, torch.int32, (B,), dev) and _is(device_round, torch.int32, (1,), dev) and
+            _is_law(draft_law, (B, K), dev) and _is_law(target_law, (B, K), dev)):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    if out is not None and not (_is(out.accept_len, torch.int32, (B,), dev) and _is(out.tokens, torch.int32, (B, K), dev) and
+                                _is(out.conf, torch.float32, (B, K), dev) and _is(out.device_status, torch.int32, (1,), dev)):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    _check_scratch(workspace, dev, where)
+    with _at(dev, stream):
+        if out is None:
+            out = VerifyResult(torch.empty(B, dtype=torch.int32, device=dev), torch.empty((B, K), dtype=torch.int32, device=dev),
+                               torch.empty((B, K), dtype=torch.float32, device=dev),
+                               torch.empty(1, dtype=torch.int32, device=dev))
+        if workspace is None:
+            workspace = torch.empty(max(fef_spec_verify_workspace_bytes(B, K, V, code), 256), dtype=torch.uint8, device=dev)
+        st = load().fef_spec_verify_truncated(
+            draft_logits.data_ptr(), target_logits.data_ptr(), draft_tokens.data_ptr(), draft_law.log2_norm.data_ptr(),
+            draft_law.cut_logit.data_ptr(), draft_law.cut_id.data_ptr(), target_law.log2_norm.data_ptr(),
+            target_law.cut_logit.data_ptr(), target_law.cut_id.data_ptr(), _ptr(row_len), B, K, V, ld, code, float(temperature),
+            int(seed) & 0xFFFFFFFFFFFFFFFF, int(step) & 0xFFFFFFFF, _ptr(device_round), out.accept_len.data_ptr(),
+            out.tokens.data_ptr(), out.conf.data_ptr(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+            _ptr(out.device_status), _raw_stream(dev, stream))
+    if st != FEF_OK:
+        raise FefError(st, where)
+    return out
+
+
+# ----------------------------------------------------------------- hidden states ahead of the output layer ----
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+
+
+def fef_hidden_transform(hidden: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                         residual: Optional[torch.Tensor] = None, activation: str = "none", dtype=torch.bfloat16,
+                         out: Optional[torch.Tensor] = None, stream=None):
+    """``activation(hidden @ weight.T + bias) + residual`` in one kernel (see ``fef_hidden_transform`` in include/fef.h):
+    a prediction head's layer between a model's last hidden states and the output layer.
+
+    ``hidden`` ``[rows, d]`` and ``residual`` ``[rows, n]`` bfloat16 with any row pitch (``hidden``'s a multiple of 8),
+    ``weight`` ``[n, d]`` bfloat16 contiguous, ``bias`` ``[n]`` bfloat16; ``activation`` one of ``ACTIVATIONS``.  Returns
+    ``(out [rows, n], device_status)``, float32 or bfloat16 (``dtype``, or that of ``out``, which may be ``residual``).
+    """
+    where = "fef_hidden_transform"
+    _all_cuda(hidden, weight, bias, residual, out)
+    if activation not in ACTIVATIONS:
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    dev = hidden.device
+    if hidden.dim() != 2 or weight.dim() != 2 or hidden.shape[1] != weight.shape[1] or hidden.dtype != torch.bfloat16 or \
+            not _is(weight, torch.bfloat16, weight.shape, dev):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    (rows, d), n = hidden.shape, weight.shape[0]
+
+    def pitch(t, columns):
+        """Row pitch of a matrix whose rows are contiguous (elements); what a single row's stride says is not looked at."""
+        if columns > 1 and t.stride(1) != 1:
+            raise FefError(FEF_ERR_INVALID_ARG, where)
+        return t.stride(0) if rows > 1 else columns
+
+    if not _is(bias, torch.bfloat16, (n,), dev):
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    for t in (residual, out):
+        if t is not None and (t.shape != (rows, n) or t.device != dev):
+            raise FefError(FEF_ERR_INVALID_ARG, where)
+    if residual is not None and residual.dtype != torch.bfloat16:
+        raise FefError(FEF_ERR_INVALID_ARG, where)
+    dtype = dtype if out is None else out.dtype
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise FefError(FEF_ERR_DTYPE, where)
+    with _at(dev, stream):
+        if out is None:
+            out = torch.empty((rows, n), dtype=dtype, device=dev)
+        status = torch.empty(1, dtype=torch.int32, device=dev)
+        st = load().fef_hidden_transform(
+            hidden.data_ptr(), pitch(hidden, d), weight.data_ptr(), _ptr(bias), _ptr(residual),
+            0 if residual is None else pitch(residual, n), rows, n, d, ACTIVATIONS[activation], out.data_ptr(), pitch(out, n),
+            FEF_F32 if dtype == torch.float32 else FEF_BF16, status.data_ptr(), _raw_stream(dev, stream))
+    if st != FEF_OK:
+        raise FefError(st, where)
+    return out, status
+
+
 __all__ += ["QuantizedLayer", "fef_lmhead_quantize", "fef_lmhead_dequantize", "fef_lmhead_logits_quantized",
             "fef_lmhead_logits_quantized_workspace_bytes", "AdjustResult", "fef_logits_adjust",
-            "fef_logits_adjust_workspace_bytes"]
+            "fef_logits_adjust_workspace_bytes", "TruncatedLaw", "TruncatedDraft", "fef_law_truncate",
+            "fef_draft_sample_truncated", "fef_spec_verify_truncated", "ACTIVATIONS", "fef_hidden_transform"]

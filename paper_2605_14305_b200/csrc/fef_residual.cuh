@@ -122,8 +122,8 @@ static __device__ void block_sum2(double& a, double& b, ResidualShared& sh) {
 // are passed over after one multiply, as in the fast pass.  Whole CTA; every thread returns the
 // same (Z, pi(Z)).  Slow (a pass of double-precision exponentials by one CTA): only for draws that
 // the bounds of the fast pass cannot decide.
-template <int DT>
-__device__ void exact_row_draw(const VerifyParams& P, const char* prow, const char* qrow, uint32_t ub, uint32_t upos,
+template <int DT, bool CUT>
+__device__ void exact_row_draw(const VerifyParams& P, const char* prow, const char* qrow, const Cuts<CUT>& cuts, uint32_t ub, uint32_t upos,
                                double kp_nom, double kq_nom, float slack, float floor_w, ResidualShared& sh, int& Z,
                                double& piZ) {
     const int V = P.geo.V;
@@ -131,7 +131,7 @@ __device__ void exact_row_draw(const VerifyParams& P, const char* prow, const ch
     // normalisers: sum_x 2^(l_x c - k_nominal) is within 1e-5 of one, so nothing can overflow
     double sp = 0.0, sq = 0.0;
     for (int x = threadIdx.x; x < V; x += kResidualThreads) {
-        const double lp = load_logit<DT>(prow, x), lq = load_logit<DT>(qrow, x);
+        const double lp = law_logit<DT, CUT>(prow, x, cuts.p), lq = law_logit<DT, CUT>(qrow, x, cuts.q);
         if (lp > -INFINITY) sp += exp2(lp * c - kp_nom);
         if (lq > -INFINITY) sq += exp2(lq * c - kq_nom);
     }
@@ -151,7 +151,7 @@ __device__ void exact_row_draw(const VerifyParams& P, const char* prow, const ch
             for (int k = 0; k < 4; ++k) {
                 const int x = x0 + k;
                 if (x >= V) break;
-                const float lpf = load_logit<DT>(prow, x), lqf = load_logit<DT>(qrow, x);
+                const float lpf = law_logit<DT, CUT>(prow, x, cuts.p), lqf = law_logit<DT, CUT>(qrow, x, cuts.q);
                 const float ep = exp2_scaled<DT>(lpf, P.c_hi, P.c_lo, kp32);
                 const float rs = fmaf(ep, slack, ep - exp2_scaled<DT>(lqf, P.c_hi, P.c_lo, kq32));
                 const uint32_t word = pick_word(w, k);
@@ -176,7 +176,7 @@ __device__ void exact_row_draw(const VerifyParams& P, const char* prow, const ch
         score = -INFINITY;
         best = 0x7FFFFFFF;
         for (int x = threadIdx.x; x < V; x += kResidualThreads) {
-            const double l = load_logit<DT>(prow, x);
+            const double l = law_logit<DT, CUT>(prow, x, cuts.p);
             if (l > score) {
                 score = l;
                 best = x;
@@ -185,7 +185,7 @@ __device__ void exact_row_draw(const VerifyParams& P, const char* prow, const ch
         block_argmax(score, best, sh);
     }
     Z = best;
-    piZ = (best >= 0 && best < V) ? exp2(static_cast<double>(load_logit<DT>(prow, best)) * c - kp) : 0.0;
+    piZ = (best >= 0 && best < V) ? exp2(static_cast<double>(law_logit<DT, CUT>(prow, best, cuts.p)) * c - kp) : 0.0;
 }
 
 // Rare path of the residual pass, out of line so that the loop around it stays small: the id's
@@ -238,8 +238,10 @@ __device__ __forceinline__ float shared_floor(const unsigned* best3) {
 // best ids are compared afterwards by their scores under the shared normalisers, so the decision
 // among this slice's candidates is taken on those scores (candidates within a band of the largest
 // bound are scored in double precision) and reported instead of committed.
-// prow, qrow: the target and draft logits of the rejected position; out_row: where tokens / conf go.
-template <int DT, bool REPORT, bool CLUSTER>
+// prow, qrow: the target and draft logits of the rejected position; out_row: where tokens / conf go (and where the laws'
+// cuts stand).
+// CUT: both laws are cut (their normalisers are the cut laws' own): an entry outside a law is read as -inf.
+template <int DT, bool REPORT, bool CLUSTER, bool CUT = false>
 __device__ void residual_draw(const VerifyParams& P, int b, int pos, double kp_d, double kq_d, const char* prow,
                               const char* qrow, int64_t out_row, int part, int parts, ResidualShared& sh) {
     constexpr int N = Elem<DT>::kPerVec;
@@ -257,6 +259,8 @@ __device__ void residual_draw(const VerifyParams& P, int b, int pos, double kp_d
 
     PhiloxRow rng;
     rng.prepare(P.keys, ub, upos, step_of(P));
+    Cuts<CUT> cuts;
+    cuts.fetch(P, out_row);
 
     Top3 top;
     top.clear();
@@ -286,6 +290,13 @@ __device__ void residual_draw(const VerifyParams& P, int b, int pos, double kp_d
         float lp[N], lq[N];
         unpack<DT>(wp, lp);
         unpack<DT>(wq, lq);
+        if constexpr (CUT) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                lp[i] = cuts.p.apply(lp[i], vec * N + i);
+                lq[i] = cuts.q.apply(lq[i], vec * N + i);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const float ep = exp2_scaled<DT>(lp[i], P.c_hi, P.c_lo, kp);
@@ -363,8 +374,8 @@ __device__ void residual_draw(const VerifyParams& P, int b, int pos, double kp_d
     // tail elements (beyond the last whole vector) belong to part 0
     if (part == 0) {
         for (int x = G.vec_elems + threadIdx.x; x < G.V; x += kResidualThreads) {
-            const float ep = exp2_scaled<DT>(load_logit<DT>(prow, x), P.c_hi, P.c_lo, kp);
-            const float rsx = fmaf(ep, slack, ep - exp2_scaled<DT>(load_logit<DT>(qrow, x), P.c_hi, P.c_lo, kq));
+            const float ep = exp2_scaled<DT>(law_logit<DT, CUT>(prow, x, cuts.p), P.c_hi, P.c_lo, kp);
+            const float rsx = fmaf(ep, slack, ep - exp2_scaled<DT>(law_logit<DT, CUT>(qrow, x, cuts.q), P.c_hi, P.c_lo, kq));
             if (rsx > 0.f) {
                 const uint4 w = rng.draw(P.keys, (kStreamResidual << 30) | (static_cast<uint32_t>(x + P.vocab_offset) >> 2));
                 top = offer_bound(top, rsx, one_minus_uniform(pick_word(w, x & 3)), x, sh.best3);
@@ -451,8 +462,8 @@ __device__ void residual_draw(const VerifyParams& P, int b, int pos, double kp_d
             float lpf = 0.f, lqf = 0.f, lb32 = -1.f, ub32 = 0.f;
             uint32_t word = 0u;
             if (have) {
-                lpf = load_logit<DT>(prow, xe);
-                lqf = load_logit<DT>(qrow, xe);
+                lpf = law_logit<DT, CUT>(prow, xe, cuts.p);
+                lqf = law_logit<DT, CUT>(qrow, xe, cuts.q);
                 word = pick_word(rng.draw(P.keys, (kStreamResidual << 30) | (static_cast<uint32_t>(xe + P.vocab_offset) >> 2)),
                                  xe & 3);
                 const float ep = exp2_scaled<DT>(lpf, P.c_hi, P.c_lo, kp);
@@ -501,7 +512,7 @@ __device__ void residual_draw(const VerifyParams& P, int b, int pos, double kp_d
         if (!sh.exact) return;
         int Z;
         double piZ;
-        exact_row_draw<DT>(P, prow, qrow, ub, upos, kp_d, kq_d, slack, sh.exact_floor, sh, Z, piZ);
+        exact_row_draw<DT, CUT>(P, prow, qrow, cuts, ub, upos, kp_d, kq_d, slack, sh.exact_floor, sh, Z, piZ);
         if (threadIdx.x == 0) {
             if (Z < 0 || Z >= G.V) {  // no finite target logit: the scan has reported such a row already
                 P.tokens[out_row] = -1;

@@ -864,7 +864,7 @@ __device__ __forceinline__ int accept_test(const VerifyParams& P, int b, int i, 
 // What the acceptance tests need besides the normalisers, fetched before those are waited for: the
 // draft token of "my" position and the two logits at it.  Thread form: position threadIdx.x.  Warp
 // form (wide): lane j of warp w holds position w + j * kResidualWarps.
-template <int DT>
+template <int DT, bool CUT>
 __device__ __forceinline__ void fetch_my_position(const VerifyParams& P, int b, int n, bool wide, int& my, int& x,
                                                   double& lpx, double& lqx) {
     const Geometry& G = P.geo;
@@ -878,8 +878,10 @@ __device__ __forceinline__ void fetch_my_position(const VerifyParams& P, int b, 
         const int64_t row = static_cast<int64_t>(b) * G.K + my;
         x = __ldg(P.draft_tokens + row);
         if (x >= 0 && x < G.V) {
-            lpx = load_logit<DT>(P.target + row * G.ld_bytes, x);
-            lqx = load_logit<DT>(P.draft + row * G.ld_bytes, x);
+            Cuts<CUT> cuts;
+            cuts.fetch(P, row);
+            lpx = law_logit<DT, CUT>(P.target + row * G.ld_bytes, x, cuts.p);
+            lqx = law_logit<DT, CUT>(P.draft + row * G.ld_bytes, x, cuts.q);
         }
     }
 }
@@ -982,7 +984,7 @@ __device__ __forceinline__ void write_window_undecided(const VerifyParams& P, in
     if (threadIdx.x == 0) P.accept_len[b] = -1;
 }
 
-template <int DT, bool CLUSTER>
+template <int DT, bool CLUSTER, bool CUT>
 __global__ void __launch_bounds__(kResidualThreads, kResidualCtasPerSm) tail_kernel(const __grid_constant__ VerifyParams P) {
     const Geometry& G = P.geo;
     __shared__ TailShared ts;
@@ -996,7 +998,7 @@ __global__ void __launch_bounds__(kResidualThreads, kResidualCtasPerSm) tail_ker
 
     int my, x;
     double lpx, lqx;
-    fetch_my_position<DT>(P, b, n, wide, my, x, lpx, lqx);
+    fetch_my_position<DT, CUT>(P, b, n, wide, my, x, lpx, lqx);
     if (threadIdx.x == 0) {
         ts.rejected[0] = ts.rejected[1] = 0u;
         ts.err = 0;
@@ -1015,7 +1017,7 @@ __global__ void __launch_bounds__(kResidualThreads, kResidualCtasPerSm) tail_ker
     if (part == 0) write_window(P, b, a, err, ts);
     if (err || a >= n) return;  // uniform over the CTA (and over the window's CTAs)
     const int64_t row = static_cast<int64_t>(b) * G.K + a;
-    residual_draw<DT, false, CLUSTER>(P, b, a, ts.kp[a], ts.kq[a], P.target + row * G.ld_bytes,
+    residual_draw<DT, false, CLUSTER, CUT>(P, b, a, ts.kp[a], ts.kq[a], P.target + row * G.ld_bytes,
                                                                     P.draft + row * G.ld_bytes, row, part,
                                                                     static_cast<int>(gridDim.x), sh);
 }
@@ -1493,10 +1495,10 @@ static cudaError_t launch_all(const VerifyParams& P, int dev, cudaStream_t strea
                                      stream, P);
             if (e != cudaSuccess) return e;
             if (G.residual_ctas <= kMaxClusterCtas)
-                e = launch_dependent_cluster(G.residual_ctas, tail_kernel<DT, true>, dim3(G.residual_ctas, G.B),
+                e = launch_dependent_cluster(G.residual_ctas, tail_kernel<DT, true, false>, dim3(G.residual_ctas, G.B),
                                              dim3(kResidualThreads), 0, stream, P);
             else
-                e = launch_dependent(tail_kernel<DT, false>, dim3(G.residual_ctas, G.B), dim3(kResidualThreads), 0, stream, P);
+                e = launch_dependent(tail_kernel<DT, false, false>, dim3(G.residual_ctas, G.B), dim3(kResidualThreads), 0, stream, P);
             if (e != cudaSuccess) return e;
             return cudaGetLastError();
         }
@@ -1534,11 +1536,13 @@ static cudaError_t launch_all(const VerifyParams& P, int dev, cudaStream_t strea
             e = launch_dependent(scan_kernel<DT>, dim3((G.B + kScanWarps - 1) / kScanWarps), dim3(kScanWarps * 32), 0,
                                  stream, P);
     } else {
+        const bool cut = P.target_cut_logit != nullptr;
         if (G.residual_ctas <= kMaxClusterCtas)
-            e = launch_dependent_cluster(G.residual_ctas, tail_kernel<DT, true>, dim3(G.residual_ctas, G.B),
-                                         dim3(kResidualThreads), 0, stream, P);
+            e = launch_dependent_cluster(G.residual_ctas, cut ? tail_kernel<DT, true, true> : tail_kernel<DT, true, false>,
+                                         dim3(G.residual_ctas, G.B), dim3(kResidualThreads), 0, stream, P);
         else
-            e = launch_dependent(tail_kernel<DT, false>, dim3(G.residual_ctas, G.B), dim3(kResidualThreads), 0, stream, P);
+            e = launch_dependent(cut ? tail_kernel<DT, false, true> : tail_kernel<DT, false, false>, dim3(G.residual_ctas, G.B),
+                                 dim3(kResidualThreads), 0, stream, P);
     }
     if (e != cudaSuccess) return e;
     mark(events, 2, stream);
@@ -1598,13 +1602,23 @@ extern "C" void fef_test_withhold_stage_once(int stage, unsigned long long limit
 }
 #endif
 
+namespace fef {
+struct CutLaws {  // where the laws are cut (fef_spec_verify_truncated): the last entry of each
+    const float* draft_logit;
+    const int32_t* draft_id;
+    const float* target_logit;
+    const int32_t* target_id;
+};
+}  // namespace fef
+
 // Every verification entry point ends here.
 static fef_status verify_impl(const void* draft_logits, const void* target_logits, const int32_t* draft_tokens,
                               const int32_t* row_len, const double* draft_log2_norm, int B, int K, int V, int64_t ld,
                               fef_dtype dt, float temperature, uint64_t seed, uint32_t step, int32_t* accept_len,
                               int32_t* tokens, float* conf, void* workspace, size_t workspace_bytes,
                               int32_t* device_status, void* cuda_stream, void* const* stage_events,
-                              const uint32_t* device_round = nullptr, const double* target_log2_norm = nullptr) {
+                              const uint32_t* device_round = nullptr, const double* target_log2_norm = nullptr,
+                              const fef::CutLaws* cut = nullptr) {
     using namespace fef;
     if (dt != FEF_F32 && dt != FEF_BF16) return FEF_ERR_DTYPE;
     if (!draft_logits || !target_logits || !draft_tokens || !accept_len || !tokens || !conf)
@@ -1664,6 +1678,10 @@ static fef_status verify_impl(const void* draft_logits, const void* target_logit
     P.row_len = row_len;
     P.draft_norm = greedy ? nullptr : draft_log2_norm;
     P.target_norm = (greedy || !draft_log2_norm) ? nullptr : target_log2_norm;
+    P.draft_cut_logit = cut ? cut->draft_logit : nullptr;
+    P.draft_cut_id = cut ? cut->draft_id : nullptr;
+    P.target_cut_logit = cut ? cut->target_logit : nullptr;
+    P.target_cut_id = cut ? cut->target_id : nullptr;
     P.seed = seed;
     P.keys = philox_round_keys(seed);
     P.step = step;
@@ -1737,6 +1755,27 @@ fef_status fef_spec_verify_with_norms(const void* draft_logits, const void* targ
     return verify_impl(draft_logits, target_logits, draft_tokens, row_len, draft_log2_norm, B, K, V, ld, dt,
                        temperature, seed, step, accept_len, tokens, conf, workspace, workspace_bytes, device_status,
                        cuda_stream, nullptr, device_round, target_log2_norm);
+}
+
+fef_status fef_spec_verify_truncated(const void* draft_logits, const void* target_logits, const int32_t* draft_tokens,
+                                     const double* draft_log2_norm, const float* draft_cut_logit,
+                                     const int32_t* draft_cut_id, const double* target_log2_norm,
+                                     const float* target_cut_logit, const int32_t* target_cut_id, const int32_t* row_len,
+                                     int B, int K, int V, int64_t ld, fef_dtype dt, float temperature, uint64_t seed,
+                                     uint32_t step, const uint32_t* device_round, int32_t* accept_len, int32_t* tokens,
+                                     float* conf, void* workspace, size_t workspace_bytes, int32_t* device_status,
+                                     void* cuda_stream) {
+    if (!draft_log2_norm || !target_log2_norm || !draft_cut_logit || !draft_cut_id || !target_cut_logit || !target_cut_id)
+        return FEF_ERR_INVALID_ARG;
+    if (!(temperature > 0.0f)) return FEF_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(draft_log2_norm) & 7) || (reinterpret_cast<uintptr_t>(target_log2_norm) & 7) ||
+        (reinterpret_cast<uintptr_t>(draft_cut_logit) & 3) || (reinterpret_cast<uintptr_t>(draft_cut_id) & 3) ||
+        (reinterpret_cast<uintptr_t>(target_cut_logit) & 3) || (reinterpret_cast<uintptr_t>(target_cut_id) & 3))
+        return FEF_ERR_ALIGNMENT;
+    const fef::CutLaws cut = {draft_cut_logit, draft_cut_id, target_cut_logit, target_cut_id};
+    return verify_impl(draft_logits, target_logits, draft_tokens, row_len, draft_log2_norm, B, K, V, ld, dt, temperature, seed,
+                       step, accept_len, tokens, conf, workspace, workspace_bytes, device_status, cuda_stream, nullptr,
+                       device_round, target_log2_norm, &cut);
 }
 
 fef_status fef_spec_verify_at_round(const void* draft_logits, const void* target_logits,

@@ -2,6 +2,7 @@
 // residual draw (fef_residual.cuh), which the hidden-state entry point reuses.
 #pragma once
 
+#include <math.h>
 #include <stdint.h>
 
 #include "fef.h"
@@ -41,6 +42,10 @@ struct VerifyParams {
     const double* draft_norm;  // [B*K] log2 normalisers of the draft laws, or null: stream the draft rows
     const double* target_norm; // [B*K] log2 normalisers of the target laws, or null (given only together with draft_norm:
                                // then nothing is streamed)
+    const float* draft_cut_logit;   // [B*K] last entry of each draft law that is cut, or null: laws that are not cut.  All
+    const int32_t* draft_cut_id;    // four are given, together with both normalisers, or none
+    const float* target_cut_logit;
+    const int32_t* target_cut_id;
     float c_hi, c_lo;     // log2(e)/T split in two binary32 numbers, c_lo > 0 (or 0 for bfloat16)
     double c_exact;       // log2(e)/T in double precision (the double-precision pass of the residual draw)
     double norm_scale;    // c_hi + c_lo over log2(e)/T: what given normalisers are multiplied by.  A bfloat16 law is evaluated with
@@ -68,6 +73,31 @@ struct VerifyParams {
 // (read when the kernel runs, so that a replayed CUDA graph draws fresh random numbers).
 __device__ __forceinline__ uint32_t step_of(const VerifyParams& P) {
     return P.step + (P.round ? __ldg(P.round) : 0u);
+}
+
+// The last entry of a cut law: entries with a smaller logit, or the same logit and a larger id, have probability zero.
+struct Cut {
+    float logit;
+    int id;
+    __device__ __forceinline__ float apply(float l, int x) const { return l > logit || (l == logit && x <= id) ? l : -INFINITY; }
+};
+// The cuts of one position's two laws (not read where CUT is false).
+template <bool CUT>
+struct Cuts {
+    Cut p, q;
+    __device__ __forceinline__ void fetch(const VerifyParams& P, int64_t row) {
+        if constexpr (CUT) {
+            p.logit = __ldg(P.target_cut_logit + row);
+            p.id = __ldg(P.target_cut_id + row);
+            q.logit = __ldg(P.draft_cut_logit + row);
+            q.id = __ldg(P.draft_cut_id + row);
+        }
+    }
+};
+template <int DT, bool CUT>
+__device__ __forceinline__ float law_logit(const void* row, int64_t v, const Cut& cut) {
+    const float l = load_logit<DT>(row, v);
+    return CUT ? cut.apply(l, static_cast<int>(v)) : l;
 }
 
 }  // namespace fef
