@@ -24,8 +24,14 @@ namespace trunc {
 
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBins = 2048;
+constexpr int kBins = 1024;                          // of a selection
+constexpr int kBinsLog2 = 10;
 constexpr int kBinsPerThread = kBins / kThreads;
+constexpr int kSampleBins = 2048;
+constexpr int kSampleBinsPerThread = kSampleBins / kThreads;
+constexpr int kSample = 8192;                        // entries a row's sample holds
+constexpr int kWarpList = 512;                       // candidates a warp can note down
+constexpr int kList = kWarps * kWarpList;
 constexpr uint32_t kStreamDraft = 2u;   // the draft draws' Philox stream
 
 struct Params {
@@ -52,14 +58,32 @@ struct Params {
     int32_t* status;
 };
 
+struct Border {                      // an entry, and what stands before it
+    unsigned long long place, above_mass;
+    unsigned above_count;
+};
+
 struct Shared {
-    unsigned long long mass[kBins];
-    unsigned count[kBins];
+    union {
+        struct {
+            unsigned long long mass[kBins];
+            unsigned count[kBins];
+        };
+        unsigned sample[kSampleBins];
+    };
+    uint32_t id[kList];              // candidates: warp w's at w * kWarpList
+    uint32_t key[kList];             // their logits' order
+    unsigned listed[kWarps];
     unsigned long long warp_mass[kWarps];
     unsigned warp_count[kWarps];
     double red[kWarps];
-    unsigned long long found, lo, hi, above_mass;
+    float red_f[kWarps][2];
+    unsigned long long few_place[32], few_weight[32];   // a bin with few entries
+    unsigned few;
+    unsigned long long lo, hi, above_mass;
     unsigned above_count, in_bin;
+    Border border;
+    float from;                      // candidates are the logits from here on
     int bad;
 };
 
@@ -119,24 +143,34 @@ __device__ unsigned long long block_sum(unsigned long long v, Shared& sh) {
     return v;
 }
 
+__device__ unsigned long long block_min(unsigned long long v, Shared& sh) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = min(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sh.warp_mass[threadIdx.x >> 5] = v;
+    __syncthreads();
+    for (int w = 0; w < kWarps; ++w) v = min(v, sh.warp_mass[w]);
+    return v;
+}
+
 // The first place, from the largest down, at which `enough(count, mass)` of the entries down to it holds; the places are
-// those that each(f) hands to f(place, weight), all in [lo, hi], and all distinct.  `enough` is monotone and true for all of
-// them together (otherwise the last place with an entry is returned).  Every level cuts the range into 2048 bins and goes on
-// with the one the border is in.
+// those that each(f) hands to f(place, weight), all in [lo, hi], and all distinct.  `enough` is monotone; where it does not hold
+// for all of them together, the last place is returned.  Every level cuts the range into 1024 bins and goes on with the one
+// the border is in; one with at most 32 entries is settled by a warp.
 template <class Each, class Enough>
-__device__ unsigned long long select(Each each, Enough enough, unsigned long long lo, unsigned long long hi, Shared& sh) {
+__device__ Border select(Each each, Enough enough, unsigned long long lo, unsigned long long hi, Shared& sh) {
     unsigned long long above_mass = 0;
     unsigned above_count = 0;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (;;) {
         const int bits = 64 - __clzll(static_cast<long long>(hi - lo) | 1ll);
-        const int shift = bits > 11 ? bits - 11 : 0;
+        const int shift = bits > kBinsLog2 ? bits - kBinsLog2 : 0;
         __syncthreads();
         for (int b = threadIdx.x; b < kBins; b += kThreads) {
             sh.mass[b] = 0;
             sh.count[b] = 0;
         }
-        if (threadIdx.x == 0) sh.in_bin = 0;
+        if (threadIdx.x == 0) sh.few = 0;
         __syncthreads();
         each([&](unsigned long long place, auto&& weight) {
             if (place >= lo && place <= hi) {
@@ -174,12 +208,14 @@ __device__ unsigned long long select(Each each, Enough enough, unsigned long lon
         pn += above_count - ns;
         pm += above_mass - ms;
         unsigned all = above_count;
+#pragma unroll
         for (int w = 0; w < kWarps; ++w) {
+            const unsigned wn = sh.warp_count[w];
             if (w < warp) {
-                pn += sh.warp_count[w];
+                pn += wn;
                 pm += sh.warp_mass[w];
             }
-            all += sh.warp_count[w];
+            all += wn;
         }
 #pragma unroll
         for (int j = 0; j < kBinsPerThread; ++j) {
@@ -190,7 +226,8 @@ __device__ unsigned long long select(Each each, Enough enough, unsigned long lon
                     sh.above_count = pn;
                     sh.above_mass = pm;
                     sh.in_bin = n[j];
-                    const unsigned long long from = lo + (static_cast<unsigned long long>(kBins - 1 - (threadIdx.x * kBinsPerThread + j)) << shift);
+                    const unsigned long long from =
+                        lo + (static_cast<unsigned long long>(kBins - 1 - (threadIdx.x * kBinsPerThread + j)) << shift);
                     sh.lo = from;
                     const unsigned long long to = from + ((1ull << shift) - 1);
                     sh.hi = to < hi ? to : hi;
@@ -204,67 +241,125 @@ __device__ unsigned long long select(Each each, Enough enough, unsigned long lon
         hi = sh.hi;
         above_count = sh.above_count;
         above_mass = sh.above_mass;
-        if (shift == 0) return lo;
-        if (sh.in_bin <= 1) {   // (0: there was no entry at all)
-            each([&](unsigned long long place, auto&&) {
-                if (place >= lo && place <= hi) sh.found = place;
+        if (sh.in_bin <= 32) {
+            each([&](unsigned long long place, auto&& weight) {
+                if (place >= lo && place <= hi) {
+                    const unsigned at = atomicAdd(&sh.few, 1u);
+                    sh.few_place[at] = place;
+                    sh.few_weight[at] = weight();
+                }
             });
             __syncthreads();
-            return sh.found;
+            if (warp == 0) {
+                const int have = static_cast<int>(sh.few);
+                const unsigned long long mine = lane < have ? sh.few_place[lane] : 0ull;
+                unsigned c = above_count;
+                unsigned long long s = above_mass;
+                for (int j = 0; j < have; ++j)
+                    if (sh.few_place[j] > mine) {
+                        ++c;
+                        s += sh.few_weight[j];
+                    }
+                const bool before = c > 0 && enough(c, s);
+                if (lane < have && !before && (c + 1 == above_count + have || enough(c + 1, s + sh.few_weight[lane]))) {
+                    sh.border.place = mine;
+                    sh.border.above_mass = s;
+                    sh.border.above_count = c;
+                }
+            }
+            __syncthreads();
+            return sh.border;
         }
     }
 }
 
-// One row by the whole CTA, every step a pass over the row.
-template <int DT>
-__device__ void row_by_passes(const Params& P, int64_t at, int b, int i, Shared& sh) {
-    Row r;
-    r.base = P.logits + at * P.ld_bytes;
-    r.V = P.V;
-    r.vec_elems = P.vec_elems;
-    r.c = P.c;
-    r.one = P.one;
+// What a position asks for.
+struct Limits {
+    int k;
+    float p, m;
+    double u;
+    bool k_on, p_on, m_on, bad;
+    // w >= m where l - M >= this
+    __device__ __forceinline__ double least(const Params& P) const { return P.T * log(fmin(static_cast<double>(m), 1.0)); }
+};
 
-    float top = -INFINITY;
-    int bad = 0;
-    for_each<DT>(r, [&](float l, int) {
-        bad |= !(l < INFINITY);
-        top = fmaxf(top, l);
-    });
-    const int k = P.top_k ? __ldg(P.top_k + b) : 0;
-    const float p = P.top_p ? __ldg(P.top_p + b) : 1.f, m = P.min_p ? __ldg(P.min_p + b) : 0.f;
-    double u = 0.0;
+__device__ __forceinline__ Limits limits_of(const Params& P, int64_t at, int b, int i) {
+    Limits r;
+    r.k = P.top_k ? __ldg(P.top_k + b) : 0;
+    r.p = P.top_p ? __ldg(P.top_p + b) : 1.f;
+    r.m = P.min_p ? __ldg(P.min_p + b) : 0.f;
+    r.u = 0.0;
     if (P.tokens) {
         if (P.uniforms) {
-            u = __ldg(P.uniforms + at);
+            r.u = __ldg(P.uniforms + at);
         } else {
             const uint4 w = philox4x32_10(make_uint4(kStreamDraft << 30, static_cast<uint32_t>(b), static_cast<uint32_t>(i),
                                                      P.step + (P.round ? __ldg(P.round) : 0u)),
                                           make_uint2(static_cast<uint32_t>(P.seed), static_cast<uint32_t>(P.seed >> 32)));
-            u = uniform_from_word(w.x);
+            r.u = uniform_from_word(w.x);
         }
     }
-    bad |= p != p || m != m || u != u;
+    r.k_on = r.k > 0 && r.k < P.V;
+    r.p_on = r.p < 1.f;
+    r.m_on = r.m > 0.f;
+    r.bad = r.p != r.p || r.m != r.m || r.u != r.u;
+    r.u = fmin(fmax(r.u, 0.0), 1.0 - 0x1p-24);
+    return r;
+}
+
+// A position without a law: behind its window's end, or (error) one whose row or limits are no numbers.
+__device__ __forceinline__ void write_none(const Params& P, int64_t at, bool error) {
+    const float nan = __int_as_float(0x7FC00000);
+    P.log2_norm[at] = error ? nan : 0.0;
+    P.cut_logit[at] = error ? nan : 0.f;
+    P.cut_id[at] = -1;
+    if (P.kept) P.kept[at] = 0;
+    if (P.tokens) P.tokens[at] = -1;
+    if (P.conf) P.conf[at] = -1.f;
+    if (error) report(P.status, FEF_ERR_NONFINITE);
+}
+
+// The law is known: its smallest place (0: nothing is cut), its weight and its entries.
+__device__ __forceinline__ void write_law(const Params& P, int64_t at, const Row& r, unsigned long long cut,
+                                          unsigned long long total, unsigned kept) {
+    P.log2_norm[at] = static_cast<double>(r.top) * P.c + log2(static_cast<double>(total) / P.one);
+    P.cut_logit[at] = cut ? logit_of(static_cast<uint32_t>(cut >> 32)) : -INFINITY;
+    P.cut_id[at] = cut ? static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(cut)) : -1;
+    if (P.kept) P.kept[at] = static_cast<int>(kept);
+}
+
+template <int DT>
+__device__ __forceinline__ void write_token(const Params& P, int64_t at, const Row& r, unsigned long long total, int x) {
+    P.tokens[at] = x;
+    if (P.conf)
+        P.conf[at] = static_cast<float>(exp2((static_cast<double>(load_logit<DT>(r.base, x)) - static_cast<double>(r.top)) * P.c) *
+                                        (P.one / static_cast<double>(total)));
+}
+
+// Ids as places: the lowest comes first.
+__device__ __forceinline__ unsigned long long place_of_id(int x) { return 0xFFFFFFFFull - static_cast<unsigned>(x); }
+
+// ------------------------------------------------------------------ passes over the row ----
+// One row by the whole CTA, every step a pass over the row: right for every row, and slow.
+template <int DT>
+__device__ void row_by_passes(const Params& P, int64_t at, const Limits& lim, Row& r, Shared& sh) {
+    float top = -INFINITY;
+    int bad = lim.bad;
+    for_each<DT>(r, [&](float l, int) {
+        bad |= !(l < INFINITY);
+        top = fmaxf(top, l);
+    });
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     __syncthreads();
     if (threadIdx.x == 0) sh.bad = 0;
-    if ((threadIdx.x & 31) == 0) sh.red[threadIdx.x >> 5] = top;
+    if ((threadIdx.x & 31) == 0) sh.red_f[threadIdx.x >> 5][0] = top;
     __syncthreads();
     if (bad) sh.bad = 1;
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, static_cast<float>(sh.red[w]));
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh.red_f[w][0]);
     __syncthreads();
     if (sh.bad || top == -INFINITY) {
-        if (threadIdx.x == 0) {
-            const float nan = __int_as_float(0x7FC00000);
-            P.log2_norm[at] = nan;
-            P.cut_logit[at] = nan;
-            P.cut_id[at] = -1;
-            if (P.kept) P.kept[at] = 0;
-            if (P.tokens) P.tokens[at] = -1;
-            if (P.conf) P.conf[at] = -1.f;
-            report(P.status, FEF_ERR_NONFINITE);
-        }
+        if (threadIdx.x == 0) write_none(P, at, true);
         return;
     }
     r.top = top;
@@ -273,33 +368,25 @@ __device__ void row_by_passes(const Params& P, int64_t at, int b, int i, Shared&
         for_each<DT>(r, [&](float l, int x) { f(place_of(l, x), [&] { return r.weight(l); }); });
     };
     const unsigned long long first = place_of(-3.402823466e38f, 0x7FFFFFFF), last = place_of(top, 0);
-    const bool k_on = k > 0 && k < P.V, p_on = p < 1.f, m_on = m > 0.f;
     unsigned long long cut = 0;   // the smallest place in the law; 0: all of them
-    if (k_on) {
-        const unsigned most = static_cast<unsigned>(k);
-        cut = select(places, [=](unsigned n, unsigned long long) { return n >= most; }, first, last, sh);
+    if (lim.k_on) {
+        const unsigned most = static_cast<unsigned>(lim.k);
+        cut = select(places, [=](unsigned n, unsigned long long) { return n >= most; }, first, last, sh).place;
     }
-    if (p_on) {
+    if (lim.p_on) {
         unsigned long long sum = 0;
         for_each<DT>(r, [&](float l, int x) { sum += place_of(l, x) >= cut ? r.weight(l) : 0ull; });
-        const double target = static_cast<double>(p) * static_cast<double>(block_sum(sum, sh));
-        const unsigned long long cut_p =
-            select(places, [=](unsigned, unsigned long long s) { return static_cast<double>(s) >= target; }, first, last, sh);
-        cut = max(cut, cut_p);
+        const double target = static_cast<double>(lim.p) * static_cast<double>(block_sum(sum, sh));
+        cut = max(cut, select(places, [=](unsigned, unsigned long long s) { return static_cast<double>(s) >= target; }, first, last,
+                              sh).place);
     }
-    if (m_on) {   // w >= m where l - M >= T ln m
-        const double least = P.T * log(fmin(static_cast<double>(m), 1.0));
+    if (lim.m_on) {
+        const double least = lim.least(P);
         unsigned long long lowest = ~0ull;
         for_each<DT>(r, [&](float l, int x) {
             if (static_cast<double>(l) - static_cast<double>(top) >= least) lowest = min(lowest, place_of(l, x));
         });
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) lowest = min(lowest, __shfl_xor_sync(0xFFFFFFFFu, lowest, o));
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) sh.warp_mass[threadIdx.x >> 5] = lowest;
-        __syncthreads();
-        for (int w = 0; w < kWarps; ++w) lowest = min(lowest, sh.warp_mass[w]);
-        cut = max(cut, lowest);
+        cut = max(cut, block_min(lowest, sh));
     }
     unsigned long long sum = 0;
     unsigned n = 0;
@@ -311,51 +398,426 @@ __device__ void row_by_passes(const Params& P, int64_t at, int b, int i, Shared&
     });
     const unsigned long long total = block_sum(sum, sh);
     const unsigned kept = static_cast<unsigned>(block_sum(n, sh));
-    if (threadIdx.x == 0) {
-        P.log2_norm[at] = static_cast<double>(top) * P.c + log2(static_cast<double>(total) / P.one);
-        P.cut_logit[at] = cut ? logit_of(static_cast<uint32_t>(cut >> 32)) : -INFINITY;
-        P.cut_id[at] = cut ? static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(cut)) : -1;
-        if (P.kept) P.kept[at] = static_cast<int>(kept);
-    }
+    if (threadIdx.x == 0) write_law(P, at, r, cut, total, kept);
     if (!P.tokens) return;
-    const double target = fmin(fmax(u, 0.0), 1.0 - 0x1p-24) * static_cast<double>(total);
+    const double target = lim.u * static_cast<double>(total);
     auto by_id = [&](auto f) {
         for_each<DT>(r, [&](float l, int x) {
-            if (place_of(l, x) >= cut) f(0xFFFFFFFFull - static_cast<unsigned>(x), [&] { return r.weight(l); });
+            if (place_of(l, x) >= cut) f(place_of_id(x), [&] { return r.weight(l); });
         });
     };
-    const unsigned long long drawn =
-        select(by_id, [=](unsigned, unsigned long long s) { return static_cast<double>(s) > target; },
-               0xFFFFFFFFull - static_cast<unsigned>(P.V - 1), 0xFFFFFFFFull, sh);
-    if (threadIdx.x == 0) {
-        const int x = static_cast<int>(0xFFFFFFFFull - drawn);
-        P.tokens[at] = x;
-        if (P.conf)
-            P.conf[at] = static_cast<float>(exp2((static_cast<double>(load_logit<DT>(r.base, x)) - static_cast<double>(top)) * P.c) *
-                                            (P.one / static_cast<double>(total)));
+    const unsigned long long drawn = select(by_id, [=](unsigned, unsigned long long s) { return static_cast<double>(s) > target; },
+                                            place_of_id(P.V - 1), place_of_id(0), sh).place;
+    if (threadIdx.x == 0) write_token<DT>(P, at, r, total, static_cast<int>(0xFFFFFFFFull - drawn));
+}
+
+// ---------------------------------------------------------------------- candidates ----
+// One pass over the row.  A sample of it says from which logit on the entries are noted down ("candidates") so that the law's
+// border is among them; the rest is only summed, in binary32, where top_p needs the whole row's weight.  What the sample says is
+// a guess and is checked afterwards: the candidates are the row's first entries in any case, so a border among them is the
+// border, provided that their exact weight and the rest's, whatever its rounding, put it there.
+
+template <int DT>
+__device__ constexpr float lowest_logit() {
+    return DT == FEF_F32 ? -3.402823466e38f : -3.38953139e38f;
+}
+
+// From which logit on?  False: no rule, or more candidates than there is room for.
+template <int DT>
+__device__ bool candidates_from(const Params& P, const Row& r, const Limits& lim, Shared& sh, float& ref_logit) {
+    constexpr int N = Elem<DT>::kPerVec;
+    constexpr int kPerWarp = kSample / (kWarps * 32 * N);   // vectors of a lane
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr float lowest = lowest_logit<DT>();
+    ref_logit = 0.f;
+    if (r.V <= kList) {   // room for all
+        if (threadIdx.x == 0) sh.from = lowest;
+        return true;
     }
+    if (!lim.k_on && !lim.p_on && !lim.m_on) return false;
+    const int chunks = r.vec_elems / (32 * N);   // of 512 bytes; V > kList = kSample: there are as many as the sample takes
+    float x[kPerWarp * N], top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < kPerWarp; ++j) {
+        const int s = warp * kPerWarp + j;
+        const int chunk = static_cast<int>((static_cast<int64_t>(2 * s + 1) * chunks) / (2 * kPerWarp * kWarps));
+        unpack<DT>(ld_global_nc_v4(r.base + (static_cast<int64_t>(chunk) * 32 + lane) * 16), *reinterpret_cast<float(*)[N]>(x + j * N));
+    }
+#pragma unroll
+    for (int j = 0; j < kPerWarp * N; ++j) top = fmaxf(top, x[j]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    if (lane == 0) sh.red_f[warp][0] = top;
+    for (int b = threadIdx.x; b < kSampleBins; b += kThreads) sh.sample[b] = 0;
+    if (threadIdx.x == 0) {
+        sh.from = lowest;
+        sh.few = 0;   // candidates in the sample
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh.red_f[w][0]);
+    __syncthreads();
+    if (top == -INFINITY) return true;   // (nothing but masked entries seen: those that are left may be few)
+    if (!(top < INFINITY)) return false;
+    ref_logit = top;
+    // distance below the largest sampled logit, in powers of two of the weight; 256 bins per octave of (distance + 1)
+    const float c = static_cast<float>(P.c);
+#pragma unroll
+    for (int j = 0; j < kPerWarp * N; ++j)
+        if (x[j] > -INFINITY)
+            atomicAdd(&sh.sample[min((__float_as_uint(fmaf(top - x[j], c, 1.f)) - 0x3F800000u) >> 15, kSampleBins - 1u)], 1u);
+    __syncthreads();
+    auto edge = [](int b) { return __uint_as_float(0x3F800000u + (static_cast<unsigned>(b) << 15)) - 1.f; };
+    unsigned n[kSampleBinsPerThread], cn = 0;
+    float w[kSampleBinsPerThread], cw = 0.f;
+    const int b0 = threadIdx.x * kSampleBinsPerThread;
+#pragma unroll
+    for (int j = 0; j < kSampleBinsPerThread; ++j) {
+        n[j] = sh.sample[b0 + j];
+        w[j] = static_cast<float>(n[j]) * ex2_approx(-0.5f * (edge(b0 + j) + edge(b0 + j + 1)));
+        cn += n[j];
+        cw += w[j];
+    }
+    unsigned pn = cn;
+    float pw = cw;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned on = __shfl_up_sync(0xFFFFFFFFu, pn, o);
+        const float ow = __shfl_up_sync(0xFFFFFFFFu, pw, o);
+        if (lane >= o) {
+            pn += on;
+            pw += ow;
+        }
+    }
+    if (lane == 31) {
+        sh.warp_count[warp] = pn;
+        sh.red_f[warp][1] = pw;
+    }
+    __syncthreads();
+    pn -= cn;
+    pw -= cw;
+    float all = 0.f;
+#pragma unroll
+    for (int v = 0; v < kWarps; ++v) {
+        if (v < warp) {
+            pn += sh.warp_count[v];
+            pw += sh.red_f[v][1];
+        }
+        all += sh.red_f[v][1];
+    }
+    const float share = static_cast<float>(kSample) / static_cast<float>(r.V);
+    int bin = -1;   // the candidates go down to this bin's end
+    if (lim.k_on) {   // as many in the sample as the first k have there five standard deviations above the mean
+        const float mean = static_cast<float>(lim.k) * share;
+        const unsigned need = static_cast<unsigned>(mean + 5.f * sqrtf(mean) + 5.f);
+        unsigned at = pn;
+#pragma unroll
+        for (int j = 0; j < kSampleBinsPerThread; ++j) {
+            if (at < need && at + n[j] >= need) bin = b0 + j;
+            at += n[j];
+        }
+    } else if (lim.p_on) {
+        // The row's weight, rather too low than too high: the sample's largest four count as themselves, the others for their share.
+        float single = 0.f;
+        unsigned at = pn;
+#pragma unroll
+        for (int j = 0; j < kSampleBinsPerThread; ++j) {
+            at += n[j];
+            if (at <= 4) single += w[j];
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) single += __shfl_xor_sync(0xFFFFFFFFu, single, o);
+        if (lane == 0) sh.red_f[warp][0] = single;
+        __syncthreads();
+        single = 0.f;
+#pragma unroll
+        for (int v = 0; v < kWarps; ++v) single += sh.red_f[v][0];
+        const float whole = single + (all - single) / share;
+        const float may_miss = (1.f - fmaxf(lim.p, 0.f)) * whole * share * 0.85f;   // what the sample may hold below the border
+        float below = all - pw;
+#pragma unroll
+        for (int j = 0; j < kSampleBinsPerThread; ++j) {
+            const float next = below - w[j];
+            if (n[j] && below > may_miss && next <= may_miss) bin = b0 + j;
+            below = next;
+        }
+    }
+    if (bin >= 0 && bin < kSampleBins - 1) {   // (one thread, give or take the sums' rounding)
+        sh.from = top - edge(bin + 1) / c;
+        unsigned at = pn;
+#pragma unroll
+        for (int j = 0; j < kSampleBinsPerThread; ++j)
+            if (b0 + j <= bin) at += n[j];
+        sh.few = at;
+    }
+    __syncthreads();
+    const bool many = static_cast<float>(sh.few) > 0.8f * share * kList;
+    float from = fmaxf(sh.from, lowest);
+    if (lim.m_on && !(lim.k_on && lim.p_on))   // (top_p of the first k needs all of them)
+        from = fmaxf(from, __double2float_rd(fmax(static_cast<double>(top) + lim.least(P), static_cast<double>(lowest))));
+    if (DT == FEF_BF16) {   // rounded down
+        uint32_t bits = __float_as_uint(from);
+        if (bits & 0x80000000u) bits += 0xFFFFu;
+        from = fmaxf(__uint_as_float(bits & 0xFFFF0000u), lowest);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) sh.from = from;
+    return !many;
+}
+
+// Bits of the halves of a packed pair that are at least `from` (both halves of from2), all or none set.
+__device__ __forceinline__ uint32_t at_least(uint32_t w, uint32_t from2) {
+    uint32_t r;
+    asm("set.ge.u32.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(from2));
+    return r;
+}
+
+// The pass: ids of the entries from `from` on into the warps' lists, and with SUM the others' sum of 2^(l c - ref).
+// NaN anywhere makes the sum NaN (without SUM it is looked for).  Returns the thread's sum.
+template <int DT, bool SUM>
+__device__ float note_candidates(const Row& r, float from, float c, float ref, Shared& sh) {
+    constexpr int N = Elem<DT>::kPerVec;
+    constexpr int kBatch = 4;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned before = (1u << lane) - 1u;
+    uint32_t* list = sh.id + warp * kWarpList;
+    unsigned listed = 0;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    const int chunks = r.vec_elems / (32 * N);
+    constexpr uint32_t kMinusInf = DT == FEF_F32 ? 0xFF800000u : 0xFF80FF80u;
+
+    auto note = [&](bool hit, int x) {
+        const unsigned hits = __ballot_sync(0xFFFFFFFFu, hit);
+        const unsigned at = listed + __popc(hits & before);
+        if (hit && at < kWarpList) list[at] = static_cast<uint32_t>(x);
+        listed += __popc(hits);
+    };
+    auto fetch = [&](int chunk, uint4 (&w)[kBatch]) {
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int at = chunk + j * kWarps;
+            w[j] = make_uint4(kMinusInf, kMinusInf, kMinusInf, kMinusInf);
+            if (at < chunks) w[j] = ld_global_nc_v4(r.base + (static_cast<int64_t>(at) * 32 + lane) * 16);
+        }
+    };
+    uint4 w[kBatch], next[kBatch];
+    fetch(warp, w);
+#pragma unroll 1
+    for (int chunk = warp; chunk < chunks; chunk += kBatch * kWarps) {
+        fetch(chunk + kBatch * kWarps, next);
+        uint32_t mask = 0;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+            if constexpr (DT == FEF_BF16) {
+                const uint32_t from2 = __float_as_uint(from) | __float_as_uint(from) >> 16;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t hit = at_least(v[q], from2);
+                    mask |= hit & (0x00010001u << (4 * j + q));
+                    if constexpr (SUM) v[q] = (v[q] & ~hit) | (0xFF80FF80u & hit);
+                    const float a = __uint_as_float(v[q] << 16), b = __uint_as_float(v[q] & 0xFFFF0000u);
+                    if constexpr (SUM) {
+                        sum[(2 * q) & 3] += ex2_approx(fmaf(a, c, -ref));
+                        sum[(2 * q + 1) & 3] += ex2_approx(fmaf(b, c, -ref));
+                    } else {
+                        sum[0] += a != a || b != b ? 1.f : 0.f;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float a = __uint_as_float(v[q]);
+                    const bool hit = a >= from;
+                    mask |= hit ? 1u << (4 * j + q) : 0u;
+                    if constexpr (SUM)
+                        sum[q] += ex2_approx(fmaf(hit ? -INFINITY : a, c, -ref));
+                    else
+                        sum[0] += a != a ? 1.f : 0.f;
+                }
+            }
+        }
+        while (__any_sync(0xFFFFFFFFu, mask != 0u)) {
+            const int bit = __ffs(mask) - 1;
+            int x;
+            if constexpr (DT == FEF_BF16)   // bit 16 h + 4 j + q: half h of word q of vector j
+                x = ((chunk + ((bit >> 2) & 3) * kWarps) * 32 + lane) * N + (bit & 3) * 2 + (bit >> 4);
+            else
+                x = ((chunk + (bit >> 2) * kWarps) * 32 + lane) * N + (bit & 3);
+            note(mask != 0u, x);
+            mask &= mask - 1u;
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) w[j] = next[j];
+    }
+    for (int x0 = chunks * 32 * N + warp * 32; x0 < r.V; x0 += kThreads) {   // what is behind the last whole chunk
+        const int x = x0 + lane;
+        const float a = x < r.V ? load_logit<DT>(r.base, x) : -INFINITY;
+        const bool hit = a >= from;
+        note(hit, x);
+        if constexpr (SUM)
+            sum[0] += ex2_approx(fmaf(hit ? -INFINITY : a, c, -ref));
+        else
+            sum[0] += a != a ? 1.f : 0.f;
+    }
+    if (lane == 0) sh.listed[warp] = listed;
+    const float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    return SUM ? s : (s > 0.f ? __int_as_float(0x7FC00000) : 0.f);
+}
+
+// False: the row needs the other path (nothing has been written).
+template <int DT>
+__device__ bool row_by_candidates(const Params& P, int64_t at, const Limits& lim, Row& r, Shared& sh) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float ref_logit;
+    if (!candidates_from<DT>(P, r, lim, sh, ref_logit)) return false;
+    __syncthreads();
+    const float from = sh.from, c = static_cast<float>(P.c), ref = ref_logit * c;
+    const bool with_sum = lim.p_on && !lim.k_on;
+    const float mine = with_sum ? note_candidates<DT, true>(r, from, c, ref, sh) : note_candidates<DT, false>(r, from, c, ref, sh);
+    __syncwarp();
+    const unsigned listed = sh.listed[warp];
+    uint32_t* id = sh.id + warp * kWarpList;
+    uint32_t* key = sh.key + warp * kWarpList;
+    uint32_t top = 0;
+    for (unsigned j = lane; j < min(listed, static_cast<unsigned>(kWarpList)); j += 32) {
+        key[j] = order_of(load_logit<DT>(r.base, id[j]));
+        top = max(top, key[j]);
+    }
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    const double part = warp_sum(static_cast<double>(mine));
+    if (lane == 0) {
+        sh.red[warp] = part;
+        sh.warp_count[warp] = top;
+    }
+    __syncthreads();
+    double rest = 0.0;
+    unsigned all = 0, most = 0;
+    for (int v = 0; v < kWarps; ++v) {
+        rest += sh.red[v];
+        top = max(top, sh.warp_count[v]);
+        all += sh.listed[v];
+        most = max(most, sh.listed[v]);
+    }
+    __syncthreads();
+    if (!(rest < INFINITY) || most > kWarpList || all == 0) return false;
+    r.top = logit_of(top);
+    if (!(r.top < INFINITY)) return false;
+
+    auto each = [&](auto f) {
+        for (unsigned j = lane; j < listed; j += 32) {
+            const uint32_t k = key[j];
+            f(static_cast<unsigned long long>(k) << 32 | (0xFFFFFFFFu - id[j]), [&] { return r.weight(logit_of(k)); });
+        }
+    };
+    const unsigned long long first = place_of(from, 0x7FFFFFFF), last = place_of(r.top, 0);
+    const bool everything = from == lowest_logit<DT>();
+    // in units of the weights; the terms' relative error: their argument (its rounding and c's, 2^-24 of at most 40; smaller
+    // terms are below 2^-40), the exponential's 2^-22, and as many additions as a thread makes in a row
+    rest = with_sum ? rest * exp2(static_cast<double>(ref) - static_cast<double>(r.top) * static_cast<double>(c)) * P.one : 0.0;
+    double slack = 4.0e-6 + (static_cast<double>(r.V) / (4 * kThreads) + 32.0) * 0x1p-24;
+    unsigned long long cut = 0;
+    if (lim.k_on) {
+        if (all < static_cast<unsigned>(lim.k) && !everything) {
+            if (lim.p_on || !lim.m_on) return false;
+        } else {
+            const unsigned n_k = static_cast<unsigned>(lim.k);
+            cut = select(each, [=](unsigned n, unsigned long long) { return n >= n_k; }, first, last, sh).place;
+        }
+    }
+    if (lim.p_on) {
+        unsigned long long mine_sum = 0;
+        each([&](unsigned long long place, auto&& weight) { mine_sum += place >= cut ? weight() : 0ull; });
+        const double listed_sum = static_cast<double>(block_sum(mine_sum, sh)), p = lim.p;
+        for (;;) {
+            const double least = p * (listed_sum + rest * (1.0 - slack)), most_of_it = p * (listed_sum + rest * (1.0 + slack) + slack * 0x1p-20 * P.one);
+            if (listed_sum < least) {   // beyond the candidates
+                if (!lim.m_on) return false;
+                break;
+            }
+            const double target = p * (listed_sum + rest);
+            const Border b = select(each, [=](unsigned, unsigned long long s) { return static_cast<double>(s) >= target; }, first, last, sh);
+            const double with_it = static_cast<double>(b.above_mass + r.weight(logit_of(static_cast<uint32_t>(b.place >> 32))));
+            const bool sure = with_it >= (rest > 0.0 ? most_of_it : target) && (b.above_count == 0 || static_cast<double>(b.above_mass) < least);
+            if (sure || rest == 0.0 || slack == 0.0) {
+                if (!(with_it >= target)) return false;
+                cut = max(cut, b.place);
+                break;
+            }
+            // too near to call: the rest once more, exactly
+            unsigned long long sum = 0;
+            for_each<DT>(r, [&](float l, int) { sum += l < from ? r.weight(l) : 0ull; });
+            rest = static_cast<double>(block_sum(sum, sh));
+            slack = 0.0;
+        }
+    }
+    if (lim.m_on) {
+        const double least = lim.least(P);
+        unsigned long long lowest = ~0ull;
+        each([&](unsigned long long place, auto&&) {
+            if (static_cast<double>(logit_of(static_cast<uint32_t>(place >> 32))) - static_cast<double>(r.top) >= least)
+                lowest = min(lowest, place);
+        });
+        lowest = block_min(lowest, sh);
+        // (entries beyond the candidates may belong to the set too: then it is no border, and another rule's is above it)
+        if (everything || static_cast<double>(from) - static_cast<double>(r.top) <= least) cut = max(cut, lowest);
+    }
+    if (!cut && !everything) return false;
+    unsigned long long sum = 0;
+    unsigned n = 0;
+    each([&](unsigned long long place, auto&& weight) {
+        if (place >= cut) {
+            sum += weight();
+            ++n;
+        }
+    });
+    const unsigned long long total = block_sum(sum, sh);
+    const unsigned kept = static_cast<unsigned>(block_sum(n, sh));
+    if (threadIdx.x == 0) write_law(P, at, r, cut, total, kept);
+    if (!P.tokens) return true;
+    const double target = lim.u * static_cast<double>(total);
+    auto by_id = [&](auto f) {
+        each([&](unsigned long long place, auto&& weight) {
+            if (place >= cut) f(place & 0xFFFFFFFFull, weight);
+        });
+    };
+    const unsigned long long drawn = select(by_id, [=](unsigned, unsigned long long s) { return static_cast<double>(s) > target; },
+                                            place_of_id(P.V - 1), place_of_id(0), sh).place;
+    if (threadIdx.x == 0) write_token<DT>(P, at, r, total, static_cast<int>(0xFFFFFFFFull - drawn));
+    return true;
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kThreads) truncate_kernel(const __grid_constant__ Params P) {
-    __shared__ Shared sh;
-    const int64_t rows = static_cast<int64_t>(P.B) * P.K;
-    for (int64_t at = blockIdx.x; at < rows; at += gridDim.x) {
-        const int b = static_cast<int>(at / P.K), i = static_cast<int>(at - static_cast<int64_t>(b) * P.K);
-        if (P.row_len && i >= __ldg(P.row_len + b)) {
-            if (threadIdx.x == 0) {
-                P.log2_norm[at] = 0.0;
-                P.cut_logit[at] = 0.f;
-                P.cut_id[at] = -1;
-                if (P.kept) P.kept[at] = 0;
-                if (P.tokens) P.tokens[at] = -1;
-                if (P.conf) P.conf[at] = -1.f;
-            }
-            continue;
-        }
-        row_by_passes<DT>(P, at, b, i, sh);
-        __syncthreads();
+__global__ void __launch_bounds__(kThreads, 2) truncate_kernel(const __grid_constant__ Params P) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem);
+    const int64_t at = blockIdx.x;
+    const int b = static_cast<int>(at / P.K), i = static_cast<int>(at - static_cast<int64_t>(b) * P.K);
+    if (P.row_len && i >= __ldg(P.row_len + b)) {
+        if (threadIdx.x == 0) write_none(P, at, false);
+        return;
     }
+    const Limits lim = limits_of(P, at, b, i);
+    Row r;
+    r.base = P.logits + at * P.ld_bytes;
+    r.V = P.V;
+    r.vec_elems = P.vec_elems;
+    r.c = P.c;
+    r.one = P.one;
+    if (!lim.bad && row_by_candidates<DT>(P, at, lim, r, sh)) return;
+    row_by_passes<DT>(P, at, lim, r, sh);
+}
+
+template <int DT>
+static cudaError_t launch(const Params& P, int dev, cudaStream_t stream) {
+    static bool allowed[64];   // large shared memory, per device
+    if (dev >= 64 || !allowed[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(truncate_kernel<DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shared));
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev] = true;
+    }
+    truncate_kernel<DT><<<static_cast<unsigned>(P.B * P.K), kThreads, sizeof(Shared), stream>>>(P);
+    return cudaGetLastError();
 }
 
 static fef_status truncate(const void* logits, const int32_t* row_len, int B, int K, int V, int64_t ld, fef_dtype dt,
@@ -378,10 +840,8 @@ static fef_status truncate(const void* logits, const int32_t* row_len, int B, in
                           static_cast<const void*>(device_status)})
         if (reinterpret_cast<uintptr_t>(q) & 3) return FEF_ERR_ALIGNMENT;
     if (reinterpret_cast<uintptr_t>(log2_norm) & 7) return FEF_ERR_ALIGNMENT;
-    int dev = -1, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1)
-        return FEF_ERR_CUDA;
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) return FEF_ERR_CUDA;
 
     Params P = {};
     P.logits = static_cast<const char*>(logits);
@@ -412,13 +872,8 @@ static fef_status truncate(const void* logits, const int32_t* row_len, int B, in
     P.status = device_status;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     if (device_status && cudaMemsetAsync(device_status, 0, sizeof(int32_t), stream) != cudaSuccess) return FEF_ERR_CUDA;
-    const int64_t rows = static_cast<int64_t>(B) * K, most = static_cast<int64_t>(sms) * 4;
-    const unsigned grid = static_cast<unsigned>(rows < most ? rows : most);
-    if (dt == FEF_F32)
-        truncate_kernel<FEF_F32><<<grid, kThreads, 0, stream>>>(P);
-    else
-        truncate_kernel<FEF_BF16><<<grid, kThreads, 0, stream>>>(P);
-    return cudaGetLastError() == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
+    const cudaError_t e = dt == FEF_F32 ? launch<FEF_F32>(P, dev, stream) : launch<FEF_BF16>(P, dev, stream);
+    return e == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
 }
 
 }  // namespace trunc
