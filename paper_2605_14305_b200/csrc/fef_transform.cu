@@ -3,12 +3,18 @@
 // products of bfloat16 numbers summed in binary32, everything behind them in binary32, one rounding to the output's type.
 #include <cuda_runtime.h>
 #include <cuda_bf16.h>
+#include <cooperative_groups.h>
 #include <math.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "fef.h"
 #include "fef_common.cuh"
 #include "fef_device_math.cuh"
+#include "fef_tensor_core.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace fef {
 namespace head {
@@ -21,7 +27,14 @@ struct Params {
     void* out;
     int64_t ld_hidden, ld_residual, ldo;
     int rows, n, d;
+    int act;        // fef_activation
+    int out_f32;    // the output is float32, not bfloat16
+    int split;      // CTAs (one cluster) that share a tile's depth
+    unsigned long long wait_ns;
     int32_t* status;
+#ifdef FEF_TEST_HOOKS
+    int withhold;   // CTA 0 never delivers its stage of this number (-1: none)
+#endif
 };
 
 template <int ACT>
@@ -37,62 +50,386 @@ __device__ __forceinline__ float activate(float y) {
     return y;
 }
 
-template <class T>
-__device__ __forceinline__ void store(void* out, int64_t at, float y) {
-    if constexpr (sizeof(T) == 4)
-        static_cast<float*>(out)[at] = y;
-    else
-        static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(y);
+// ---- kernel ----
+// A CTA takes 128 columns of the output (rows of the weight: the left operand, M = 128) by BN rows (hidden states: the right
+// operand, N = BN), so that few hidden rows cost few columns of tensor memory and no padding of the weight stream.  Warp 0 brings
+// 64-deep blocks of both operands through a ring by TMA (one thread), warp 1 issues the MMAs (one thread), warps 2-5 are the
+// epilogue, a column of the output per lane: a store of a warp is 32 neighbours of one row.  Accumulators are double-buffered.
+// With fewer tiles than SMs the CTAs of a thread-block cluster share a tile's depth: each leaves its sums in shared memory and
+// finishes a share of the rows, adding the others' over distributed shared memory.
+constexpr int kBM = 128, kBK = 64;
+constexpr int kWBytes = kBM * kBK * 2;
+constexpr int kThreads = 192;
+constexpr int kEpilogueWarps = 4;
+constexpr int kMaxSplit = 8;
+constexpr unsigned long long kWaitNs = 1000000000ull;
+
+template <int BN>
+struct Shape {
+    static constexpr int kHBytes = BN * kBK * 2;
+    static constexpr int kStageBytes = kWBytes + kHBytes;
+    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 8 : 10;
+    static constexpr int kTmemCols = 2 * BN < 32 ? 32 : 2 * BN;
+    static constexpr int kChunk = BN < 32 ? BN : 32;   // columns of tensor memory read at a time
+    static constexpr size_t kRing = static_cast<size_t>(kStages) * kStageBytes;
+    static_assert(kRing >= static_cast<size_t>(BN) * kBM * 4, "a tile's sums fit into the ring");
+    // binary32 accumulator, bfloat16 operands, both K-major
+    static constexpr uint32_t kInstr = (1u << 4) | (1u << 7) | (1u << 10) | ((BN >> 3) << 17) | ((kBM >> 4) << 24);
+};
+
+template <int BN>
+struct Shared {
+    uint64_t full[Shape<BN>::kStages];
+    uint64_t empty[Shape<BN>::kStages];
+    uint64_t tmem_full[2];
+    uint64_t tmem_empty[2];
+    uint64_t drained;
+    uint32_t tmem_base;
+    int abort_flag;
+};
+template <int BN>
+constexpr size_t smem_bytes() {
+    return Shape<BN>::kRing + sizeof(Shared<BN>) + 1024;
 }
 
-constexpr int kTile = 64, kDeep = 32;
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[COLS]) {
+    if constexpr (COLS == 16)
+        tmem_load16(addr, v);
+    else
+        tmem_load32(addr, v);
+}
 
-template <int ACT, class T>
-__global__ void __launch_bounds__(256) transform_kernel(const __grid_constant__ Params P) {
-    __shared__ float a[kDeep][kTile + 4], w[kDeep][kTile + 4];
-    const int r0 = blockIdx.y * kTile, j0 = blockIdx.x * kTile;
-    const int tr = threadIdx.x / 16, tj = threadIdx.x % 16;
-    float acc[4][4] = {};
-    for (int k0 = 0; k0 < P.d; k0 += kDeep) {
-        for (int e = threadIdx.x; e < kTile * kDeep; e += 256) {
-            const int row = e / kDeep, k = e % kDeep;
-            const bool in = k0 + k < P.d;
-            a[k][row] = in && r0 + row < P.rows ? __bfloat162float(P.hidden[static_cast<int64_t>(r0 + row) * P.ld_hidden + k0 + k]) : 0.f;
-            w[k][row] = in && j0 + row < P.n ? __bfloat162float(P.weight[static_cast<int64_t>(j0 + row) * P.d + k0 + k]) : 0.f;
-        }
-        __syncthreads();
-        for (int k = 0; k < kDeep; ++k)
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-#pragma unroll
-                for (int y = 0; y < 4; ++y) acc[x][y] = fmaf(a[k][tr * 4 + x], w[k][tj * 4 + y], acc[x][y]);
-        __syncthreads();
+// f with the activation as a constant.
+template <class F>
+__device__ __forceinline__ void with_activation(int act, F f) {
+    switch (act) {
+        case FEF_ACT_RELU: f(std::integral_constant<int, FEF_ACT_RELU>()); break;
+        case FEF_ACT_SILU: f(std::integral_constant<int, FEF_ACT_SILU>()); break;
+        case FEF_ACT_GELU: f(std::integral_constant<int, FEF_ACT_GELU>()); break;
+        case FEF_ACT_GELU_TANH: f(std::integral_constant<int, FEF_ACT_GELU_TANH>()); break;
+        default: f(std::integral_constant<int, FEF_ACT_NONE>()); break;
     }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const int r = r0 + tr * 4 + x, j = j0 + tj * 4 + y;
-            if (r >= P.rows || j >= P.n) continue;
-            float v = acc[x][y];
-            if (P.bias) v += __bfloat162float(P.bias[j]);
-            v = activate<ACT>(v);
-            if (P.residual) v += __bfloat162float(P.residual[static_cast<int64_t>(r) * P.ld_residual + j]);
-            store<T>(P.out, static_cast<int64_t>(r) * P.ldo + j, v);
-        }
 }
 
-template <int ACT>
-static void launch(const Params& P, fef_dtype dt, cudaStream_t stream) {
-    const dim3 grid((P.n + kTile - 1) / kTile, (P.rows + kTile - 1) / kTile);
-    if (dt == FEF_F32)
-        transform_kernel<ACT, float><<<grid, 256, 0, stream>>>(P);
-    else
-        transform_kernel<ACT, __nv_bfloat16><<<grid, 256, 0, stream>>>(P);
+// COLS rows of one output column: sums in v, rows r0 .. , column j.
+template <int COLS>
+__device__ __forceinline__ void finish_column(const Params& P, float (&v)[COLS], int r0, int j) {
+    if (j >= P.n) return;
+    const int rows = min(COLS, P.rows - r0);
+    const float bias = P.bias ? __bfloat162float(P.bias[j]) : 0.f;
+    float add[COLS];
+    const __nv_bfloat16* res = P.residual + static_cast<int64_t>(r0) * P.ld_residual + j;
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) {
+        add[i] = 0.f;
+        if (P.residual && i < rows) add[i] = __bfloat162float(res[i * P.ld_residual]);
+    }
+    with_activation(P.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < COLS; ++i) v[i] = activate<decltype(act)::value>(v[i] + bias) + add[i];
+    });
+    if (P.out_f32) {
+        float* out = static_cast<float*>(P.out) + static_cast<int64_t>(r0) * P.ldo + j;
+#pragma unroll
+        for (int i = 0; i < COLS; ++i)
+            if (i < rows) out[i * P.ldo] = v[i];
+    } else {
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(P.out) + static_cast<int64_t>(r0) * P.ldo + j;
+#pragma unroll
+        for (int i = 0; i < COLS; ++i)
+            if (i < rows) out[i * P.ldo] = __float2bfloat16_rn(v[i]);
+    }
+}
+
+template <int BN, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 1)
+transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h,
+                 const __grid_constant__ Params P) {
+    using S = Shape<BN>;
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    Shared<BN>& sh = *reinterpret_cast<Shared<BN>*>(smem + S::kRing);
+    volatile int* abort_flag = &sh.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        // (cleared here and not by a launch of its own: the earliest report comes after a wait of a second)
+        if (blockIdx.x == 0 && P.status) *P.status = FEF_OK;
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(sh.full + s, 1);
+            mbar_init(sh.empty + s, 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(sh.tmem_full + a, 1);
+            mbar_init(sh.tmem_empty + a, kEpilogueWarps);
+        }
+        mbar_init(&sh.drained, 1);
+        sh.abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) tmem_alloc(&sh.tmem_base, S::kTmemCols);   // (one CTA per SM: the columns are always free)
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&sh.tmem_base);
+
+    const int row_tiles = (P.rows + BN - 1) / BN, tiles = row_tiles * ((P.n + kBM - 1) / kBM);
+    const int blocks = (P.d + kBK - 1) / kBK;
+    const int rank = SPLIT ? static_cast<int>(blockIdx.x) % P.split : 0;
+    const int first_tile = SPLIT ? static_cast<int>(blockIdx.x) / P.split : static_cast<int>(blockIdx.x);
+    const int stride = SPLIT ? tiles : static_cast<int>(gridDim.x);   // (SPLIT: one tile per cluster)
+    const int kb_begin = SPLIT ? static_cast<int>(static_cast<int64_t>(rank) * blocks / P.split) : 0;
+    const int kb_end = SPLIT ? static_cast<int>(static_cast<int64_t>(rank + 1) * blocks / P.split) : blocks;
+    int issued = 0;   // stages put in flight (producer thread)
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int tile = first_tile; ok && tile < tiles; tile += stride) {
+                const int j0 = tile / row_tiles * kBM, r0 = tile % row_tiles * BN;
+                for (int kb = kb_begin; kb < kb_end; ++kb) {
+#ifdef FEF_TEST_HOOKS
+                    // Test build: nothing is copied from here on and nothing arrives, so the waits for it run out.
+                    if (blockIdx.x == 0 && P.withhold >= 0 && issued >= P.withhold) {
+                        ok = false;
+                        break;
+                    }
+#endif
+                    if (!mbar_wait_bounded(sh.empty + stage, phase ^ 1u, abort_flag, P.wait_ns)) {
+                        *abort_flag = 1;
+                        report(P.status, FEF_ERR_TIMEOUT);
+                        ok = false;
+                        break;
+                    }
+                    unsigned char* dst = smem + stage * S::kStageBytes;
+                    mbar_arrive_expect_tx(sh.full + stage, S::kStageBytes);
+                    tma_load_2d(dst, &map_w, kb * kBK, j0, sh.full + stage);
+                    tma_load_2d(dst + kWBytes, &map_h, kb * kBK, r0, sh.full + stage);
+                    ++issued;
+                    if (++stage == S::kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            unsigned uses[2] = {0u, 0u}, count = 0;
+            bool ok = true;
+            for (int tile = first_tile; ok && tile < tiles; tile += stride, ++count) {
+                const int acc = count & 1;
+                // the epilogue must have drained this accumulator (passes at once on its first use)
+                if (!mbar_wait_bounded(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns)) {
+                    *abort_flag = 1;
+                    report(P.status, FEF_ERR_TIMEOUT);
+                    break;
+                }
+                ++uses[acc];
+                tc_fence_after();
+                const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
+                for (int kb = kb_begin; kb < kb_end; ++kb) {
+                    if (!mbar_wait_bounded(sh.full + stage, phase, abort_flag, P.wait_ns)) {
+                        *abort_flag = 1;
+                        report(P.status, FEF_ERR_TIMEOUT);
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t at = smem_u32(smem + stage * S::kStageBytes);
+                    const uint64_t desc_w = smem_desc_sw128(at), desc_h = smem_desc_sw128(at + kWBytes);
+#pragma unroll
+                    for (int k = 0; k < kBK / 16; ++k)   // 32 bytes further along K inside the swizzle row
+                        tc_mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k), S::kInstr,
+                               (kb > kb_begin || k) ? 1u : 0u);
+                    tc_commit(sh.empty + stage);   // arrives when these MMAs have read the stage
+                    if (++stage == S::kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+                if (ok) tc_commit(sh.tmem_full + acc);   // arrives when the tile's accumulator is complete
+            }
+            // everything issued has finished before the tensor memory goes back, after a wait that ran out too: this one does
+            // not look at the abort flag
+            tc_commit(&sh.drained);
+            volatile int never = 0;
+            mbar_wait_bounded(&sh.drained, 0u, &never, kWaitNs);
+        }
+    } else {
+        const int quarter = warp & 3;   // the tensor-memory lanes this warp may read
+        const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+        unsigned uses[2] = {0u, 0u}, count = 0;
+        for (int tile = first_tile; tile < tiles; tile += stride, ++count) {
+            const int acc = count & 1;
+            const int j = tile / row_tiles * kBM + quarter * 32 + lane, r0 = tile % row_tiles * BN;
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns))) {
+                *abort_flag = 1;
+                report(P.status, FEF_ERR_TIMEOUT);
+                break;
+            }
+            ++uses[acc];
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < BN; c += S::kChunk) {
+                if (r0 + c >= P.rows) break;   // (uniform over the warp)
+                float v[S::kChunk];
+                tmem_load<S::kChunk>(lane_addr + static_cast<uint32_t>(acc * BN + c), v);
+                if constexpr (SPLIT) {
+                    // every copy into the ring has been read by an MMA that is complete: it is free
+                    float* part = reinterpret_cast<float*>(smem);
+#pragma unroll
+                    for (int i = 0; i < S::kChunk; ++i) part[(c + i) * kBM + quarter * 32 + lane] = v[i];
+                } else {
+                    finish_column<S::kChunk>(P, v, r0 + c, j);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.tmem_empty + acc);   // the accumulator may be overwritten
+        }
+    }
+
+    // ---- teardown: copies still in flight after an abort get a bounded chance to land; then the tensor memory goes back
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag && threadIdx.x == 0) {
+        const int first = issued > S::kStages ? issued - S::kStages : 0;
+        for (int k = first; k < issued; ++k) {
+            volatile int never = 0;
+            mbar_wait_bounded(sh.full + (k % S::kStages), static_cast<uint32_t>((k / S::kStages) & 1), &never, kWaitNs);
+        }
+    }
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem_base, S::kTmemCols);
+    }
+    if constexpr (SPLIT) {
+        cg::cluster_group cluster = cg::this_cluster();
+        cluster.sync();
+        const int j0 = first_tile / row_tiles * kBM + lane * 4, r0 = first_tile % row_tiles * BN;
+        const int rows = min(BN, P.rows - r0);
+        const float* part[kMaxSplit];
+#pragma unroll
+        for (int s = 0; s < kMaxSplit; ++s)
+            part[s] = cluster.map_shared_rank(reinterpret_cast<float*>(smem), s < P.split ? s : 0) + lane * 4;
+        // row r of the tile is finished by CTA r % split, a warp at a time, four neighbouring columns per lane
+        for (int r = rank + warp * P.split; r < rows; r += kThreads / 32 * P.split) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            float4 x[kMaxSplit];
+#pragma unroll
+            for (int s = 0; s < kMaxSplit; ++s)
+                if (s < P.split) x[s] = *reinterpret_cast<const float4*>(part[s] + r * kBM);
+#pragma unroll
+            for (int s = 0; s < kMaxSplit; ++s)
+                if (s < P.split) {
+                    v[0] += x[s].x;
+                    v[1] += x[s].y;
+                    v[2] += x[s].z;
+                    v[3] += x[s].w;
+                }
+            const int64_t row = r0 + r;
+            with_activation(P.act, [&](auto act) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = j0 + i;
+                    if (j >= P.n) continue;
+                    float y = activate<decltype(act)::value>(v[i] + (P.bias ? __bfloat162float(P.bias[j]) : 0.f));
+                    if (P.residual) y += __bfloat162float(P.residual[row * P.ld_residual + j]);
+                    v[i] = y;
+                }
+            });
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = j0 + i;
+                if (j >= P.n) continue;
+                if (P.out_f32)
+                    static_cast<float*>(P.out)[row * P.ldo + j] = v[i];
+                else
+                    static_cast<__nv_bfloat16*>(P.out)[row * P.ldo + j] = __float2bfloat16_rn(v[i]);
+            }
+        }
+        cluster.sync();   // (nobody's shared memory goes while another reads it)
+    }
+}
+
+// ---- host ----
+template <int BN, bool SPLIT>
+static cudaError_t launch(const CUtensorMap& w, const CUtensorMap& h, const Params& P, int grid, int dev, cudaStream_t stream) {
+    constexpr size_t smem = smem_bytes<BN>();
+    static bool allowed[64];   // large shared memory, per device
+    if (dev >= 64 || !allowed[dev]) {
+        const cudaError_t e =
+            cudaFuncSetAttribute(transform_kernel<BN, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+        if (e != cudaSuccess) return e;
+        if (dev < 64) allowed[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(SPLIT ? P.split : 1);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = SPLIT ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, transform_kernel<BN, SPLIT>, w, h, P);
+}
+
+template <int BN>
+static cudaError_t run(Params& P, int split, int sms, int dev, cudaStream_t stream) {
+    CUtensorMap w, h;
+    if (!map_2d(&w, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, P.weight, P.d, P.n, static_cast<uint64_t>(P.d) * 2, kBK, kBM,
+                CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !map_2d(&h, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, P.hidden, P.d, P.rows, static_cast<uint64_t>(P.ld_hidden) * 2, kBK, BN,
+                CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorUnknown;
+    const int64_t tiles = static_cast<int64_t>((P.rows + BN - 1) / BN) * ((P.n + kBM - 1) / kBM);
+    P.split = split;
+    if (split > 1) return launch<BN, true>(w, h, P, static_cast<int>(tiles) * split, dev, stream);
+    return launch<BN, false>(w, h, P, static_cast<int>(tiles < sms ? tiles : sms), dev, stream);
+}
+
+// CTAs that share a tile's depth: as many as there are SMs for, with two blocks of the depth each at least.
+static int split_of(int64_t tiles, int d, int sms) {
+    const int blocks = (d + kBK - 1) / kBK;
+    int split = 1;
+    while (split < kMaxSplit && tiles * split * 2 <= sms && blocks >= split * 4) split *= 2;
+    return split;
 }
 
 }  // namespace head
 }  // namespace fef
+
+#ifdef FEF_TEST_HOOKS
+// Test builds only: CTA 0 of the next call withholds its stages from this number on, and waits give up after `limit_ns`.
+static int g_test_withhold = -1;
+static unsigned long long g_test_wait_ns = 0;
+extern "C" void fef_test_withhold_transform_once(int stage, unsigned long long limit_ns) {
+    g_test_withhold = stage;
+    g_test_wait_ns = limit_ns;
+}
+#endif
 
 extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden, const void* weight, const void* bias,
                                            const void* residual, int64_t ld_residual, int rows, int n, int d,
@@ -104,7 +441,7 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
     if (rows < 1 || rows > FEF_MAX_TRANSFORM || n < 1 || n > FEF_MAX_TRANSFORM || d < 8 || d > FEF_MAX_TRANSFORM || d % 8)
         return FEF_ERR_INVALID_ARG;
     if (ld_hidden < d || ldo < n || (residual && ld_residual < n)) return FEF_ERR_INVALID_ARG;
-    const int64_t most = 1ll << 40;   // (pitches in elements)
+    const int64_t most = 1ll << 38;   // (pitches in elements)
     if (ld_hidden > most || ldo > most || (residual && ld_residual > most)) return FEF_ERR_INVALID_ARG;
     if (activation < FEF_ACT_NONE || activation > FEF_ACT_GELU_TANH) return FEF_ERR_INVALID_ARG;
     const int esize = dt == FEF_F32 ? 4 : 2;
@@ -125,8 +462,10 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
     if (residual && o.meets(Range(residual, rows, ld_residual, n, 2)) &&
         !(residual == out && dt == FEF_BF16 && (ld_residual == ldo || rows == 1)))
         return FEF_ERR_INVALID_ARG;
-    int dev = -1;
-    if (cudaGetDevice(&dev) != cudaSuccess) return FEF_ERR_CUDA;
+    int dev = -1, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1)
+        return FEF_ERR_CUDA;
 
     Params P = {};
     P.hidden = static_cast<const __nv_bfloat16*>(hidden);
@@ -140,15 +479,31 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
     P.rows = rows;
     P.n = n;
     P.d = d;
+    P.act = activation;
+    P.out_f32 = dt == FEF_F32;
+    P.wait_ns = kWaitNs;
     P.status = device_status;
+#ifdef FEF_TEST_HOOKS
+    P.withhold = g_test_withhold;
+    if (g_test_withhold >= 0) P.wait_ns = g_test_wait_ns;   // one call only
+    g_test_withhold = -1;
+#endif
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (device_status && cudaMemsetAsync(device_status, 0, sizeof(int32_t), stream) != cudaSuccess) return FEF_ERR_CUDA;
-    switch (activation) {
-        case FEF_ACT_NONE: launch<FEF_ACT_NONE>(P, dt, stream); break;
-        case FEF_ACT_RELU: launch<FEF_ACT_RELU>(P, dt, stream); break;
-        case FEF_ACT_SILU: launch<FEF_ACT_SILU>(P, dt, stream); break;
-        case FEF_ACT_GELU: launch<FEF_ACT_GELU>(P, dt, stream); break;
-        default: launch<FEF_ACT_GELU_TANH>(P, dt, stream); break;
+    const int64_t columns = (n + kBM - 1) / kBM;
+    cudaError_t e;
+    if (rows <= 16) {
+        e = run<16>(P, split_of(columns, d, sms), sms, dev, stream);
+    } else if (rows <= 32) {
+        e = run<32>(P, split_of(columns, d, sms), sms, dev, stream);
+    } else if (rows <= 64) {
+        e = run<64>(P, split_of(columns, d, sms), sms, dev, stream);
+    } else {
+        // tiles of 128 or of 256 rows: whichever keeps the SMs busy for less time (a block's time goes with the operands' rows)
+        const int64_t t128 = columns * ((rows + 127) / 128), t256 = columns * ((rows + 255) / 256);
+        const int s128 = split_of(t128, d, sms), s256 = split_of(t256, d, sms);
+        const double c128 = static_cast<double>((t128 * s128 + sms - 1) / sms) * (128 + 128) / s128;
+        const double c256 = static_cast<double>((t256 * s256 + sms - 1) / sms) * (256 + 128) / s256;
+        e = c128 < c256 ? run<128>(P, s128, sms, dev, stream) : run<256>(P, s256, sms, dev, stream);
     }
-    return cudaGetLastError() == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
+    return e == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
 }
