@@ -6,6 +6,7 @@
 #include <cooperative_groups.h>
 #include <math.h>
 #include <stdint.h>
+#include <string.h>
 
 #include <type_traits>
 
@@ -29,6 +30,7 @@ struct Params {
     int rows, n, d;
     int act;        // fef_activation
     int out_f32;    // the output is float32, not bfloat16
+    int wide_out, wide_residual;   // eight neighbours lie on 16-byte boundaries in every row
     int split;      // CTAs (one cluster) that share a tile's depth
     unsigned long long wait_ns;
     int32_t* status;
@@ -62,6 +64,7 @@ constexpr int kWBytes = kBM * kBK * 2;
 constexpr int kThreads = 192;
 constexpr int kEpilogueWarps = 4;
 constexpr int kMaxSplit = 8;
+constexpr int kTurnPitch = 36;   // (rows of 16 bytes that start in different banks)
 constexpr unsigned long long kWaitNs = 1000000000ull;
 
 template <int BN>
@@ -86,6 +89,7 @@ struct Shared {
     uint64_t drained;
     uint32_t tmem_base;
     int abort_flag;
+    alignas(16) float turn[kEpilogueWarps][32 * kTurnPitch];   // where a warp turns 32 x 32 sums round
 };
 template <int BN>
 constexpr size_t smem_bytes() {
@@ -123,35 +127,70 @@ __device__ __forceinline__ void with_activation(int act, F f) {
     }
 }
 
-// COLS rows of one output column: sums in v, rows r0 .. , column j.
-template <int COLS>
-__device__ __forceinline__ void finish_column(const Params& P, float (&v)[COLS], int r0, int j) {
-    if (j >= P.n) return;
-    const int rows = min(COLS, P.rows - r0);
-    const float bias = P.bias ? __bfloat162float(P.bias[j]) : 0.f;
-    float add[COLS];
-    const __nv_bfloat16* res = P.residual + static_cast<int64_t>(r0) * P.ld_residual + j;
-#pragma unroll
-    for (int i = 0; i < COLS; ++i) {
-        add[i] = 0.f;
-        if (P.residual && i < rows) add[i] = __bfloat162float(res[i * P.ld_residual]);
-    }
-    with_activation(P.act, [&](auto act) {
-#pragma unroll
-        for (int i = 0; i < COLS; ++i) v[i] = activate<decltype(act)::value>(v[i] + bias) + add[i];
-    });
-    if (P.out_f32) {
-        float* out = static_cast<float*>(P.out) + static_cast<int64_t>(r0) * P.ldo + j;
-#pragma unroll
-        for (int i = 0; i < COLS; ++i)
-            if (i < rows) out[i * P.ldo] = v[i];
+// Eight neighbours of one row of the output, columns j .. j + 7.  WHOLE: all of them exist and lie on 16-byte boundaries.
+struct Eight {
+    float v[8];
+};
+template <bool WHOLE>
+__device__ __forceinline__ Eight load_eight(const __nv_bfloat16* p, int j, int n) {
+    Eight r;
+    if constexpr (WHOLE) {
+        unpack<FEF_BF16>(*reinterpret_cast<const uint4*>(p + j), r.v);
     } else {
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(P.out) + static_cast<int64_t>(r0) * P.ldo + j;
 #pragma unroll
-        for (int i = 0; i < COLS; ++i)
-            if (i < rows) out[i * P.ldo] = __float2bfloat16_rn(v[i]);
+        for (int i = 0; i < 8; ++i) r.v[i] = j + i < n ? __bfloat162float(p[j + i]) : 0.f;
+    }
+    return r;
+}
+template <int ACT>
+__device__ __forceinline__ void finish_eight(const Params& P, Eight y, const Eight& bias, const Eight& residual, int64_t row, int j,
+                                             bool whole) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y.v[i] = activate<ACT>(y.v[i] + bias.v[i]) + residual.v[i];
+    if (P.out_f32) {
+        float* out = static_cast<float*>(P.out) + row * P.ldo + j;
+        if (whole) {
+            *reinterpret_cast<float4*>(out) = make_float4(y.v[0], y.v[1], y.v[2], y.v[3]);
+            *reinterpret_cast<float4*>(out + 4) = make_float4(y.v[4], y.v[5], y.v[6], y.v[7]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (j + i < P.n) out[i] = y.v[i];
+        }
+    } else {
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(P.out) + row * P.ldo + j;
+        if (whole) {
+            uint4 w;
+            __nv_bfloat162 h[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(y.v[2 * i], y.v[2 * i + 1]);
+            memcpy(&w, h, 16);
+            *reinterpret_cast<uint4*>(out) = w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (j + i < P.n) out[i] = __float2bfloat16_rn(y.v[i]);
+        }
     }
 }
+// What a lane keeps for its eight columns.
+struct Columns {
+    int j;
+    bool in, whole_out, whole_residual;
+    Eight bias;
+    __device__ __forceinline__ void set(const Params& P, int first) {
+        j = first;
+        in = j < P.n;
+        whole_out = P.wide_out && j + 8 <= P.n;
+        whole_residual = P.wide_residual && j + 8 <= P.n;
+        bias = P.bias ? load_eight<false>(P.bias, j, P.n) : Eight{};
+    }
+    __device__ __forceinline__ Eight residual(const Params& P, int64_t row) const {
+        if (!P.residual || !in) return Eight{};
+        const __nv_bfloat16* p = P.residual + row * P.ld_residual;
+        return whole_residual ? load_eight<true>(p, j, P.n) : load_eight<false>(p, j, P.n);
+    }
+};
 
 template <int BN, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -275,10 +314,20 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     } else {
         const int quarter = warp & 3;   // the tensor-memory lanes this warp may read
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+        float* turn = sh.turn[quarter];
         unsigned uses[2] = {0u, 0u}, count = 0;
         for (int tile = first_tile; tile < tiles; tile += stride, ++count) {
             const int acc = count & 1;
-            const int j = tile / row_tiles * kBM + quarter * 32 + lane, r0 = tile % row_tiles * BN;
+            const int r0 = tile % row_tiles * BN;
+            // a lane reads sums as one column of 32 rows and finishes eight columns of every eighth row
+            Columns col;
+            Eight next[4];
+            if constexpr (!SPLIT) {
+                col.set(P, tile / row_tiles * kBM + quarter * 32 + (lane & 3) * 8);
+#pragma unroll
+                for (int k = 0; k < S::kChunk / 8; ++k)
+                    if (r0 + 8 * k + (lane >> 2) < P.rows) next[k] = col.residual(P, r0 + 8 * k + (lane >> 2));
+            }
             if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns))) {
                 *abort_flag = 1;
                 report(P.status, FEF_ERR_TIMEOUT);
@@ -297,7 +346,27 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 #pragma unroll
                     for (int i = 0; i < S::kChunk; ++i) part[(c + i) * kBM + quarter * 32 + lane] = v[i];
                 } else {
-                    finish_column<S::kChunk>(P, v, r0 + c, j);
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < S::kChunk; ++i) turn[i * kTurnPitch + lane] = v[i];
+                    Eight add[S::kChunk / 8];
+#pragma unroll
+                    for (int k = 0; k < S::kChunk / 8; ++k) {
+                        add[k] = next[k];
+                        const int row = r0 + c + S::kChunk + 8 * k + (lane >> 2);   // the next chunk's
+                        if (c + S::kChunk < BN && row < P.rows) next[k] = col.residual(P, row);
+                    }
+                    __syncwarp();
+                    with_activation(P.act, [&](auto act) {
+#pragma unroll
+                        for (int k = 0; k < S::kChunk / 8; ++k) {
+                            const int in_chunk = 8 * k + (lane >> 2), row = r0 + c + in_chunk;
+                            const float4* from = reinterpret_cast<const float4*>(turn + in_chunk * kTurnPitch + (lane & 3) * 8);
+                            const float4 a = from[0], b = from[1];
+                            const Eight y = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+                            if (row < P.rows && col.in) finish_eight<decltype(act)::value>(P, y, col.bias, add[k], row, col.j, col.whole_out);
+                        }
+                    });
                 }
             }
             tc_fence_before();
@@ -325,47 +394,32 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     if constexpr (SPLIT) {
         cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
-        const int j0 = first_tile / row_tiles * kBM + lane * 4, r0 = first_tile % row_tiles * BN;
+        const int r0 = first_tile % row_tiles * BN;
         const int rows = min(BN, P.rows - r0);
+        Columns col;
+        col.set(P, first_tile / row_tiles * kBM + (lane & 15) * 8);
         const float* part[kMaxSplit];
 #pragma unroll
         for (int s = 0; s < kMaxSplit; ++s)
-            part[s] = cluster.map_shared_rank(reinterpret_cast<float*>(smem), s < P.split ? s : 0) + lane * 4;
-        // row r of the tile is finished by CTA r % split, a warp at a time, four neighbouring columns per lane
-        for (int r = rank + warp * P.split; r < rows; r += kThreads / 32 * P.split) {
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            float4 x[kMaxSplit];
-#pragma unroll
-            for (int s = 0; s < kMaxSplit; ++s)
-                if (s < P.split) x[s] = *reinterpret_cast<const float4*>(part[s] + r * kBM);
+            part[s] = cluster.map_shared_rank(reinterpret_cast<float*>(smem), s < P.split ? s : 0) + (lane & 15) * 8;
+        // rows of the tile go round the CTAs, two of a CTA's to a warp at a time, eight columns per lane
+        for (int q = warp * 2 + (lane >> 4); rank + q * P.split < rows; q += kThreads / 16) {
+            const int r = rank + q * P.split;
+            const Eight add = col.residual(P, r0 + r);
+            Eight y = {};
 #pragma unroll
             for (int s = 0; s < kMaxSplit; ++s)
                 if (s < P.split) {
-                    v[0] += x[s].x;
-                    v[1] += x[s].y;
-                    v[2] += x[s].z;
-                    v[3] += x[s].w;
-                }
-            const int64_t row = r0 + r;
-            with_activation(P.act, [&](auto act) {
+                    const float4* from = reinterpret_cast<const float4*>(part[s] + r * kBM);
+                    const float4 a = from[0], b = from[1];
+                    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = j0 + i;
-                    if (j >= P.n) continue;
-                    float y = activate<decltype(act)::value>(v[i] + (P.bias ? __bfloat162float(P.bias[j]) : 0.f));
-                    if (P.residual) y += __bfloat162float(P.residual[row * P.ld_residual + j]);
-                    v[i] = y;
+                    for (int i = 0; i < 8; ++i) y.v[i] += x[i];
                 }
-            });
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = j0 + i;
-                if (j >= P.n) continue;
-                if (P.out_f32)
-                    static_cast<float*>(P.out)[row * P.ldo + j] = v[i];
-                else
-                    static_cast<__nv_bfloat16*>(P.out)[row * P.ldo + j] = __float2bfloat16_rn(v[i]);
-            }
+            if (col.in)
+                with_activation(P.act, [&](auto act) {
+                    finish_eight<decltype(act)::value>(P, y, col.bias, add, r0 + r, col.j, col.whole_out);
+                });
         }
         cluster.sync();   // (nobody's shared memory goes while another reads it)
     }
@@ -481,6 +535,8 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
     P.d = d;
     P.act = activation;
     P.out_f32 = dt == FEF_F32;
+    P.wide_out = !(reinterpret_cast<uintptr_t>(out) & 15) && ldo * esize % 16 == 0;
+    P.wide_residual = !(reinterpret_cast<uintptr_t>(residual) & 15) && ld_residual % 8 == 0;
     P.wait_ns = kWaitNs;
     P.status = device_status;
 #ifdef FEF_TEST_HOOKS
