@@ -43,27 +43,39 @@ template <int ACT>
 __device__ __forceinline__ float activate(float y) {
     if constexpr (ACT == FEF_ACT_RELU) return y <= 0.f ? 0.f : y;   // (NaN stays)
     if constexpr (ACT == FEF_ACT_SILU) return __fdividef(y, 1.f + ex2_approx(-1.4426950408889634f * y));
-    if constexpr (ACT == FEF_ACT_GELU) return 0.5f * y * erfcf(-0.70710678118654752f * y);
+    if constexpr (ACT == FEF_ACT_GELU) {
+        // Phi from Abramowitz and Stegun 7.1.26: erfc x = (a1 t + .. + a5 t^5) e^(-x^2), t = 1 / (1 + p x), within 1.5e-7 for x >= 0
+        const float x = 0.70710678118654752f * fabsf(y);
+        const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+        const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+        const float tail = 0.5f * poly * ex2_approx(-1.4426950408889634f * x * x);
+        return y * (y > 0.f ? 1.f - tail : tail);
+    }
     if constexpr (ACT == FEF_ACT_GELU_TANH) {
         // (1 + tanh z) / 2 = 1 / (1 + e^(-2 z)),  z = sqrt(2 / pi) (y + 0.044715 y^3)
         const float z2 = y * fmaf(0.044715f * y, y, 1.f) * (2.f * 0.79788456080286536f * 1.4426950408889634f);
-        return y / (1.f + ex2_approx(-z2));
+        return __fdividef(y, 1.f + ex2_approx(-z2));
     }
     return y;
 }
 
-// ---- kernel ----
-// A CTA takes 128 columns of the output (rows of the weight: the left operand, M = 128) by BN rows (hidden states: the right
-// operand, N = BN), so that few hidden rows cost few columns of tensor memory and no padding of the weight stream.  Warp 0 brings
-// 64-deep blocks of both operands through a ring by TMA (one thread), warp 1 issues the MMAs (one thread), warps 2-5 are the
-// epilogue, a column of the output per lane: a store of a warp is 32 neighbours of one row.  Accumulators are double-buffered.
-// With fewer tiles than SMs the CTAs of a thread-block cluster share a tile's depth: each leaves its sums in shared memory and
-// finishes a share of the rows, adding the others' over distributed shared memory.
+// ---- kernels ----
+// transform_kernel: a CTA takes 128 columns of the output (rows of the weight: the left operand, M = 128) by BN rows (hidden
+// states: the right operand, N = BN), so that few hidden rows cost few columns of tensor memory and no padding of the weight
+// stream.  Warp 0 brings 64-deep blocks of both operands through a ring by TMA (one thread), warp 1 issues the MMAs (one thread),
+// warps 2-9 are the epilogue.  Accumulators are double-buffered.  With fewer tiles than SMs the CTAs of a thread-block cluster
+// share a tile's depth: each leaves its sums in shared memory and finishes a share of the rows, adding the others' over
+// distributed shared memory.
+//
+// transform_pair_kernel: two CTAs (a cluster) take 256 columns by 256 rows with tcgen05.mma.cta_group::2: each brings its own 128
+// columns' weights and half of the hidden rows, which both tensor cores read.  Per SM a block is 32 KiB instead of the 48 KiB of
+// a 128 x 256 tile of its own, whose copies and operand reads together are more than shared memory's 128 bytes a clock.
 constexpr int kBM = 128, kBK = 64;
 constexpr int kWBytes = kBM * kBK * 2;
-constexpr int kThreads = 192;
-constexpr int kEpilogueWarps = 4;
+constexpr int kEpilogueWarps = 8;
+constexpr int kThreads = 64 + 32 * kEpilogueWarps;
 constexpr int kMaxSplit = 8;
+constexpr int kChunk = 16;       // columns of tensor memory (rows of the output) that an epilogue warp takes at a time
 constexpr int kTurnPitch = 36;   // (rows of 16 bytes that start in different banks)
 constexpr unsigned long long kWaitNs = 1000000000ull;
 
@@ -72,28 +84,29 @@ struct Shape {
     static constexpr int kHBytes = BN * kBK * 2;
     static constexpr int kStageBytes = kWBytes + kHBytes;
     static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 8 : 10;
-    static constexpr int kTmemCols = 2 * BN < 32 ? 32 : 2 * BN;
-    static constexpr int kChunk = BN < 32 ? BN : 32;   // columns of tensor memory read at a time
+    static constexpr int kTmemCols = 2 * BN;
     static constexpr size_t kRing = static_cast<size_t>(kStages) * kStageBytes;
     static_assert(kRing >= static_cast<size_t>(BN) * kBM * 4, "a tile's sums fit into the ring");
-    // binary32 accumulator, bfloat16 operands, both K-major
-    static constexpr uint32_t kInstr = (1u << 4) | (1u << 7) | (1u << 10) | ((BN >> 3) << 17) | ((kBM >> 4) << 24);
 };
+// binary32 accumulator, bfloat16 operands, both K-major
+__device__ constexpr uint32_t instruction(int m, int n) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
 
-template <int BN>
+template <int STAGES>
 struct Shared {
-    uint64_t full[Shape<BN>::kStages];
-    uint64_t empty[Shape<BN>::kStages];
+    uint64_t full[STAGES];
+    uint64_t empty[STAGES];
     uint64_t tmem_full[2];
     uint64_t tmem_empty[2];
     uint64_t drained;
     uint32_t tmem_base;
     int abort_flag;
-    alignas(16) float turn[kEpilogueWarps][32 * kTurnPitch];   // where a warp turns 32 x 32 sums round
+    alignas(16) float turn[kEpilogueWarps][kChunk * kTurnPitch];   // where a warp turns 16 x 32 sums round
 };
-template <int BN>
-constexpr size_t smem_bytes() {
-    return Shape<BN>::kRing + sizeof(Shared<BN>) + 1024;
+template <int STAGES>
+constexpr size_t smem_bytes(size_t ring) {
+    return ring + sizeof(Shared<STAGES>) + 1024;
 }
 
 __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
@@ -106,13 +119,6 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
-}
-template <int COLS>
-__device__ __forceinline__ void tmem_load(uint32_t addr, float (&v)[COLS]) {
-    if constexpr (COLS == 16)
-        tmem_load16(addr, v);
-    else
-        tmem_load32(addr, v);
 }
 
 // f with the activation as a constant.
@@ -127,70 +133,122 @@ __device__ __forceinline__ void with_activation(int act, F f) {
     }
 }
 
-// Eight neighbours of one row of the output, columns j .. j + 7.  WHOLE: all of them exist and lie on 16-byte boundaries.
-struct Eight {
-    float v[8];
-};
-template <bool WHOLE>
-__device__ __forceinline__ Eight load_eight(const __nv_bfloat16* p, int j, int n) {
-    Eight r;
-    if constexpr (WHOLE) {
-        unpack<FEF_BF16>(*reinterpret_cast<const uint4*>(p + j), r.v);
-    } else {
+// Eight neighbours of one row of the output, columns j .. j + 7, as the eight bfloat16 numbers of a 16-byte vector.
+__device__ __forceinline__ uint4 load_eight(const __nv_bfloat16* p, int j, int n, bool whole) {
+    if (whole) return *reinterpret_cast<const uint4*>(p + j);
+    uint32_t w[4];
+    const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) r.v[i] = j + i < n ? __bfloat162float(p[j + i]) : 0.f;
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = j + 2 * i < n ? h[j + 2 * i] : 0u, b = j + 2 * i + 1 < n ? h[j + 2 * i + 1] : 0u;
+        w[i] = a | b << 16;
     }
-    return r;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
-template <int ACT>
-__device__ __forceinline__ void finish_eight(const Params& P, Eight y, const Eight& bias, const Eight& residual, int64_t row, int j,
-                                             bool whole) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y.v[i] = activate<ACT>(y.v[i] + bias.v[i]) + residual.v[i];
-    if (P.out_f32) {
-        float* out = static_cast<float*>(P.out) + row * P.ldo + j;
-        if (whole) {
-            *reinterpret_cast<float4*>(out) = make_float4(y.v[0], y.v[1], y.v[2], y.v[3]);
-            *reinterpret_cast<float4*>(out + 4) = make_float4(y.v[4], y.v[5], y.v[6], y.v[7]);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (j + i < P.n) out[i] = y.v[i];
-        }
-    } else {
-        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(P.out) + row * P.ldo + j;
-        if (whole) {
-            uint4 w;
-            __nv_bfloat162 h[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(y.v[2 * i], y.v[2 * i + 1]);
-            memcpy(&w, h, 16);
-            *reinterpret_cast<uint4*>(out) = w;
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (j + i < P.n) out[i] = __float2bfloat16_rn(y.v[i]);
-        }
-    }
-}
+
 // What a lane keeps for its eight columns.
 struct Columns {
     int j;
     bool in, whole_out, whole_residual;
-    Eight bias;
+    uint4 bias;
     __device__ __forceinline__ void set(const Params& P, int first) {
         j = first;
         in = j < P.n;
         whole_out = P.wide_out && j + 8 <= P.n;
         whole_residual = P.wide_residual && j + 8 <= P.n;
-        bias = P.bias ? load_eight<false>(P.bias, j, P.n) : Eight{};
+        bias = P.bias ? load_eight(P.bias, j, P.n, false) : make_uint4(0u, 0u, 0u, 0u);
     }
-    __device__ __forceinline__ Eight residual(const Params& P, int64_t row) const {
-        if (!P.residual || !in) return Eight{};
-        const __nv_bfloat16* p = P.residual + row * P.ld_residual;
-        return whole_residual ? load_eight<true>(p, j, P.n) : load_eight<false>(p, j, P.n);
+    __device__ __forceinline__ uint4 residual(const Params& P, int64_t row) const {
+        if (!P.residual || !in || row >= P.rows) return make_uint4(0u, 0u, 0u, 0u);
+        return load_eight(P.residual + row * P.ld_residual, j, P.n, whole_residual);
+    }
+    template <int ACT>
+    __device__ __forceinline__ void finish(const Params& P, const float (&sum)[8], const uint4& residual, int64_t row) const {
+        if (!in || row >= P.rows) return;
+        float b[8], r[8], y[8];
+        unpack<FEF_BF16>(bias, b);
+        unpack<FEF_BF16>(residual, r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = activate<ACT>(sum[i] + b[i]) + r[i];
+        if (P.out_f32) {
+            float* out = static_cast<float*>(P.out) + row * P.ldo + j;
+            if (whole_out) {
+                *reinterpret_cast<float4*>(out) = make_float4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<float4*>(out + 4) = make_float4(y[4], y[5], y[6], y[7]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (j + i < P.n) out[i] = y[i];
+            }
+        } else {
+            __nv_bfloat16* out = static_cast<__nv_bfloat16*>(P.out) + row * P.ldo + j;
+            if (whole_out) {
+                uint4 w;
+                __nv_bfloat162 h[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+                memcpy(&w, h, 16);
+                *reinterpret_cast<uint4*>(out) = w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (j + i < P.n) out[i] = __float2bfloat16_rn(y[i]);
+            }
+        }
     }
 };
+
+// The epilogue of one tile by one warp: its 32 columns of the output, every second chunk of 16 rows.  A lane reads sums as one column
+// of 16 rows and finishes eight columns of every eighth row; residuals are fetched three chunks ahead, the first before the wait.
+struct Residuals {
+    uint4 ahead[3][2];
+    __device__ __forceinline__ void fetch(const Params& P, const Columns& col, int r0, uint4 (&to)[2]) const {
+        const int row = r0 + ((threadIdx.x & 31) >> 2);
+        to[0] = col.residual(P, row);
+        to[1] = col.residual(P, row + 8);
+    }
+    __device__ __forceinline__ void first(const Params& P, const Columns& col, int r0) {
+#pragma unroll
+        for (int q = 0; q < 3; ++q) fetch(P, col, r0 + q * 2 * kChunk, ahead[q]);
+    }
+};
+template <int BN>
+__device__ __forceinline__ void finish_tile(const Params& P, uint32_t tmem, const Columns& col, Residuals& res, int r0, int half,
+                                            float* turn) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int c = half * kChunk; c < BN; c += 2 * kChunk) {
+        if (r0 + c >= P.rows) break;   // (uniform over the warp)
+        float v[kChunk];
+        tmem_load16(tmem + static_cast<uint32_t>(c), v);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) turn[i * kTurnPitch + lane] = v[i];
+        const uint4 now[2] = {res.ahead[0][0], res.ahead[0][1]};
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            res.ahead[q][0] = res.ahead[q + 1][0];
+            res.ahead[q][1] = res.ahead[q + 1][1];
+        }
+        if (c + 6 * kChunk < BN) res.fetch(P, col, r0 + c + 6 * kChunk, res.ahead[2]);
+        __syncwarp();
+        with_activation(P.act, [&](auto act) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int in_chunk = 8 * k + (lane >> 2);
+                const float4* from = reinterpret_cast<const float4*>(turn + in_chunk * kTurnPitch + (lane & 3) * 8);
+                const float4 a = from[0], b = from[1];
+                const float y[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                col.finish<decltype(act)::value>(P, y, now[k], r0 + c + in_chunk);
+            }
+        });
+    }
+}
+
+__device__ __forceinline__ void give_up(const Params& P, volatile int* abort_flag) {
+    *abort_flag = 1;
+    report(P.status, FEF_ERR_TIMEOUT);
+}
 
 template <int BN, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -199,7 +257,7 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     using S = Shape<BN>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    Shared<BN>& sh = *reinterpret_cast<Shared<BN>*>(smem + S::kRing);
+    Shared<S::kStages>& sh = *reinterpret_cast<Shared<S::kStages>*>(smem + S::kRing);
     volatile int* abort_flag = &sh.abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -249,8 +307,7 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                     }
 #endif
                     if (!mbar_wait_bounded(sh.empty + stage, phase ^ 1u, abort_flag, P.wait_ns)) {
-                        *abort_flag = 1;
-                        report(P.status, FEF_ERR_TIMEOUT);
+                        give_up(P, abort_flag);
                         ok = false;
                         break;
                     }
@@ -276,8 +333,7 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 const int acc = count & 1;
                 // the epilogue must have drained this accumulator (passes at once on its first use)
                 if (!mbar_wait_bounded(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns)) {
-                    *abort_flag = 1;
-                    report(P.status, FEF_ERR_TIMEOUT);
+                    give_up(P, abort_flag);
                     break;
                 }
                 ++uses[acc];
@@ -285,8 +341,7 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
                     if (!mbar_wait_bounded(sh.full + stage, phase, abort_flag, P.wait_ns)) {
-                        *abort_flag = 1;
-                        report(P.status, FEF_ERR_TIMEOUT);
+                        give_up(P, abort_flag);
                         ok = false;
                         break;
                     }
@@ -295,8 +350,8 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                     const uint64_t desc_w = smem_desc_sw128(at), desc_h = smem_desc_sw128(at + kWBytes);
 #pragma unroll
                     for (int k = 0; k < kBK / 16; ++k)   // 32 bytes further along K inside the swizzle row
-                        tc_mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k), S::kInstr,
-                               (kb > kb_begin || k) ? 1u : 0u);
+                        tc_mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
+                               instruction(kBM, BN), (kb > kb_begin || k) ? 1u : 0u);
                     tc_commit(sh.empty + stage);   // arrives when these MMAs have read the stage
                     if (++stage == S::kStages) {
                         stage = 0;
@@ -312,62 +367,36 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             mbar_wait_bounded(&sh.drained, 0u, &never, kWaitNs);
         }
     } else {
-        const int quarter = warp & 3;   // the tensor-memory lanes this warp may read
+        const int quarter = warp & 3, half = (warp - 2) >> 2;   // the tensor-memory lanes this warp may read; its chunks
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
-        float* turn = sh.turn[quarter];
         unsigned uses[2] = {0u, 0u}, count = 0;
         for (int tile = first_tile; tile < tiles; tile += stride, ++count) {
-            const int acc = count & 1;
-            const int r0 = tile % row_tiles * BN;
-            // a lane reads sums as one column of 32 rows and finishes eight columns of every eighth row
+            const int acc = count & 1, r0 = tile % row_tiles * BN;
             Columns col;
-            Eight next[4];
+            Residuals res;
             if constexpr (!SPLIT) {
                 col.set(P, tile / row_tiles * kBM + quarter * 32 + (lane & 3) * 8);
-#pragma unroll
-                for (int k = 0; k < S::kChunk / 8; ++k)
-                    if (r0 + 8 * k + (lane >> 2) < P.rows) next[k] = col.residual(P, r0 + 8 * k + (lane >> 2));
+                res.first(P, col, r0 + half * kChunk);
             }
             if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns))) {
-                *abort_flag = 1;
-                report(P.status, FEF_ERR_TIMEOUT);
+                give_up(P, abort_flag);
                 break;
             }
             ++uses[acc];
             tc_fence_after();
+            if constexpr (SPLIT) {
+                // every copy into the ring has been read by an MMA that is complete: it is free
+                float* part = reinterpret_cast<float*>(smem) + quarter * 32 + lane;
 #pragma unroll 1
-            for (int c = 0; c < BN; c += S::kChunk) {
-                if (r0 + c >= P.rows) break;   // (uniform over the warp)
-                float v[S::kChunk];
-                tmem_load<S::kChunk>(lane_addr + static_cast<uint32_t>(acc * BN + c), v);
-                if constexpr (SPLIT) {
-                    // every copy into the ring has been read by an MMA that is complete: it is free
-                    float* part = reinterpret_cast<float*>(smem);
+                for (int c = half * kChunk; c < BN; c += 2 * kChunk) {
+                    if (r0 + c >= P.rows) break;   // (uniform over the warp)
+                    float v[kChunk];
+                    tmem_load16(lane_addr + static_cast<uint32_t>(acc * BN + c), v);
 #pragma unroll
-                    for (int i = 0; i < S::kChunk; ++i) part[(c + i) * kBM + quarter * 32 + lane] = v[i];
-                } else {
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < S::kChunk; ++i) turn[i * kTurnPitch + lane] = v[i];
-                    Eight add[S::kChunk / 8];
-#pragma unroll
-                    for (int k = 0; k < S::kChunk / 8; ++k) {
-                        add[k] = next[k];
-                        const int row = r0 + c + S::kChunk + 8 * k + (lane >> 2);   // the next chunk's
-                        if (c + S::kChunk < BN && row < P.rows) next[k] = col.residual(P, row);
-                    }
-                    __syncwarp();
-                    with_activation(P.act, [&](auto act) {
-#pragma unroll
-                        for (int k = 0; k < S::kChunk / 8; ++k) {
-                            const int in_chunk = 8 * k + (lane >> 2), row = r0 + c + in_chunk;
-                            const float4* from = reinterpret_cast<const float4*>(turn + in_chunk * kTurnPitch + (lane & 3) * 8);
-                            const float4 a = from[0], b = from[1];
-                            const Eight y = {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
-                            if (row < P.rows && col.in) finish_eight<decltype(act)::value>(P, y, col.bias, add[k], row, col.j, col.whole_out);
-                        }
-                    });
+                    for (int i = 0; i < kChunk; ++i) part[(c + i) * kBM] = v[i];
                 }
+            } else {
+                finish_tile<BN>(P, lane_addr + static_cast<uint32_t>(acc * BN), col, res, r0, half, sh.turn[warp - 2]);
             }
             tc_fence_before();
             __syncwarp();
@@ -393,20 +422,21 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     }
     if constexpr (SPLIT) {
         cg::cluster_group cluster = cg::this_cluster();
-        cluster.sync();
         const int r0 = first_tile % row_tiles * BN;
         const int rows = min(BN, P.rows - r0);
         Columns col;
         col.set(P, first_tile / row_tiles * kBM + (lane & 15) * 8);
+        // rows of the tile go round the CTAs, two of a CTA's to a warp at a time, eight columns per lane
+        const int q0 = warp * 2 + (lane >> 4);
+        uint4 add = col.residual(P, r0 + rank + q0 * P.split);
+        cluster.sync();
         const float* part[kMaxSplit];
 #pragma unroll
         for (int s = 0; s < kMaxSplit; ++s)
             part[s] = cluster.map_shared_rank(reinterpret_cast<float*>(smem), s < P.split ? s : 0) + (lane & 15) * 8;
-        // rows of the tile go round the CTAs, two of a CTA's to a warp at a time, eight columns per lane
-        for (int q = warp * 2 + (lane >> 4); rank + q * P.split < rows; q += kThreads / 16) {
+        for (int q = q0; rank + q * P.split < rows; q += kThreads / 16) {
             const int r = rank + q * P.split;
-            const Eight add = col.residual(P, r0 + r);
-            Eight y = {};
+            float y[8] = {};
 #pragma unroll
             for (int s = 0; s < kMaxSplit; ++s)
                 if (s < P.split) {
@@ -414,28 +444,253 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                     const float4 a = from[0], b = from[1];
                     const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) y.v[i] += x[i];
+                    for (int i = 0; i < 8; ++i) y[i] += x[i];
                 }
-            if (col.in)
-                with_activation(P.act, [&](auto act) {
-                    finish_eight<decltype(act)::value>(P, y, col.bias, add, r0 + r, col.j, col.whole_out);
-                });
+            const uint4 next = col.residual(P, r0 + r + kThreads / 16 * P.split);
+            with_activation(P.act, [&](auto act) { col.finish<decltype(act)::value>(P, y, add, r0 + r); });
+            add = next;
         }
         cluster.sync();   // (nobody's shared memory goes while another reads it)
     }
 }
 
-// ---- host ----
-template <int BN, bool SPLIT>
-static cudaError_t launch(const CUtensorMap& w, const CUtensorMap& h, const Params& P, int grid, int dev, cudaStream_t stream) {
-    constexpr size_t smem = smem_bytes<BN>();
-    static bool allowed[64];   // large shared memory, per device
-    if (dev >= 64 || !allowed[dev]) {
-        const cudaError_t e =
-            cudaFuncSetAttribute(transform_kernel<BN, SPLIT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-        if (e != cudaSuccess) return e;
-        if (dev < 64) allowed[dev] = true;
+// ------------------------------------------------------------------------ pairs ----
+namespace pair {
+
+constexpr int kStages = 6;
+constexpr int kStageBytes = 2 * kWBytes;   // this CTA's 128 columns' weights and 128 of the pair's 256 hidden rows
+constexpr size_t kRing = static_cast<size_t>(kStages) * kStageBytes;
+constexpr int kTile = 256;                 // columns and rows of a pair's tile
+constexpr int kTmemCols = 512;
+
+// The address that a barrier of this CTA has in the pair's first CTA.
+__device__ __forceinline__ uint32_t in_first(const uint64_t* bar) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(bar)));
+    return r;
+}
+__device__ __forceinline__ void load_2d(void* dst, const CUtensorMap* map, int c0, int c1, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];" ::"r"(
+            smem_u32(dst)),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void alloc(uint32_t* slot, uint32_t cols) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void dealloc(uint32_t base, uint32_t cols) {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void mma(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t"
+        "}\n" ::"r"(tmem_d),
+        "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Arrives at both CTAs' barriers when everything issued so far has finished.
+__device__ __forceinline__ void commit_both(uint64_t* bar) {
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+                     smem_u32(bar)),
+                 "h"(static_cast<uint16_t>(3))
+                 : "memory");
+}
+__device__ __forceinline__ void arrive_in(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+// As mbar_wait_bounded, for arrivals from the other CTA.
+__device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+    if (try_wait_cluster(bar, parity)) return true;
+    const unsigned long long start = globaltimer_ns();
+    for (int round = 0; round < kSpinRounds; ++round) {
+        for (int spin = 0; spin < 64; ++spin)
+            if (try_wait_cluster(bar, parity)) return true;
+        if (*abort_flag) return false;
+        if (globaltimer_ns() - start > limit_ns) return false;
     }
+    return false;
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h,
+                      const __grid_constant__ Params P) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    Shared<kStages>& sh = *reinterpret_cast<Shared<kStages>*>(smem + kRing);
+    volatile int* abort_flag = &sh.abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = static_cast<int>(cluster.block_rank());
+
+    if (threadIdx.x == 0) {
+        if (blockIdx.x == 0 && P.status) *P.status = FEF_OK;   // (as above)
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(sh.full + s, 1);
+            mbar_init(sh.empty + s, 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(sh.tmem_full + a, 1);
+            mbar_init(sh.tmem_empty + a, 2 * kEpilogueWarps);
+        }
+        mbar_init(&sh.drained, 1);
+        sh.abort_flag = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) alloc(&sh.tmem_base, kTmemCols);   // (one CTA per SM: the columns are always free)
+    tc_fence_before();
+    __syncthreads();
+    cluster.sync();   // both CTAs' barriers stand before either is signalled from the other side
+    tc_fence_after();
+    const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&sh.tmem_base);
+
+    const int row_tiles = (P.rows + kTile - 1) / kTile, tiles = row_tiles * ((P.n + kTile - 1) / kTile);
+    const int blocks = (P.d + kBK - 1) / kBK;
+    const int first_tile = static_cast<int>(blockIdx.x) / 2, stride = static_cast<int>(gridDim.x) / 2;
+    int issued = 0;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int tile = first_tile; ok && tile < tiles; tile += stride) {
+                const int j0 = tile / row_tiles * kTile + rank * 128, r0 = tile % row_tiles * kTile + rank * 128;
+                for (int kb = 0; kb < blocks; ++kb) {
+#ifdef FEF_TEST_HOOKS
+                    if (blockIdx.x == 0 && P.withhold >= 0 && issued >= P.withhold) {
+                        ok = false;
+                        break;
+                    }
+#endif
+                    if (!mbar_wait_bounded(sh.empty + stage, phase ^ 1u, abort_flag, P.wait_ns)) {
+                        give_up(P, abort_flag);
+                        ok = false;
+                        break;
+                    }
+                    unsigned char* dst = smem + stage * kStageBytes;
+                    // the first CTA's barrier counts both CTAs' bytes (its phase cannot end before its own thread's arrival)
+                    if (rank == 0) mbar_arrive_expect_tx(sh.full + stage, 2 * kStageBytes);
+                    const uint32_t bar = in_first(sh.full + stage);
+                    load_2d(dst, &map_w, kb * kBK, j0, bar);
+                    load_2d(dst + kWBytes, &map_h, kb * kBK, r0, bar);
+                    ++issued;
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            int stage = 0;
+            uint32_t phase = 0;
+            unsigned uses[2] = {0u, 0u}, count = 0;
+            bool ok = true;
+            for (int tile = first_tile; ok && tile < tiles; tile += stride, ++count) {
+                const int acc = count & 1;
+                if (!wait_cluster(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns)) {
+                    give_up(P, abort_flag);
+                    break;
+                }
+                ++uses[acc];
+                tc_fence_after();
+                const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * kTile);
+                for (int kb = 0; kb < blocks; ++kb) {
+                    if (!wait_cluster(sh.full + stage, phase, abort_flag, P.wait_ns)) {
+                        give_up(P, abort_flag);
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint32_t at = smem_u32(smem + stage * kStageBytes);
+                    const uint64_t desc_w = smem_desc_sw128(at), desc_h = smem_desc_sw128(at + kWBytes);
+#pragma unroll
+                    for (int k = 0; k < kBK / 16; ++k)
+                        mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
+                            instruction(256, kTile), (kb | k) != 0 ? 1u : 0u);
+                    commit_both(sh.empty + stage);
+                    if (++stage == kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
+                }
+                if (ok) commit_both(sh.tmem_full + acc);
+            }
+            commit_both(&sh.drained);
+            volatile int never = 0;
+            mbar_wait_bounded(&sh.drained, 0u, &never, kWaitNs);
+        }
+    } else {
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
+        unsigned uses[2] = {0u, 0u}, count = 0;
+        for (int tile = first_tile; tile < tiles; tile += stride, ++count) {
+            const int acc = count & 1, r0 = tile % row_tiles * kTile;
+            Columns col;
+            Residuals res;
+            col.set(P, tile / row_tiles * kTile + rank * 128 + quarter * 32 + (lane & 3) * 8);
+            res.first(P, col, r0 + half * kChunk);
+            if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns))) {
+                give_up(P, abort_flag);
+                break;
+            }
+            ++uses[acc];
+            tc_fence_after();
+            finish_tile<kTile>(P, lane_addr + static_cast<uint32_t>(acc * kTile), col, res, r0, half, sh.turn[warp - 2]);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_in(in_first(sh.tmem_empty + acc));
+        }
+    }
+
+    // ---- teardown, as above; the first CTA's barriers answer for both CTAs' copies, and neither leaves before the other is done
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag && rank == 0 && threadIdx.x == 0) {
+        const int first = issued > kStages ? issued - kStages : 0;
+        for (int k = first; k < issued; ++k) {
+            volatile int never = 0;
+            mbar_wait_bounded(sh.full + (k % kStages), static_cast<uint32_t>((k / kStages) & 1), &never, kWaitNs);
+        }
+    }
+    __syncthreads();
+    cluster.sync();
+    if (warp == 1) {
+        tc_fence_after();
+        dealloc(tmem_base, kTmemCols);
+    }
+    cluster.sync();
+}
+
+}  // namespace pair
+
+// ---- host ----
+static cudaError_t allow_smem(const void* kernel, size_t smem, bool (&allowed)[64], int dev) {
+    if (dev < 64 && allowed[dev]) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e == cudaSuccess && dev < 64) allowed[dev] = true;
+    return e;
+}
+static cudaError_t launch_clusters(void (*kernel)(CUtensorMap, CUtensorMap, Params), const CUtensorMap& w, const CUtensorMap& h,
+                                   const Params& P, int grid, int cluster, size_t smem, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
     cfg.blockDim = dim3(kThreads);
@@ -443,25 +698,46 @@ static cudaError_t launch(const CUtensorMap& w, const CUtensorMap& h, const Para
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(SPLIT ? P.split : 1);
+    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = SPLIT ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, transform_kernel<BN, SPLIT>, w, h, P);
+    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, w, h, P);
+}
+// Boxes of 64 columns by w_box rows of the weight and h_box rows of the hidden states.
+static bool maps(const Params& P, int w_box, int h_box, CUtensorMap* w, CUtensorMap* h) {
+    return map_2d(w, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, P.weight, P.d, P.n, static_cast<uint64_t>(P.d) * 2, kBK, w_box,
+                  CU_TENSOR_MAP_SWIZZLE_128B) &&
+           map_2d(h, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, P.hidden, P.d, P.rows, static_cast<uint64_t>(P.ld_hidden) * 2, kBK, h_box,
+                  CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
+template <int BN, bool SPLIT>
+static cudaError_t launch(const CUtensorMap& w, const CUtensorMap& h, const Params& P, int grid, int dev, cudaStream_t stream) {
+    constexpr size_t smem = smem_bytes<Shape<BN>::kStages>(Shape<BN>::kRing);
+    static bool allowed[64];   // large shared memory, per device
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(transform_kernel<BN, SPLIT>), smem, allowed, dev);
+    if (e != cudaSuccess) return e;
+    return launch_clusters(transform_kernel<BN, SPLIT>, w, h, P, grid, SPLIT ? P.split : 1, smem, stream);
+}
 template <int BN>
 static cudaError_t run(Params& P, int split, int sms, int dev, cudaStream_t stream) {
     CUtensorMap w, h;
-    if (!map_2d(&w, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, P.weight, P.d, P.n, static_cast<uint64_t>(P.d) * 2, kBK, kBM,
-                CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !map_2d(&h, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, P.hidden, P.d, P.rows, static_cast<uint64_t>(P.ld_hidden) * 2, kBK, BN,
-                CU_TENSOR_MAP_SWIZZLE_128B))
-        return cudaErrorUnknown;
+    if (!maps(P, kBM, BN, &w, &h)) return cudaErrorUnknown;
     const int64_t tiles = static_cast<int64_t>((P.rows + BN - 1) / BN) * ((P.n + kBM - 1) / kBM);
     P.split = split;
     if (split > 1) return launch<BN, true>(w, h, P, static_cast<int>(tiles) * split, dev, stream);
     return launch<BN, false>(w, h, P, static_cast<int>(tiles < sms ? tiles : sms), dev, stream);
+}
+static cudaError_t run_pairs(const Params& P, int sms, int dev, cudaStream_t stream) {
+    CUtensorMap w, h;
+    if (!maps(P, 128, 128, &w, &h)) return cudaErrorUnknown;
+    constexpr size_t smem = smem_bytes<pair::kStages>(pair::kRing);
+    static bool allowed[64];
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(pair::transform_pair_kernel), smem, allowed, dev);
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = static_cast<int64_t>((P.rows + 255) / 256) * ((P.n + 255) / 256);
+    return launch_clusters(pair::transform_pair_kernel, w, h, P, 2 * static_cast<int>(tiles < sms / 2 ? tiles : sms / 2), 2, smem, stream);
 }
 
 // CTAs that share a tile's depth: as many as there are SMs for, with two blocks of the depth each at least.
@@ -553,6 +829,8 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
         e = run<32>(P, split_of(columns, d, sms), sms, dev, stream);
     } else if (rows <= 64) {
         e = run<64>(P, split_of(columns, d, sms), sms, dev, stream);
+    } else if (columns * ((rows + 255) / 256) > sms / 2) {
+        e = run_pairs(P, sms, dev, stream);   // (enough tiles of 256 columns by 256 rows for every pair of SMs, or nearly)
     } else {
         // tiles of 128 or of 256 rows: whichever keeps the SMs busy for less time (a block's time goes with the operands' rows)
         const int64_t t128 = columns * ((rows + 127) / 128), t256 = columns * ((rows + 255) / 256);

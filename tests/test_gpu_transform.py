@@ -67,7 +67,8 @@ def _check(fef, rows, n, d, act="none", bias=False, residual=False, dtype=torch.
 
 SIZES = [(1, 1, 8), (1, 128, 64), (2, 7, 16), (3, 130, 72), (5, 1000, 1056), (8, 257, 520), (9, 5003, 1056), (16, 4096, 4096),
          (17, 333, 248), (31, 64, 4096), (33, 1024, 1000), (64, 3584, 3584), (65, 129, 64), (100, 700, 2048), (128, 512, 512),
-         (129, 300, 136), (200, 2000, 1024), (257, 1111, 328), (300, 4096, 1024), (515, 640, 4096), (1000, 513, 200), (2048, 256, 64)]
+         (129, 300, 136), (200, 2000, 1024), (257, 1111, 328), (300, 4096, 1024), (515, 640, 4096), (1000, 513, 200), (2048, 256, 64),
+         (257, 5003, 72), (520, 4000, 264), (1030, 2500, 1000), (2048, 1300, 136), (2048, 4096, 512), (5000, 1111, 520)]
 
 
 @pytest.mark.parametrize("rows,n,d", SIZES)
@@ -79,7 +80,7 @@ def test_sizes(fef, rows, n, d):
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_activations_and_epilogues(fef, act, dtype):
-    for rows in (3, 70, 300):
+    for rows in (3, 70, 300, 7000):
         for bias in (False, True):
             for residual in (False, True):
                 _check(fef, rows, 390, 264, act, bias, residual, dtype, seed=5)
@@ -94,7 +95,7 @@ def test_every_row_count_up_to_a_tile(fef):
 
 def test_strided_operands_and_what_is_left_alone(fef):
     g = torch.Generator(device="cuda").manual_seed(1)
-    for rows, n, d in ((5, 37, 40), (70, 301, 200), (260, 129, 64)):
+    for rows, n, d in ((5, 37, 40), (70, 301, 200), (260, 129, 64), (2600, 1025, 72)):
         big = torch.randn((rows, 2 * d + 8), generator=g, device="cuda").to(torch.bfloat16)
         res = torch.randn((rows, n + 3), generator=g, device="cuda").to(torch.bfloat16)
         w = torch.randn((n, d), generator=g, device="cuda").to(torch.bfloat16)
@@ -112,7 +113,7 @@ def test_strided_operands_and_what_is_left_alone(fef):
 
 
 def test_in_place_on_the_residual(fef):
-    for rows, n, d in ((1, 512, 512), (40, 1024, 1024), (300, 520, 520)):
+    for rows, n, d in ((1, 512, 512), (40, 1024, 1024), (300, 520, 520), (1500, 2056, 2056)):
         h, w, b, r, want = _check(fef, rows, n, d, "silu", True, True)
         got, _ = fef.fef_hidden_transform(h, w, bias=b, residual=r, activation="silu", out=r)
         torch.cuda.synchronize()
@@ -120,7 +121,7 @@ def test_in_place_on_the_residual(fef):
 
 
 def test_a_bad_row_stays_alone(fef):
-    for rows, n, d in ((4, 300, 256), (50, 300, 256), (300, 300, 256)):
+    for rows, n, d in ((4, 300, 256), (50, 300, 256), (300, 300, 256), (9000, 300, 256)):
         h, w, b, r, want = _check(fef, rows, n, d, "gelu_tanh", True, True)
         bad = rows // 2
         for value in (math.nan, math.inf):
@@ -147,7 +148,12 @@ def test_large_weights_and_infinities_of_the_bias(fef):
 
 def test_rows_do_not_depend_on_their_neighbours(fef):
     """The same row gives the same bits in any place of any call with as many rows; twice the same call, the same bits."""
-    h, w, b, r, first = _check(fef, 300, 640, 1024, "silu", True, True)
+    for rows in (300, 4000):
+        _same_rows(fef, rows)
+
+
+def _same_rows(fef, rows):
+    h, w, b, r, first = _check(fef, rows, 640, 1024, "silu", True, True)
     again, _ = fef.fef_hidden_transform(h, w, bias=b, residual=r, activation="silu")
     assert torch.equal(first, again)
     turned, _ = fef.fef_hidden_transform(h.flip(0).contiguous(), w, bias=b, residual=r.flip(0).contiguous(), activation="silu")
@@ -155,7 +161,7 @@ def test_rows_do_not_depend_on_their_neighbours(fef):
 
 
 def test_streams_and_graphs(fef):
-    for rows in (2, 100, 600):
+    for rows in (2, 100, 600, 3000):
         h, w, b, r, want = _check(fef, rows, 1000, 512, "gelu", True, True)
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
@@ -176,7 +182,7 @@ def test_streams_and_graphs(fef):
 
 def test_two_calls_at_once(fef):
     streams = [torch.cuda.Stream() for _ in range(3)]
-    work = [_check(fef, rows, 2000, 1024, "silu", True, False, seed=rows) for rows in (1, 64, 700)]
+    work = [_check(fef, rows, 2000, 1024, "silu", True, False, seed=rows) for rows in (1, 64, 1700)]
     torch.cuda.synchronize()
     got = []
     for _ in range(5):
