@@ -31,7 +31,9 @@ struct Params {
     int act;        // fef_activation
     int out_f32;    // the output is float32, not bfloat16
     int wide_out, wide_residual;   // eight neighbours lie on 16-byte boundaries in every row
-    int split;      // CTAs (one cluster) that share a tile's depth
+    int row_tiles, tiles, blocks;   // tiles of rows, all tiles, 64-deep blocks
+    int split, split_log2;          // CTAs (one cluster) that share a tile's depth
+    int share_log2;                 // rows of a tile that one of them finishes
     unsigned long long wait_ns;
     int32_t* status;
 #ifdef FEF_TEST_HOOKS
@@ -64,8 +66,8 @@ __device__ __forceinline__ float activate(float y) {
 // states: the right operand, N = BN), so that few hidden rows cost few columns of tensor memory and no padding of the weight
 // stream.  Warp 0 brings 64-deep blocks of both operands through a ring by TMA (one thread), warp 1 issues the MMAs (one thread),
 // warps 2-9 are the epilogue.  Accumulators are double-buffered.  With fewer tiles than SMs the CTAs of a thread-block cluster
-// share a tile's depth: each leaves its sums in shared memory and finishes a share of the rows, adding the others' over
-// distributed shared memory.
+// share a tile's depth: each finishes a share of the rows, whose sums the others write into its shared memory (writing takes a
+// third of the time of reading them from there).
 //
 // transform_pair_kernel: two CTAs (a cluster) take 256 columns by 256 rows with tcgen05.mma.cta_group::2: each brings its own 128
 // columns' weights and half of the hidden rows, which both tensor cores read.  Per SM a block is 32 KiB instead of the 48 KiB of
@@ -83,10 +85,15 @@ template <int BN>
 struct Shape {
     static constexpr int kHBytes = BN * kBK * 2;
     static constexpr int kStageBytes = kWBytes + kHBytes;
-    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 6 : BN == 64 ? 8 : 10;
+    static constexpr int kStages = BN == 256 ? 4 : BN == 128 ? 4 : BN == 64 ? 6 : 8;
     static constexpr int kTmemCols = 2 * BN;
     static constexpr size_t kRing = static_cast<size_t>(kStages) * kStageBytes;
-    static_assert(kRing >= static_cast<size_t>(BN) * kBM * 4, "a tile's sums fit into the ring");
+    // Where the cluster's CTAs put what they add up to the rows that this one finishes: BN / split rows of 128 sums from each.  With 256
+    // rows there is no room beside the ring, and a barrier more frees the ring for it.
+    static constexpr size_t kSums = static_cast<size_t>(BN) * kBM * 4;
+    static constexpr bool kSumsInRing = BN == 256;
+    static constexpr size_t kBuffers = kRing + (kSumsInRing ? 0 : kSums);
+    static_assert(!kSumsInRing || kRing >= kSums, "a tile's sums fit into the ring");
 };
 // binary32 accumulator, bfloat16 operands, both K-major
 __device__ constexpr uint32_t instruction(int m, int n) {
@@ -245,6 +252,10 @@ __device__ __forceinline__ void finish_tile(const Params& P, uint32_t tmem, cons
     }
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory");
+}
+
 __device__ __forceinline__ void give_up(const Params& P, volatile int* abort_flag) {
     *abort_flag = 1;
     report(P.status, FEF_ERR_TIMEOUT);
@@ -257,13 +268,13 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     using S = Shape<BN>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    Shared<S::kStages>& sh = *reinterpret_cast<Shared<S::kStages>*>(smem + S::kRing);
+    Shared<S::kStages>& sh = *reinterpret_cast<Shared<S::kStages>*>(smem + S::kBuffers);
     volatile int* abort_flag = &sh.abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        // (cleared here and not by a launch of its own: the earliest report comes after a wait of a second)
-        if (blockIdx.x == 0 && P.status) *P.status = FEF_OK;
+        prefetch_map(&map_w);
+        prefetch_map(&map_h);
         for (int s = 0; s < S::kStages; ++s) {
             mbar_init(sh.full + s, 1);
             mbar_init(sh.empty + s, 1);
@@ -282,13 +293,16 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     tc_fence_after();
     const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&sh.tmem_base);
 
-    const int row_tiles = (P.rows + BN - 1) / BN, tiles = row_tiles * ((P.n + kBM - 1) / kBM);
-    const int blocks = (P.d + kBK - 1) / kBK;
-    const int rank = SPLIT ? static_cast<int>(blockIdx.x) % P.split : 0;
-    const int first_tile = SPLIT ? static_cast<int>(blockIdx.x) / P.split : static_cast<int>(blockIdx.x);
+    cudaGridDependencySynchronize();
+    // (cleared here and not by a launch of its own: the earliest report comes after a wait of a second)
+    if (threadIdx.x == 0 && blockIdx.x == 0 && P.status) *P.status = FEF_OK;
+
+    const int row_tiles = P.row_tiles, tiles = P.tiles;
+    const int rank = SPLIT ? static_cast<int>(blockIdx.x) & (P.split - 1) : 0;   // (a power of two)
+    const int first_tile = SPLIT ? static_cast<int>(blockIdx.x) >> P.split_log2 : static_cast<int>(blockIdx.x);
     const int stride = SPLIT ? tiles : static_cast<int>(gridDim.x);   // (SPLIT: one tile per cluster)
-    const int kb_begin = SPLIT ? static_cast<int>(static_cast<int64_t>(rank) * blocks / P.split) : 0;
-    const int kb_end = SPLIT ? static_cast<int>(static_cast<int64_t>(rank + 1) * blocks / P.split) : blocks;
+    const int kb_begin = SPLIT ? rank * P.blocks >> P.split_log2 : 0;
+    const int kb_end = SPLIT ? (rank + 1) * P.blocks >> P.split_log2 : P.blocks;
     int issued = 0;   // stages put in flight (producer thread)
 
     if (warp == 0) {
@@ -384,20 +398,8 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
             }
             ++uses[acc];
             tc_fence_after();
-            if constexpr (SPLIT) {
-                // every copy into the ring has been read by an MMA that is complete: it is free
-                float* part = reinterpret_cast<float*>(smem) + quarter * 32 + lane;
-#pragma unroll 1
-                for (int c = half * kChunk; c < BN; c += 2 * kChunk) {
-                    if (r0 + c >= P.rows) break;   // (uniform over the warp)
-                    float v[kChunk];
-                    tmem_load16(lane_addr + static_cast<uint32_t>(acc * BN + c), v);
-#pragma unroll
-                    for (int i = 0; i < kChunk; ++i) part[(c + i) * kBM] = v[i];
-                }
-            } else {
-                finish_tile<BN>(P, lane_addr + static_cast<uint32_t>(acc * BN), col, res, r0, half, sh.turn[warp - 2]);
-            }
+            if constexpr (SPLIT) break;   // (one tile: it is finished below, by the whole cluster)
+            finish_tile<BN>(P, lane_addr + static_cast<uint32_t>(acc * BN), col, res, r0, half, sh.turn[warp - 2]);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.tmem_empty + acc);   // the accumulator may be overwritten
@@ -416,41 +418,54 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         }
     }
     __syncthreads();
+    if constexpr (SPLIT) {
+        cg::cluster_group cluster = cg::this_cluster();
+        unsigned char* sums = smem + (S::kSumsInRing ? 0 : S::kRing);
+        const int r0 = first_tile % row_tiles * BN, rows = min(BN, P.rows - r0);
+        const int share = BN >> P.split_log2;   // rows that a CTA finishes (of the tile's BN)
+        // (every CTA's MMAs are complete and have read its ring, so it is free)
+        if (S::kSumsInRing) cluster.sync();
+        if (warp >= 2) {
+            const int quarter = warp & 3, half = (warp - 2) >> 2;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = half * kChunk; c < rows; c += 2 * kChunk) {
+                float v[kChunk];
+                tmem_load16(tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(c), v);
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) {
+                    const int owner = (c + i) >> P.share_log2;
+                    float* to = cluster.map_shared_rank(reinterpret_cast<float*>(sums), owner);
+                    to[(rank * share + ((c + i) & (share - 1))) * kBM + quarter * 32 + lane] = v[i];
+                }
+            }
+            tc_fence_before();
+        }
+        Columns col;
+        col.set(P, first_tile / row_tiles * kBM + (lane & 15) * 8);
+        // this CTA's rows, two to a warp at a time, eight columns per lane
+        constexpr int kStep = kThreads / 16;
+        const int own = min(share, rows - rank * share), q0 = warp * 2 + (lane >> 4);
+        uint4 add = q0 < own ? col.residual(P, r0 + rank * share + q0) : make_uint4(0u, 0u, 0u, 0u);
+        cluster.sync();
+        for (int q = q0; q < own; q += kStep) {
+            float y[8] = {};
+            for (int s = 0; s < P.split; ++s) {
+                const float4* from = reinterpret_cast<const float4*>(sums) + (s * share + q) * (kBM / 4) + (lane & 15) * 2;
+                const float4 a = from[0], b = from[1];
+                const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] += x[i];
+            }
+            const int64_t row = r0 + rank * share + q;
+            const uint4 next = q + kStep < own ? col.residual(P, row + kStep) : make_uint4(0u, 0u, 0u, 0u);
+            with_activation(P.act, [&](auto act) { col.finish<decltype(act)::value>(P, y, add, row); });
+            add = next;
+        }
+    }
     if (warp == 1) {
         tc_fence_after();
         tmem_dealloc(tmem_base, S::kTmemCols);
-    }
-    if constexpr (SPLIT) {
-        cg::cluster_group cluster = cg::this_cluster();
-        const int r0 = first_tile % row_tiles * BN;
-        const int rows = min(BN, P.rows - r0);
-        Columns col;
-        col.set(P, first_tile / row_tiles * kBM + (lane & 15) * 8);
-        // rows of the tile go round the CTAs, two of a CTA's to a warp at a time, eight columns per lane
-        const int q0 = warp * 2 + (lane >> 4);
-        uint4 add = col.residual(P, r0 + rank + q0 * P.split);
-        cluster.sync();
-        const float* part[kMaxSplit];
-#pragma unroll
-        for (int s = 0; s < kMaxSplit; ++s)
-            part[s] = cluster.map_shared_rank(reinterpret_cast<float*>(smem), s < P.split ? s : 0) + (lane & 15) * 8;
-        for (int q = q0; rank + q * P.split < rows; q += kThreads / 16) {
-            const int r = rank + q * P.split;
-            float y[8] = {};
-#pragma unroll
-            for (int s = 0; s < kMaxSplit; ++s)
-                if (s < P.split) {
-                    const float4* from = reinterpret_cast<const float4*>(part[s] + r * kBM);
-                    const float4 a = from[0], b = from[1];
-                    const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] += x[i];
-                }
-            const uint4 next = col.residual(P, r0 + r + kThreads / 16 * P.split);
-            with_activation(P.act, [&](auto act) { col.finish<decltype(act)::value>(P, y, add, r0 + r); });
-            add = next;
-        }
-        cluster.sync();   // (nobody's shared memory goes while another reads it)
     }
 }
 
@@ -539,7 +554,8 @@ transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     const int rank = static_cast<int>(cluster.block_rank());
 
     if (threadIdx.x == 0) {
-        if (blockIdx.x == 0 && P.status) *P.status = FEF_OK;   // (as above)
+        prefetch_map(&map_w);
+        prefetch_map(&map_h);
         for (int s = 0; s < kStages; ++s) {
             mbar_init(sh.full + s, 1);
             mbar_init(sh.empty + s, 1);
@@ -559,8 +575,10 @@ transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     tc_fence_after();
     const uint32_t tmem_base = *reinterpret_cast<volatile uint32_t*>(&sh.tmem_base);
 
-    const int row_tiles = (P.rows + kTile - 1) / kTile, tiles = row_tiles * ((P.n + kTile - 1) / kTile);
-    const int blocks = (P.d + kBK - 1) / kBK;
+    cudaGridDependencySynchronize();
+    if (threadIdx.x == 0 && blockIdx.x == 0 && P.status) *P.status = FEF_OK;   // (as above)
+
+    const int row_tiles = P.row_tiles, tiles = P.tiles, blocks = P.blocks;
     const int first_tile = static_cast<int>(blockIdx.x) / 2, stride = static_cast<int>(gridDim.x) / 2;
     int issued = 0;
 
@@ -696,12 +714,14 @@ static cudaError_t launch_clusters(void (*kernel)(CUtensorMap, CUtensorMap, Para
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // barriers and tensor memory are set up while the
+    attr[0].val.programmaticStreamSerializationAllowed = 1;            // kernel before this one drains
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = cluster > 1 ? 1 : 0;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, w, h, P);
 }
 // Boxes of 64 columns by w_box rows of the weight and h_box rows of the hidden states.
@@ -714,30 +734,39 @@ static bool maps(const Params& P, int w_box, int h_box, CUtensorMap* w, CUtensor
 
 template <int BN, bool SPLIT>
 static cudaError_t launch(const CUtensorMap& w, const CUtensorMap& h, const Params& P, int grid, int dev, cudaStream_t stream) {
-    constexpr size_t smem = smem_bytes<Shape<BN>::kStages>(Shape<BN>::kRing);
+    constexpr size_t smem = smem_bytes<Shape<BN>::kStages>(Shape<BN>::kBuffers);
     static bool allowed[64];   // large shared memory, per device
     const cudaError_t e = allow_smem(reinterpret_cast<const void*>(transform_kernel<BN, SPLIT>), smem, allowed, dev);
     if (e != cudaSuccess) return e;
     return launch_clusters(transform_kernel<BN, SPLIT>, w, h, P, grid, SPLIT ? P.split : 1, smem, stream);
 }
+static int log2_of(int power) {
+    int r = 0;
+    while ((1 << r) < power) ++r;
+    return r;
+}
 template <int BN>
 static cudaError_t run(Params& P, int split, int sms, int dev, cudaStream_t stream) {
     CUtensorMap w, h;
     if (!maps(P, kBM, BN, &w, &h)) return cudaErrorUnknown;
-    const int64_t tiles = static_cast<int64_t>((P.rows + BN - 1) / BN) * ((P.n + kBM - 1) / kBM);
+    P.row_tiles = (P.rows + BN - 1) / BN;
+    P.tiles = P.row_tiles * ((P.n + kBM - 1) / kBM);   // (2^26 at most)
     P.split = split;
-    if (split > 1) return launch<BN, true>(w, h, P, static_cast<int>(tiles) * split, dev, stream);
-    return launch<BN, false>(w, h, P, static_cast<int>(tiles < sms ? tiles : sms), dev, stream);
+    P.split_log2 = log2_of(split);
+    P.share_log2 = log2_of(BN / split);
+    if (split > 1) return launch<BN, true>(w, h, P, P.tiles * split, dev, stream);
+    return launch<BN, false>(w, h, P, P.tiles < sms ? P.tiles : sms, dev, stream);
 }
-static cudaError_t run_pairs(const Params& P, int sms, int dev, cudaStream_t stream) {
+static cudaError_t run_pairs(Params& P, int sms, int dev, cudaStream_t stream) {
     CUtensorMap w, h;
     if (!maps(P, 128, 128, &w, &h)) return cudaErrorUnknown;
     constexpr size_t smem = smem_bytes<pair::kStages>(pair::kRing);
     static bool allowed[64];
     const cudaError_t e = allow_smem(reinterpret_cast<const void*>(pair::transform_pair_kernel), smem, allowed, dev);
     if (e != cudaSuccess) return e;
-    const int64_t tiles = static_cast<int64_t>((P.rows + 255) / 256) * ((P.n + 255) / 256);
-    return launch_clusters(pair::transform_pair_kernel, w, h, P, 2 * static_cast<int>(tiles < sms / 2 ? tiles : sms / 2), 2, smem, stream);
+    P.row_tiles = (P.rows + pair::kTile - 1) / pair::kTile;
+    P.tiles = P.row_tiles * ((P.n + pair::kTile - 1) / pair::kTile);
+    return launch_clusters(pair::transform_pair_kernel, w, h, P, 2 * (P.tiles < sms / 2 ? P.tiles : sms / 2), 2, smem, stream);
 }
 
 // CTAs that share a tile's depth: as many as there are SMs for, with two blocks of the depth each at least.
@@ -811,6 +840,7 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
     P.d = d;
     P.act = activation;
     P.out_f32 = dt == FEF_F32;
+    P.blocks = (d + kBK - 1) / kBK;
     P.wide_out = !(reinterpret_cast<uintptr_t>(out) & 15) && ldo * esize % 16 == 0;
     P.wide_residual = !(reinterpret_cast<uintptr_t>(residual) & 15) && ld_residual % 8 == 0;
     P.wait_ns = kWaitNs;
