@@ -128,6 +128,26 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+// A whole warp's wait.  The producer and the MMA issuer run as whole warps, with one elected lane for the copies and MMAs
+// themselves: descriptors, addresses and flags then are warp-uniform values.  With one lane in a branch of its own a block cost each of
+// the two over 600 clocks, more than the MMAs of a 128 x 256 x 64 block.
+__device__ __forceinline__ bool all_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+    return __all_sync(0xFFFFFFFFu, mbar_wait_bounded(bar, parity, abort_flag, limit_ns));
+}
+
+// An epilogue warp's wait for a tile: one lane polls, and not all the time.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned long long limit_ns) {
+    int ok = 0;
+    if ((threadIdx.x & 31) == 0) {
+        for (int spin = 0; spin < 64 && !ok; ++spin) {
+            ok = mbar_try_wait(bar, parity);
+            if (!ok) __nanosleep(64);
+        }
+        if (!ok) ok = mbar_wait_bounded(bar, parity, abort_flag, limit_ns);
+    }
+    return __shfl_sync(0xFFFFFFFFu, ok, 0) != 0;
+}
+
 // f with the activation as a constant.
 template <class F>
 __device__ __forceinline__ void with_activation(int act, F f) {
@@ -306,80 +326,83 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     int issued = 0;   // stages put in flight (producer thread)
 
     if (warp == 0) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (int tile = first_tile; ok && tile < tiles; tile += stride) {
-                const int j0 = tile / row_tiles * kBM, r0 = tile % row_tiles * BN;
-                for (int kb = kb_begin; kb < kb_end; ++kb) {
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int tile = first_tile; ok && tile < tiles; tile += stride) {
+            const int j0 = tile / row_tiles * kBM, r0 = tile % row_tiles * BN;
+            for (int kb = kb_begin; kb < kb_end; ++kb) {
 #ifdef FEF_TEST_HOOKS
-                    // Test build: nothing is copied from here on and nothing arrives, so the waits for it run out.
-                    if (blockIdx.x == 0 && P.withhold >= 0 && issued >= P.withhold) {
-                        ok = false;
-                        break;
-                    }
+                // Test build: nothing is copied from here on and nothing arrives, so the waits for it run out.
+                if (blockIdx.x == 0 && P.withhold >= 0 && issued >= P.withhold) {
+                    ok = false;
+                    break;
+                }
 #endif
-                    if (!mbar_wait_bounded(sh.empty + stage, phase ^ 1u, abort_flag, P.wait_ns)) {
-                        give_up(P, abort_flag);
-                        ok = false;
-                        break;
-                    }
+                if (!all_wait(sh.empty + stage, phase ^ 1u, abort_flag, P.wait_ns)) {
+                    give_up(P, abort_flag);
+                    ok = false;
+                    break;
+                }
+                if (elect_one()) {
                     unsigned char* dst = smem + stage * S::kStageBytes;
                     mbar_arrive_expect_tx(sh.full + stage, S::kStageBytes);
                     tma_load_2d(dst, &map_w, kb * kBK, j0, sh.full + stage);
                     tma_load_2d(dst + kWBytes, &map_h, kb * kBK, r0, sh.full + stage);
-                    ++issued;
-                    if (++stage == S::kStages) {
-                        stage = 0;
-                        phase ^= 1u;
-                    }
+                }
+                __syncwarp();
+                ++issued;
+                if (++stage == S::kStages) {
+                    stage = 0;
+                    phase ^= 1u;
                 }
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            unsigned uses[2] = {0u, 0u}, count = 0;
-            bool ok = true;
-            for (int tile = first_tile; ok && tile < tiles; tile += stride, ++count) {
-                const int acc = count & 1;
-                // the epilogue must have drained this accumulator (passes at once on its first use)
-                if (!mbar_wait_bounded(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns)) {
+        int stage = 0;
+        uint32_t phase = 0;
+        unsigned uses[2] = {0u, 0u}, count = 0;
+        bool ok = true;
+        const uint64_t desc = smem_desc_sw128(smem_u32(smem));
+        for (int tile = first_tile; ok && tile < tiles; tile += stride, ++count) {
+            const int acc = count & 1;
+            // the epilogue must have drained this accumulator (passes at once on its first use)
+            if (!all_wait(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns)) {
+                give_up(P, abort_flag);
+                break;
+            }
+            ++uses[acc];
+            const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
+            for (int kb = kb_begin; kb < kb_end; ++kb) {
+                if (!all_wait(sh.full + stage, phase, abort_flag, P.wait_ns)) {
                     give_up(P, abort_flag);
+                    ok = false;
                     break;
                 }
-                ++uses[acc];
                 tc_fence_after();
-                const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
-                for (int kb = kb_begin; kb < kb_end; ++kb) {
-                    if (!mbar_wait_bounded(sh.full + stage, phase, abort_flag, P.wait_ns)) {
-                        give_up(P, abort_flag);
-                        ok = false;
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t at = smem_u32(smem + stage * S::kStageBytes);
-                    const uint64_t desc_w = smem_desc_sw128(at), desc_h = smem_desc_sw128(at + kWBytes);
+                if (elect_one()) {
+                    const uint64_t desc_w = desc + static_cast<uint64_t>(stage * (S::kStageBytes >> 4));   // (16-byte units)
+                    const uint64_t desc_h = desc_w + static_cast<uint64_t>(kWBytes >> 4);
 #pragma unroll
                     for (int k = 0; k < kBK / 16; ++k)   // 32 bytes further along K inside the swizzle row
                         tc_mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
                                instruction(kBM, BN), (kb > kb_begin || k) ? 1u : 0u);
                     tc_commit(sh.empty + stage);   // arrives when these MMAs have read the stage
-                    if (++stage == S::kStages) {
-                        stage = 0;
-                        phase ^= 1u;
-                    }
+                    if (kb == kb_end - 1) tc_commit(sh.tmem_full + acc);   // arrives when the tile's accumulator is complete
                 }
-                if (ok) tc_commit(sh.tmem_full + acc);   // arrives when the tile's accumulator is complete
+                __syncwarp();
+                if (++stage == S::kStages) {
+                    stage = 0;
+                    phase ^= 1u;
+                }
             }
-            // everything issued has finished before the tensor memory goes back, after a wait that ran out too: this one does
-            // not look at the abort flag
-            tc_commit(&sh.drained);
-            volatile int never = 0;
-            mbar_wait_bounded(&sh.drained, 0u, &never, kWaitNs);
         }
+        // everything issued has finished before the tensor memory goes back, after a wait that ran out too: this one does
+        // not look at the abort flag
+        if (elect_one()) tc_commit(&sh.drained);
+        __syncwarp();
+        volatile int never = 0;
+        mbar_wait_bounded(&sh.drained, 0u, &never, kWaitNs);
     } else {
         const int quarter = warp & 3, half = (warp - 2) >> 2;   // the tensor-memory lanes this warp may read; its chunks
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
@@ -392,7 +415,7 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
                 col.set(P, tile / row_tiles * kBM + quarter * 32 + (lane & 3) * 8);
                 res.first(P, col, r0 + half * kChunk);
             }
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns))) {
+            if (!warp_wait(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns)) {
                 give_up(P, abort_flag);
                 break;
             }
@@ -472,11 +495,14 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 // ------------------------------------------------------------------------ pairs ----
 namespace pair {
 
-constexpr int kStages = 6;
-constexpr int kStageBytes = 2 * kWBytes;   // this CTA's 128 columns' weights and 128 of the pair's 256 hidden rows
-constexpr size_t kRing = static_cast<size_t>(kStages) * kStageBytes;
-constexpr int kTile = 256;                 // columns and rows of a pair's tile
-constexpr int kTmemCols = 512;
+template <int TN>   // rows of a pair's tile
+struct Shape {
+    static constexpr int kHBytes = TN / 2 * kBK * 2;
+    static constexpr int kStageBytes = kWBytes + kHBytes;   // this CTA's 128 columns' weights and half of the pair's hidden rows
+    static constexpr int kStages = TN == 256 ? 6 : TN == 128 ? 8 : 9;
+    static constexpr size_t kRing = static_cast<size_t>(kStages) * kStageBytes;
+};
+constexpr int kTileN = 256;                // columns of a pair's tile
 
 // The address that a barrier of this CTA has in the pair's first CTA.
 __device__ __forceinline__ uint32_t in_first(const uint64_t* bar) {
@@ -542,12 +568,15 @@ __device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, vol
     return false;
 }
 
+template <int TN>
 __global__ void __launch_bounds__(kThreads, 1)
 transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h,
                       const __grid_constant__ Params P) {
+    using S = Shape<TN>;
+    constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes, kTmemCols = 2 * TN;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    Shared<kStages>& sh = *reinterpret_cast<Shared<kStages>*>(smem + kRing);
+    Shared<kStages>& sh = *reinterpret_cast<Shared<kStages>*>(smem + S::kRing);
     volatile int* abort_flag = &sh.abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     cg::cluster_group cluster = cg::this_cluster();
@@ -583,75 +612,80 @@ transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     int issued = 0;
 
     if (warp == 0) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (int tile = first_tile; ok && tile < tiles; tile += stride) {
-                const int j0 = tile / row_tiles * kTile + rank * 128, r0 = tile % row_tiles * kTile + rank * 128;
-                for (int kb = 0; kb < blocks; ++kb) {
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        for (int tile = first_tile; ok && tile < tiles; tile += stride) {
+            const int j0 = tile / row_tiles * kTileN + rank * 128, r0 = tile % row_tiles * TN + rank * (TN / 2);
+            for (int kb = 0; kb < blocks; ++kb) {
 #ifdef FEF_TEST_HOOKS
-                    if (blockIdx.x == 0 && P.withhold >= 0 && issued >= P.withhold) {
-                        ok = false;
-                        break;
-                    }
+                if (blockIdx.x == 0 && P.withhold >= 0 && issued >= P.withhold) {
+                    ok = false;
+                    break;
+                }
 #endif
-                    if (!mbar_wait_bounded(sh.empty + stage, phase ^ 1u, abort_flag, P.wait_ns)) {
-                        give_up(P, abort_flag);
-                        ok = false;
-                        break;
-                    }
+                if (!all_wait(sh.empty + stage, phase ^ 1u, abort_flag, P.wait_ns)) {
+                    give_up(P, abort_flag);
+                    ok = false;
+                    break;
+                }
+                if (elect_one()) {
                     unsigned char* dst = smem + stage * kStageBytes;
                     // the first CTA's barrier counts both CTAs' bytes (its phase cannot end before its own thread's arrival)
                     if (rank == 0) mbar_arrive_expect_tx(sh.full + stage, 2 * kStageBytes);
                     const uint32_t bar = in_first(sh.full + stage);
                     load_2d(dst, &map_w, kb * kBK, j0, bar);
                     load_2d(dst + kWBytes, &map_h, kb * kBK, r0, bar);
-                    ++issued;
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1u;
-                    }
+                }
+                __syncwarp();
+                ++issued;
+                if (++stage == kStages) {
+                    stage = 0;
+                    phase ^= 1u;
                 }
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             int stage = 0;
             uint32_t phase = 0;
             unsigned uses[2] = {0u, 0u}, count = 0;
             bool ok = true;
+            const uint64_t desc = smem_desc_sw128(smem_u32(smem));
             for (int tile = first_tile; ok && tile < tiles; tile += stride, ++count) {
                 const int acc = count & 1;
-                if (!wait_cluster(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns)) {
+                if (!__all_sync(0xFFFFFFFFu, wait_cluster(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns))) {
                     give_up(P, abort_flag);
                     break;
                 }
                 ++uses[acc];
-                tc_fence_after();
-                const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * kTile);
+                const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * TN);
                 for (int kb = 0; kb < blocks; ++kb) {
-                    if (!wait_cluster(sh.full + stage, phase, abort_flag, P.wait_ns)) {
+                    if (!__all_sync(0xFFFFFFFFu, wait_cluster(sh.full + stage, phase, abort_flag, P.wait_ns))) {
                         give_up(P, abort_flag);
                         ok = false;
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t at = smem_u32(smem + stage * kStageBytes);
-                    const uint64_t desc_w = smem_desc_sw128(at), desc_h = smem_desc_sw128(at + kWBytes);
+                    if (elect_one()) {
+                        const uint64_t desc_w = desc + static_cast<uint64_t>(stage * (kStageBytes >> 4));
+                        const uint64_t desc_h = desc_w + static_cast<uint64_t>(kWBytes >> 4);
 #pragma unroll
-                    for (int k = 0; k < kBK / 16; ++k)
-                        mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
-                            instruction(256, kTile), (kb | k) != 0 ? 1u : 0u);
-                    commit_both(sh.empty + stage);
+                        for (int k = 0; k < kBK / 16; ++k)
+                            mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
+                                instruction(256, TN), (kb | k) != 0 ? 1u : 0u);
+                        commit_both(sh.empty + stage);
+                        if (kb == blocks - 1) commit_both(sh.tmem_full + acc);
+                    }
+                    __syncwarp();
                     if (++stage == kStages) {
                         stage = 0;
                         phase ^= 1u;
                     }
                 }
-                if (ok) commit_both(sh.tmem_full + acc);
             }
-            commit_both(&sh.drained);
+            if (elect_one()) commit_both(&sh.drained);
+            __syncwarp();
             volatile int never = 0;
             mbar_wait_bounded(&sh.drained, 0u, &never, kWaitNs);
         }
@@ -660,18 +694,18 @@ transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
         unsigned uses[2] = {0u, 0u}, count = 0;
         for (int tile = first_tile; tile < tiles; tile += stride, ++count) {
-            const int acc = count & 1, r0 = tile % row_tiles * kTile;
+            const int acc = count & 1, r0 = tile % row_tiles * TN;
             Columns col;
             Residuals res;
-            col.set(P, tile / row_tiles * kTile + rank * 128 + quarter * 32 + (lane & 3) * 8);
+            col.set(P, tile / row_tiles * kTileN + rank * 128 + quarter * 32 + (lane & 3) * 8);
             res.first(P, col, r0 + half * kChunk);
-            if (!__all_sync(0xFFFFFFFFu, mbar_wait_bounded(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns))) {
+            if (!warp_wait(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns)) {
                 give_up(P, abort_flag);
                 break;
             }
             ++uses[acc];
             tc_fence_after();
-            finish_tile<kTile>(P, lane_addr + static_cast<uint32_t>(acc * kTile), col, res, r0, half, sh.turn[warp - 2]);
+            finish_tile<TN>(P, lane_addr + static_cast<uint32_t>(acc * TN), col, res, r0, half, sh.turn[warp - 2]);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_in(in_first(sh.tmem_empty + acc));
@@ -757,16 +791,17 @@ static cudaError_t run(Params& P, int split, int sms, int dev, cudaStream_t stre
     if (split > 1) return launch<BN, true>(w, h, P, P.tiles * split, dev, stream);
     return launch<BN, false>(w, h, P, P.tiles < sms ? P.tiles : sms, dev, stream);
 }
+template <int TN>
 static cudaError_t run_pairs(Params& P, int sms, int dev, cudaStream_t stream) {
     CUtensorMap w, h;
-    if (!maps(P, 128, 128, &w, &h)) return cudaErrorUnknown;
-    constexpr size_t smem = smem_bytes<pair::kStages>(pair::kRing);
+    if (!maps(P, 128, TN / 2, &w, &h)) return cudaErrorUnknown;
+    constexpr size_t smem = smem_bytes<pair::Shape<TN>::kStages>(pair::Shape<TN>::kRing);
     static bool allowed[64];
-    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(pair::transform_pair_kernel), smem, allowed, dev);
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(pair::transform_pair_kernel<TN>), smem, allowed, dev);
     if (e != cudaSuccess) return e;
-    P.row_tiles = (P.rows + pair::kTile - 1) / pair::kTile;
-    P.tiles = P.row_tiles * ((P.n + pair::kTile - 1) / pair::kTile);
-    return launch_clusters(pair::transform_pair_kernel, w, h, P, 2 * (P.tiles < sms / 2 ? P.tiles : sms / 2), 2, smem, stream);
+    P.row_tiles = (P.rows + TN - 1) / TN;
+    P.tiles = P.row_tiles * ((P.n + pair::kTileN - 1) / pair::kTileN);
+    return launch_clusters(pair::transform_pair_kernel<TN>, w, h, P, 2 * (P.tiles < sms / 2 ? P.tiles : sms / 2), 2, smem, stream);
 }
 
 // CTAs that share a tile's depth: as many as there are SMs for, with two blocks of the depth each at least.
@@ -860,7 +895,7 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
     } else if (rows <= 64) {
         e = run<64>(P, split_of(columns, d, sms), sms, dev, stream);
     } else if (columns * ((rows + 255) / 256) > sms / 2) {
-        e = run_pairs(P, sms, dev, stream);   // (enough tiles of 256 columns by 256 rows for every pair of SMs, or nearly)
+        e = run_pairs<256>(P, sms, dev, stream);   // (enough tiles of 256 columns by 256 rows for every pair of SMs, or nearly)
     } else {
         // tiles of 128 or of 256 rows: whichever keeps the SMs busy for less time (a block's time goes with the operands' rows)
         const int64_t t128 = columns * ((rows + 127) / 128), t256 = columns * ((rows + 255) / 256);
