@@ -804,12 +804,43 @@ static cudaError_t run_pairs(Params& P, int sms, int dev, cudaStream_t stream) {
     return launch_clusters(pair::transform_pair_kernel<TN>, w, h, P, 2 * (P.tiles < sms / 2 ? P.tiles : sms / 2), 2, smem, stream);
 }
 
-// CTAs that share a tile's depth: as many as there are SMs for, with two blocks of the depth each at least.
-static int split_of(int64_t tiles, int d, int sms) {
+// Which tiles, and how many CTAs to a tile.  Every choice is right for every call; what each takes was measured over 23 sizes (1 to
+// 2048 rows, 256 to 8192 columns, 512 to 8192 deep), in microseconds and within a tenth or two:
+//   a 64-deep block   0.22 + 0.00065 BN (a CTA of its own)   0.175 + 0.0006 TN (a pair)
+//   the last epilogue   0.4 + 0.01 BN       setup   3.5, a pair's 4.7
+//   handing the sums of a shared tile over   0.3 + 0.029 BN, with two CTAs 0.7 of that
+// e.g. 64 rows x 3584 x 3584: BN = 64 and four CTAs 9.0 (predicted 9.3), one CTA 18.4 (18.8); 512 x 4096 x 4096: pairs of 128 rows
+// 21.4 (22.4), BN = 128 25.1 (24.6); 1024 x 1024 x 1024: BN = 64 8.7 (8.7), pairs of 256 rows 15.1 (11.7).
+struct Choice {
+    int tile, split;
+    bool pair;
+};
+static Choice choose(int rows, int n, int d, int sms) {
+    const int64_t columns = (n + kBM - 1) / kBM, pair_columns = (n + 255) / 256;
     const int blocks = (d + kBK - 1) / kBK;
-    int split = 1;
-    while (split < kMaxSplit && tiles * split * 2 <= sms && blocks >= split * 4) split *= 2;
-    return split;
+    Choice best = {256, 1, false};
+    double least = 1e300;
+    auto offer = [&](int tile, int split, bool pair, double us) {
+        if (us < least) {
+            least = us;
+            best = {tile, split, pair};
+        }
+    };
+    for (int bn = 16; bn <= 256; bn *= 2) {
+        if (bn >= 32 && bn >= 2 * rows) break;   // (the tile before holds all rows)
+        const int64_t tiles = columns * ((rows + bn - 1) / bn);
+        const double block = 0.22 + 0.00065 * bn;
+        offer(bn, 1, false, 3.5 + 0.4 + 0.01 * bn + static_cast<double>((tiles + sms - 1) / sms) * blocks * block);
+        // a cluster's CTAs run at the same time, each on an SM of its own; clusters of eight do not fill all of a GPU's
+        for (int split = 2; split <= kMaxSplit && split * 2 <= blocks && tiles * split <= (split == 8 ? sms * 3 / 4 : sms); split *= 2)
+            offer(bn, split, false, 3.5 + (blocks + split - 1) / split * block + (0.3 + 0.029 * bn) * (split == 2 ? 0.7 : 1.0));
+    }
+    for (int tn = 64; tn <= 256; tn *= 2) {
+        const int64_t tiles = pair_columns * ((rows + tn - 1) / tn), pairs = sms / 2;
+        if (pairs)
+            offer(tn, 1, true, 4.7 + 0.4 + 0.01 * tn + static_cast<double>((tiles + pairs - 1) / pairs) * blocks * (0.175 + 0.0006 * tn));
+    }
+    return best;
 }
 
 }  // namespace head
@@ -886,23 +917,17 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
     g_test_withhold = -1;
 #endif
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const int64_t columns = (n + kBM - 1) / kBM;
+    const Choice c = choose(rows, n, d, sms);
     cudaError_t e;
-    if (rows <= 16) {
-        e = run<16>(P, split_of(columns, d, sms), sms, dev, stream);
-    } else if (rows <= 32) {
-        e = run<32>(P, split_of(columns, d, sms), sms, dev, stream);
-    } else if (rows <= 64) {
-        e = run<64>(P, split_of(columns, d, sms), sms, dev, stream);
-    } else if (columns * ((rows + 255) / 256) > sms / 2) {
-        e = run_pairs<256>(P, sms, dev, stream);   // (enough tiles of 256 columns by 256 rows for every pair of SMs, or nearly)
-    } else {
-        // tiles of 128 or of 256 rows: whichever keeps the SMs busy for less time (a block's time goes with the operands' rows)
-        const int64_t t128 = columns * ((rows + 127) / 128), t256 = columns * ((rows + 255) / 256);
-        const int s128 = split_of(t128, d, sms), s256 = split_of(t256, d, sms);
-        const double c128 = static_cast<double>((t128 * s128 + sms - 1) / sms) * (128 + 128) / s128;
-        const double c256 = static_cast<double>((t256 * s256 + sms - 1) / sms) * (256 + 128) / s256;
-        e = c128 < c256 ? run<128>(P, s128, sms, dev, stream) : run<256>(P, s256, sms, dev, stream);
-    }
+    if (c.pair)
+        e = c.tile == 64    ? run_pairs<64>(P, sms, dev, stream)
+            : c.tile == 128 ? run_pairs<128>(P, sms, dev, stream)
+                            : run_pairs<256>(P, sms, dev, stream);
+    else
+        e = c.tile == 16    ? run<16>(P, c.split, sms, dev, stream)
+            : c.tile == 32  ? run<32>(P, c.split, sms, dev, stream)
+            : c.tile == 64  ? run<64>(P, c.split, sms, dev, stream)
+            : c.tile == 128 ? run<128>(P, c.split, sms, dev, stream)
+                            : run<256>(P, c.split, sms, dev, stream);
     return e == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
 }
