@@ -30,7 +30,8 @@ constexpr int kBinsPerThread = kBins / kThreads;
 constexpr int kSampleBins = 2048;
 constexpr int kSampleBinsPerThread = kSampleBins / kThreads;
 constexpr int kSample = 8192;                        // entries a row's sample holds
-constexpr int kWarpList = 512;                       // candidates a warp can note down
+constexpr int kAll = 8192;                           // rows of so many entries are noted down whole
+constexpr int kWarpList = kAll / kWarps + 32;        // candidates a warp can note down (its share of such a row, and of the row's end)
 constexpr int kList = kWarps * kWarpList;
 constexpr uint32_t kStreamDraft = 2u;   // the draft draws' Philox stream
 
@@ -44,7 +45,7 @@ struct Params {
     int B, K, V;
     int vec_elems;              // entries of a row in whole 16-byte vectors
     double T, c;                // temperature and log2(e) / T
-    double one;                 // 2^F: the weight 1
+    double one, ones;           // 2^F, the weight 1, and F
     const float* uniforms;      // [B, K], or null: Philox
     uint64_t seed;
     uint32_t step;
@@ -58,26 +59,37 @@ struct Params {
     int32_t* status;
 };
 
+constexpr int kMaxChunks = 256;                      // stretches of a row whose kept weight is summed up for the draw
+constexpr int kValueBins = 3842;                     // of one sign: 30 binades of 128 bfloat16 numbers, what is below, what is above
+constexpr int kRowBins = 2 * kValueBins;
+constexpr int kRowBinsPerThread = 16;
+static_assert(kRowBinsPerThread * kThreads >= kRowBins, "every bin has a thread");
+
 struct Border {                      // an entry, and what stands before it
     unsigned long long place, above_mass;
     unsigned above_count;
 };
 
 struct Shared {
+    double table[256];               // 2^(i / 256)
     union {
-        struct {
+        struct {                     // a selection
             unsigned long long mass[kBins];
             unsigned count[kBins];
         };
         unsigned sample[kSampleBins];
     };
     uint32_t id[kList];              // candidates: warp w's at w * kWarpList
-    uint32_t key[kList];             // their logits' order
+    union {
+        uint32_t key[kList];         // their logits' order
+        unsigned bin[kRowBins];      // entries by value, until the candidates are noted down
+    };
     unsigned listed[kWarps];
+    unsigned long long chunk[kMaxChunks + 1];
     unsigned long long warp_mass[kWarps];
     unsigned warp_count[kWarps];
-    double red[kWarps];
     float red_f[kWarps][2];
+    double red[kWarps];
     unsigned long long few_place[32], few_weight[32];   // a bin with few entries
     unsigned few;
     unsigned long long lo, hi, above_mass;
@@ -85,7 +97,9 @@ struct Shared {
     Border border;
     float from;                      // candidates are the logits from here on
     int bad;
+    int first_rank, last_rank;
 };
+extern __shared__ __align__(16) unsigned char trunc_smem[];
 
 // Monotone map of a binary32 number that is no NaN to 32 bits, and back.
 __device__ __forceinline__ uint32_t order_of(float l) {
@@ -103,8 +117,22 @@ struct Row {
     int V, vec_elems;
     float top;            // largest logit
     double c, one;
+    double ones;          // F: the weight 1 is 2^F
+    // 2^((l - top) c) in units of 2^-F, rounded: 2^y = 2^(k / 256) 2^(f / 256) with k the nearest whole number to 256 y, the first
+    // factor from a table, the second as its Taylor series (|f| <= 1/2: the next term is below 2^-53)
     __device__ __forceinline__ unsigned long long weight(float l) const {
-        return __double2ull_rn(exp2((static_cast<double>(l) - static_cast<double>(top)) * c) * one);
+        const double y = fma(static_cast<double>(l) - static_cast<double>(top), c, ones);
+        if (!(y >= -1.0)) return 0ull;
+        constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: whole numbers stand in the low bits
+        constexpr double g = 0.6931471805599453094 / 256.0;
+        const double m = fma(y, 256.0, kRound);
+        const int k = __double2loint(m);
+        const double f = fma(y, 256.0, kRound - m);
+        double t = fma(f, g * g * g * g / 24.0, g * g * g / 6.0);
+        t = fma(f, t, g * g / 2.0);
+        t = fma(f, t, g);
+        t = fma(f, t, 1.0) * reinterpret_cast<const Shared*>(trunc_smem)->table[k & 255];
+        return __double2ull_rn(__hiloint2double(__double2hiint(t) + ((k >> 8) << 20), __double2loint(t)));
     }
 };
 
@@ -157,10 +185,10 @@ __device__ unsigned long long block_min(unsigned long long v, Shared& sh) {
 // those that each(f) hands to f(place, weight), all in [lo, hi], and all distinct.  `enough` is monotone; where it does not hold
 // for all of them together, the last place is returned.  Every level cuts the range into 1024 bins and goes on with the one
 // the border is in; one with at most 32 entries is settled by a warp.
+// above_count, above_mass: what stands before all of them.
 template <class Each, class Enough>
-__device__ Border select(Each each, Enough enough, unsigned long long lo, unsigned long long hi, Shared& sh) {
-    unsigned long long above_mass = 0;
-    unsigned above_count = 0;
+__device__ Border select(Each each, Enough enough, unsigned long long lo, unsigned long long hi, Shared& sh, unsigned above_count = 0,
+                         unsigned long long above_mass = 0) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     for (;;) {
         const int bits = 64 - __clzll(static_cast<long long>(hi - lo) | 1ll);
@@ -430,12 +458,12 @@ __device__ bool candidates_from(const Params& P, const Row& r, const Limits& lim
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     constexpr float lowest = lowest_logit<DT>();
     ref_logit = 0.f;
-    if (r.V <= kList) {   // room for all
+    if (r.V <= kAll) {   // room for all
         if (threadIdx.x == 0) sh.from = lowest;
         return true;
     }
     if (!lim.k_on && !lim.p_on && !lim.m_on) return false;
-    const int chunks = r.vec_elems / (32 * N);   // of 512 bytes; V > kList = kSample: there are as many as the sample takes
+    const int chunks = r.vec_elems / (32 * N);   // of 512 bytes; V > kAll = kSample: there are as many as the sample takes
     float x[kPerWarp * N], top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < kPerWarp; ++j) {
@@ -787,16 +815,654 @@ __device__ bool row_by_candidates(const Params& P, int64_t at, const Limits& lim
     return true;
 }
 
+// --------------------------------------------------------------------- values counted ----
+// Where candidates are too many, or the sample misled: one pass counts the row's entries by value, which places the border; a second
+// pass notes down the few entries near it and sums the weights before it, stretch by stretch for the draw.
+//   bfloat16: a bin is one number (30 binades of either sign), so all sums over the row follow from the counts, exactly, and the
+//   second pass looks for the entries equal to the border's number.
+//   binary32: bins are 1/96 of a power of two of the weight wide, masses are estimates, and the border is looked for among the bins
+//   within the estimates' error of it; the second pass sums exactly, over the whole row where top_p needs that.
+// A row of either kind that its bins do not hold (values out of their range that matter, borders in a bin of leftovers, more equal
+// entries than there is room for) takes the passes above.
+
+// Bins in the order of the entries ("ranks") and what stands in them.
+template <int DT>
+struct Bins {
+    static constexpr float kAbove = 16.f, kScale = 96.f;   // binary32: powers of two above the sampled largest, bins per power
+    float c, anchor;   // binary32: c and the sampled largest logit
+    uint32_t low;      // bfloat16: the magnitude (as bits) that bin 0 of a sign ends below
+
+    __device__ __forceinline__ int of(float l) const {   // (binary32)
+        return min(max(static_cast<int>(fmaf(anchor - l, c, kAbove) * kScale), 0), kRowBins - 1);
+    }
+    // bfloat16: table index of a rank and back to its number
+    __device__ static __forceinline__ int at(int rank) { return DT == FEF_F32 ? rank : rank < kValueBins ? kValueBins - 1 - rank : rank; }
+    __device__ __forceinline__ float value(int rank) const {
+        if constexpr (DT == FEF_F32) {
+            return anchor - ((static_cast<float>(rank) + 0.5f) / kScale - kAbove) / c;
+        } else {
+            const int m = rank < kValueBins ? kValueBins - 1 - rank : rank - kValueBins;   // magnitude
+            const uint32_t bits = m == 0 ? 0u : (low - 1u + static_cast<uint32_t>(m)) << 16;
+            return __uint_as_float(rank < kValueBins ? bits : bits | 0x80000000u);
+        }
+    }
+};
+
+// The first pass.  Returns the thread's largest logit (binary32), and sets bad where there is a NaN (or, bfloat16, anything a bin
+// of leftovers cannot tell from one).
+template <int DT>
+__device__ __forceinline__ float count_values(const Row& r, const Bins<DT>& bins, Shared& sh, bool& bad) {
+    constexpr int N = Elem<DT>::kPerVec;
+    constexpr int kBatch = 4;
+    const int vectors = r.vec_elems / N;
+    float top = -INFINITY;
+    uint32_t largest = 0;
+    char* table = reinterpret_cast<char*>(sh.bin);
+    const uint32_t low2 = (bins.low - 1u) * 0x10001u, high2 = (bins.low - 1u + kValueBins - 1) * 0x10001u;
+    auto count_bf16 = [&](uint32_t w, bool second) {   // a pair, as two indexes of four bytes each
+        const uint32_t a = w & 0x7FFF7FFFu;
+        largest = __vmaxu2(largest, a);
+        const uint32_t t = (__vminu2(__vmaxu2(a, low2), high2) - low2 + ((w >> 15) & 0x00010001u) * kValueBins) << 2;
+        atomicAdd(reinterpret_cast<unsigned*>(table + (t & 0xFFFFu)), 1u);
+        if (second) atomicAdd(reinterpret_cast<unsigned*>(table + (t >> 16)), 1u);
+    };
+    auto count_f32 = [&](float l) {
+        bad |= !(l < INFINITY);
+        top = fmaxf(top, l);
+        atomicAdd(&sh.bin[bins.of(l)], 1u);
+    };
+#pragma unroll 1
+    for (int v0 = threadIdx.x; v0 < vectors; v0 += kBatch * kThreads) {
+        uint4 w[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (v0 + j * kThreads < vectors) w[j] = ld_global_nc_v4(r.base + static_cast<int64_t>(v0 + j * kThreads) * 16);
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j)
+            if (v0 + j * kThreads < vectors) {
+                const uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    if constexpr (DT == FEF_BF16)
+                        count_bf16(v[q], true);
+                    else
+                        count_f32(__uint_as_float(v[q]));
+                }
+            }
+    }
+    for (int x = r.vec_elems + threadIdx.x; x < r.V; x += kThreads) {
+        const float l = load_logit<DT>(r.base, x);
+        if constexpr (DT == FEF_BF16)
+            count_bf16(__float_as_uint(l) >> 16, false);
+        else
+            count_f32(l);
+    }
+    if constexpr (DT == FEF_BF16) bad |= (largest & 0xFFFFu) > 0x7F80u || (largest >> 16) > 0x7F80u;
+    return top;
+}
+
+// The second pass.  kind(l): 0 before the border, 1 near it, 2 behind.  Ids of the entries near it go into the warps' lists; with ABOVE
+// the weights before it are summed into sh.chunk, with REST the thread's sum of those behind is returned.
+template <int DT, bool ABOVE, bool REST, class Kind>
+__device__ __forceinline__ unsigned long long gather_near(const Row& r, int pieces_per_chunk, Kind kind, Shared& sh) {
+    constexpr int N = Elem<DT>::kPerVec;
+    constexpr int kBatch = 4;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned lower = (1u << lane) - 1u;
+    const int pieces = r.vec_elems / (32 * N);
+    const int chunks = (pieces + pieces_per_chunk - 1) / pieces_per_chunk;
+    uint32_t* list = sh.id + warp * kWarpList;
+    unsigned listed = 0;
+    unsigned long long rest = 0;
+    auto note = [&](bool hit, int x) {
+        const unsigned hits = __ballot_sync(0xFFFFFFFFu, hit);
+        const unsigned at = listed + __popc(hits & lower);
+        if (hit && at < kWarpList) list[at] = static_cast<uint32_t>(x);
+        listed += __popc(hits);
+    };
+    // (chunk `chunks` is what is behind the last whole piece)
+    for (int c = warp; c <= chunks; c += kWarps) {
+        unsigned long long sum = 0;
+        if (c < chunks) {
+            const int end = min((c + 1) * pieces_per_chunk, pieces);
+#pragma unroll 1
+            for (int p = c * pieces_per_chunk; p < end; p += kBatch) {   // (pieces_per_chunk is a multiple of kBatch)
+                uint4 w[kBatch];
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+                    if (p + j < end) w[j] = ld_global_nc_v4(r.base + (static_cast<int64_t>(p + j) * 32 + lane) * 16);
+                uint32_t mask = 0;
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j)
+                    if (p + j < end) {
+                        float l[N];
+                        unpack<DT>(w[j], l);
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int k = kind(l[i]);
+                            mask |= k == 1 ? 1u << (j * N + i) : 0u;
+                            if (ABOVE && k == 0) sum += r.weight(l[i]);
+                            if (REST && k == 2) rest += r.weight(l[i]);
+                        }
+                    }
+                while (__any_sync(0xFFFFFFFFu, mask != 0u)) {
+                    const int bit = max(__ffs(mask) - 1, 0);
+                    note(mask != 0u, ((p + bit / N) * 32 + lane) * N + bit % N);
+                    mask &= mask - 1u;
+                }
+            }
+        } else {
+            for (int x0 = pieces * 32 * N; x0 < r.V; x0 += 32) {
+                const int x = x0 + lane;
+                const float l = x < r.V ? load_logit<DT>(r.base, x) : -INFINITY;
+                const int k = x < r.V ? kind(l) : 3;
+                note(k == 1, x);
+                if (ABOVE && k == 0) sum += r.weight(l);
+                if (REST && k == 2) rest += r.weight(l);
+            }
+        }
+        if (ABOVE) {
+            sum = warp_sum_u64(sum);
+            if (lane == 0) sh.chunk[c] = sum;
+        }
+    }
+    if (lane == 0) sh.listed[warp] = listed;
+    return rest;
+}
+
+// False: the row needs the passes (nothing has been written).
+template <int DT>
+__device__ bool row_by_values(const Params& P, int64_t at, const Limits& lim, Row& r, Shared& sh) {
+    constexpr int N = Elem<DT>::kPerVec;
+    constexpr int kPerThread = kRowBinsPerThread;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (r.V <= kAll) return false;
+    if (DT == FEF_F32 && lim.k_on && lim.p_on) return false;   // (two borders, one inside the other)
+    const float c = static_cast<float>(P.c);
+
+    // ---- where the bins lie, from a sample
+    Bins<DT> bins;
+    bins.c = c;
+    {
+        constexpr int kPerWarp = kSample / (kWarps * 32 * N);
+        const int pieces = r.vec_elems / (32 * N);
+        float x[kPerWarp * N], top = -INFINITY, size = 0.f;
+#pragma unroll
+        for (int j = 0; j < kPerWarp; ++j) {
+            const int s = warp * kPerWarp + j;
+            const int piece = static_cast<int>((static_cast<int64_t>(2 * s + 1) * pieces) / (2 * kPerWarp * kWarps));
+            unpack<DT>(ld_global_nc_v4(r.base + (static_cast<int64_t>(piece) * 32 + lane) * 16), *reinterpret_cast<float(*)[N]>(x + j * N));
+        }
+#pragma unroll
+        for (int j = 0; j < kPerWarp * N; ++j) top = fmaxf(top, x[j]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        __syncthreads();
+        if (lane == 0) sh.red_f[warp][0] = top;
+        __syncthreads();
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh.red_f[w][0]);
+        if (!(top > -INFINITY && top < INFINITY)) return false;
+        bins.anchor = top;
+        bins.low = 0;
+        if constexpr (DT == FEF_BF16) {
+            // the binades of what may weigh anything (64 powers of two below the largest sampled weight end it), and one more; with
+            // smaller logits about, the range reaches so far that what lies beyond it weighs nothing
+            const float end = top - 64.f / c;
+            int far = 0;
+#pragma unroll
+            for (int j = 0; j < kPerWarp * N; ++j) {
+                if (x[j] >= end)
+                    size = fmaxf(size, fabsf(x[j]));
+                else
+                    far = 1;
+            }
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) size = fmaxf(size, __shfl_xor_sync(0xFFFFFFFFu, size, o));
+            far = __any_sync(0xFFFFFFFFu, far);
+            __syncthreads();
+            if (lane == 0) {
+                sh.red_f[warp][0] = size;
+                sh.red_f[warp][1] = far ? 1.f : 0.f;
+            }
+            __syncthreads();
+            float any_far = 0.f;
+            for (int w = 0; w < kWarps; ++w) {
+                size = fmaxf(size, sh.red_f[w][0]);
+                any_far = fmaxf(any_far, sh.red_f[w][1]);
+            }
+            if (any_far > 0.f) size = fmaxf(size, 64.f / c);
+            // binades low .. low + 29, the last but one that of `size`
+            const int exponent = static_cast<int>(__float_as_uint(size) >> 23) + 1;
+            const int first = min(max(exponent - 29, 1), 254 - 29);
+            bins.low = static_cast<uint32_t>(first) << 7;
+        }
+    }
+    for (int b = threadIdx.x; b < kRowBins; b += kThreads) sh.bin[b] = 0;
+    if (threadIdx.x == 0) {
+        sh.bad = 0;
+        sh.first_rank = kRowBins;
+        sh.last_rank = -1;
+    }
+    __syncthreads();
+
+    // ---- first pass
+    bool bad = false;
+    float top = count_values<DT>(r, bins, sh, bad);
+    if (bad) sh.bad = 1;
+    __syncthreads();
+    unsigned n[kPerThread], ns = 0;
+    const int rank0 = threadIdx.x * kPerThread;
+#pragma unroll
+    for (int j = 0; j < kPerThread; ++j) {
+        const int rank = rank0 + j;
+        n[j] = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
+        ns += n[j];
+    }
+    // the largest logit
+    if constexpr (DT == FEF_F32) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        if (lane == 0) sh.red_f[warp][0] = top;
+    } else {
+        unsigned first = kRowBins;
+#pragma unroll
+        for (int j = kPerThread - 1; j >= 0; --j)
+            if (n[j]) first = rank0 + j;
+        first = __reduce_min_sync(0xFFFFFFFFu, first);
+        if (lane == 0) sh.warp_count[warp] = first;
+    }
+    __syncthreads();
+    if constexpr (DT == FEF_F32) {
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, sh.red_f[w][0]);
+    } else {
+        unsigned first = kRowBins;
+        for (int w = 0; w < kWarps; ++w) first = min(first, sh.warp_count[w]);
+        top = bins.value(static_cast<int>(first));
+    }
+    // Leftovers.  Above the range: the passes.  Behind it: nothing that weighs anything, or the passes.
+    const unsigned above_range = sh.bin[Bins<DT>::at(0)], behind = sh.bin[Bins<DT>::at(kRowBins - 1)];
+    __syncthreads();
+    if (sh.bad || above_range) return false;
+    r.top = top;
+    if (behind && r.weight(bins.value(kRowBins - 1))) return false;
+    constexpr int kLowFirst = kValueBins - 1;   // (bfloat16) the ranks of what is too small to tell apart: the zeros, or the passes
+    if constexpr (DT == FEF_BF16) {
+        if (sh.bin[Bins<DT>::at(kLowFirst)] + sh.bin[Bins<DT>::at(kLowFirst + 1)]) {
+            const float smallest = __uint_as_float(bins.low << 16);
+            bool other = false;
+            for_each<DT>(r, [&](float l, int) { other |= l != 0.f && fabsf(l) < smallest; });
+            if (__syncthreads_or(other)) return false;
+        }
+    }
+    auto leftover = [&](int rank) { return rank == kRowBins - 1 || (DT == FEF_BF16 && (rank == kLowFirst || rank == kLowFirst + 1)); };
+
+    // ---- counts and weights before each thread's bins
+    auto mass_of = [&](int rank, unsigned count) {
+        return count && rank != kRowBins - 1 ? r.weight(bins.value(rank)) * count : 0ull;
+    };
+    unsigned long long ms = 0;
+#pragma unroll 1
+    for (int j = 0; j < kPerThread; ++j) {
+        const int rank = rank0 + j;
+        if (rank < kRowBins) ms += mass_of(rank, sh.bin[Bins<DT>::at(rank)]);
+    }
+    unsigned pn = ns;
+    unsigned long long pm = ms;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const unsigned on = __shfl_up_sync(0xFFFFFFFFu, pn, o);
+        const unsigned long long om = __shfl_up_sync(0xFFFFFFFFu, pm, o);
+        if (lane >= o) {
+            pn += on;
+            pm += om;
+        }
+    }
+    if (lane == 31) {
+        sh.warp_count[warp] = pn;
+        sh.warp_mass[warp] = pm;
+    }
+    __syncthreads();
+    pn -= ns;
+    pm -= ms;
+    unsigned long long mass = 0;
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) {
+            pn += sh.warp_count[w];
+            pm += sh.warp_mass[w];
+        }
+        mass += sh.warp_mass[w];
+    }
+    const bool cut_on = lim.k_on || lim.p_on || lim.m_on;
+    const double least = lim.m_on ? lim.least(P) : 0.0;
+
+    // ---- the ranks the border is among
+    int rank_a, rank_b;          // first and last
+    unsigned before_n;           // entries before them,
+    unsigned long long before_m = 0;   // and (bfloat16) their weight
+    unsigned want = 0;           // (bfloat16) entries in the law
+    if (!cut_on) {
+        rank_a = kRowBins;
+        rank_b = kRowBins;
+        before_n = static_cast<unsigned>(r.V) - behind;
+        if (behind) {            // those of them that are not -inf belong to the law
+            unsigned finite = 0;
+            for_each<DT>(r, [&](float, int) { ++finite; });
+            before_n = static_cast<unsigned>(block_sum(finite, sh));
+        }
+        before_m = mass;
+    } else if constexpr (DT == FEF_BF16) {
+        // how many entries each rule keeps; the fewest are the law
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            sh.above_count = 0xFFFFFFFFu;   // entries in the law
+            sh.above_mass = mass;           // weight of what top_k leaves
+        }
+        __syncthreads();
+        if (lim.k_on) {
+            const unsigned k = static_cast<unsigned>(lim.k);
+            if (pn < k && pn + ns >= k) {   // one thread, or none
+                unsigned cn = pn;
+                unsigned long long cm = pm;
+                for (int j = 0; j < kPerThread; ++j) {
+                    const int rank = rank0 + j;
+                    const unsigned count = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
+                    if (cn + count >= k) {
+                        sh.above_mass = cm + mass_of(rank, k - cn);
+                        sh.above_count = k;
+                        break;
+                    }
+                    cn += count;
+                    cm += mass_of(rank, count);
+                }
+            }
+            __syncthreads();
+            if (sh.above_count == 0xFFFFFFFFu) return false;
+        }
+        if (lim.p_on) {
+            const double target = static_cast<double>(lim.p) * static_cast<double>(sh.above_mass);
+            __syncthreads();
+            if (ns && !(pn > 0 && static_cast<double>(pm) >= target) && static_cast<double>(pm + ms) >= target) {
+                unsigned cn = pn;
+                unsigned long long cm = pm;
+                for (int j = 0; j < kPerThread; ++j) {
+                    const int rank = rank0 + j;
+                    const unsigned count = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
+                    const unsigned long long w = mass_of(rank, 1), m = w * count;
+                    if (count && static_cast<double>(cm + m) >= target) {
+                        // the fewest of this number's entries that reach it (one at least)
+                        unsigned lo = 1, hi = count;
+                        while (lo < hi) {
+                            const unsigned mid = lo + (hi - lo) / 2;
+                            if (static_cast<double>(cm + w * mid) >= target)
+                                hi = mid;
+                            else
+                                lo = mid + 1;
+                        }
+                        atomicMin(&sh.above_count, cn + lo);
+                        break;
+                    }
+                    cn += count;
+                    cm += m;
+                }
+            }
+        }
+        if (lim.m_on) {
+            unsigned cn = pn;
+            int last = -1;
+            for (int j = 0; j < kPerThread; ++j) {
+                const int rank = rank0 + j;
+                const unsigned count = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
+                cn += count;
+                if (count && static_cast<double>(bins.value(rank)) - static_cast<double>(top) >= least) last = static_cast<int>(cn);
+            }
+            const unsigned kept = __reduce_max_sync(0xFFFFFFFFu, static_cast<unsigned>(max(last, 0)));
+            __syncthreads();
+            if (lane == 0) sh.warp_count[warp] = kept;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                unsigned all = 0;
+                for (int w = 0; w < kWarps; ++w) all = max(all, sh.warp_count[w]);
+                atomicMin(&sh.above_count, all);
+            }
+        }
+        __syncthreads();
+        want = sh.above_count;
+        __syncthreads();
+        if (want == 0xFFFFFFFFu || want == 0) return false;
+        if (pn < want && pn + ns >= want) {
+            unsigned cn = pn;
+            unsigned long long cm = pm;
+            for (int j = 0; j < kPerThread; ++j) {
+                const int rank = rank0 + j;
+                const unsigned count = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
+                if (cn + count >= want) {
+                    sh.first_rank = rank;
+                    sh.above_count = cn;
+                    sh.above_mass = cm;
+                    break;
+                }
+                cn += count;
+                cm += mass_of(rank, count);
+            }
+        }
+        __syncthreads();
+        rank_a = rank_b = sh.first_rank;
+        before_n = sh.above_count;
+        before_m = sh.above_mass;
+        if (rank_a >= kRowBins || leftover(rank_a)) return false;
+    } else {
+        // every rule gives a range of ranks; the border is not before the first range's first rank nor behind its last
+        const double k = lim.k_on ? static_cast<double>(lim.k) : 0.0;
+        const double p = lim.p, whole = static_cast<double>(mass);
+        // (a bin's weight is off by less than 0.4 % where it matters, on either side of the border)
+        const double error = 0.02 * fmax(p, 0.0) * (1.0 - fmax(p, 0.0)) * whole;
+        const int rank_m = lim.m_on ? bins.of(static_cast<float>(static_cast<double>(top) + least)) : 0;
+        unsigned cn = pn;
+        unsigned long long cm = pm;
+        int a = kRowBins, b = kRowBins;
+        for (int j = 0; j < kPerThread; ++j) {
+            const int rank = rank0 + j;
+            if (rank >= kRowBins) break;
+            const unsigned count = sh.bin[rank];
+            const unsigned long long m = mass_of(rank, count);
+            cn += count;
+            cm += m;
+            if (lim.k_on && static_cast<double>(cn) >= k) {
+                a = min(a, rank);
+                b = min(b, rank);
+            }
+            if (lim.p_on) {
+                if (cn && static_cast<double>(cm) >= p * whole - error) a = min(a, rank);
+                if (cn && static_cast<double>(cm) >= p * whole + error) b = min(b, rank);
+            }
+            if (lim.m_on) {
+                if (rank >= rank_m - 1) a = min(a, rank);
+                if (rank >= rank_m + 1) b = min(b, rank);
+            }
+        }
+        a = __reduce_min_sync(0xFFFFFFFFu, a);
+        b = __reduce_min_sync(0xFFFFFFFFu, b);
+        __syncthreads();
+        if (lane == 0) {
+            atomicMin(&sh.first_rank, a);
+            sh.warp_count[warp] = static_cast<unsigned>(b);
+        }
+        __syncthreads();
+        rank_a = sh.first_rank;
+        rank_b = kRowBins;
+        for (int w = 0; w < kWarps; ++w) rank_b = min(rank_b, static_cast<int>(sh.warp_count[w]));
+        __syncthreads();
+        if (rank_a > rank_b || rank_b >= kRowBins - 1) return false;
+        if (rank0 <= rank_a && rank_a < rank0 + kPerThread) {
+            unsigned count = pn;
+            for (int j = 0; rank0 + j < rank_a; ++j) count += sh.bin[rank0 + j];
+            sh.above_count = count;
+        }
+        __syncthreads();
+        before_n = sh.above_count;
+    }
+    __syncthreads();   // (the bins make room for the candidates)
+
+    // ---- second pass
+    const int pieces = r.vec_elems / (32 * N);
+    const int per_chunk = ((pieces + kMaxChunks - 1) / kMaxChunks + 3) / 4 * 4;
+    const int chunks = (pieces + per_chunk - 1) / per_chunk;
+    const float border = DT == FEF_BF16 && cut_on ? bins.value(rank_a) : -INFINITY;
+    auto kind = [&](float l) {
+        if constexpr (DT == FEF_BF16)
+            return l > border ? 0 : l == border && cut_on ? 1 : 2;
+        else {
+            if (l == -INFINITY) return 2;
+            const int rank = bins.of(l);
+            return rank < rank_a ? 0 : rank <= rank_b ? 1 : 2;
+        }
+    };
+    const bool need_rest = DT == FEF_F32 && lim.p_on;
+    unsigned long long rest = 0;
+    const bool need_above = DT == FEF_F32 || P.tokens != nullptr;
+    if (need_rest)
+        rest = gather_near<DT, true, true>(r, per_chunk, kind, sh);
+    else if (need_above)
+        gather_near<DT, true, false>(r, per_chunk, kind, sh);
+    else if (cut_on)
+        gather_near<DT, false, false>(r, per_chunk, kind, sh);
+    else if (lane == 0)
+        sh.listed[warp] = 0;
+    __syncthreads();
+    if (need_rest) rest = block_sum(rest, sh);
+    if (DT == FEF_F32) {
+        unsigned long long sum = 0;
+        for (int i = threadIdx.x; i <= chunks; i += kThreads) sum += sh.chunk[i];
+        before_m = block_sum(sum, sh);
+    }
+    const unsigned listed = sh.listed[warp];
+    unsigned most = 0;
+    for (int w = 0; w < kWarps; ++w) most = max(most, sh.listed[w]);
+    if (most > kWarpList) return false;
+    uint32_t* id = sh.id + warp * kWarpList;
+    uint32_t* key = sh.key + warp * kWarpList;
+    for (unsigned j = lane; j < listed; j += 32) key[j] = order_of(load_logit<DT>(r.base, id[j]));
+    __syncwarp();
+    auto each = [&](auto f) {
+        for (unsigned j = lane; j < listed; j += 32) {
+            const uint32_t k = key[j];
+            f(static_cast<unsigned long long>(k) << 32 | (0xFFFFFFFFu - id[j]), [&] { return r.weight(logit_of(k)); });
+        }
+    };
+
+    // ---- the border
+    const unsigned long long first = place_of(lowest_logit<DT>(), 0x7FFFFFFF), last = place_of(r.top, 0);
+    unsigned long long cut = 0;
+    if constexpr (DT == FEF_BF16) {
+        if (cut_on) cut = select(each, [=](unsigned n, unsigned long long) { return n >= want; }, first, last, sh, before_n, before_m).place;
+    } else if (cut_on) {
+        unsigned long long near_mine = 0;
+        unsigned near_n = 0;
+        each([&](unsigned long long, auto&& weight) {
+            near_mine += weight();
+            ++near_n;
+        });
+        const unsigned long long near = block_sum(near_mine, sh);
+        near_n = static_cast<unsigned>(block_sum(near_n, sh));
+        if (near_n == 0) return false;
+        if (lim.k_on && before_n + near_n >= static_cast<unsigned>(lim.k)) {
+            const unsigned k = static_cast<unsigned>(lim.k);
+            if (before_n >= k) return false;
+            cut = select(each, [=](unsigned n, unsigned long long) { return n >= k; }, first, last, sh, before_n, before_m).place;
+        }
+        if (lim.p_on) {
+            const double target = static_cast<double>(lim.p) * static_cast<double>(before_m + near + rest);
+            if (before_n && static_cast<double>(before_m) >= target) return false;
+            if (static_cast<double>(before_m + near) >= target)
+                cut = max(cut, select(each, [=](unsigned, unsigned long long s) { return static_cast<double>(s) >= target; }, first, last, sh,
+                                      before_n, before_m).place);
+        }
+        if (lim.m_on) {
+            unsigned long long lowest = ~0ull;
+            unsigned behind_it = 0;
+            each([&](unsigned long long place, auto&&) {
+                if (static_cast<double>(logit_of(static_cast<uint32_t>(place >> 32))) - static_cast<double>(r.top) >= least)
+                    lowest = min(lowest, place);
+                else
+                    behind_it = 1;
+            });
+            lowest = block_min(lowest, sh);
+            behind_it = static_cast<unsigned>(block_sum(behind_it, sh));
+            if (lowest == ~0ull) return false;          // it lies before the candidates
+            // the last candidate that belongs to the set is its last entry if a candidate that does not follows, or the candidates go
+            // further down than the limit
+            if (behind_it || rank_b >= bins.of(static_cast<float>(static_cast<double>(r.top) + least)) + 1) cut = max(cut, lowest);
+        }
+        if (!cut) return false;
+    }
+    unsigned long long sum = 0;
+    unsigned kept = 0;
+    const int entries_per_chunk = per_chunk * 32 * N;
+    each([&](unsigned long long place, auto&& weight) {
+        if (place >= cut) {
+            const unsigned long long w = weight();
+            sum += w;
+            ++kept;
+            const int x = static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(place));
+            if (P.tokens) atomicAdd(&sh.chunk[x < pieces * 32 * N ? x / entries_per_chunk : chunks], w);
+        }
+    });
+    const unsigned long long total = before_m + block_sum(sum, sh);
+    kept = before_n + static_cast<unsigned>(block_sum(kept, sh));
+    if (threadIdx.x == 0) write_law(P, at, r, cut, total, kept);
+    if (!P.tokens) return true;
+
+    // ---- the draw: the stretch that the number falls into, then the entry
+    const double target = lim.u * static_cast<double>(total);
+    if (threadIdx.x == 0) {
+        sh.in_bin = 0;
+        sh.above_mass = 0;
+    }
+    __syncthreads();
+    {
+        static_assert(kMaxChunks < kThreads, "a thread for each stretch");
+        const unsigned long long m = static_cast<int>(threadIdx.x) <= chunks ? sh.chunk[threadIdx.x] : 0ull;
+        unsigned long long upto = m;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned long long om = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            if (lane >= o) upto += om;
+        }
+        if (lane == 31) sh.warp_mass[warp] = upto;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) upto += sh.warp_mass[w];
+        if (m && static_cast<double>(upto) > target && !(static_cast<double>(upto - m) > target)) {   // one thread
+            sh.in_bin = threadIdx.x;
+            sh.above_mass = upto - m;
+        }
+    }
+    __syncthreads();
+    const int stretch = static_cast<int>(sh.in_bin);
+    const unsigned long long before_it = sh.above_mass;
+    const int x_begin = stretch * entries_per_chunk < pieces * 32 * N && stretch < chunks ? stretch * entries_per_chunk : pieces * 32 * N;
+    const int x_end = stretch < chunks ? min(x_begin + entries_per_chunk, pieces * 32 * N) : r.V;
+    auto by_id = [&](auto f) {
+        for (int x = x_begin + threadIdx.x; x < x_end; x += kThreads) {
+            const float l = load_logit<DT>(r.base, x);
+            if (l != -INFINITY && place_of(l, x) >= cut) f(place_of_id(x), [&] { return r.weight(l); });
+        }
+    };
+    const unsigned long long drawn = select(by_id, [=](unsigned, unsigned long long s) { return static_cast<double>(s) > target; },
+                                            place_of_id(x_end - 1), place_of_id(x_begin), sh, 1u, before_it).place;
+    if (threadIdx.x == 0) write_token<DT>(P, at, r, total, static_cast<int>(0xFFFFFFFFull - drawn));
+    return true;
+}
+
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 2) truncate_kernel(const __grid_constant__ Params P) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    Shared& sh = *reinterpret_cast<Shared*>(smem);
+    Shared& sh = *reinterpret_cast<Shared*>(trunc_smem);
     const int64_t at = blockIdx.x;
     const int b = static_cast<int>(at / P.K), i = static_cast<int>(at - static_cast<int64_t>(b) * P.K);
     if (P.row_len && i >= __ldg(P.row_len + b)) {
         if (threadIdx.x == 0) write_none(P, at, false);
         return;
     }
+    if (threadIdx.x < 256) sh.table[threadIdx.x] = exp2(static_cast<double>(threadIdx.x) / 256.0);
     const Limits lim = limits_of(P, at, b, i);
     Row r;
     r.base = P.logits + at * P.ld_bytes;
@@ -804,7 +1470,9 @@ __global__ void __launch_bounds__(kThreads, 2) truncate_kernel(const __grid_cons
     r.vec_elems = P.vec_elems;
     r.c = P.c;
     r.one = P.one;
-    if (!lim.bad && row_by_candidates<DT>(P, at, lim, r, sh)) return;
+    r.ones = P.ones;
+    __syncthreads();
+    if (!lim.bad && (row_by_candidates<DT>(P, at, lim, r, sh) || row_by_values<DT>(P, at, lim, r, sh))) return;
     row_by_passes<DT>(P, at, lim, r, sh);
 }
 
@@ -858,6 +1526,7 @@ static fef_status truncate(const void* logits, const int32_t* row_len, int B, in
     P.c = c;
     int bits = 0;   // the weights of V entries, each at most 2^F, sum to at most 2^62
     while ((1 << bits) < V) ++bits;
+    P.ones = 62 - bits;
     P.one = static_cast<double>(1ull << (62 - bits));
     P.uniforms = uniforms;
     P.seed = seed;
