@@ -22,15 +22,17 @@
 namespace fef {
 namespace trunc {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBins = 1024;                          // of a selection
-constexpr int kBinsLog2 = 10;
+constexpr int kCtasPerSm = 4;                        // rows at a time on an SM: one's selections hide behind the others' streams
+constexpr int kBins = 512;                           // of a selection
+constexpr int kBinsLog2 = 9;
 constexpr int kBinsPerThread = kBins / kThreads;
-constexpr int kSampleBins = 2048;
+constexpr int kSampleBins = 1024;
 constexpr int kSampleBinsPerThread = kSampleBins / kThreads;
-constexpr int kSample = 8192;                        // entries a row's sample holds
-constexpr int kAll = 8192;                           // rows of so many entries are noted down whole
+constexpr int kSampleOctaveLog2 = 7;                 // bins per octave of the distance below the sample's largest
+constexpr int kSample = 4096;                        // entries a row's sample holds
+constexpr int kAll = 4096;                           // rows of so many entries are noted down whole
 constexpr int kWarpList = kAll / kWarps + 32;        // candidates a warp can note down (its share of such a row, and of the row's end)
 constexpr int kList = kWarps * kWarpList;
 constexpr uint32_t kStreamDraft = 2u;   // the draft draws' Philox stream
@@ -59,11 +61,11 @@ struct Params {
     int32_t* status;
 };
 
-constexpr int kMaxChunks = 256;                      // stretches of a row whose kept weight is summed up for the draw
+constexpr int kMaxChunks = 252;                      // stretches of a row whose kept weight is summed up for the draw
 constexpr int kValueBins = 3842;                     // of one sign: 30 binades of 128 bfloat16 numbers, what is below, what is above
 constexpr int kRowBins = 2 * kValueBins;
-constexpr int kRowBinsPerThread = 16;
-static_assert(kRowBinsPerThread * kThreads >= kRowBins, "every bin has a thread");
+constexpr int kRowBinsPerThread = (kRowBins + kThreads - 1) / kThreads;
+static_assert(kRowBins * 4 <= kList * 8, "they fit where the candidates are later");
 
 struct Border {                      // an entry, and what stands before it
     unsigned long long place, above_mass;
@@ -79,9 +81,11 @@ struct Shared {
         };
         unsigned sample[kSampleBins];
     };
-    uint32_t id[kList];              // candidates: warp w's at w * kWarpList
     union {
-        uint32_t key[kList];         // their logits' order
+        struct {
+            uint32_t id[kList];      // candidates: warp w's at w * kWarpList
+            uint32_t key[kList];     // their logits' order
+        };
         unsigned bin[kRowBins];      // entries by value, until the candidates are noted down
     };
     unsigned listed[kWarps];
@@ -121,8 +125,7 @@ struct Row {
     // 2^((l - top) c) in units of 2^-F, rounded: 2^y = 2^(k / 256) 2^(f / 256) with k the nearest whole number to 256 y, the first
     // factor from a table, the second as its Taylor series (|f| <= 1/2: the next term is below 2^-53)
     __device__ __forceinline__ unsigned long long weight(float l) const {
-        const double y = fma(static_cast<double>(l) - static_cast<double>(top), c, ones);
-        if (!(y >= -1.0)) return 0ull;
+        const double y = fmax(fma(static_cast<double>(l) - static_cast<double>(top), c, ones), -3.0);   // (2^-1 and less is 0)
         constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: whole numbers stand in the low bits
         constexpr double g = 0.6931471805599453094 / 256.0;
         const double m = fma(y, 256.0, kRound);
@@ -183,7 +186,7 @@ __device__ unsigned long long block_min(unsigned long long v, Shared& sh) {
 
 // The first place, from the largest down, at which `enough(count, mass)` of the entries down to it holds; the places are
 // those that each(f) hands to f(place, weight), all in [lo, hi], and all distinct.  `enough` is monotone; where it does not hold
-// for all of them together, the last place is returned.  Every level cuts the range into 1024 bins and goes on with the one
+// for all of them together, the last place is returned.  Every level cuts the range into 512 bins and goes on with the one
 // the border is in; one with at most 32 entries is settled by a warp.
 // above_count, above_mass: what stands before all of them.
 template <class Each, class Enough>
@@ -488,14 +491,14 @@ __device__ bool candidates_from(const Params& P, const Row& r, const Limits& lim
     if (top == -INFINITY) return true;   // (nothing but masked entries seen: those that are left may be few)
     if (!(top < INFINITY)) return false;
     ref_logit = top;
-    // distance below the largest sampled logit, in powers of two of the weight; 256 bins per octave of (distance + 1)
+    // distance below the largest sampled logit, in powers of two of the weight; 128 bins per octave of (distance + 1)
     const float c = static_cast<float>(P.c);
 #pragma unroll
     for (int j = 0; j < kPerWarp * N; ++j)
         if (x[j] > -INFINITY)
-            atomicAdd(&sh.sample[min((__float_as_uint(fmaf(top - x[j], c, 1.f)) - 0x3F800000u) >> 15, kSampleBins - 1u)], 1u);
+            atomicAdd(&sh.sample[min((__float_as_uint(fmaf(top - x[j], c, 1.f)) - 0x3F800000u) >> (23 - kSampleOctaveLog2), kSampleBins - 1u)], 1u);
     __syncthreads();
-    auto edge = [](int b) { return __uint_as_float(0x3F800000u + (static_cast<unsigned>(b) << 15)) - 1.f; };
+    auto edge = [](int b) { return __uint_as_float(0x3F800000u + (static_cast<unsigned>(b) << (23 - kSampleOctaveLog2))) - 1.f; };
     unsigned n[kSampleBinsPerThread], cn = 0;
     float w[kSampleBinsPerThread], cw = 0.f;
     const int b0 = threadIdx.x * kSampleBinsPerThread;
@@ -600,6 +603,26 @@ __device__ __forceinline__ uint32_t at_least(uint32_t w, uint32_t from2) {
     return r;
 }
 
+__device__ __forceinline__ uint32_t max_nan_two(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+// Two binary32 numbers as one operand.
+__device__ __forceinline__ uint64_t two(float a, float b) { return static_cast<uint64_t>(__float_as_uint(b)) << 32 | __float_as_uint(a); }
+__device__ __forceinline__ float first_of(uint64_t x) { return __uint_as_float(static_cast<uint32_t>(x)); }
+__device__ __forceinline__ float second_of(uint64_t x) { return __uint_as_float(static_cast<uint32_t>(x >> 32)); }
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 // The pass: ids of the entries from `from` on into the warps' lists, and with SUM the others' sum of 2^(l c - ref).
 // NaN anywhere makes the sum NaN (without SUM it is looked for).  Returns the thread's sum.
 template <int DT, bool SUM>
@@ -610,7 +633,11 @@ __device__ float note_candidates(const Row& r, float from, float c, float ref, S
     const unsigned before = (1u << lane) - 1u;
     uint32_t* list = sh.id + warp * kWarpList;
     unsigned listed = 0;
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    uint64_t sum[2] = {0u, 0u};       // two binary32 sums each
+    uint32_t seen[2] = {0u, 0u};      // (bfloat16) the largest so far, NaN where there was one
+    bool nan = false;
+    const uint32_t from2 = __float_as_uint(from) | __float_as_uint(from) >> 16;
+    const uint64_t c2 = two(c, c), ref2 = two(-ref, -ref);
     const int chunks = r.vec_elems / (32 * N);
     constexpr uint32_t kMinusInf = DT == FEF_F32 ? 0xFF800000u : 0xFF80FF80u;
 
@@ -638,30 +665,30 @@ __device__ float note_candidates(const Row& r, float from, float c, float ref, S
         for (int j = 0; j < kBatch; ++j) {
             uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
             if constexpr (DT == FEF_BF16) {
-                const uint32_t from2 = __float_as_uint(from) | __float_as_uint(from) >> 16;
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const uint32_t hit = at_least(v[q], from2);
                     mask |= hit & (0x00010001u << (4 * j + q));
-                    if constexpr (SUM) v[q] = (v[q] & ~hit) | (0xFF80FF80u & hit);
-                    const float a = __uint_as_float(v[q] << 16), b = __uint_as_float(v[q] & 0xFFFF0000u);
                     if constexpr (SUM) {
-                        sum[(2 * q) & 3] += ex2_approx(fmaf(a, c, -ref));
-                        sum[(2 * q + 1) & 3] += ex2_approx(fmaf(b, c, -ref));
+                        v[q] = (v[q] & ~hit) | (0xFF80FF80u & hit);
+                        const uint64_t x = fma_two(static_cast<uint64_t>(v[q] & 0xFFFF0000u) << 32 | v[q] << 16, c2, ref2);
+                        sum[q & 1] = add_two(sum[q & 1], two(ex2_approx(first_of(x)), ex2_approx(second_of(x))));
                     } else {
-                        sum[0] += a != a || b != b ? 1.f : 0.f;
+                        seen[q & 1] = max_nan_two(seen[q & 1], v[q]);
                     }
                 }
             } else {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const float a = __uint_as_float(v[q]);
-                    const bool hit = a >= from;
-                    mask |= hit ? 1u << (4 * j + q) : 0u;
-                    if constexpr (SUM)
-                        sum[q] += ex2_approx(fmaf(hit ? -INFINITY : a, c, -ref));
-                    else
-                        sum[0] += a != a ? 1.f : 0.f;
+                for (int q = 0; q < 4; q += 2) {
+                    const float a = __uint_as_float(v[q]), b = __uint_as_float(v[q + 1]);
+                    const bool hit_a = a >= from, hit_b = b >= from;
+                    mask |= (hit_a ? 1u << (4 * j + q) : 0u) | (hit_b ? 2u << (4 * j + q) : 0u);
+                    if constexpr (SUM) {
+                        const uint64_t x = fma_two(two(hit_a ? -INFINITY : a, hit_b ? -INFINITY : b), c2, ref2);
+                        sum[q >> 1] = add_two(sum[q >> 1], two(ex2_approx(first_of(x)), ex2_approx(second_of(x))));
+                    } else {
+                        nan |= a != a || b != b;
+                    }
                 }
             }
         }
@@ -684,13 +711,17 @@ __device__ float note_candidates(const Row& r, float from, float c, float ref, S
         const bool hit = a >= from;
         note(hit, x);
         if constexpr (SUM)
-            sum[0] += ex2_approx(fmaf(hit ? -INFINITY : a, c, -ref));
+            sum[0] = add_two(sum[0], two(ex2_approx(fmaf(hit ? -INFINITY : a, c, -ref)), 0.f));
         else
-            sum[0] += a != a ? 1.f : 0.f;
+            nan |= a != a;
     }
     if (lane == 0) sh.listed[warp] = listed;
-    const float s = (sum[0] + sum[1]) + (sum[2] + sum[3]);
-    return SUM ? s : (s > 0.f ? __int_as_float(0x7FC00000) : 0.f);
+    if constexpr (SUM) return (first_of(sum[0]) + second_of(sum[0])) + (first_of(sum[1]) + second_of(sum[1]));
+    if constexpr (DT == FEF_BF16) {
+        const uint32_t all = max_nan_two(seen[0], seen[1]);
+        nan |= (all & 0x7FFFu) > 0x7F80u || (all >> 16 & 0x7FFFu) > 0x7F80u;
+    }
+    return nan ? __int_as_float(0x7FC00000) : 0.f;
 }
 
 // False: the row needs the other path (nothing has been written).
@@ -937,12 +968,22 @@ __device__ __forceinline__ unsigned long long gather_near(const Row& r, int piec
                     if (p + j < end) {
                         float l[N];
                         unpack<DT>(w[j], l);
+                        uint32_t before = 0, behind = 0;
 #pragma unroll
                         for (int i = 0; i < N; ++i) {
                             const int k = kind(l[i]);
                             mask |= k == 1 ? 1u << (j * N + i) : 0u;
-                            if (ABOVE && k == 0) sum += r.weight(l[i]);
-                            if (REST && k == 2) rest += r.weight(l[i]);
+                            if (ABOVE) before |= k == 0 ? 1u << i : 0u;
+                            if (REST) behind |= k == 2 ? 1u << i : 0u;
+                        }
+                        // (no branch per entry: the evaluations of a vector overlap)
+                        if (ABOVE && __any_sync(0xFFFFFFFFu, (before | behind) != 0u)) {
+#pragma unroll
+                            for (int i = 0; i < N; ++i) {
+                                const unsigned long long x = r.weight(l[i]);
+                                sum += before >> i & 1u ? x : 0ull;
+                                if (REST) rest += behind >> i & 1u ? x : 0ull;
+                            }
                         }
                     }
                 while (__any_sync(0xFFFFFFFFu, mask != 0u)) {
@@ -1050,13 +1091,14 @@ __device__ bool row_by_values(const Params& P, int64_t at, const Limits& lim, Ro
     float top = count_values<DT>(r, bins, sh, bad);
     if (bad) sh.bad = 1;
     __syncthreads();
-    unsigned n[kPerThread], ns = 0;
+    unsigned ns = 0;
+    int first_used = kRowBins;   // the thread's first rank with an entry
     const int rank0 = threadIdx.x * kPerThread;
-#pragma unroll
     for (int j = 0; j < kPerThread; ++j) {
         const int rank = rank0 + j;
-        n[j] = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
-        ns += n[j];
+        const unsigned n = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
+        if (n && !ns) first_used = rank;
+        ns += n;
     }
     // the largest logit
     if constexpr (DT == FEF_F32) {
@@ -1064,12 +1106,8 @@ __device__ bool row_by_values(const Params& P, int64_t at, const Limits& lim, Ro
         for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         if (lane == 0) sh.red_f[warp][0] = top;
     } else {
-        unsigned first = kRowBins;
-#pragma unroll
-        for (int j = kPerThread - 1; j >= 0; --j)
-            if (n[j]) first = rank0 + j;
-        first = __reduce_min_sync(0xFFFFFFFFu, first);
-        if (lane == 0) sh.warp_count[warp] = first;
+        const int first = __reduce_min_sync(0xFFFFFFFFu, first_used);
+        if (lane == 0) sh.warp_count[warp] = static_cast<unsigned>(first);
     }
     __syncthreads();
     if constexpr (DT == FEF_F32) {
@@ -1454,7 +1492,7 @@ __device__ bool row_by_values(const Params& P, int64_t at, const Limits& lim, Ro
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kThreads, 2) truncate_kernel(const __grid_constant__ Params P) {
+__global__ void __launch_bounds__(kThreads, kCtasPerSm) truncate_kernel(const __grid_constant__ Params P) {
     Shared& sh = *reinterpret_cast<Shared*>(trunc_smem);
     const int64_t at = blockIdx.x;
     const int b = static_cast<int>(at / P.K), i = static_cast<int>(at - static_cast<int64_t>(b) * P.K);
@@ -1462,7 +1500,8 @@ __global__ void __launch_bounds__(kThreads, 2) truncate_kernel(const __grid_cons
         if (threadIdx.x == 0) write_none(P, at, false);
         return;
     }
-    if (threadIdx.x < 256) sh.table[threadIdx.x] = exp2(static_cast<double>(threadIdx.x) / 256.0);
+    static_assert(kThreads == 256, "a thread for each entry of the table");
+    sh.table[threadIdx.x] = exp2(static_cast<double>(threadIdx.x) / 256.0);
     const Limits lim = limits_of(P, at, b, i);
     Row r;
     r.base = P.logits + at * P.ld_bytes;
