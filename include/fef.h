@@ -566,7 +566,8 @@ fef_status fef_logits_adjust(const void* logits, void* out, int B, int K, int V,
  *           1 or more turns it off
  *   min_p   keeps the entries with w_x >= min_p; 0 and less turn it off, more than 1 is 1
  * and the law keeps the shortest of these prefixes: pi(x) = w_x / (sum of the kept weights) there, 0 elsewhere.
- * Borders are decided on sums of weights in 64 bits, the same in every call and on every device.
+ * Borders and draws are decided on sums of weights in units of 2^-(62 - ceil(log2 V)) of the largest weight, 64-bit whole numbers: the
+ * same in every call and on every device.  (An entry of less than half a unit is never drawn.)
  *
  * A cut law is handed from call to call as three numbers per position, and used with the logits it belongs to:
  *   log2_norm   device out, [B, K] float64: log2 of the sum over the kept entries of 2^(l_x * log2(e) / T), as elsewhere

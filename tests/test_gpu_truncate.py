@@ -54,7 +54,9 @@ def _row(l, T, k, p, m, u):
     weights = np.zeros(V)
     weights[order[:n]] = w[:n]
     upto = np.cumsum(weights)
-    x = int(np.searchsorted(upto, min(max(u, 0.0), 1 - 2.0 ** -24) * upto[-1], side="right"))
+    unit = 2.0 ** -(62 - max(V - 1, 0).bit_length())   # the draw's unit: what rounds to none of it is never drawn, by u = 0 neither
+    drawn = np.cumsum(np.where(weights <= unit / 2, 0.0, weights))
+    x = int(np.searchsorted(drawn, min(max(u, 0.0), 1 - 2.0 ** -24) * drawn[-1], side="right"))
     cut = (l[order[n - 1]], order[n - 1]) if 0 < k < V or p < 1 or m > 0 else (-np.inf, -1)
     return x, weights[x] / upto[-1], l[order[0]] * (LOG2E / T) + math.log2(upto[-1]), *cut, n
 
@@ -245,6 +247,63 @@ def test_orders_of_the_vocabulary(fef, dtype):
                 x = x.sort(descending=place == "sorted").values
             for kind in ("k", "p", "kpm") if n != 40 else ("p", "m", "none"):
                 _check(fef, x.to(dtype).expand(4, 1, V).contiguous(), uniforms=u, **_rules(kind, 4))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_of_unusual_numbers(fef, dtype):
+    """Many zeros (of both signs), numbers too small to tell apart, small or shifted laws with masked entries, few different values,
+    steep laws: what the counting of values has to leave to another path, or to treat with care."""
+    V = 20000
+    g = torch.Generator(device="cuda").manual_seed(6)
+    normal = torch.randn(V, generator=g, device="cuda")
+    rnd = torch.rand(V, generator=g, device="cuda")
+    u = torch.tensor([[0.0], [0.3], [0.71], [0.9999999]], device="cuda")
+    low = torch.finfo(dtype).min
+    rows = {
+        "zeros": torch.where(rnd < 0.5, torch.zeros_like(normal), normal),
+        "signed zeros": torch.where(rnd < 0.3, -torch.zeros_like(normal), torch.where(rnd < 0.6, torch.zeros_like(normal), -normal.abs())),
+        "relu": normal.clamp(min=0) * 3,
+        "tiny": torch.where(rnd < 0.5, normal * 1e-12, normal),
+        "all tiny": normal * 1e-30,
+        "denormal": torch.where(rnd < 0.2, normal * 1e-39, normal),
+        "small and masked": torch.where(rnd < 0.6, torch.full_like(normal, -math.inf), normal * 0.02),
+        "small and lowest": torch.where(rnd < 0.6, torch.full_like(normal, low), normal * 0.02),
+        "shifted up": normal * 2 + 300,
+        "shifted down and masked": torch.where(rnd < 0.6, torch.full_like(normal, -math.inf), normal * 2 - 900),
+        "few values": (normal * 2).round(),
+        "two values": torch.where(rnd < 0.5, torch.zeros_like(normal) + 1, torch.zeros_like(normal) + 2),
+        "one far above": torch.where(rnd == rnd.max(), torch.full_like(normal, 80.0), normal * 2),
+        "far below": torch.where(rnd < 0.5, normal * 2 - 70, normal * 2),
+        "huge": normal * 1e30,
+        "ladder": -torch.arange(V, device="cuda") * 0.01,
+    }
+    for name, x in rows.items():
+        x = x.to(dtype).expand(4, 1, V).contiguous()
+        for kind in ("k", "p", "m", "kpm", "none", "edges"):
+            for T in ((1.0, 0.05) if kind in ("p", "none") else (1.0,)):
+                _check(fef, x, T, uniforms=u, **_rules(kind, 4))
+        # limits that reach far into the row
+        _check(fef, x, uniforms=u, top_k=_i32(9000, 15000, 19990, 6000))
+        _check(fef, x, uniforms=u, top_k=_i32(9000, 15000, 19990, 6000), top_p=_f32(0.99, 0.6, 0.9, 0.999), min_p=_f32(0, 1e-3, 1e-6, 0.2))
+        _check(fef, x, uniforms=u, min_p=_f32(1e-3, 1e-8, 1e-20, 1e-37))
+        _check(fef, x, uniforms=u, top_p=_f32(0.99, 0.9999, 0.999999, 0.3), min_p=_f32(1e-3, 1e-8, 1e-3, 1e-37))
+
+
+@pytest.mark.parametrize("rows", [2, 200, 400])    # (as many threads to a row as there are for it)
+def test_every_share_of_threads(fef, rows):
+    for V in (4097, 8193, 16385, 40961):
+        for dtype in (torch.float32, torch.bfloat16):
+            x, u = _logits(rows // 2, 2, V, dtype, V, std=1.5, boost=V % 3 == 0)
+            few = slice(0, 6)
+            for kind in ("p", "kp", "m", "none"):
+                rules = _rules(kind, rows // 2)
+                d = fef.fef_draft_sample_truncated(x, 1.0, uniforms=u, V=V, **rules)
+                sub = _check(fef, x[few].contiguous(), uniforms=u[few].contiguous(), V=V, **{n: t[few].contiguous() for n, t in rules.items()})
+                for a, b in zip((*d[:2], *d.law[:4]), (*sub[:2], *sub.law[:4])):
+                    if a.dtype == torch.int32 or a is d.law.cut_logit:
+                        assert torch.equal(a[few], b)
+                    else:
+                        assert ((a[few] - b).abs() <= 2 * NORM_TOL * (1 + b.abs())).all()
 
 
 def test_largest_vocabulary_and_temperatures(fef):
