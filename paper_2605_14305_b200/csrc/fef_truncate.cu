@@ -15,6 +15,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "fef.h"
 #include "fef_common.cuh"
 #include "fef_device_math.cuh"
@@ -64,10 +66,26 @@ __device__ __forceinline__ uint32_t order_of(float l) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
-// An entry's place in the order: the larger, the earlier.
-__device__ __forceinline__ unsigned long long place_of(float l, int x) {
-    return static_cast<unsigned long long>(order_of(l)) << 32 | (0xFFFFFFFFu - static_cast<uint32_t>(x));
+// An entry's place in the order: the larger, the earlier.  (bfloat16: the lower half of a logit's order says nothing.)
+constexpr int kIdBits = 20;
+constexpr uint32_t kIdMask = (1u << kIdBits) - 1u;
+static_assert(FEF_MAX_TRUNCATE_V <= 1 << kIdBits, "ids fit");
+template <int DT>
+__device__ __forceinline__ unsigned long long place_of_order(uint32_t k, uint32_t x) {
+    return static_cast<unsigned long long>(DT == FEF_F32 ? k : k >> 16) << kIdBits | (kIdMask - x);
 }
+template <int DT>
+__device__ __forceinline__ unsigned long long place_of(float l, int x) {
+    return place_of_order<DT>(order_of(l), static_cast<uint32_t>(x));
+}
+template <int DT>
+__device__ __forceinline__ float logit_at(unsigned long long place) {
+    const uint32_t k = static_cast<uint32_t>(place >> kIdBits);
+    return logit_of(DT == FEF_F32 ? k : k & 0x8000u ? k << 16 : k << 16 | 0xFFFFu);
+}
+__device__ __forceinline__ int id_at(unsigned long long place) { return static_cast<int>(kIdMask - (static_cast<uint32_t>(place) & kIdMask)); }
+// Ids as places: the lowest comes first.
+__device__ __forceinline__ unsigned long long place_of_id(int x) { return kIdMask - static_cast<unsigned>(x); }
 
 struct Row {
     const char* base;
@@ -76,9 +94,9 @@ struct Row {
     double c, one;
     double ones;          // F: the weight 1 is 2^F
     // 2^((l - top) c) in units of 2^-F, as the product of two numbers: 2^y = 2^(k / 256) 2^(f / 256) with k the nearest whole number
-    // to 256 y, the first factor from a table, the second as its Taylor series (|f| <= 1/2: the next term is below 2^-53).
+    // to 256 y, the first factor from a table, the second as its Taylor series (|f| <= 1/2: the next term is below 2^-53).  For y > -900.
     __device__ __forceinline__ void factors(float l, double& a, double& b) const {
-        const double y = fmax(fma(static_cast<double>(l) - static_cast<double>(top), c, ones), -900.0);   // (nothing, in these units)
+        const double y = fma(static_cast<double>(l) - static_cast<double>(top), c, ones);
         constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: whole numbers stand in the low bits
         constexpr double g = 0.6931471805599453094 / 256.0;
         const double m = fma(y, 256.0, kRound);
@@ -95,7 +113,7 @@ struct Row {
     __device__ __forceinline__ unsigned long long weight(float l) const {
         double a, b;
         factors(l, a, b);
-        return __double2ull_rn(a * b);
+        return (static_cast<double>(l) - static_cast<double>(top)) * c >= -1.0 - ones ? __double2ull_rn(a * b) : 0ull;
     }
 };
 
@@ -212,11 +230,12 @@ __device__ __forceinline__ void write_none(const Params& P, int64_t at, bool err
 }
 
 // The law is known: its smallest place (0: nothing is cut), its weight and its entries.
+template <int DT>
 __device__ __forceinline__ void write_law(const Params& P, int64_t at, const Row& r, unsigned long long cut,
                                           unsigned long long total, unsigned kept) {
     P.log2_norm[at] = static_cast<double>(r.top) * P.c + log2(static_cast<double>(total) / P.one);
-    P.cut_logit[at] = cut ? logit_of(static_cast<uint32_t>(cut >> 32)) : -INFINITY;
-    P.cut_id[at] = cut ? static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(cut)) : -1;
+    P.cut_logit[at] = cut ? logit_at<DT>(cut) : -INFINITY;
+    P.cut_id[at] = cut ? id_at(cut) : -1;
     if (P.kept) P.kept[at] = static_cast<int>(kept);
 }
 
@@ -227,9 +246,6 @@ __device__ __forceinline__ void write_token(const Params& P, int64_t at, const R
         P.conf[at] = static_cast<float>(exp2((static_cast<double>(load_logit<DT>(r.base, x)) - static_cast<double>(r.top)) * P.c) *
                                         (P.one / static_cast<double>(total)));
 }
-
-// Ids as places: the lowest comes first.
-__device__ __forceinline__ unsigned long long place_of_id(int x) { return 0xFFFFFFFFull - static_cast<unsigned>(x); }
 
 // One row by a CTA of kThreads threads.
 template <int kThreads>
@@ -278,7 +294,9 @@ struct Rows {
         Border border;
         float from;                      // candidates are the logits from here on
         int bad;
-        int first_rank, last_rank;
+        int loc_rank;                    // a border among the bins: its bin, what stands before it
+        unsigned loc_n;
+        unsigned long long loc_m;
     };
 
     // f(logit, id) for every entry of the row but -inf.
@@ -466,9 +484,9 @@ struct Rows {
         r.top = top;
 
         auto places = [&](auto f) {
-            for_each<DT>(r, [&](float l, int x) { f(place_of(l, x), [&] { return r.weight(l); }); });
+            for_each<DT>(r, [&](float l, int x) { f(place_of<DT>(l, x), [&] { return r.weight(l); }); });
         };
-        const unsigned long long first = place_of(-3.402823466e38f, 0x7FFFFFFF), last = place_of(top, 0);
+        const unsigned long long first = place_of<DT>(lowest_logit<DT>(), P.V - 1), last = place_of<DT>(top, 0);
         unsigned long long cut = 0;   // the smallest place in the law; 0: all of them
         if (lim.k_on) {
             const unsigned most = static_cast<unsigned>(lim.k);
@@ -476,7 +494,7 @@ struct Rows {
         }
         if (lim.p_on) {
             unsigned long long sum = 0;
-            for_each<DT>(r, [&](float l, int x) { sum += place_of(l, x) >= cut ? r.weight(l) : 0ull; });
+            for_each<DT>(r, [&](float l, int x) { sum += place_of<DT>(l, x) >= cut ? r.weight(l) : 0ull; });
             const double target = static_cast<double>(lim.p) * static_cast<double>(block_sum(sum, sh));
             cut = max(cut, select(places, [=](unsigned, unsigned long long s) { return static_cast<double>(s) >= target; }, first, last,
                                   sh).place);
@@ -485,31 +503,31 @@ struct Rows {
             const double least = lim.least(P);
             unsigned long long lowest = ~0ull;
             for_each<DT>(r, [&](float l, int x) {
-                if (static_cast<double>(l) - static_cast<double>(top) >= least) lowest = min(lowest, place_of(l, x));
+                if (static_cast<double>(l) - static_cast<double>(top) >= least) lowest = min(lowest, place_of<DT>(l, x));
             });
             cut = max(cut, block_min(lowest, sh));
         }
         unsigned long long sum = 0;
         unsigned n = 0;
         for_each<DT>(r, [&](float l, int x) {
-            if (place_of(l, x) >= cut) {
+            if (place_of<DT>(l, x) >= cut) {
                 sum += r.weight(l);
                 ++n;
             }
         });
         const unsigned long long total = block_sum(sum, sh);
         const unsigned kept = static_cast<unsigned>(block_sum(n, sh));
-        if (threadIdx.x == 0) write_law(P, at, r, cut, total, kept);
+        if (threadIdx.x == 0) write_law<DT>(P, at, r, cut, total, kept);
         if (!P.tokens) return;
         const double target = lim.u * static_cast<double>(total);
         auto by_id = [&](auto f) {
             for_each<DT>(r, [&](float l, int x) {
-                if (place_of(l, x) >= cut) f(place_of_id(x), [&] { return r.weight(l); });
+                if (place_of<DT>(l, x) >= cut) f(place_of_id(x), [&] { return r.weight(l); });
             });
         };
         const unsigned long long drawn = select(by_id, [=](unsigned, unsigned long long s) { return static_cast<double>(s) > target; },
                                                 place_of_id(P.V - 1), place_of_id(0), sh).place;
-        if (threadIdx.x == 0) write_token<DT>(P, at, r, total, static_cast<int>(0xFFFFFFFFull - drawn));
+        if (threadIdx.x == 0) write_token<DT>(P, at, r, total, id_at(drawn));
     }
 
     // ---------------------------------------------------------------------- candidates ----
@@ -805,10 +823,10 @@ struct Rows {
         auto each = [&](auto f) {
             for (unsigned j = lane; j < listed; j += 32) {
                 const uint32_t k = key[j];
-                f(static_cast<unsigned long long>(k) << 32 | (0xFFFFFFFFu - id[j]), [&] { return r.weight(logit_of(k)); });
+                f(place_of_order<DT>(k, id[j]), [&] { return r.weight(logit_of(k)); });
             }
         };
-        const unsigned long long first = place_of(from, 0x7FFFFFFF), last = place_of(r.top, 0);
+        const unsigned long long first = place_of<DT>(from, P.V - 1), last = place_of<DT>(r.top, 0);
         const bool everything = from == lowest_logit<DT>();
         // in units of the weights; the terms' relative error: their argument (its rounding and c's, 2^-24 of at most 40; smaller
         // terms are below 2^-40), the exponential's 2^-22, and as many additions as a thread makes in a row
@@ -835,7 +853,7 @@ struct Rows {
                 }
                 const double target = p * (listed_sum + rest);
                 const Border b = select(each, [=](unsigned, unsigned long long s) { return static_cast<double>(s) >= target; }, first, last, sh);
-                const double with_it = static_cast<double>(b.above_mass + r.weight(logit_of(static_cast<uint32_t>(b.place >> 32))));
+                const double with_it = static_cast<double>(b.above_mass + r.weight(logit_at<DT>(b.place)));
                 const bool sure = with_it >= (rest > 0.0 ? most_of_it : target) && (b.above_count == 0 || static_cast<double>(b.above_mass) < least);
                 if (sure || rest == 0.0 || slack == 0.0) {
                     if (!(with_it >= target)) return false;
@@ -853,7 +871,7 @@ struct Rows {
             const double least = lim.least(P);
             unsigned long long lowest = ~0ull;
             each([&](unsigned long long place, auto&&) {
-                if (static_cast<double>(logit_of(static_cast<uint32_t>(place >> 32))) - static_cast<double>(r.top) >= least)
+                if (static_cast<double>(logit_at<DT>(place)) - static_cast<double>(r.top) >= least)
                     lowest = min(lowest, place);
             });
             lowest = block_min(lowest, sh);
@@ -871,17 +889,17 @@ struct Rows {
         });
         const unsigned long long total = block_sum(sum, sh);
         const unsigned kept = static_cast<unsigned>(block_sum(n, sh));
-        if (threadIdx.x == 0) write_law(P, at, r, cut, total, kept);
+        if (threadIdx.x == 0) write_law<DT>(P, at, r, cut, total, kept);
         if (!P.tokens) return true;
         const double target = lim.u * static_cast<double>(total);
         auto by_id = [&](auto f) {
             each([&](unsigned long long place, auto&& weight) {
-                if (place >= cut) f(place & 0xFFFFFFFFull, weight);
+                if (place >= cut) f(place & kIdMask, weight);
             });
         };
         const unsigned long long drawn = select(by_id, [=](unsigned, unsigned long long s) { return static_cast<double>(s) > target; },
                                                 place_of_id(P.V - 1), place_of_id(0), sh).place;
-        if (threadIdx.x == 0) write_token<DT>(P, at, r, total, static_cast<int>(0xFFFFFFFFull - drawn));
+        if (threadIdx.x == 0) write_token<DT>(P, at, r, total, id_at(drawn));
         return true;
     }
 
@@ -1095,11 +1113,7 @@ struct Rows {
             }
         }
         for (int b = threadIdx.x; b < kRowBins; b += kThreads) sh.bin[b] = 0;
-        if (threadIdx.x == 0) {
-            sh.bad = 0;
-            sh.first_rank = kRowBins;
-            sh.last_rank = -1;
-        }
+        if (threadIdx.x == 0) sh.bad = 0;
         __syncthreads();
 
         // ---- first pass
@@ -1150,22 +1164,31 @@ struct Rows {
         }
         auto leftover = [&](int rank) { return rank == kRowBins - 1 || (DT == FEF_BF16 && (rank == kLowFirst || rank == kLowFirst + 1)); };
 
-        // ---- counts and weights before each thread's bins
-        auto mass_of = [&](int rank, unsigned count) {
-            return count && rank != kRowBins - 1 ? r.weight(bins.value(rank)) * count : 0ull;
+        // ---- counts and weights before each thread's bins (binary32: weights are estimates, of a bin's middle)
+        auto count_at = [&](int rank) { return rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u; };
+        using Mass = typename std::conditional<DT == FEF_BF16, unsigned long long, double>::type;
+        auto bits_of = [](Mass m) {
+            if constexpr (DT == FEF_BF16) return m;
+            else return static_cast<unsigned long long>(__double_as_longlong(m));
         };
-        unsigned long long ms = 0;
-    #pragma unroll 1
-        for (int j = 0; j < kPerThread; ++j) {
-            const int rank = rank0 + j;
-            if (rank < kRowBins) ms += mass_of(rank, sh.bin[Bins<DT>::at(rank)]);
-        }
+        auto mass_of = [](unsigned long long b) {
+            if constexpr (DT == FEF_BF16) return b;
+            else return __longlong_as_double(static_cast<long long>(b));
+        };
+        auto weight_at = [&](int rank) -> Mass {
+            if (rank >= kRowBins - 1) return 0;
+            if constexpr (DT == FEF_BF16) return r.weight(bins.value(rank));
+            else return static_cast<double>(ex2_approx(Bins<DT>::kAbove - (static_cast<float>(rank) + 0.5f) / Bins<DT>::kScale));
+        };
+        Mass ms = 0;
+    #pragma unroll 4
+        for (int j = 0; j < kPerThread; ++j) ms += weight_at(rank0 + j) * count_at(rank0 + j);
         unsigned pn = ns;
-        unsigned long long pm = ms;
+        Mass pm = ms;
     #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const unsigned on = __shfl_up_sync(0xFFFFFFFFu, pn, o);
-            const unsigned long long om = __shfl_up_sync(0xFFFFFFFFu, pm, o);
+            const Mass om = __shfl_up_sync(0xFFFFFFFFu, pm, o);
             if (lane >= o) {
                 pn += on;
                 pm += om;
@@ -1173,187 +1196,142 @@ struct Rows {
         }
         if (lane == 31) {
             sh.warp_count[warp] = pn;
-            sh.warp_mass[warp] = pm;
+            sh.warp_mass[warp] = bits_of(pm);
         }
         __syncthreads();
         pn -= ns;
         pm -= ms;
-        unsigned long long mass = 0;
+        Mass mass = 0;
         for (int w = 0; w < kWarps; ++w) {
             if (w < warp) {
                 pn += sh.warp_count[w];
-                pm += sh.warp_mass[w];
+                pm += mass_of(sh.warp_mass[w]);
             }
-            mass += sh.warp_mass[w];
+            mass += mass_of(sh.warp_mass[w]);
         }
+        // The first bin, from the largest down, with which `enough` holds: sh.loc_rank, and what stands before it (false: there is none).
+        // The thread it belongs to is found first, then a warp looks at that thread's bins.
+        auto locate = [&](auto enough) {
+            __syncthreads();
+            if (threadIdx.x == 0) sh.loc_rank = -1;
+            __syncthreads();
+            if (ns && !(pn > 0 && enough(pn, pm)) && enough(pn + ns, pm + ms)) {
+                sh.loc_rank = rank0;
+                sh.loc_n = pn;
+                sh.loc_m = bits_of(pm);
+            }
+            __syncthreads();
+            if (sh.loc_rank < 0) return false;
+            if (warp == 0) {
+                static_assert(kPerThread <= 32, "a lane for each of a thread's bins");
+                const int rank = sh.loc_rank + lane;
+                const unsigned n = lane < kPerThread ? count_at(rank) : 0u;
+                const Mass m = n ? weight_at(rank) * n : 0;
+                unsigned un = n;
+                Mass um = m;
+    #pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const unsigned on = __shfl_up_sync(0xFFFFFFFFu, un, o);
+                    const Mass om = __shfl_up_sync(0xFFFFFFFFu, um, o);
+                    if (lane >= o) {
+                        un += on;
+                        um += om;
+                    }
+                }
+                un += sh.loc_n;
+                um += mass_of(sh.loc_m);
+                const unsigned there = __ballot_sync(0xFFFFFFFFu, n && enough(un, um));
+                if (lane == __ffs(there) - 1) {
+                    sh.loc_rank = rank;
+                    sh.loc_n = un - n;
+                    sh.loc_m = bits_of(um - m);
+                }
+            }
+            __syncthreads();
+            return true;
+        };
         const bool cut_on = lim.k_on || lim.p_on || lim.m_on;
         const double least = lim.m_on ? lim.least(P) : 0.0;
 
         // ---- the ranks the border is among
-        int rank_a, rank_b;          // first and last
-        unsigned before_n;           // entries before them,
-        unsigned long long before_m = 0;   // and (bfloat16) their weight
-        unsigned want = 0;           // (bfloat16) entries in the law
+        int rank_a = kRowBins, rank_b = kRowBins;   // first and last
+        unsigned before_n;                          // entries before them,
+        unsigned long long before_m = 0;            // and (bfloat16) their weight
+        unsigned want = 0xFFFFFFFFu;                // (bfloat16) entries in the law
         if (!cut_on) {
-            rank_a = kRowBins;
-            rank_b = kRowBins;
             before_n = static_cast<unsigned>(r.V) - behind;
-            if (behind) {            // those of them that are not -inf belong to the law
+            if (behind) {   // those of them that are not -inf belong to the law
                 unsigned finite = 0;
                 for_each<DT>(r, [&](float, int) { ++finite; });
                 before_n = static_cast<unsigned>(block_sum(finite, sh));
             }
-            before_m = mass;
+            if constexpr (DT == FEF_BF16) before_m = mass;
         } else if constexpr (DT == FEF_BF16) {
             // how many entries each rule keeps; the fewest are the law
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                sh.above_count = 0xFFFFFFFFu;   // entries in the law
-                sh.above_mass = mass;           // weight of what top_k leaves
-            }
-            __syncthreads();
+            unsigned long long of_first = mass;   // weight of what top_k leaves
             if (lim.k_on) {
-                const unsigned k = static_cast<unsigned>(lim.k);
-                if (pn < k && pn + ns >= k) {   // one thread, or none
-                    unsigned cn = pn;
-                    unsigned long long cm = pm;
-                    for (int j = 0; j < kPerThread; ++j) {
-                        const int rank = rank0 + j;
-                        const unsigned count = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
-                        if (cn + count >= k) {
-                            sh.above_mass = cm + mass_of(rank, k - cn);
-                            sh.above_count = k;
-                            break;
-                        }
-                        cn += count;
-                        cm += mass_of(rank, count);
-                    }
-                }
-                __syncthreads();
-                if (sh.above_count == 0xFFFFFFFFu) return false;
+                want = static_cast<unsigned>(lim.k);
+                if (!locate([=](unsigned n, unsigned long long) { return n >= want; })) return false;
+                of_first = sh.loc_m + weight_at(sh.loc_rank) * (want - sh.loc_n);
             }
             if (lim.p_on) {
-                const double target = static_cast<double>(lim.p) * static_cast<double>(sh.above_mass);
-                __syncthreads();
-                if (ns && !(pn > 0 && static_cast<double>(pm) >= target) && static_cast<double>(pm + ms) >= target) {
-                    unsigned cn = pn;
-                    unsigned long long cm = pm;
-                    for (int j = 0; j < kPerThread; ++j) {
-                        const int rank = rank0 + j;
-                        const unsigned count = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
-                        const unsigned long long w = mass_of(rank, 1), m = w * count;
-                        if (count && static_cast<double>(cm + m) >= target) {
-                            // the fewest of this number's entries that reach it (one at least)
-                            unsigned lo = 1, hi = count;
-                            while (lo < hi) {
-                                const unsigned mid = lo + (hi - lo) / 2;
-                                if (static_cast<double>(cm + w * mid) >= target)
-                                    hi = mid;
-                                else
-                                    lo = mid + 1;
-                            }
-                            atomicMin(&sh.above_count, cn + lo);
-                            break;
-                        }
-                        cn += count;
-                        cm += m;
-                    }
+                const double target = static_cast<double>(lim.p) * static_cast<double>(of_first);
+                if (!locate([=](unsigned, unsigned long long m) { return static_cast<double>(m) >= target; })) return false;
+                // the fewest of the number's entries that reach it (one at least)
+                const unsigned long long w = weight_at(sh.loc_rank), m = sh.loc_m;
+                unsigned few = 1, many = count_at(sh.loc_rank);
+                while (few < many) {
+                    const unsigned mid = few + (many - few) / 2;
+                    if (static_cast<double>(m + w * mid) >= target)
+                        many = mid;
+                    else
+                        few = mid + 1;
                 }
+                want = min(want, sh.loc_n + few);
             }
             if (lim.m_on) {
-                unsigned cn = pn;
-                int last = -1;
+                unsigned upto = 0, n = pn;   // entries down to the thread's last bin that belongs to the set
                 for (int j = 0; j < kPerThread; ++j) {
-                    const int rank = rank0 + j;
-                    const unsigned count = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
-                    cn += count;
-                    if (count && static_cast<double>(bins.value(rank)) - static_cast<double>(top) >= least) last = static_cast<int>(cn);
+                    const unsigned count = count_at(rank0 + j);
+                    n += count;
+                    if (count && static_cast<double>(bins.value(rank0 + j)) - static_cast<double>(top) >= least) upto = n;
                 }
-                const unsigned kept = __reduce_max_sync(0xFFFFFFFFu, static_cast<unsigned>(max(last, 0)));
-                __syncthreads();
-                if (lane == 0) sh.warp_count[warp] = kept;
-                __syncthreads();
-                if (threadIdx.x == 0) {
-                    unsigned all = 0;
-                    for (int w = 0; w < kWarps; ++w) all = max(all, sh.warp_count[w]);
-                    atomicMin(&sh.above_count, all);
-                }
+                want = min(want, 0xFFFFFFFFu - static_cast<unsigned>(block_min(0xFFFFFFFFu - upto, sh)));
             }
-            __syncthreads();
-            want = sh.above_count;
-            __syncthreads();
-            if (want == 0xFFFFFFFFu || want == 0) return false;
-            if (pn < want && pn + ns >= want) {
-                unsigned cn = pn;
-                unsigned long long cm = pm;
-                for (int j = 0; j < kPerThread; ++j) {
-                    const int rank = rank0 + j;
-                    const unsigned count = rank < kRowBins ? sh.bin[Bins<DT>::at(rank)] : 0u;
-                    if (cn + count >= want) {
-                        sh.first_rank = rank;
-                        sh.above_count = cn;
-                        sh.above_mass = cm;
-                        break;
-                    }
-                    cn += count;
-                    cm += mass_of(rank, count);
-                }
-            }
-            __syncthreads();
-            rank_a = rank_b = sh.first_rank;
-            before_n = sh.above_count;
-            before_m = sh.above_mass;
-            if (rank_a >= kRowBins || leftover(rank_a)) return false;
+            if (want == 0 || !locate([=](unsigned n, unsigned long long) { return n >= want; })) return false;
+            rank_a = rank_b = sh.loc_rank;
+            before_n = sh.loc_n;
+            before_m = sh.loc_m;
+            if (leftover(rank_a)) return false;
         } else {
             // every rule gives a range of ranks; the border is not before the first range's first rank nor behind its last
-            const double k = lim.k_on ? static_cast<double>(lim.k) : 0.0;
-            const double p = lim.p, whole = static_cast<double>(mass);
-            // (a bin's weight is off by less than 0.4 % where it matters, on either side of the border)
-            const double error = 0.02 * fmax(p, 0.0) * (1.0 - fmax(p, 0.0)) * whole;
-            const int rank_m = lim.m_on ? bins.of(static_cast<float>(static_cast<double>(top) + least)) : 0;
-            unsigned cn = pn;
-            unsigned long long cm = pm;
-            int a = kRowBins, b = kRowBins;
-            for (int j = 0; j < kPerThread; ++j) {
-                const int rank = rank0 + j;
-                if (rank >= kRowBins) break;
-                const unsigned count = sh.bin[rank];
-                const unsigned long long m = mass_of(rank, count);
-                cn += count;
-                cm += m;
-                if (lim.k_on && static_cast<double>(cn) >= k) {
-                    a = min(a, rank);
-                    b = min(b, rank);
-                }
-                if (lim.p_on) {
-                    if (cn && static_cast<double>(cm) >= p * whole - error) a = min(a, rank);
-                    if (cn && static_cast<double>(cm) >= p * whole + error) b = min(b, rank);
-                }
-                if (lim.m_on) {
-                    if (rank >= rank_m - 1) a = min(a, rank);
-                    if (rank >= rank_m + 1) b = min(b, rank);
-                }
+            if (lim.k_on) {
+                const unsigned k = static_cast<unsigned>(lim.k);
+                if (!locate([=](unsigned n, double) { return n >= k; })) return false;
+                rank_a = rank_b = sh.loc_rank;
             }
-            a = __reduce_min_sync(0xFFFFFFFFu, a);
-            b = __reduce_min_sync(0xFFFFFFFFu, b);
-            __syncthreads();
-            if (lane == 0) {
-                atomicMin(&sh.first_rank, a);
-                sh.warp_count[warp] = static_cast<unsigned>(b);
+            if (lim.p_on) {
+                // (a bin's weight is off by less than 0.4 % where it matters, on either side of the border)
+                const double p = lim.p, whole = mass, error = 0.02 * fmax(p, 0.0) * (1.0 - fmax(p, 0.0)) * whole;
+                if (!locate([=](unsigned, double m) { return m >= p * whole - error; })) return false;
+                rank_a = min(rank_a, sh.loc_rank);
+                if (!locate([=](unsigned, double m) { return m >= p * whole + error; })) return false;
+                rank_b = min(rank_b, sh.loc_rank);
             }
-            __syncthreads();
-            rank_a = sh.first_rank;
-            rank_b = kRowBins;
-            for (int w = 0; w < kWarps; ++w) rank_b = min(rank_b, static_cast<int>(sh.warp_count[w]));
-            __syncthreads();
+            if (lim.m_on) {
+                const int rank = bins.of(static_cast<float>(static_cast<double>(top) + least));
+                rank_a = min(rank_a, rank - 1);
+                rank_b = min(rank_b, rank + 1);
+            }
             if (rank_a > rank_b || rank_b >= kRowBins - 1) return false;
+            __syncthreads();
             if (rank0 <= rank_a && rank_a < rank0 + kPerThread) {
                 unsigned count = pn;
                 for (int j = 0; rank0 + j < rank_a; ++j) count += sh.bin[rank0 + j];
-                sh.above_count = count;
+                sh.loc_n = count;
             }
             __syncthreads();
-            before_n = sh.above_count;
+            before_n = sh.loc_n;
         }
         __syncthreads();   // (the bins make room for the candidates)
 
@@ -1362,12 +1340,13 @@ struct Rows {
         const int per_chunk = ((pieces + kMaxChunks - 1) / kMaxChunks + 3) / 4 * 4;
         const int chunks = (pieces + per_chunk - 1) / per_chunk;
         const float border = DT == FEF_BF16 && cut_on ? bins.value(rank_a) : -INFINITY;
+        const float weightless = top - 64.f / c;   // (so far below the largest logit nothing has a weight)
         auto kind = [&](float l) {
             if constexpr (DT == FEF_BF16)
-                return l > border ? 0 : l == border && cut_on ? 1 : 2;
+                return l > border && l >= weightless ? 0 : l == border && cut_on ? 1 : 3;
             else {
                 const int rank = bins.of(l);
-                return rank == kRowBins - 1 && (l == -INFINITY || cut_on) ? 3 : rank < rank_a ? 0 : rank <= rank_b ? 1 : 2;
+                return rank == kRowBins - 1 ? 3 : rank < rank_a ? 0 : rank <= rank_b ? 1 : 2;
             }
         };
         const bool need_rest = DT == FEF_F32 && lim.p_on;
@@ -1426,13 +1405,20 @@ struct Rows {
         auto each = [&](auto f) {
             for (unsigned j = lane; j < listed; j += 32) {
                 const uint32_t k = key[j];
-                f(static_cast<unsigned long long>(k) << 32 | (0xFFFFFFFFu - id[j]), [&] { return r.weight(logit_of(k)); });
+                f(place_of_order<DT>(k, id[j]), [&] { return r.weight(logit_of(k)); });
             }
         };
 
         // ---- the border
-        const unsigned long long first = place_of(lowest_logit<DT>(), 0x7FFFFFFF), last = place_of(r.top, 0);
-        unsigned long long cut = 0;
+        unsigned long long first = ~0ull, last = 0, cut = 0;   // (where the candidates stand, so that the first level's bins divide them)
+        if (cut_on) {
+            each([&](unsigned long long place, auto&&) {
+                first = min(first, place);
+                last = max(last, place);
+            });
+            first = block_min(first, sh);
+            last = ~block_min(~last, sh);
+        }
         if constexpr (DT == FEF_BF16) {
             if (cut_on) cut = select(each, [=](unsigned n, unsigned long long) { return n >= want; }, first, last, sh, before_n, before_m).place;
         } else if (cut_on) {
@@ -1461,7 +1447,7 @@ struct Rows {
                 unsigned long long lowest = ~0ull;
                 unsigned behind_it = 0;
                 each([&](unsigned long long place, auto&&) {
-                    if (static_cast<double>(logit_of(static_cast<uint32_t>(place >> 32))) - static_cast<double>(r.top) >= least)
+                    if (static_cast<double>(logit_at<DT>(place)) - static_cast<double>(r.top) >= least)
                         lowest = min(lowest, place);
                     else
                         behind_it = 1;
@@ -1483,25 +1469,25 @@ struct Rows {
                 const unsigned long long w = weight();
                 sum += w;
                 ++kept;
-                const int x = static_cast<int>(0xFFFFFFFFu - static_cast<uint32_t>(place));
+                const int x = id_at(place);
                 if (by_chunks) atomicAdd(&sh.chunk[x < pieces * 32 * N ? x / entries_per_chunk : chunks], w);
             }
         });
         const unsigned long long total = before_m + block_sum(sum, sh);
         kept = before_n + static_cast<unsigned>(block_sum(kept, sh));
-        if (threadIdx.x == 0) write_law(P, at, r, cut, total, kept);
+        if (threadIdx.x == 0) write_law<DT>(P, at, r, cut, total, kept);
         if (!P.tokens) return true;
 
         const double target = lim.u * static_cast<double>(total);
         if (!by_chunks) {
             auto by_id = [&](auto f) {
                 each([&](unsigned long long place, auto&& weight) {
-                    if (place >= cut) f(place & 0xFFFFFFFFull, weight);
+                    if (place >= cut) f(place & kIdMask, weight);
                 });
             };
             const unsigned long long drawn = select(by_id, [=](unsigned, unsigned long long s) { return static_cast<double>(s) > target; },
                                                     place_of_id(P.V - 1), place_of_id(0), sh).place;
-            if (threadIdx.x == 0) write_token<DT>(P, at, r, total, static_cast<int>(0xFFFFFFFFull - drawn));
+            if (threadIdx.x == 0) write_token<DT>(P, at, r, total, id_at(drawn));
             return true;
         }
 
@@ -1535,12 +1521,12 @@ struct Rows {
         auto by_id = [&](auto f) {
             for (int x = x_begin + threadIdx.x; x < x_end; x += kThreads) {
                 const float l = load_logit<DT>(r.base, x);
-                if (l != -INFINITY && place_of(l, x) >= cut) f(place_of_id(x), [&] { return r.weight(l); });
+                if (l != -INFINITY && place_of<DT>(l, x) >= cut) f(place_of_id(x), [&] { return r.weight(l); });
             }
         };
         const unsigned long long drawn = select(by_id, [=](unsigned, unsigned long long s) { return static_cast<double>(s) > target; },
                                                 place_of_id(x_end - 1), place_of_id(x_begin), sh, 1u, before_it).place;
-        if (threadIdx.x == 0) write_token<DT>(P, at, r, total, static_cast<int>(0xFFFFFFFFull - drawn));
+        if (threadIdx.x == 0) write_token<DT>(P, at, r, total, id_at(drawn));
         return true;
     }
 };
