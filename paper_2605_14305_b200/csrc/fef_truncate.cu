@@ -39,7 +39,8 @@ struct Params {
     int B, K, V;
     int vec_elems;              // entries of a row in whole 16-byte vectors
     double T, c;                // temperature and log2(e) / T
-    double one, ones;           // 2^F, the weight 1, and F
+    double one;                 // 2^F, the weight 1,
+    int ones;                   // and F
     const float* uniforms;      // [B, K], or null: Philox
     uint64_t seed;
     uint32_t step;
@@ -92,28 +93,29 @@ struct Row {
     int V, vec_elems;
     float top;            // largest logit
     double c, one;
-    double ones;          // F: the weight 1 is 2^F
-    // 2^((l - top) c) in units of 2^-F, as the product of two numbers: 2^y = 2^(k / 256) 2^(f / 256) with k the nearest whole number
-    // to 256 y, the first factor from a table, the second as its Taylor series (|f| <= 1/2: the next term is below 2^-53).  For y > -900.
+    double c256;          // 256 c,
+    float c256_f;         // in binary32
+    int ones;             // F: the weight 1 is 2^F
+    // 2^((l - top) c) in units of 2^-F, as the product of two numbers: with y its exponent, 2^y = 2^(k / 256) 2^(f / 256), k a whole
+    // number next to 256 y (from binary32), the first factor from a table, the second as its Taylor series (|f| < 0.51: the next term
+    // is 1.5 10^-13).  For y > -900.  It takes seven operations in double precision, an addition of the product included: these set the
+    // pace where every entry's weight is needed.
     __device__ __forceinline__ void factors(float l, double& a, double& b) const {
-        const double y = fma(static_cast<double>(l) - static_cast<double>(top), c, ones);
         constexpr double kRound = 6755399441055744.0;   // 1.5 * 2^52: whole numbers stand in the low bits
         constexpr double g = 0.6931471805599453094 / 256.0;
-        const double m = fma(y, 256.0, kRound);
-        const int k = __double2loint(m);
-        const double f = fma(y, 256.0, kRound - m);
-        double t = fma(f, g * g * g * g / 24.0, g * g * g / 6.0);
-        t = fma(f, t, g * g / 2.0);
+        const int k = __float2int_rn((l - top) * c256_f);
+        const double f = fma(static_cast<double>(l) - static_cast<double>(top), c256, kRound - __hiloint2double(0x43380000 - (k < 0), k));
+        double t = fma(f, g * g * g / 6.0, g * g / 2.0);
         t = fma(f, t, g);
         a = fma(f, t, 1.0);
         const double power = reinterpret_cast<const double*>(trunc_smem)[k & 255];
-        b = __hiloint2double(__double2hiint(power) + ((k >> 8) << 20), __double2loint(power));
+        b = __hiloint2double(__double2hiint(power) + (((k >> 8) + ones) << 20), __double2loint(power));
     }
     // The same, rounded to a whole number; 2^-1 and less is 0.
     __device__ __forceinline__ unsigned long long weight(float l) const {
         double a, b;
         factors(l, a, b);
-        return (static_cast<double>(l) - static_cast<double>(top)) * c >= -1.0 - ones ? __double2ull_rn(a * b) : 0ull;
+        return (l - top) * c256_f >= -256.f * 64.f ? __double2ull_rn(a * b) : 0ull;   // (64 powers of two below: nothing, by far)
     }
 };
 
@@ -1045,6 +1047,85 @@ struct Rows {
         return rest;
     }
 
+    // The same for bfloat16 where the border is a positive number: weights come from a table of all positive numbers from it on.  False:
+    // there are more entries equal to the border than there is room for beside the table.
+    static constexpr int kTies = 128;
+    static_assert((kValueBins - 2) * 8 + kWarps * kTies * 4 <= kList * 8, "the table and the ties fit where the candidates are otherwise");
+    static __device__ __forceinline__ bool gather_with_table(const Row& r, int pieces_per_chunk, float border, uint32_t low, Shared& sh) {
+        constexpr int N = Elem<FEF_BF16>::kPerVec;
+        constexpr int kBatch = 4;
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const unsigned lower = (1u << lane) - 1u;
+        unsigned long long* table = reinterpret_cast<unsigned long long*>(sh.id);
+        uint32_t* list = reinterpret_cast<uint32_t*>(table + kValueBins - 2) + warp * kTies;
+        const uint32_t at_border = __float_as_uint(border) >> 16, at_top = __float_as_uint(r.top) >> 16;
+        for (uint32_t a = at_border + threadIdx.x; a <= at_top; a += kThreads) table[a - low] = r.weight(__uint_as_float(a << 16));
+        __syncthreads();
+        const uint32_t border2 = at_border * 0x10001u;
+        const int pieces = r.vec_elems / (32 * N);
+        const int chunks = (pieces + pieces_per_chunk - 1) / pieces_per_chunk;
+        unsigned listed = 0;
+        auto note = [&](bool hit, int x) {
+            const unsigned hits = __ballot_sync(0xFFFFFFFFu, hit);
+            const unsigned at = listed + __popc(hits & lower);
+            if (hit && at < kTies) list[at] = static_cast<uint32_t>(x);
+            listed += __popc(hits);
+        };
+        for (int c = warp; c <= chunks; c += kWarps) {   // (chunk `chunks` is what is behind the last whole piece)
+            unsigned long long sum = 0;
+            if (c < chunks) {
+                const int end = min((c + 1) * pieces_per_chunk, pieces);
+    #pragma unroll 1
+                for (int p = c * pieces_per_chunk; p < end; p += kBatch) {
+                    uint4 w[kBatch];
+    #pragma unroll
+                    for (int j = 0; j < kBatch; ++j) {
+                        w[j] = make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+                        if (p + j < end) w[j] = ld_global_nc_v4(r.base + (static_cast<int64_t>(p + j) * 32 + lane) * 16);
+                    }
+                    uint32_t mask = 0;
+    #pragma unroll
+                    for (int j = 0; j < kBatch; ++j) {
+                        const uint32_t v[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+    #pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const uint32_t a = v[q] & 0xFFFFu, b = v[q] >> 16;   // (a negative number is beyond the largest)
+                            mask |= equal_to(v[q], border2) & (0x00010001u << (4 * j + q));
+                            if (a - at_border - 1u < at_top - at_border) sum += table[a - low];
+                            if (b - at_border - 1u < at_top - at_border) sum += table[b - low];
+                        }
+                    }
+                    while (__any_sync(0xFFFFFFFFu, mask != 0u)) {
+                        const int bit = max(__ffs(mask) - 1, 0);   // bit 16 h + 4 j + q: half h of word q of vector j
+                        note(mask != 0u, ((p + (bit >> 2 & 3)) * 32 + lane) * N + (bit & 3) * 2 + (bit >> 4));
+                        mask &= mask - 1u;
+                    }
+                }
+            } else {
+                for (int x0 = pieces * 32 * N; x0 < r.V; x0 += 32) {
+                    const int x = x0 + lane;
+                    const float l = x < r.V ? load_logit<FEF_BF16>(r.base, x) : -INFINITY;
+                    note(l == border, x);
+                    if (l > border) sum += r.weight(l);
+                }
+            }
+            sum = warp_sum_u64(sum);
+            if (lane == 0) sh.chunk[c] = sum;
+        }
+        const bool fits = listed <= kTies;
+        if (__syncthreads_and(fits) == 0) return false;
+        // the ties move to where the warps' lists are
+        uint32_t mine[(kTies + 31) / 32];
+    #pragma unroll
+        for (int j = 0; j < (kTies + 31) / 32; ++j) mine[j] = j * 32 + lane < listed ? list[j * 32 + lane] : 0u;
+        __syncthreads();
+    #pragma unroll
+        for (int j = 0; j < (kTies + 31) / 32; ++j)
+            if (j * 32 + lane < listed) sh.id[warp * kWarpList + j * 32 + lane] = mine[j];
+        if (lane == 0) sh.listed[warp] = listed;
+        return true;
+    }
+
     // False: the row needs the passes (nothing has been written).
     template <int DT>
     static __device__ bool row_by_values(const Params& P, int64_t at, const Limits& lim, Row& r, Shared& sh) {
@@ -1358,7 +1439,7 @@ struct Rows {
                 else if (lane == 0) sh.listed[warp] = 0;
             } else {
                 bool noted = false;
-                if (P.tokens && want <= static_cast<unsigned>(kList) / 4 * 3) {   // a law of few entries: all of them are candidates
+                if (P.tokens && want <= static_cast<unsigned>(kList) / 8 * 7) {   // a law of few entries: all of them are candidates
                     note_candidates<DT, false>(r, border, 0.f, 0.f, sh);
                     __syncthreads();
                     unsigned longest = 0;
@@ -1371,7 +1452,10 @@ struct Rows {
                     before_n = 0;
                     before_m = 0;
                 } else if (P.tokens) {
-                    gather_near<DT, false>(r, per_chunk, kind, sh);
+                    if (!(border > 0.f && gather_with_table(r, per_chunk, border, bins.low, sh))) {
+                        __syncthreads();
+                        gather_near<DT, false>(r, per_chunk, kind, sh);
+                    }
                 } else {
                     note_candidates<DT, false, true>(r, border, 0.f, 0.f, sh);
                 }
@@ -1550,6 +1634,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) truncate_kernel(con
     r.c = P.c;
     r.one = P.one;
     r.ones = P.ones;
+    r.c256 = 256.0 * P.c;
+    r.c256_f = static_cast<float>(r.c256);
     __syncthreads();
     if (!lim.bad && (R::template row_by_candidates<DT>(P, at, lim, r, sh) || R::template row_by_values<DT>(P, at, lim, r, sh))) return;
     R::template row_by_passes<DT>(P, at, lim, r, sh);
