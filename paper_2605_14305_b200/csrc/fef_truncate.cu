@@ -170,7 +170,7 @@ struct Bins {
     uint32_t low;      // bfloat16: the magnitude (as bits) that bin 0 of a sign ends below
 
     __device__ __forceinline__ int of(float l) const {   // (binary32)
-        return min(max(static_cast<int>(fmaf(anchor - l, c, kAbove) * kScale), 0), kRowBins - 1);
+        return static_cast<int>(min(__float2uint_rz(fmaf(anchor - l, c, kAbove) * kScale), static_cast<unsigned>(kRowBins - 1)));
     }
     // bfloat16: table index of a rank and back to its number
     __device__ static __forceinline__ int at(int rank) { return DT == FEF_F32 ? rank : rank < kValueBins ? kValueBins - 1 - rank : rank; }
@@ -934,8 +934,7 @@ struct Rows {
             if (second) atomicAdd(reinterpret_cast<unsigned*>(table + (t >> 16)), 1u);
         };
         auto count_f32 = [&](float l) {
-            bad |= !(l < INFINITY);
-            top = fmaxf(top, l);
+            asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(top), "f"(l));
             atomicAdd(&sh.bin[bins.of(l)], 1u);
         };
     #pragma unroll 1
@@ -964,15 +963,21 @@ struct Rows {
             else
                 count_f32(l);
         }
-        if constexpr (DT == FEF_BF16) bad |= (largest & 0xFFFFu) > 0x7F80u || (largest >> 16) > 0x7F80u;
+        if constexpr (DT == FEF_BF16)
+            bad |= (largest & 0xFFFFu) > 0x7F80u || (largest >> 16) > 0x7F80u;
+        else
+            bad |= !(top < INFINITY);
         return top;
     }
 
-    // The second pass.  kind(l): 0 before the border, 1 near it, 2 behind, 3 behind and without weight.  Ids of the entries near it go
-    // into the warps' lists; the weights before it are summed into sh.chunk, with REST the thread's sum of those behind is returned.
-    // (Sums in double precision, in a fixed order, and rounded to the weights' units stretch by stretch.)
-    template <int DT, bool REST, class Kind>
-    static __device__ __forceinline__ double gather_near(const Row& r, int pieces_per_chunk, Kind kind, Shared& sh) {
+    // The second pass.  Entries from `weigh` on have their weights summed into sh.chunk, those of [near, before) go into the warps' lists
+    // (their ids), and with REST the weights of [far, near) are summed up for the thread.  (Sums in double precision, in a fixed
+    // order, and rounded to the weights' units stretch by stretch.)
+    struct Limits4 {
+        float weigh, before, near, far;
+    };
+    template <int DT, bool REST>
+    static __device__ __forceinline__ double gather_near(const Row& r, int pieces_per_chunk, const Limits4& at, Shared& sh) {
         constexpr int N = Elem<DT>::kPerVec;
         constexpr int kBatch = 4;
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -1005,22 +1010,19 @@ struct Rows {
                         if (p + j < end) {
                             float l[N];
                             unpack<DT>(w[j], l);
-                            uint32_t before = 0, behind = 0;
+                            bool any = false;
     #pragma unroll
                             for (int i = 0; i < N; ++i) {
-                                const int k = kind(l[i]);
-                                mask |= k == 1 ? 1u << (j * N + i) : 0u;
-                                before |= k == 0 ? 1u << i : 0u;
-                                if (REST) behind |= k == 2 ? 1u << i : 0u;
+                                mask |= l[i] >= at.near && l[i] < at.before ? 1u << (j * N + i) : 0u;
+                                any |= l[i] >= at.weigh;
                             }
-                            // (no branch per entry: the evaluations of a vector overlap)
-                            if (__any_sync(0xFFFFFFFFu, (before | behind) != 0u)) {
-#pragma unroll
+                            if (REST || __any_sync(0xFFFFFFFFu, any)) {
+    #pragma unroll
                                 for (int i = 0; i < N; ++i) {
                                     double a, b;
                                     r.factors(l[i], a, b);
-                                    if (before >> i & 1u) sum = fma(a, b, sum);
-                                    if (REST && (behind >> i & 1u)) rest = fma(a, b, rest);
+                                    if (l[i] >= at.weigh) sum = fma(a, b, sum);
+                                    if (REST && l[i] >= at.far && l[i] < at.near) rest = fma(a, b, rest);
                                 }
                             }
                         }
@@ -1034,10 +1036,9 @@ struct Rows {
                 for (int x0 = pieces * 32 * N; x0 < r.V; x0 += 32) {
                     const int x = x0 + lane;
                     const float l = x < r.V ? load_logit<DT>(r.base, x) : -INFINITY;
-                    const int k = x < r.V ? kind(l) : 3;
-                    note(k == 1, x);
-                    if (k == 0) sum += static_cast<double>(r.weight(l));
-                    if (REST && k == 2) rest += static_cast<double>(r.weight(l));
+                    note(l >= at.near && l < at.before && x < r.V, x);
+                    if (l >= at.weigh) sum += static_cast<double>(r.weight(l));
+                    if (REST && l >= at.far && l < at.near) rest += static_cast<double>(r.weight(l));
                 }
             }
             sum = warp_sum(sum);
@@ -1421,21 +1422,42 @@ struct Rows {
         const int per_chunk = ((pieces + kMaxChunks - 1) / kMaxChunks + 3) / 4 * 4;
         const int chunks = (pieces + per_chunk - 1) / per_chunk;
         const float border = DT == FEF_BF16 && cut_on ? bins.value(rank_a) : -INFINITY;
-        const float weightless = top - 64.f / c;   // (so far below the largest logit nothing has a weight)
-        auto kind = [&](float l) {
-            if constexpr (DT == FEF_BF16)
-                return l > border && l >= weightless ? 0 : l == border && cut_on ? 1 : 3;
-            else {
-                const int rank = bins.of(l);
-                return rank == kRowBins - 1 ? 3 : rank < rank_a ? 0 : rank <= rank_b ? 1 : 2;
+        Limits4 where;
+        if constexpr (DT == FEF_BF16) {
+            const float weightless = top - 64.f / c;   // (so far below the largest logit nothing has a weight)
+            where.before = cut_on ? nextafterf(border, INFINITY) : -INFINITY;
+            where.near = cut_on ? border : -INFINITY;
+            where.weigh = fmaxf(where.before, weightless);
+            where.far = where.weigh;
+        } else {
+            // the lowest numbers of the ranks before rank_a, up to rank_b and before the last: found by halving, so that an entry is
+            // placed by comparisons
+            __syncthreads();
+            if (threadIdx.x < 3) {
+                const int rank = threadIdx.x == 0 ? min(rank_a - 1, kRowBins - 2) : threadIdx.x == 1 ? min(rank_b, kRowBins - 2) : kRowBins - 2;
+                uint32_t in = order_of(top), out = order_of(lowest_logit<DT>()) - 1u;   // (the largest logit's rank is at most rank_b)
+                if (bins.of(top) > rank) in += 1u;   // nothing is before the border
+                while (in - out > 1u && in <= order_of(top)) {
+                    const uint32_t mid = out + (in - out) / 2;
+                    if (bins.of(logit_of(mid)) <= rank)
+                        in = mid;
+                    else
+                        out = mid;
+                }
+                sh.red_f[threadIdx.x][0] = logit_of(in);
             }
-        };
+            __syncthreads();
+            where.before = where.weigh = sh.red_f[0][0];
+            where.near = cut_on ? sh.red_f[1][0] : where.before;
+            where.far = sh.red_f[2][0];
+            __syncthreads();
+        }
         const bool need_rest = DT == FEF_F32 && lim.p_on;
         bool by_chunks = P.tokens != nullptr;   // the draw goes by the stretches' sums, not by the candidates
         unsigned long long rest = 0;
         if constexpr (DT == FEF_BF16) {
             if (!cut_on) {
-                if (P.tokens) gather_near<DT, false>(r, per_chunk, kind, sh);
+                if (P.tokens) gather_near<DT, false>(r, per_chunk, where, sh);
                 else if (lane == 0) sh.listed[warp] = 0;
             } else {
                 bool noted = false;
@@ -1454,7 +1476,7 @@ struct Rows {
                 } else if (P.tokens) {
                     if (!(border > 0.f && gather_with_table(r, per_chunk, border, bins.low, sh))) {
                         __syncthreads();
-                        gather_near<DT, false>(r, per_chunk, kind, sh);
+                        gather_near<DT, false>(r, per_chunk, where, sh);
                     }
                 } else {
                     note_candidates<DT, false, true>(r, border, 0.f, 0.f, sh);
@@ -1463,9 +1485,9 @@ struct Rows {
         } else {
             double mine = 0.0;
             if (need_rest)
-                mine = gather_near<DT, true>(r, per_chunk, kind, sh);
+                mine = gather_near<DT, true>(r, per_chunk, where, sh);
             else
-                gather_near<DT, false>(r, per_chunk, kind, sh);
+                gather_near<DT, false>(r, per_chunk, where, sh);
             mine = warp_sum(mine);
             if (lane == 0) sh.red[warp] = mine;
         }
