@@ -24,6 +24,7 @@
 namespace fef {
 namespace trunc {
 
+constexpr float kManyCandidates = 4000.f;   // with more of them counting all values is faster (1 window x 32: 55 against 110 us)
 constexpr int kMaxChunks = 252;    // stretches of a row whose kept weight is summed up for the draw
 constexpr int kValueBins = 3842;   // of one sign: 30 binades of 128 bfloat16 numbers, what is below, what is above
 constexpr int kRowBins = 2 * kValueBins;
@@ -54,10 +55,22 @@ struct Params {
     int32_t* status;
 };
 
-struct Border {                      // an entry, and what stands before it
-    unsigned long long place, above_mass;
+struct Border {                      // an entry with its weight, what stands before it, and the weight of all
+    unsigned long long place, mass, above_mass, all_mass;
     unsigned above_count;
 };
+// For selections: so much of all weights (and of `rest`, which is not among them).
+struct Share {
+    double p, rest, target;
+    __device__ __forceinline__ void begin(unsigned long long all_mass) { target = p * (static_cast<double>(all_mass) + rest); }
+    __device__ __forceinline__ bool operator()(unsigned, unsigned long long mass) const { return static_cast<double>(mass) >= target; }
+};
+template <class Enough>
+__device__ __forceinline__ auto tell_all(Enough& enough, unsigned long long all_mass, int) -> decltype(enough.begin(all_mass)) {
+    enough.begin(all_mass);
+}
+template <class Enough>
+__device__ __forceinline__ void tell_all(Enough&, unsigned long long, long) {}
 
 extern __shared__ __align__(16) unsigned char trunc_smem[];   // (begins with the table of 2^(i / 256))
 
@@ -344,12 +357,13 @@ struct Rows {
     // those that each(f) hands to f(place, weight), all in [lo, hi], and all distinct.  `enough` is monotone; where it does not hold
     // for all of them together, the last place is returned.  Every level cuts the range into 512 bins and goes on with the one
     // the border is in; one with at most 32 entries is settled by a warp.
-    // above_count, above_mass: what stands before all of them.
+    // above_count, above_mass: what stands before all of them.  `enough` is told their weight first, if it asks for it.
     template <class Each, class Enough>
     static __device__ Border select(Each each, Enough enough, unsigned long long lo, unsigned long long hi, Shared& sh, unsigned above_count = 0,
                              unsigned long long above_mass = 0) {
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        for (;;) {
+        unsigned long long all_mass = 0;
+        for (bool first = true;; first = false) {
             const int bits = 64 - __clzll(static_cast<long long>(hi - lo) | 1ll);
             const int shift = bits > kBinsLog2 ? bits - kBinsLog2 : 0;
             __syncthreads();
@@ -395,14 +409,21 @@ struct Rows {
             pn += above_count - ns;
             pm += above_mass - ms;
             unsigned all = above_count;
+            unsigned long long here = 0;
     #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
                 const unsigned wn = sh.warp_count[w];
+                const unsigned long long wm = sh.warp_mass[w];
                 if (w < warp) {
                     pn += wn;
-                    pm += sh.warp_mass[w];
+                    pm += wm;
                 }
                 all += wn;
+                here += wm;
+            }
+            if (first) {
+                all_mass = here;
+                tell_all(enough, all_mass, 0);
             }
     #pragma unroll
             for (int j = 0; j < kBinsPerThread; ++j) {
@@ -450,6 +471,8 @@ struct Rows {
                     const bool before = c > 0 && enough(c, s);
                     if (lane < have && !before && (c + 1 == above_count + have || enough(c + 1, s + sh.few_weight[lane]))) {
                         sh.border.place = mine;
+                        sh.border.mass = sh.few_weight[lane];
+                        sh.border.all_mass = all_mass;
                         sh.border.above_mass = s;
                         sh.border.above_count = c;
                     }
@@ -667,7 +690,7 @@ struct Rows {
             sh.few = at;
         }
         __syncthreads();
-        const bool many = static_cast<float>(sh.few) > 0.8f * share * kList;
+        const bool many = static_cast<float>(sh.few) > share * fminf(0.8f * kList, kManyCandidates);
         float from = fmaxf(sh.from, lowest);
         if (lim.m_on && !(lim.k_on && lim.p_on))   // (top_p of the first k needs all of them)
             from = fmaxf(from, __double2float_rd(fmax(static_cast<double>(top) + lim.least(P), static_cast<double>(lowest))));
@@ -834,32 +857,41 @@ struct Rows {
         // terms are below 2^-40), the exponential's 2^-22, and as many additions as a thread makes in a row
         rest = with_sum ? rest * exp2(static_cast<double>(ref) - static_cast<double>(r.top) * static_cast<double>(c)) * P.one : 0.0;
         double slack = 4.0e-6 + (static_cast<double>(r.V) / (4 * kThreads) + 32.0) * 0x1p-24;
-        unsigned long long cut = 0;
+        unsigned long long cut = 0, total = 0;   // the border, and
+        unsigned kept = 0;                       // what stands down to it (0: not known yet)
+        auto take = [&](const Border& b) {
+            if (b.place >= cut) {
+                cut = b.place;
+                total = b.above_mass + b.mass;
+                kept = b.above_count + 1u;
+            }
+        };
         if (lim.k_on) {
             if (all < static_cast<unsigned>(lim.k) && !everything) {
                 if (lim.p_on || !lim.m_on) return false;
             } else {
                 const unsigned n_k = static_cast<unsigned>(lim.k);
-                cut = select(each, [=](unsigned n, unsigned long long) { return n >= n_k; }, first, last, sh).place;
+                take(select(each, [=](unsigned n, unsigned long long) { return n >= n_k; }, first, last, sh));
             }
         }
-        if (lim.p_on) {
-            unsigned long long mine_sum = 0;
-            each([&](unsigned long long place, auto&& weight) { mine_sum += place >= cut ? weight() : 0ull; });
-            const double listed_sum = static_cast<double>(block_sum(mine_sum, sh)), p = lim.p;
+        if (lim.p_on && lim.k_on) {   // of what top_k leaves
+            const double target = static_cast<double>(lim.p) * static_cast<double>(total);
+            take(select(each, [=](unsigned, unsigned long long s) { return static_cast<double>(s) >= target; }, first, last, sh));
+        } else if (lim.p_on) {
+            const double p = lim.p;
             for (;;) {
+                const Border b = select(each, Share{p, rest, 0.0}, first, last, sh);
+                const double listed_sum = static_cast<double>(b.all_mass), target = p * (listed_sum + rest);
                 const double least = p * (listed_sum + rest * (1.0 - slack)), most_of_it = p * (listed_sum + rest * (1.0 + slack) + slack * 0x1p-20 * P.one);
                 if (listed_sum < least) {   // beyond the candidates
                     if (!lim.m_on) return false;
                     break;
                 }
-                const double target = p * (listed_sum + rest);
-                const Border b = select(each, [=](unsigned, unsigned long long s) { return static_cast<double>(s) >= target; }, first, last, sh);
-                const double with_it = static_cast<double>(b.above_mass + r.weight(logit_at<DT>(b.place)));
+                const double with_it = static_cast<double>(b.above_mass + b.mass);
                 const bool sure = with_it >= (rest > 0.0 ? most_of_it : target) && (b.above_count == 0 || static_cast<double>(b.above_mass) < least);
                 if (sure || rest == 0.0 || slack == 0.0) {
                     if (!(with_it >= target)) return false;
-                    cut = max(cut, b.place);
+                    take(b);
                     break;
                 }
                 // too near to call: the rest once more, exactly
@@ -878,19 +910,24 @@ struct Rows {
             });
             lowest = block_min(lowest, sh);
             // (entries beyond the candidates may belong to the set too: then it is no border, and another rule's is above it)
-            if (everything || static_cast<double>(from) - static_cast<double>(r.top) <= least) cut = max(cut, lowest);
+            if ((everything || static_cast<double>(from) - static_cast<double>(r.top) <= least) && lowest > cut) {
+                cut = lowest;
+                kept = 0;
+            }
         }
         if (!cut && !everything) return false;
-        unsigned long long sum = 0;
-        unsigned n = 0;
-        each([&](unsigned long long place, auto&& weight) {
-            if (place >= cut) {
-                sum += weight();
-                ++n;
-            }
-        });
-        const unsigned long long total = block_sum(sum, sh);
-        const unsigned kept = static_cast<unsigned>(block_sum(n, sh));
+        if (kept == 0) {
+            unsigned long long sum = 0;
+            unsigned n = 0;
+            each([&](unsigned long long place, auto&& weight) {
+                if (place >= cut) {
+                    sum += weight();
+                    ++n;
+                }
+            });
+            total = block_sum(sum, sh);
+            kept = static_cast<unsigned>(block_sum(n, sh));
+        }
         if (threadIdx.x == 0) write_law<DT>(P, at, r, cut, total, kept);
         if (!P.tokens) return true;
         const double target = lim.u * static_cast<double>(total);

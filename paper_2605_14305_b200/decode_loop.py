@@ -83,21 +83,36 @@ def run_decode_loop(B: int, L: int, K: int, n_steps: int, remask_k: int,
     return dict(tokens=tokens, conf=conf, rounds=rnd - first_round, committed_per_round=committed_hist)
 
 
-def _adjusted_draws(fef, adjust, rnd, q, p, tokens, window, row_len, temperature, seed, step, V, device_round=None):
-    """Draft logits adjusted, draws, target logits adjusted: (q, p, draws, the target rows' normalisers)."""
+def _adjusted_draws(fef, adjust, rnd, q, p, tokens, window, row_len, temperature, seed, step, V, device_round=None, truncate=None):
+    """Draft logits adjusted, draws, target logits adjusted: (q, p, draws, the target rows' normalisers, or None with
+    ``truncate``, whose laws are normalised when they are cut)."""
     rules = adjust if callable(adjust) else (lambda *_: adjust)
     common = dict(tokens=tokens, row_len=row_len, V=V, temperature=temperature)
     q = fef.fef_logits_adjust(q, **common, **rules(rnd, window, row_len, None)).logits
-    draft = fef.fef_draft_sample(q, temperature, seed, step, row_len=row_len, V=V, device_round=device_round)
-    p, p_norm = fef.fef_logits_adjust(p, draft_tokens=draft.tokens, with_norm=True, **common,
+    draft = _draws(fef, q, truncate, temperature, seed, step, row_len, V, device_round)
+    p, p_norm = fef.fef_logits_adjust(p, draft_tokens=draft.tokens, with_norm=truncate is None, **common,
                                       **rules(rnd, window, row_len, draft.tokens))
     return q, p, draft, p_norm
+
+
+def _draws(fef, q, truncate, temperature, seed, step, row_len, V, device_round=None, **more):
+    """The draft draws, from laws cut by ``truncate`` or whole."""
+    if truncate is None:
+        return fef.fef_draft_sample(q, temperature, seed, step, row_len=row_len, V=V, device_round=device_round, **more)
+    return fef.fef_draft_sample_truncated(q, temperature, seed, step, row_len=row_len, V=V, device_round=device_round, **truncate)
+
+
+def _verify_cut(fef, q, p, draft, truncate, temperature, seed, step, row_len, V, device_round=None):
+    """The target laws cut like the draft laws, and the verification of both."""
+    law = fef.fef_law_truncate(p, temperature, row_len=row_len, V=V, **truncate)
+    return fef.fef_spec_verify_truncated(q, p, draft.tokens, temperature, seed, step, draft.law, law, row_len=row_len, V=V,
+                                         device_round=device_round)
 
 
 def run_decode_loop_device(fef, B: int, L: int, K: int, n_steps: int, remask_k: int, logits_fn: Callable,
                            temperature: float, seed: int, on_round: Optional[Callable] = None,
                            first_round: int = 0, reuse_draft_norm: bool = True, build_inputs: bool = False,
-                           reuse_target_norm: bool = False, V: Optional[int] = None, adjust=None):
+                           reuse_target_norm: bool = False, V: Optional[int] = None, adjust=None, truncate=None):
     """Algorithm 2 with the whole state resident on the device: every step of a round is one
     library call (``fef_loop_next_window`` -> [``fef_loop_verification_inputs``] ->
     ``fef_draft_sample`` -> ``fef_spec_verify`` -> ``fef_loop_commit``), and a denoising step ends
@@ -116,9 +131,13 @@ def run_decode_loop_device(fef, B: int, L: int, K: int, n_steps: int, remask_k: 
     draft_tokens or None) that returns one.  The draft logits are adjusted before the draws, by the tokens
     resolved so far; the target logits after them, by those and the window's earlier drafts, and their
     normalisers go to the verification with the draws' own.  The hook then sees the adjusted logits.
+    truncate: sampling limits of every request: a dict of ``top_k``, ``top_p``, ``min_p`` ([B] each, see
+    ``fef_law_truncate``).  Both laws are cut by them: the drafts come from ``fef_draft_sample_truncated``, the verification is
+    ``fef_spec_verify_truncated``.  At temperature 0 they change nothing and are not used.
 
     Returns dict(tokens [B,L] int32, conf [B,L] float32 (CUDA), rounds, committed_per_round, loop_seconds).
     """
+    truncate = truncate if temperature > 0 else None
     dev = torch.device("cuda")
     tokens = torch.full((B, L), MASK, dtype=torch.int32, device=dev)
     conf = torch.full((B, L), -1.0, dtype=torch.float32, device=dev)
@@ -135,16 +154,20 @@ def run_decode_loop_device(fef, B: int, L: int, K: int, n_steps: int, remask_k: 
             inputs = None
             q, p = logits_fn(rnd, window, row_len, None)
             if adjust is not None:
-                q, p, draft, p_norm = _adjusted_draws(fef, adjust, rnd, q, p, tokens, window, row_len, temperature, seed, rnd, V)
+                q, p, draft, p_norm = _adjusted_draws(fef, adjust, rnd, q, p, tokens, window, row_len, temperature, seed, rnd, V,
+                                                      truncate=truncate)
             else:
-                draft = fef.fef_draft_sample(q, temperature, seed, rnd, row_len=row_len, V=V,
-                                             target_logits=p if reuse_target_norm else None)
-                p_norm = draft.target_log2_norm if reuse_target_norm else None
+                draft = _draws(fef, q, truncate, temperature, seed, rnd, row_len, V,
+                               target_logits=p if reuse_target_norm else None)
+                p_norm = draft.target_log2_norm if reuse_target_norm and truncate is None else None
             if build_inputs:
                 inputs = fef.fef_loop_verification_inputs(tokens, window, row_len, draft.tokens)
-            norm = draft.log2_norm if (reuse_draft_norm or p_norm is not None) else None
-            res = fef.fef_spec_verify(q, p, draft.tokens, temperature, seed, rnd, row_len=row_len, V=V,
-                                      draft_log2_norm=norm, target_log2_norm=p_norm)
+            if truncate is not None:
+                res = _verify_cut(fef, q, p, draft, truncate, temperature, seed, rnd, row_len, V)
+            else:
+                norm = draft.log2_norm if (reuse_draft_norm or p_norm is not None) else None
+                res = fef.fef_spec_verify(q, p, draft.tokens, temperature, seed, rnd, row_len=row_len, V=V,
+                                          draft_log2_norm=norm, target_log2_norm=p_norm)
             before = (tokens.clone(), conf.clone(), in_step.clone()) if on_round is not None else None
             committed = fef.fef_loop_commit(window, row_len, res, tokens, conf, in_step)
             if on_round is not None:
@@ -170,7 +193,7 @@ def run_decode_loop_device(fef, B: int, L: int, K: int, n_steps: int, remask_k: 
 
 def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: int, logits_fn: Callable,
                           temperature: float, seed: int, first_round: int = 0, reuse_draft_norm: bool = True,
-                          rounds_per_check: int = 4, adjust=None):
+                          rounds_per_check: int = 4, adjust=None, truncate=None):
     """``run_decode_loop_device`` with one whole round captured as a CUDA graph and replayed.
 
     The round's number lives in a device word that ``fef_draft_sample`` / ``fef_spec_verify`` add
@@ -180,13 +203,14 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
     the last real round of a denoising step change nothing.
 
     logits_fn(device_round [1] int32 CUDA, window_pos, row_len) -> (draft_logits, target_logits):
-    must be capturable (device work only, the round read from the tensor).  ``adjust`` as there; a function
-    of it gets the round's tensor and must be capturable too.  A round in which the verification reports a
+    must be capturable (device work only, the round read from the tensor).  ``adjust`` and ``truncate`` as there; a
+    function ``adjust`` gets the round's tensor and must be capturable too.  A round in which the verification reports a
     data error (a mask that leaves nothing, logits that are no numbers) ends the loop with RuntimeError, at
     the next of those reads.
 
     Returns dict(tokens, conf (CUDA), rounds, loop_seconds: wall time of the replay loop alone).
     """
+    truncate = truncate if temperature > 0 else None
     dev = torch.device("cuda")
     tokens = torch.full((B, L), MASK, dtype=torch.int32, device=dev)
     conf = torch.full((B, L), -1.0, dtype=torch.float32, device=dev)
@@ -200,12 +224,15 @@ def run_decode_loop_graph(fef, B: int, L: int, K: int, n_steps: int, remask_k: i
         p_norm = None
         if adjust is not None:
             q, p, draft, p_norm = _adjusted_draws(fef, adjust, rnd, q, p, tokens, window, row_len, temperature, seed, first_round,
-                                                  None, device_round=rnd)
+                                                  None, device_round=rnd, truncate=truncate)
         else:
-            draft = fef.fef_draft_sample(q, temperature, seed, first_round, row_len=row_len, device_round=rnd)
-        res = fef.fef_spec_verify(q, p, draft.tokens, temperature, seed, first_round, row_len=row_len,
-                                  draft_log2_norm=draft.log2_norm if (reuse_draft_norm or p_norm is not None) else None,
-                                  device_round=rnd, target_log2_norm=p_norm)
+            draft = _draws(fef, q, truncate, temperature, seed, first_round, row_len, None, device_round=rnd)
+        if truncate is not None:
+            res = _verify_cut(fef, q, p, draft, truncate, temperature, seed, first_round, row_len, None, device_round=rnd)
+        else:
+            res = fef.fef_spec_verify(q, p, draft.tokens, temperature, seed, first_round, row_len=row_len,
+                                      draft_log2_norm=draft.log2_norm if (reuse_draft_norm or p_norm is not None) else None,
+                                      device_round=rnd, target_log2_norm=p_norm)
         torch.minimum(worst, fef.fef_loop_commit(window, row_len, res, tokens, conf, in_step), out=worst)
         fef.fef_loop_advance_round(rnd, unresolved)
         return unresolved
