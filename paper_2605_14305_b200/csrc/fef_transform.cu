@@ -128,6 +128,18 @@ __device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const float (&v)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+        :: "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+           "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])),
+           "r"(__float_as_uint(v[8])), "r"(__float_as_uint(v[9])), "r"(__float_as_uint(v[10])), "r"(__float_as_uint(v[11])),
+           "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])), "r"(__float_as_uint(v[14])), "r"(__float_as_uint(v[15])),
+           "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 // A whole warp's wait.  The producer and the MMA issuer run as whole warps, with one elected lane for the copies and MMAs
 // themselves: descriptors, addresses and flags then are warp-uniform values.  With one lane in a branch of its own a block cost each of
 // the two over 600 clocks, more than the MMAs of a 128 x 256 x 64 block.
@@ -239,6 +251,45 @@ struct Residuals {
         for (int q = 0; q < 3; ++q) fetch(P, col, r0 + q * 2 * kChunk, ahead[q]);
     }
 };
+// Sums of many products: the tensor cores truncate whenever they add to an accumulator, 2^-24 of it each time and always the same
+// way (measured against 64 bits, products of random signs: 1.3 10^-7 of the result after 128 products, 10^-6 after 1024).  Where the
+// output is binary32, an accumulator therefore takes 512 products at most; an epilogue warp adds up such parts in registers, rounding
+// to nearest, and puts their sum where the last part was, to be finished like any other.  (A bfloat16 output is rounded to 2^-9 of
+// itself: nothing to gain.)  Tiles of 256 rows would need more registers than there are; 2048 x 4096 x 4096 with a binary32
+// output takes 83 us with pairs of 128 rows, 53 us with a bfloat16 output and pairs of 256.
+constexpr int kLongBlocks = 8;
+template <int BN>
+struct Parts {
+    static constexpr int kChunks = BN >= 2 * kChunk ? BN / (2 * kChunk) : 1;   // of a warp
+    float v[kChunks][kChunk];
+    // adds a part to the sums; the first one starts them, the last one takes them
+    template <bool FIRST, bool LAST>
+    __device__ __forceinline__ void add(uint32_t tmem, int half) {
+#pragma unroll
+        for (int q = 0; q < kChunks; ++q) {
+            const int c = half * kChunk + q * 2 * kChunk;
+            if (c >= BN) continue;
+            float x[kChunk];
+            tmem_load16(tmem + static_cast<uint32_t>(c), x);
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) {
+                if (!FIRST) x[i] += v[q][i];
+                if (!LAST) v[q][i] = x[i];
+            }
+            if (LAST) tmem_store16(tmem + static_cast<uint32_t>(c), x);
+        }
+    }
+    __device__ __forceinline__ void take(int part, int parts, uint32_t tmem, int half) {
+        if (part + 1 < parts) {
+            if (part == 0) add<true, false>(tmem, half);
+            else add<false, false>(tmem, half);
+        } else if (part > 0) {
+            add<false, true>(tmem, half);
+            tmem_wait_stores();
+        }
+    }
+};
+
 template <int BN>
 __device__ __forceinline__ void finish_tile(const Params& P, uint32_t tmem, const Columns& col, Residuals& res, int r0, int half,
                                             float* turn) {
@@ -281,7 +332,7 @@ __device__ __forceinline__ void give_up(const Params& P, volatile int* abort_fla
     report(P.status, FEF_ERR_TIMEOUT);
 }
 
-template <int BN, bool SPLIT>
+template <int BN, bool SPLIT, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1)
 transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h,
                  const __grid_constant__ Params P) {
@@ -324,6 +375,8 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
     const int kb_begin = SPLIT ? rank * P.blocks >> P.split_log2 : 0;
     const int kb_end = SPLIT ? (rank + 1) * P.blocks >> P.split_log2 : P.blocks;
     int issued = 0;   // stages put in flight (producer thread)
+    const int parts_of_tile = LONG ? (kb_end - kb_begin + kLongBlocks - 1) / kLongBlocks : 1;
+    int last_acc = 0;   // the accumulator that holds a tile's last part, then its sums (epilogue)
 
     if (warp == 0) {
         int stage = 0;
@@ -364,39 +417,42 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         unsigned uses[2] = {0u, 0u}, count = 0;
         bool ok = true;
         const uint64_t desc = smem_desc_sw128(smem_u32(smem));
-        for (int tile = first_tile; ok && tile < tiles; tile += stride, ++count) {
-            const int acc = count & 1;
-            // the epilogue must have drained this accumulator (passes at once on its first use)
-            if (!all_wait(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns)) {
-                give_up(P, abort_flag);
-                break;
-            }
-            ++uses[acc];
-            const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
-            for (int kb = kb_begin; kb < kb_end; ++kb) {
-                if (!all_wait(sh.full + stage, phase, abort_flag, P.wait_ns)) {
+        for (int tile = first_tile; ok && tile < tiles; tile += stride)
+            for (int part = 0; ok && part < parts_of_tile; ++part, ++count) {
+                const int acc = count & 1;
+                // the epilogue must have drained this accumulator (passes at once on its first use)
+                if (!all_wait(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns)) {
                     give_up(P, abort_flag);
                     ok = false;
                     break;
                 }
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint64_t desc_w = desc + static_cast<uint64_t>(stage * (S::kStageBytes >> 4));   // (16-byte units)
-                    const uint64_t desc_h = desc_w + static_cast<uint64_t>(kWBytes >> 4);
+                ++uses[acc];
+                const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * BN);
+                const int from = kb_begin + part * kLongBlocks, to = LONG ? min(from + kLongBlocks, kb_end) : kb_end;
+                for (int kb = from; kb < to; ++kb) {
+                    if (!all_wait(sh.full + stage, phase, abort_flag, P.wait_ns)) {
+                        give_up(P, abort_flag);
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t desc_w = desc + static_cast<uint64_t>(stage * (S::kStageBytes >> 4));   // (16-byte units)
+                        const uint64_t desc_h = desc_w + static_cast<uint64_t>(kWBytes >> 4);
 #pragma unroll
-                    for (int k = 0; k < kBK / 16; ++k)   // 32 bytes further along K inside the swizzle row
-                        tc_mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
-                               instruction(kBM, BN), (kb > kb_begin || k) ? 1u : 0u);
-                    tc_commit(sh.empty + stage);   // arrives when these MMAs have read the stage
-                    if (kb == kb_end - 1) tc_commit(sh.tmem_full + acc);   // arrives when the tile's accumulator is complete
-                }
-                __syncwarp();
-                if (++stage == S::kStages) {
-                    stage = 0;
-                    phase ^= 1u;
+                        for (int k = 0; k < kBK / 16; ++k)   // 32 bytes further along K inside the swizzle row
+                            tc_mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
+                                   instruction(kBM, BN), (kb > from || k) ? 1u : 0u);
+                        tc_commit(sh.empty + stage);   // arrives when these MMAs have read the stage
+                        if (kb == to - 1) tc_commit(sh.tmem_full + acc);   // arrives when the accumulator is complete
+                    }
+                    __syncwarp();
+                    if (++stage == S::kStages) {
+                        stage = 0;
+                        phase ^= 1u;
+                    }
                 }
             }
-        }
         // everything issued has finished before the tensor memory goes back, after a wait that ran out too: this one does
         // not look at the abort flag
         if (elect_one()) tc_commit(&sh.drained);
@@ -407,25 +463,36 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
         const int quarter = warp & 3, half = (warp - 2) >> 2;   // the tensor-memory lanes this warp may read; its chunks
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
         unsigned uses[2] = {0u, 0u}, count = 0;
-        for (int tile = first_tile; tile < tiles; tile += stride, ++count) {
-            const int acc = count & 1, r0 = tile % row_tiles * BN;
+        bool ok = true;
+        for (int tile = first_tile; ok && tile < tiles; tile += stride) {
+            const int r0 = tile % row_tiles * BN;
             Columns col;
             Residuals res;
             if constexpr (!SPLIT) {
                 col.set(P, tile / row_tiles * kBM + quarter * 32 + (lane & 3) * 8);
                 res.first(P, col, r0 + half * kChunk);
             }
-            if (!warp_wait(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns)) {
-                give_up(P, abort_flag);
-                break;
+            Parts<LONG ? BN : 16> parts;
+            for (int part = 0; part < parts_of_tile; ++part, ++count) {
+                const int acc = count & 1;
+                if (!warp_wait(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns)) {
+                    give_up(P, abort_flag);
+                    ok = false;
+                    break;
+                }
+                ++uses[acc];
+                tc_fence_after();
+                last_acc = acc;
+                const uint32_t at = lane_addr + static_cast<uint32_t>(acc * BN);
+                if constexpr (LONG) parts.take(part, parts_of_tile, at, half);
+                if (part + 1 == parts_of_tile) {
+                    if constexpr (SPLIT) break;   // (one tile: it is finished below, by the whole cluster)
+                    finish_tile<BN>(P, at, col, res, r0, half, sh.turn[warp - 2]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(sh.tmem_empty + acc);   // the accumulator may be overwritten
             }
-            ++uses[acc];
-            tc_fence_after();
-            if constexpr (SPLIT) break;   // (one tile: it is finished below, by the whole cluster)
-            finish_tile<BN>(P, lane_addr + static_cast<uint32_t>(acc * BN), col, res, r0, half, sh.turn[warp - 2]);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(sh.tmem_empty + acc);   // the accumulator may be overwritten
         }
     }
 
@@ -454,7 +521,7 @@ transform_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constan
 #pragma unroll 1
             for (int c = half * kChunk; c < rows; c += 2 * kChunk) {
                 float v[kChunk];
-                tmem_load16(tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(c), v);
+                tmem_load16(tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + static_cast<uint32_t>(last_acc * BN + c), v);
 #pragma unroll
                 for (int i = 0; i < kChunk; ++i) {
                     const int owner = (c + i) >> P.share_log2;
@@ -568,7 +635,7 @@ __device__ __forceinline__ bool wait_cluster(uint64_t* bar, uint32_t parity, vol
     return false;
 }
 
-template <int TN>
+template <int TN, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1)
 transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_h,
                       const __grid_constant__ Params P) {
@@ -609,6 +676,7 @@ transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
 
     const int row_tiles = P.row_tiles, tiles = P.tiles, blocks = P.blocks;
     const int first_tile = static_cast<int>(blockIdx.x) / 2, stride = static_cast<int>(gridDim.x) / 2;
+    const int parts_of_tile = LONG ? (blocks + kLongBlocks - 1) / kLongBlocks : 1;
     int issued = 0;
 
     if (warp == 0) {
@@ -652,38 +720,41 @@ transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             unsigned uses[2] = {0u, 0u}, count = 0;
             bool ok = true;
             const uint64_t desc = smem_desc_sw128(smem_u32(smem));
-            for (int tile = first_tile; ok && tile < tiles; tile += stride, ++count) {
-                const int acc = count & 1;
-                if (!__all_sync(0xFFFFFFFFu, wait_cluster(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns))) {
-                    give_up(P, abort_flag);
-                    break;
-                }
-                ++uses[acc];
-                const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * TN);
-                for (int kb = 0; kb < blocks; ++kb) {
-                    if (!__all_sync(0xFFFFFFFFu, wait_cluster(sh.full + stage, phase, abort_flag, P.wait_ns))) {
+            for (int tile = first_tile; ok && tile < tiles; tile += stride)
+                for (int part = 0; ok && part < parts_of_tile; ++part, ++count) {
+                    const int acc = count & 1;
+                    if (!__all_sync(0xFFFFFFFFu, wait_cluster(sh.tmem_empty + acc, (uses[acc] & 1u) ^ 1u, abort_flag, P.wait_ns))) {
                         give_up(P, abort_flag);
                         ok = false;
                         break;
                     }
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint64_t desc_w = desc + static_cast<uint64_t>(stage * (kStageBytes >> 4));
-                        const uint64_t desc_h = desc_w + static_cast<uint64_t>(kWBytes >> 4);
+                    ++uses[acc];
+                    const uint32_t tmem_d = tmem_base + static_cast<uint32_t>(acc * TN);
+                    const int from = part * kLongBlocks, to = LONG ? min(from + kLongBlocks, blocks) : blocks;
+                    for (int kb = from; kb < to; ++kb) {
+                        if (!__all_sync(0xFFFFFFFFu, wait_cluster(sh.full + stage, phase, abort_flag, P.wait_ns))) {
+                            give_up(P, abort_flag);
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t desc_w = desc + static_cast<uint64_t>(stage * (kStageBytes >> 4));
+                            const uint64_t desc_h = desc_w + static_cast<uint64_t>(kWBytes >> 4);
 #pragma unroll
-                        for (int k = 0; k < kBK / 16; ++k)
-                            mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
-                                instruction(256, TN), (kb | k) != 0 ? 1u : 0u);
-                        commit_both(sh.empty + stage);
-                        if (kb == blocks - 1) commit_both(sh.tmem_full + acc);
-                    }
-                    __syncwarp();
-                    if (++stage == kStages) {
-                        stage = 0;
-                        phase ^= 1u;
+                            for (int k = 0; k < kBK / 16; ++k)
+                                mma(tmem_d, desc_w + static_cast<uint64_t>(2 * k), desc_h + static_cast<uint64_t>(2 * k),
+                                    instruction(256, TN), (kb > from || k) ? 1u : 0u);
+                            commit_both(sh.empty + stage);
+                            if (kb == to - 1) commit_both(sh.tmem_full + acc);
+                        }
+                        __syncwarp();
+                        if (++stage == kStages) {
+                            stage = 0;
+                            phase ^= 1u;
+                        }
                     }
                 }
-            }
             if (elect_one()) commit_both(&sh.drained);
             __syncwarp();
             volatile int never = 0;
@@ -693,22 +764,30 @@ transform_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t lane_addr = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16);
         unsigned uses[2] = {0u, 0u}, count = 0;
-        for (int tile = first_tile; tile < tiles; tile += stride, ++count) {
-            const int acc = count & 1, r0 = tile % row_tiles * TN;
+        bool ok = true;
+        for (int tile = first_tile; ok && tile < tiles; tile += stride) {
+            const int r0 = tile % row_tiles * TN;
             Columns col;
             Residuals res;
             col.set(P, tile / row_tiles * kTileN + rank * 128 + quarter * 32 + (lane & 3) * 8);
             res.first(P, col, r0 + half * kChunk);
-            if (!warp_wait(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns)) {
-                give_up(P, abort_flag);
-                break;
+            Parts<LONG ? TN : 16> parts;
+            for (int part = 0; part < parts_of_tile; ++part, ++count) {
+                const int acc = count & 1;
+                if (!warp_wait(sh.tmem_full + acc, uses[acc] & 1u, abort_flag, P.wait_ns)) {
+                    give_up(P, abort_flag);
+                    ok = false;
+                    break;
+                }
+                ++uses[acc];
+                tc_fence_after();
+                const uint32_t at = lane_addr + static_cast<uint32_t>(acc * TN);
+                if constexpr (LONG) parts.take(part, parts_of_tile, at, half);
+                if (part + 1 == parts_of_tile) finish_tile<TN>(P, at, col, res, r0, half, sh.turn[warp - 2]);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_in(in_first(sh.tmem_empty + acc));
             }
-            ++uses[acc];
-            tc_fence_after();
-            finish_tile<TN>(P, lane_addr + static_cast<uint32_t>(acc * TN), col, res, r0, half, sh.turn[warp - 2]);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) arrive_in(in_first(sh.tmem_empty + acc));
         }
     }
 
@@ -766,13 +845,13 @@ static bool maps(const Params& P, int w_box, int h_box, CUtensorMap* w, CUtensor
                   CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int BN, bool SPLIT>
+template <int BN, bool SPLIT, bool LONG>
 static cudaError_t launch(const CUtensorMap& w, const CUtensorMap& h, const Params& P, int grid, int dev, cudaStream_t stream) {
     constexpr size_t smem = smem_bytes<Shape<BN>::kStages>(Shape<BN>::kBuffers);
     static bool allowed[64];   // large shared memory, per device
-    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(transform_kernel<BN, SPLIT>), smem, allowed, dev);
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(transform_kernel<BN, SPLIT, LONG>), smem, allowed, dev);
     if (e != cudaSuccess) return e;
-    return launch_clusters(transform_kernel<BN, SPLIT>, w, h, P, grid, SPLIT ? P.split : 1, smem, stream);
+    return launch_clusters(transform_kernel<BN, SPLIT, LONG>, w, h, P, grid, SPLIT ? P.split : 1, smem, stream);
 }
 static int log2_of(int power) {
     int r = 0;
@@ -780,7 +859,7 @@ static int log2_of(int power) {
     return r;
 }
 template <int BN>
-static cudaError_t run(Params& P, int split, int sms, int dev, cudaStream_t stream) {
+static cudaError_t run(Params& P, int split, bool in_parts, int sms, int dev, cudaStream_t stream) {
     CUtensorMap w, h;
     if (!maps(P, kBM, BN, &w, &h)) return cudaErrorUnknown;
     P.row_tiles = (P.rows + BN - 1) / BN;
@@ -788,20 +867,30 @@ static cudaError_t run(Params& P, int split, int sms, int dev, cudaStream_t stre
     P.split = split;
     P.split_log2 = log2_of(split);
     P.share_log2 = log2_of(BN / split);
-    if (split > 1) return launch<BN, true>(w, h, P, P.tiles * split, dev, stream);
-    return launch<BN, false>(w, h, P, P.tiles < sms ? P.tiles : sms, dev, stream);
+    const int grid = split > 1 ? P.tiles * split : P.tiles < sms ? P.tiles : sms;
+    if constexpr (BN <= 128)   // (twice as many registers would not do for the parts of 256 rows)
+        if (in_parts)
+            return split > 1 ? launch<BN, true, true>(w, h, P, grid, dev, stream) : launch<BN, false, true>(w, h, P, grid, dev, stream);
+    return split > 1 ? launch<BN, true, false>(w, h, P, grid, dev, stream) : launch<BN, false, false>(w, h, P, grid, dev, stream);
 }
-template <int TN>
-static cudaError_t run_pairs(Params& P, int sms, int dev, cudaStream_t stream) {
-    CUtensorMap w, h;
-    if (!maps(P, 128, TN / 2, &w, &h)) return cudaErrorUnknown;
+template <int TN, bool LONG>
+static cudaError_t launch_pairs(const CUtensorMap& w, const CUtensorMap& h, const Params& P, int grid, int dev, cudaStream_t stream) {
     constexpr size_t smem = smem_bytes<pair::Shape<TN>::kStages>(pair::Shape<TN>::kRing);
     static bool allowed[64];
-    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(pair::transform_pair_kernel<TN>), smem, allowed, dev);
+    const cudaError_t e = allow_smem(reinterpret_cast<const void*>(pair::transform_pair_kernel<TN, LONG>), smem, allowed, dev);
     if (e != cudaSuccess) return e;
+    return launch_clusters(pair::transform_pair_kernel<TN, LONG>, w, h, P, grid, 2, smem, stream);
+}
+template <int TN>
+static cudaError_t run_pairs(Params& P, bool in_parts, int sms, int dev, cudaStream_t stream) {
+    CUtensorMap w, h;
+    if (!maps(P, 128, TN / 2, &w, &h)) return cudaErrorUnknown;
     P.row_tiles = (P.rows + TN - 1) / TN;
     P.tiles = P.row_tiles * ((P.n + pair::kTileN - 1) / pair::kTileN);
-    return launch_clusters(pair::transform_pair_kernel<TN>, w, h, P, 2 * (P.tiles < sms / 2 ? P.tiles : sms / 2), 2, smem, stream);
+    const int grid = 2 * (P.tiles < sms / 2 ? P.tiles : sms / 2);
+    if constexpr (TN <= 128)   // (as above)
+        if (in_parts) return launch_pairs<TN, true>(w, h, P, grid, dev, stream);
+    return launch_pairs<TN, false>(w, h, P, grid, dev, stream);
 }
 
 // Which tiles, and how many CTAs to a tile.  Every choice is right for every call; what each takes was measured over 23 sizes (1 to
@@ -813,17 +902,18 @@ static cudaError_t run_pairs(Params& P, int sms, int dev, cudaStream_t stream) {
 // 21.4 (22.4), BN = 128 25.1 (24.6); 1024 x 1024 x 1024: BN = 64 8.7 (8.7), pairs of 256 rows 15.1 (11.7).
 struct Choice {
     int tile, split;
-    bool pair;
+    bool pair, in_parts;   // in_parts: sums of more than 512 products for a binary32 output (tiles of up to 128 rows only)
 };
-static Choice choose(int rows, int n, int d, int sms) {
+static Choice choose(int rows, int n, int d, bool out_f32, int sms) {
     const int64_t columns = (n + kBM - 1) / kBM, pair_columns = (n + 255) / 256;
     const int blocks = (d + kBK - 1) / kBK;
-    Choice best = {256, 1, false};
+    Choice best = {128, 1, false, false};
     double least = 1e300;
     auto offer = [&](int tile, int split, bool pair, double us) {
-        if (us < least) {
+        const bool in_parts = out_f32 && (blocks + split - 1) / split > kLongBlocks;
+        if (us < least && !(in_parts && tile > 128)) {
             least = us;
-            best = {tile, split, pair};
+            best = {tile, split, pair, in_parts};
         }
     };
     for (int bn = 16; bn <= 256; bn *= 2) {
@@ -917,17 +1007,17 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
     g_test_withhold = -1;
 #endif
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const Choice c = choose(rows, n, d, sms);
+    const Choice c = choose(rows, n, d, dt == FEF_F32, sms);
     cudaError_t e;
     if (c.pair)
-        e = c.tile == 64    ? run_pairs<64>(P, sms, dev, stream)
-            : c.tile == 128 ? run_pairs<128>(P, sms, dev, stream)
-                            : run_pairs<256>(P, sms, dev, stream);
+        e = c.tile == 64    ? run_pairs<64>(P, c.in_parts, sms, dev, stream)
+            : c.tile == 128 ? run_pairs<128>(P, c.in_parts, sms, dev, stream)
+                            : run_pairs<256>(P, c.in_parts, sms, dev, stream);
     else
-        e = c.tile == 16    ? run<16>(P, c.split, sms, dev, stream)
-            : c.tile == 32  ? run<32>(P, c.split, sms, dev, stream)
-            : c.tile == 64  ? run<64>(P, c.split, sms, dev, stream)
-            : c.tile == 128 ? run<128>(P, c.split, sms, dev, stream)
-                            : run<256>(P, c.split, sms, dev, stream);
+        e = c.tile == 16    ? run<16>(P, c.split, c.in_parts, sms, dev, stream)
+            : c.tile == 32  ? run<32>(P, c.split, c.in_parts, sms, dev, stream)
+            : c.tile == 64  ? run<64>(P, c.split, c.in_parts, sms, dev, stream)
+            : c.tile == 128 ? run<128>(P, c.split, c.in_parts, sms, dev, stream)
+                            : run<256>(P, c.split, c.in_parts, sms, dev, stream);
     return e == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
 }

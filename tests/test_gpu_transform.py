@@ -88,6 +88,22 @@ def test_activations_and_epilogues(fef, act, dtype):
         _check(fef, rows, 390, 264, act, True, False, dtype, scale=1e-6)
 
 
+@pytest.mark.parametrize("rows,n,d", [(1, 512, 8192), (20, 300, 16384), (64, 4096, 8192), (300, 700, 5000), (700, 5003, 4104),
+                                      (1000, 4096, 8192)])
+def test_binary32_sums_of_many_products(fef, rows, n, d):
+    """Products of one sign, so that the sums grow and roundings towards zero add up."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    h, w = (torch.rand(s, generator=g, device="cuda").bfloat16() for s in ((rows, d), (n, d)))
+    got, status = fef.fef_hidden_transform(h, w, dtype=torch.float32)
+    assert int(status) == 0
+    want = h.double() @ w.double().T
+    # 512 products go to one sum, sixteen at a time: 32 additions, each within two roundings towards zero (2^-23 of the sum each: the
+    # addition's and the products'); the sums of at most d / 512 + 8 parts are added with rounding to nearest, 2^-24 each.  8192 products
+    # in one sum lose 512 x 2^-24 x half of the final sum on average, 1.5 10^-5, twice what is allowed
+    allowed = 64 * 2.0 ** -23 + (d / 512 + 9) * 2.0 ** -24
+    assert float(((got.double() - want).abs() / want).max()) <= allowed
+
+
 def test_every_row_count_up_to_a_tile(fef):
     for rows in range(1, 70):
         _check(fef, rows, 200, 128, "gelu", True, False)
