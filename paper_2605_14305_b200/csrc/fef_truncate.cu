@@ -1272,10 +1272,13 @@ struct Rows {
         if (sh.bad || above_range) return false;
         r.top = top;
         if (behind && r.weight(bins.value(kRowBins - 1))) return false;
-        constexpr int kLowFirst = kValueBins - 1;   // (bfloat16) the ranks of what is too small to tell apart: the zeros, or the passes
+        constexpr int kLowFirst = kValueBins - 1;   // (bfloat16) the ranks of what is too small to tell apart, counted as zeros
         if constexpr (DT == FEF_BF16) {
-            if (sh.bin[Bins<DT>::at(kLowFirst)] + sh.bin[Bins<DT>::at(kLowFirst + 1)]) {
-                const float smallest = __uint_as_float(bins.low << 16);
+            // Numbers that are no zeros among them put the sums out by 2^-29 of the largest logit's exponent times their weight.  A few
+            // hardly ever matter (one row in a thousand has one); where they might, by 2^-45 of the largest weight, it is the passes' turn.
+            const unsigned low = sh.bin[Bins<DT>::at(kLowFirst)] + sh.bin[Bins<DT>::at(kLowFirst + 1)];
+            const float smallest = __uint_as_float(bins.low << 16);
+            if (low && static_cast<float>(low) * ex2_approx(-top * c) * smallest * c > 0x1p-45f) {
                 bool other = false;
                 for_each<DT>(r, [&](float l, int) { other |= l != 0.f && fabsf(l) < smallest; });
                 if (__syncthreads_or(other)) return false;

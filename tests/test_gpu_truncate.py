@@ -289,6 +289,18 @@ def test_rows_of_unusual_numbers(fef, dtype):
         _check(fef, x, uniforms=u, top_p=_f32(0.99, 0.9999, 0.999999, 0.3), min_p=_f32(1e-3, 1e-8, 1e-3, 1e-37))
 
 
+@pytest.mark.parametrize("T", [0.6, 30.0])
+@pytest.mark.parametrize("k,p,m", [(0, 0.9, 0.0), (100, 1.0, 0.0), (0, 1.0, 0.001), (15000, 0.99, 0.0), (0, 1.0, 0.0)])
+def test_tiny_numbers_among_bfloat16(fef, k, p, m, T):
+    x, u = _logits(4, 1, 20000, torch.bfloat16, 31)
+    tiny = torch.tensor([1e-30, -1e-30, 2e-38, -9e-41, 0.0, -0.0], device="cuda").bfloat16()
+    x[0, 0, 5::4000] = tiny[:5]                       # a few among ordinary ones
+    x[1, 0, 30:] = tiny.repeat(4000)[30:20000]        # thirty ordinary ones among them
+    x[2, 0] = tiny.repeat(4000)[:20000]               # nothing else
+    x[3, 0, ::2] = tiny.repeat(4000)[:10000]
+    _check(fef, x, T, top_k=_i32(k, k, k, k), top_p=_f32(p, p, p, p), min_p=_f32(m, m, m, m), uniforms=u)
+
+
 @pytest.mark.parametrize("rows", [2, 200, 400])    # (as many threads to a row as there are for it)
 def test_every_share_of_threads(fef, rows):
     for V in (4097, 8193, 16385, 40961):
