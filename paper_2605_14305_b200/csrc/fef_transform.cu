@@ -66,8 +66,8 @@ __device__ __forceinline__ float activate(float y) {
 // states: the right operand, N = BN), so that few hidden rows cost few columns of tensor memory and no padding of the weight
 // stream.  Warp 0 brings 64-deep blocks of both operands through a ring by TMA (one thread), warp 1 issues the MMAs (one thread),
 // warps 2-9 are the epilogue.  Accumulators are double-buffered.  With fewer tiles than SMs the CTAs of a thread-block cluster
-// share a tile's depth: each finishes a share of the rows, whose sums the others write into its shared memory (writing takes a
-// third of the time of reading them from there).
+// share a tile's depth: each finishes a share of the rows, whose sums the others write into its shared memory (writes there do not
+// wait for an answer, reads would).
 //
 // transform_pair_kernel: two CTAs (a cluster) take 256 columns by 256 rows with tcgen05.mma.cta_group::2: each brings its own 128
 // columns' weights and half of the hidden rows, which both tensor cores read.  Per SM a block is 32 KiB instead of the 48 KiB of
@@ -966,10 +966,17 @@ extern "C" fef_status fef_hidden_transform(const void* hidden, int64_t ld_hidden
         return FEF_ERR_ALIGNMENT;
     // the output may be the residual itself, element for element, and overlaps nothing else
     struct Range {
-        uintptr_t from, to;
-        Range(const void* p, int64_t rows, int64_t pitch, int64_t cols, int64_t size)
-            : from(reinterpret_cast<uintptr_t>(p)), to(from + static_cast<uintptr_t>(((rows - 1) * pitch + cols) * size)) {}
-        bool meets(const Range& o) const { return from < o.to && o.from < to; }
+        uintptr_t from, to, pitch, width;
+        Range(const void* p, int64_t rows, int64_t ld, int64_t cols, int64_t size)
+            : from(reinterpret_cast<uintptr_t>(p)), to(from + static_cast<uintptr_t>(((rows - 1) * ld + cols) * size)),
+              pitch(static_cast<uintptr_t>(ld * size)), width(static_cast<uintptr_t>(cols * size)) {}
+        bool meets(const Range& o) const {
+            if (from >= o.to || o.from >= to) return false;
+            if (pitch != o.pitch) return true;
+            // different columns of one buffer: o's rows start `off` bytes behind this one's, and end before the next
+            const uintptr_t off = (o.from >= from ? o.from - from : pitch - (from - o.from) % pitch) % pitch;
+            return off < width || off + o.width > pitch;
+        }
     };
     const Range o(out, rows, ldo, n, esize);
     if (o.meets(Range(hidden, rows, ld_hidden, d, 2)) || o.meets(Range(weight, n, d, d, 2)) || (bias && o.meets(Range(bias, 1, n, n, 2))))

@@ -9,7 +9,7 @@
 //   token = the lowest id x for which the kept weights of ids <= x sum to more than u * (sum of the kept weights).
 //
 // Which entry a border falls on is decided by sums that differ by one entry's weight, 10^-6 of the whole and less, so weights
-// are evaluated in double precision and summed as 64-bit integers (w 2^F, F = 62 - log2 V rounded down): such sums are exact,
+// are evaluated in double precision and summed as 64-bit integers (w 2^F, F = 62 - ceil(log2 V)): such sums are exact,
 // whatever the order in which threads add them.
 #include <cuda_runtime.h>
 #include <math.h>

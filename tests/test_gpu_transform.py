@@ -136,6 +136,17 @@ def test_in_place_on_the_residual(fef):
         assert got is r and torch.equal(r, want)
 
 
+def test_columns_of_one_buffer(fef):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for rows, n, d in ((3, 40, 64), (90, 520, 512), (700, 1032, 264)):
+        buf = torch.randn((rows, d + 2 * n), generator=g, device="cuda").bfloat16()
+        w = torch.randn((n, d), generator=g, device="cuda").bfloat16()
+        before = buf.clone()
+        want, _ = fef.fef_hidden_transform(before[:, :d].contiguous(), w, residual=before[:, d + n:].contiguous(), activation="gelu")
+        fef.fef_hidden_transform(buf[:, :d], w, residual=buf[:, d + n:], activation="gelu", out=buf[:, d:d + n])
+        assert torch.equal(buf[:, d:d + n], want) and torch.equal(buf[:, :d], before[:, :d]) and torch.equal(buf[:, d + n:], before[:, d + n:])
+
+
 def test_a_bad_row_stays_alone(fef):
     for rows, n, d in ((4, 300, 256), (50, 300, 256), (300, 300, 256), (9000, 300, 256)):
         h, w, b, r, want = _check(fef, rows, n, d, "gelu_tanh", True, True)

@@ -329,6 +329,24 @@ def test_largest_vocabulary_and_temperatures(fef):
             _check(fef, x, T, uniforms=u, **_rules(kind, 4))
 
 
+def test_offsets_beyond_32_bits(fef):
+    x, u = _logits(5, 16, 3000, torch.bfloat16, 41)
+    far = torch.empty((5, 16, 1 << 26), dtype=torch.bfloat16, device="cuda")   # 2^32 entries before the last window's rows
+    far[..., :3000] = x[..., :3000]
+    k, p = _i32(40, 0, 40, 0, 40), _f32(0.9, 0.9, 1.0, 0.9, 0.7)
+    a = fef.fef_draft_sample_truncated(x, 0.8, top_k=k, top_p=p, uniforms=u, V=3000)
+    b = fef.fef_draft_sample_truncated(far, 0.8, top_k=k, top_p=p, uniforms=u, V=3000)
+    law = fef.fef_law_truncate(far, 0.8, top_k=k, V=3000)
+    for s, t in zip((a.tokens, a.conf, *a.law), (b.tokens, b.conf, *b.law)):
+        assert torch.equal(s, t)
+    near = fef.fef_law_truncate(x, 0.8, top_k=k, V=3000)
+    tokens = a.tokens.clone()
+    tokens[:, 3] = 7
+    for s, t in zip(fef.fef_spec_verify_truncated(x, x, tokens, 0.8, 1, 2, a.law, near, V=3000),
+                    fef.fef_spec_verify_truncated(far, far, tokens, 0.8, 1, 2, b.law, law, V=3000)):
+        assert torch.equal(s, t)
+
+
 def test_frequencies_follow_the_cut_law(fef):
     """A chi-square test of draws with Philox's numbers (99.99 % point of its law)."""
     from scipy.stats import chi2

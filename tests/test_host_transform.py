@@ -37,5 +37,14 @@ def test_argument_checks_return_before_touching_the_device(fef):
     for ok in (f(), f(res=O, ldr=32), f(res=O, ldr=99, rows=1), f(res=O + 4 * 32 * 2, ldr=32), f(out=O + 2), f(ldh=72, ldo=33),
                f(rows=1, n=1, d=8, ldh=8, ldo=1, act=4, dt=0), f(bias=R, res=R + 64, ldr=32, status=R)):
         assert ok == fef.FEF_ERR_CUDA
+    # columns of one buffer: side by side, or over one another by two bytes; the hidden states on either side of the output
+    wide = dict(ldh=96, ldo=96, ldr=96)
+    for ok in (f(out=H + 128, **wide), f(out=H - 64, **wide), f(out=H - 192 - 64, **wide), f(out=O, res=O + 64, **wide),
+               f(out=O, res=O + 128, **wide), f(out=O + 128, res=O, **wide)):
+        assert ok == fef.FEF_ERR_CUDA
+    for out in (H + 126, H - 62, H + 192 - 62, H + 192 * 3 + 126):
+        assert f(out=out, **wide) == bad
+    for res in (O + 62, O + 130, O - 62, O + 192 - 62, O + 192):
+        assert f(out=O, res=res, **wide) == bad
     with pytest.raises(RuntimeError):
         fef.fef_hidden_transform(torch.zeros(1, 8), torch.zeros(1, 8))
