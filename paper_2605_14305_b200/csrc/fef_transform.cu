@@ -72,6 +72,10 @@ __device__ __forceinline__ float activate(float y) {
 // transform_pair_kernel: two CTAs (a cluster) take 256 columns by 256 rows with tcgen05.mma.cta_group::2: each brings its own 128
 // columns' weights and half of the hidden rows, which both tensor cores read.  Per SM a block is 32 KiB instead of the 48 KiB of
 // a 128 x 256 tile of its own, whose copies and operand reads together are more than shared memory's 128 bytes a clock.
+//
+// Few rows are bound by the weights' stream and by starting and joining (1 row x 4096 x 4096: 7.8 us on the device for 5.2 us of bytes;
+// 64 rows 9.3), many by the tensor cores (2048 x 4096 x 4096 with silu, bias and residual 52.5 us, 1.31 PFLOP/s; the bare product by the
+// installed library 44.5).
 constexpr int kBM = 128, kBK = 64;
 constexpr int kWBytes = kBM * kBK * 2;
 constexpr int kEpilogueWarps = 8;

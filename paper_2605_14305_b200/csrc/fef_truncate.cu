@@ -11,6 +11,19 @@
 // Which entry a border falls on is decided by sums that differ by one entry's weight, 10^-6 of the whole and less, so weights
 // are evaluated in double precision and summed as 64-bit integers (w 2^F, F = 62 - ceil(log2 V)): such sums are exact,
 // whatever the order in which threads add them.
+//
+// A CTA has one row; memory bounds it from below (a row once, 259 MB and 40 us for 32 windows x 32 x 126464 bfloat16).  Three ways, each
+// handing on what it cannot decide:
+//   row_by_candidates  where the border is among few entries, as top-k's, min-p's and a steep law's top-p's are: a sample of the row tells a
+//                      floor safely below the border, one pass notes down what is above it and only sums the rest, and the border and
+//                      the draw are found among what was noted down.  One read of the row; bound by that and by the instructions of
+//                      looking at every entry (64 windows x 32 x 126464 bfloat16, top-k 50: 118 us, with draws 132; 4.4 and 3.9 TB/s)
+//   row_by_values      where it is among many (a flat law's top-p): the row is counted by value, then read once more, from L2 for the most
+//                      part.  Bound by the shared-memory atomics of the counting and, with draws, the weights of all entries before
+//                      the border (the same rows, top-p 0.9: 282 us, with draws 387; 16 windows x 32 x 152064 binary32 236 and 246)
+//   row_by_passes      whatever is left, and rows that are errors: some ten passes, 0.5 ms a row
+// Sampling and candidates against counting every row: top-k 50 of 16 windows x 32 x 152064 binary32 60 against 217 us; counting against
+// passes: 3850 against 300 us at 32 windows of flat bfloat16 rows.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -690,10 +703,22 @@ struct Rows {
             sh.few = at;
         }
         __syncthreads();
-        const bool many = static_cast<float>(sh.few) > share * fminf(0.8f * kList, kManyCandidates);
         float from = fmaxf(sh.from, lowest);
-        if (lim.m_on && !(lim.k_on && lim.p_on))   // (top_p of the first k needs all of them)
+        if (lim.m_on && !(lim.k_on && lim.p_on)) {   // (top_p of the first k needs all of them)
             from = fmaxf(from, __double2float_rd(fmax(static_cast<double>(top) + lim.least(P), static_cast<double>(lowest))));
+            unsigned few = 0;
+    #pragma unroll
+            for (int j = 0; j < kPerWarp * N; ++j) few += x[j] >= from;
+            few = __reduce_add_sync(0xFFFFFFFFu, few);
+            if (lane == 0) sh.warp_count[warp] = few;
+            __syncthreads();
+            few = 0;
+    #pragma unroll
+            for (int v = 0; v < kWarps; ++v) few += sh.warp_count[v];
+            if (threadIdx.x == 0) sh.few = few;
+            __syncthreads();
+        }
+        const bool many = static_cast<float>(sh.few) > share * fminf(0.8f * kList, kManyCandidates);
         if (DT == FEF_BF16) {   // rounded down
             uint32_t bits = __float_as_uint(from);
             if (bits & 0x80000000u) bits += 0xFFFFu;
@@ -945,8 +970,8 @@ struct Rows {
     // --------------------------------------------------------------------- values counted ----
     // Where candidates are too many, or the sample misled: one pass counts the row's entries by value, which places the border; a second
     // pass notes down the few entries near it and sums the weights before it, stretch by stretch for the draw.
-    //   bfloat16: a bin is one number (30 binades of either sign), so all sums over the row follow from the counts, exactly, and the
-    //   second pass looks for the entries equal to the border's number.
+    //   bfloat16: a bin is one number (30 binades of either sign), so all sums over the row follow from the counts, exactly (but for
+    //   numbers near zero, see there), and the second pass looks for the entries equal to the border's number.
     //   binary32: bins are 1/96 of a power of two of the weight wide, masses are estimates, and the border is looked for among the bins
     //   within the estimates' error of it; the second pass sums exactly, over the whole row where top_p needs that.
     // A row of either kind that its bins do not hold (values out of their range that matter, borders in a bin of leftovers, more equal
