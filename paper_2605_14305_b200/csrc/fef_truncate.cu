@@ -290,6 +290,9 @@ struct Rows {
     static constexpr int kWarpList = kAll / kWarps + 32;   // candidates a warp can note down (its share of such a row, and of the row's end)
     static constexpr int kList = kWarps * kWarpList;
     static constexpr int kRowBinsPerThread = (kRowBins + kThreads - 1) / kThreads;
+    // So few candidates are all compared with one another, kFewShare threads to each; the work grows with the square.
+    static constexpr int kFew = kThreads / 2 < 256 ? kThreads / 2 : 256;
+    static constexpr int kFewShare = kThreads / kFew;
     static_assert(kRowBins * 4 <= kList * 8, "the bins fit where the candidates are later");
     static_assert(kMaxChunks < kThreads, "a thread for each stretch");
 
@@ -301,6 +304,10 @@ struct Rows {
                 unsigned count[kBins];
             };
             unsigned sample[kSampleBins];
+            struct {                         // few candidates
+                ulonglong2 loose[kFew];      // place and weight, as they come; later by rank, with the id in the place's stead
+                unsigned long long ranked[kFew], upto[kFew];   // by rank: place, weight of all down to it
+            };
         };
         union {
             struct {
@@ -831,6 +838,97 @@ struct Rows {
         return nan ? __int_as_float(0x7FC00000) : 0.f;
     }
 
+    // Few candidates: each one's rank and the weight down to it, by comparing it with all; every rule then is a number of ranks.  False:
+    // the rest's weight is too near to call, or the border is not among them (nothing has been written).
+    template <int DT>
+    static __device__ __forceinline__ bool row_of_few(const Params& P, int64_t at, const Limits& lim, const Row& r, Shared& sh, int n, float from,
+                                                      double rest, double slack) {
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+        const int mine = threadIdx.x / kFewShare, part = threadIdx.x % kFewShare;
+        const unsigned listed = sh.listed[warp];
+        const unsigned before = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sh.listed[lane] : 0u);
+        for (unsigned j = lane; j < listed; j += 32) {
+            const uint32_t key = sh.key[warp * kWarpList + j];
+            sh.loose[before + j] = make_ulonglong2(place_of_order<DT>(key, sh.id[warp * kWarpList + j]), r.weight(logit_of(key)));
+        }
+        __syncthreads();
+        // the sum of those that `precede` own, over all of the first `count`
+        auto sum_over = [&](int count, unsigned long long own, unsigned& rank) {
+            unsigned long long sum = 0;
+            rank = 0;
+            if (mine < count)
+                for (int j = part; j < count; j += kFewShare) {
+                    const ulonglong2 o = sh.loose[j];
+                    if (o.x > own) {
+                        ++rank;
+                        sum += o.y;
+                    }
+                }
+    #pragma unroll
+            for (int o = 1; o < kFewShare; o <<= 1) {
+                rank += __shfl_xor_sync(0xFFFFFFFFu, rank, o);
+                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            }
+            return sum;
+        };
+        ulonglong2 own = make_ulonglong2(0ull, 0ull);
+        if (mine < n) own = sh.loose[mine];
+        unsigned rank;
+        const unsigned long long above = sum_over(n, own.x, rank);
+        const bool writes = mine < n && part == 0;
+        if (writes) {
+            sh.ranked[rank] = own.x;
+            sh.upto[rank] = above + own.y;
+        }
+        __syncthreads();
+        if (writes) sh.loose[rank] = make_ulonglong2(own.x & kIdMask, own.y);
+        const bool everything = from == lowest_logit<DT>();
+        const int t = threadIdx.x;
+        int kept = n + 1;   // entries down to the border (n + 1: not known)
+        if (lim.k_on) {
+            if (n < lim.k && !everything) {
+                if (lim.p_on || !lim.m_on) return false;
+            } else {
+                kept = min(lim.k, n);
+            }
+        }
+        if (lim.p_on) {
+            const double p = lim.p, sum = static_cast<double>(sh.upto[(lim.k_on ? kept : n) - 1]);
+            const double target = p * (sum + rest), least = p * (sum + rest * (1.0 - slack));
+            if (sum < least) {   // beyond the candidates
+                if (!lim.m_on) return false;
+            } else {
+                const int n_p = __syncthreads_count(t < n && !(static_cast<double>(sh.upto[t]) >= target)) + 1;
+                if (n_p > n) return false;
+                const double most_of_it = p * (sum + rest * (1.0 + slack) + slack * 0x1p-20 * P.one);
+                if (rest > 0.0 && !(static_cast<double>(sh.upto[n_p - 1]) >= most_of_it && (n_p == 1 || static_cast<double>(sh.upto[n_p - 2]) < least)))
+                    return false;
+                kept = min(kept, n_p);
+            }
+        }
+        if (lim.m_on) {
+            const double least = lim.least(P);
+            const int n_m = __syncthreads_count(
+                t < n && static_cast<double>(logit_at<DT>(sh.ranked[t < n ? t : 0])) - static_cast<double>(r.top) >= least);
+            // (as below: with entries beyond the candidates in the set it is no border)
+            if (everything || static_cast<double>(from) - static_cast<double>(r.top) <= least) kept = min(kept, n_m);
+        }
+        if (kept > n && !everything) return false;
+        const unsigned long long cut = kept > n ? 0ull : sh.ranked[kept - 1];
+        kept = min(kept, n);
+        const unsigned long long total = sh.upto[kept - 1];
+        if (threadIdx.x == 0) write_law<DT>(P, at, r, cut, total, static_cast<unsigned>(kept));
+        if (!P.tokens) return true;
+        // The draw: the same by the ids.
+        __syncthreads();
+        const double target = lim.u * static_cast<double>(total);
+        if (mine < kept) own = sh.loose[mine];
+        const unsigned long long lower = sum_over(kept, own.x, rank);
+        if (mine < kept && part == 0 && static_cast<double>(lower + own.y) > target && !(static_cast<double>(lower) > target))
+            write_token<DT>(P, at, r, total, id_at(own.x));   // one thread
+        return true;
+    }
+
     // False: the row needs the other path (nothing has been written).
     template <int DT>
     static __device__ bool row_by_candidates(const Params& P, int64_t at, const Limits& lim, Row& r, Shared& sh) {
@@ -882,6 +980,10 @@ struct Rows {
         // terms are below 2^-40), the exponential's 2^-22, and as many additions as a thread makes in a row
         rest = with_sum ? rest * exp2(static_cast<double>(ref) - static_cast<double>(r.top) * static_cast<double>(c)) * P.one : 0.0;
         double slack = 4.0e-6 + (static_cast<double>(r.V) / (4 * kThreads) + 32.0) * 0x1p-24;
+        if (all <= kFew) {
+            if (row_of_few<DT>(P, at, lim, r, sh, static_cast<int>(all), from, rest, slack)) return true;
+            __syncthreads();
+        }
         unsigned long long cut = 0, total = 0;   // the border, and
         unsigned kept = 0;                       // what stands down to it (0: not known yet)
         auto take = [&](const Border& b) {
@@ -1708,6 +1810,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) truncate_kernel(con
     typename R::Shared& sh = *reinterpret_cast<typename R::Shared*>(trunc_smem);
     const int64_t at = blockIdx.x;
     const int b = static_cast<int>(at / P.K), i = static_cast<int>(at - static_cast<int64_t>(b) * P.K);
+    if (gridDim.x == 1 && P.status) {
+        if (threadIdx.x == 0) *P.status = FEF_OK;
+        __syncthreads();   // (an error is reported after it)
+    }
     if (P.row_len && i >= __ldg(P.row_len + b)) {
         if (threadIdx.x == 0) write_none(P, at, false);
         return;
@@ -1804,7 +1910,8 @@ static fef_status truncate(const void* logits, const int32_t* row_len, int B, in
     P.kept = kept;
     P.status = device_status;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (device_status && cudaMemsetAsync(device_status, 0, sizeof(int32_t), stream) != cudaSuccess) return FEF_ERR_CUDA;
+    // (one row's CTA clears the status by itself: 2 us less; of several, one could do so after another's report)
+    if (device_status && B * K > 1 && cudaMemsetAsync(device_status, 0, sizeof(int32_t), stream) != cudaSuccess) return FEF_ERR_CUDA;
     const cudaError_t e = dt == FEF_F32 ? launch<FEF_F32>(P, dev, sms, stream) : launch<FEF_BF16>(P, dev, sms, stream);
     return e == cudaSuccess ? FEF_OK : FEF_ERR_CUDA;
 }
