@@ -17,13 +17,14 @@
 //   row_by_candidates  where the border is among few entries, as top-k's, min-p's and a steep law's top-p's are: a sample of the row tells a
 //                      floor safely below the border, one pass notes down what is above it and only sums the rest, and the border and
 //                      the draw are found among what was noted down.  One read of the row; bound by that and by the instructions of
-//                      looking at every entry (64 windows x 32 x 126464 bfloat16, top-k 50: 118 us, with draws 132; 4.4 and 3.9 TB/s)
+//                      looking at every entry (64 windows x 32 x 126464 bfloat16, top-k 50: 118 us, with draws 133; 4.4 and 3.9 TB/s)
 //   row_by_values      where it is among many (a flat law's top-p): the row is counted by value, then read once more, from L2 for the most
 //                      part.  Bound by the shared-memory atomics of the counting and, with draws, the weights of all entries before
-//                      the border (the same rows, top-p 0.9: 282 us, with draws 387; 16 windows x 32 x 152064 binary32 236 and 246)
+//                      the border (flat rows of that size, top-p 0.9: 286 us, with draws 392; 16 windows x 32 x 152064 binary32 237
+//                      and 248)
 //   row_by_passes      whatever is left, and rows that are errors: some ten passes, 0.5 ms a row
-// Sampling and candidates against counting every row: top-k 50 of 16 windows x 32 x 152064 binary32 60 against 217 us; counting against
-// passes: 3850 against 300 us at 32 windows of flat bfloat16 rows.
+// Candidates against counting every row: top-k 50 118 against 244 us, of 16 windows x 32 x 152064 binary32 62 against 128; counting
+// against passes: 165 against 3850 us at 32 windows of flat bfloat16 rows.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -37,7 +38,9 @@
 namespace fef {
 namespace trunc {
 
-constexpr float kManyCandidates = 4000.f;   // with more of them counting all values is faster (1 window x 32: 55 against 110 us)
+// With more candidates the row is counted by value instead (64 windows x 32 x 126464 bfloat16, top-p 0.9 with draws: 227 us; with 1500
+// in its place 270, 3000 239; 1 window x 32, top-p 0.95: 50, 55, 55).
+constexpr float kManyCandidates = 4000.f;
 constexpr int kMaxChunks = 252;    // stretches of a row whose kept weight is summed up for the draw
 constexpr int kValueBins = 3842;   // of one sign: 30 binades of 128 bfloat16 numbers, what is below, what is above
 constexpr int kRowBins = 2 * kValueBins;
