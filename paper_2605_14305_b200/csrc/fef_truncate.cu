@@ -18,10 +18,10 @@
 //                      floor safely below the border, one pass notes down what is above it and only sums the rest, and the border and
 //                      the draw are found among what was noted down.  One read of the row; bound by that and by the instructions of
 //                      looking at every entry (64 windows x 32 x 126464 bfloat16, top-k 50: 118 us, with draws 133; 4.4 and 3.9 TB/s)
-//   row_by_values      where it is among many (a flat law's top-p): the row is counted by value, then read once more (from
-//                      memory: four rows to an SM are a little more than L2 holds).  Bound by the shared-memory atomics of the counting and, with draws, the weights of all entries before
-//                      the border (flat rows of that size, top-p 0.9: 286 us, with draws 392; 16 windows x 32 x 152064 binary32 237
-//                      and 248)
+//   row_by_values      where it is among many (a flat law's top-p): the row is counted by value, then read once more (from memory: four
+//                      rows to an SM are a little more than L2 holds).  Bound by the shared-memory atomics of the counting and, with
+//                      draws, the weights of all entries before the border (flat rows of that size, top-p 0.9: 286 us, with draws 392;
+//                      16 windows x 32 x 152064 binary32 237 and 248)
 //   row_by_passes      whatever is left, and rows that are errors: some ten passes, 0.5 ms a row
 // Candidates against counting every row: top-k 50 118 against 244 us, of 16 windows x 32 x 152064 binary32 62 against 128; counting
 // against passes: 165 against 3850 us at 32 windows of flat bfloat16 rows.
