@@ -318,6 +318,33 @@ def test_every_share_of_threads(fef, rows):
                         assert ((a[few] - b).abs() <= 2 * NORM_TOL * (1 + b.abs())).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,V", [(40, 1000), (200, 5000), (40, 9000)])    # (256, 512 and 1024 threads to a row)
+def test_rows_of_so_many_finite_entries(fef, B, V, dtype):
+    g = torch.Generator(device="cuda").manual_seed(51)
+    x, u = _logits(B, 1, V, dtype, 52)
+    for finite in (1, 2, 31, 127, 128, 129, 255, 256, 257, 300):
+        y = torch.full_like(x, -math.inf)
+        for b in range(B):
+            ids = torch.randperm(V, generator=g, device="cuda")[:finite]
+            y[b, 0, ids] = x[b, 0, ids]
+        for kind in ("kpm", "p", "m", "edges"):
+            _check(fef, y, 0.9, uniforms=u, **_rules(kind, B))
+
+
+def test_a_single_row_leaves_no_status_behind(fef):
+    x, u = _logits(1, 1, 20000, torch.float32, 61)
+    bad = x.clone()
+    bad[0, 0, 777] = math.nan
+    k = _i32(9)
+    d = fef.fef_draft_sample_truncated(bad, 1.0, top_k=k, uniforms=u)
+    assert int(d.law.device_status) == fef.FEF_ERR_NONFINITE
+    for logits, lens, status in ((x, 1, 0), (bad, 1, fef.FEF_ERR_NONFINITE), (bad, 0, 0), (bad, 1, fef.FEF_ERR_NONFINITE), (x, 1, 0)):
+        fef.fef_draft_sample_truncated(logits, 1.0, top_k=k, uniforms=u, row_len=_i32(lens), out=d)
+        assert int(d.law.device_status) == status
+        assert (int(d.tokens) >= 0) == (logits is x)
+
+
 def test_largest_vocabulary_and_temperatures(fef):
     V = fef.FEF_MAX_TRUNCATE_V
     x, u = _logits(1, 1, V, torch.bfloat16, 2)
